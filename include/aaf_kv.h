@@ -297,6 +297,133 @@ int aaf_kv_import_host_chunked(aaf_kv_pool *pool, const void *src_host, const aa
                                void *staging_dev, size_t staging_bytes, int32_t chunk_tokens, aaf_ctx_t *out_ctx,
                                void *stream);
 
+/* ---- operators that compute with the payload -------------------------------------------------------------------
+ * Everything above moves KV bytes; the calls below are what a serving loop does with them, layer by layer:
+ *   aaf_kv_reserve   grow the contexts by this step's tokens (slots without payload)
+ *   aaf_kv_store     rotate the new queries and keys, write keys and values into their slots
+ *   aaf_kv_attend    attention of the new tokens over their whole contexts
+ *   aaf_kv_attn_mass what every cached token received of that attention, summed up over steps and layers
+ *   aaf_kv_prune     a new context of the tokens that matter (Alg. "KV-Evict", at the grain of tokens)
+ * The payload is then no longer opaque: elements are 16-bit floats (elt_bytes 2; dtype says which), head_dim is a
+ * multiple of 8, at most AAF_ATTN_MAX_HEAD_DIM for attention; other pools get AAF_ERR_INCOMPAT.  Dot products, scores,
+ * maxima and sums are held in 32 bits.  A query row belongs to a token and a query head; query head h reads kv head
+ * h / (n_q_heads / n_kv_heads).  Batches are packed: the tokens of ctxs[0] first, then those of ctxs[1], ...; the
+ * queries of context i are its LAST n_q[i] tokens, so token j of them is at position p = length - n_q[i] + j.
+ * All run on `stream`, behind the pool's earlier calls, and wait for nothing on the host.  They read host arrays and
+ * order streams, which a replayed graph would not do again: during stream capture they return AAF_ERR_INVALID_ARG.
+ * Catalog counters (reuse, last access) are stamped by reserve and prune, not by store, attend and attn_mass.
+ * Device buffers must not overlap each other unless said so.  A context longer than 2^30 tokens: AAF_ERR_TOO_LONG. */
+#define AAF_DTYPE_BF16 0
+#define AAF_DTYPE_F16 1
+#define AAF_ATTN_MAX_HEAD_DIM 256
+#define AAF_ROPE_MAX_DIM 1024
+
+/* reserve -- append without a payload: contexts grow by n_new[i] slots, block for block as aaf_kv_append would grow
+ * them (a shared partial tail is copied on write); the new slots keep whatever bytes they hold until aaf_kv_store
+ * fills them, one layer at a time.  Errors as aaf_kv_append. */
+int aaf_kv_reserve(aaf_kv_pool *pool, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_new, void *stream);
+
+/* store -- rotary positions and the write of one layer's new keys and values.  For the last n_new[i] tokens of context
+ * ctxs[i]: k is rotated and written with v into the token's slot of layer `layer`; with n_q_heads > 0, q is rotated
+ * into q_out (which may be q itself).  A pair (a, b) of the first rot_dim dimensions of a head becomes
+ *   (a cos w - b sin w, a sin w + b cos w) * mscale,   w = position * inv_freq[pair],
+ * pairs being (i, i + rot_dim / 2), or (2i, 2i + 1) with `interleaved`.  The angle is taken in 64 bits, the results are
+ * rounded once.  The position of a token is its index in the context, or pos[token] if pos is given (a pruned context,
+ * a context that starts elsewhere).  k, v, q, q_out: heads contiguous, *_stride elements from token to token (multiples
+ * of 8; views into a fused projection are fine).  Only slots that no other context can share are written: a call that
+ * reaches back before the tokens added since the context was last forked or merged by reference is AAF_ERR_INVALID_ARG,
+ * and so is a context listed twice. */
+typedef struct aaf_kv_store_desc {
+    uint32_t struct_size;   /* sizeof(aaf_kv_store_desc)                                     */
+    int32_t dtype;          /* AAF_DTYPE_*                                                   */
+    int32_t n_q_heads;      /* 0: keys and values only                                       */
+    int32_t rot_dim;        /* even, 0 (no rotation) .. min(head_dim, AAF_ROPE_MAX_DIM)      */
+    int32_t interleaved;
+    float mscale;
+    const double *inv_freq; /* (device) rot_dim / 2 entries                                  */
+    const int64_t *pos;     /* (device) one per token, or NULL                               */
+    const void *q;          /* (device) [tokens][n_q_heads][head_dim]                        */
+    void *q_out;            /* (device)                                                      */
+    const void *k, *v;      /* (device) [tokens][n_kv_heads][head_dim]                       */
+    int64_t q_stride, q_out_stride, k_stride, v_stride;
+} aaf_kv_store_desc;
+int aaf_kv_store(aaf_kv_pool *pool, int32_t layer, const aaf_kv_store_desc *d, int32_t n, const aaf_ctx_t *ctxs,
+                 const int32_t *n_new, void *stream);
+
+/* Rotary frequencies (host-only arithmetic): inv_freq[i] = base^(-2i / rot_dim), i < rot_dim / 2, and, for contexts
+ * longer than a model was trained on, one of
+ *   AAF_ROPE_LINEAR      every frequency divided by factor (positions interpolated)
+ *   AAF_ROPE_BASE        base * factor^(rot_dim / (rot_dim - 2)): the slowest pair stretched by factor, the fastest kept
+ *   AAF_ROPE_WAVELENGTH  by the turns that a pair makes over orig_context: at least `high` keeps its frequency, at most
+ *                        `low` divides it by factor, a linear blend between
+ *   AAF_ROPE_RAMP        a blend that is linear in the pair's index between the (whole) indices of pairs that make `high` and
+ *                        `low` turns over orig_context; *mscale_out = 0.1 ln factor + 1
+ * *mscale_out (may be NULL) is 1 otherwise.  `s` is not read for AAF_ROPE_NONE. */
+#define AAF_ROPE_NONE 0
+#define AAF_ROPE_LINEAR 1
+#define AAF_ROPE_BASE 2
+#define AAF_ROPE_WAVELENGTH 3
+#define AAF_ROPE_RAMP 4
+typedef struct aaf_kv_rope_scaling {
+    uint32_t struct_size; /* sizeof(aaf_kv_rope_scaling) */
+    uint32_t reserved;
+    double factor;        /* >= 1 */
+    double low, high;     /* turns, 0 < low < high */
+    double orig_context;  /* tokens */
+} aaf_kv_rope_scaling;
+int aaf_kv_rope_freqs(int32_t rot_dim, double base, int32_t scaling, const aaf_kv_rope_scaling *s, double *inv_freq_host,
+                      float *mscale_out);
+
+/* attend -- attention over the paged cache, one layer.  For every query row r at position p and every key t that the row sees:
+ *   x = scale * (q_r . k_t);  softcap > 0: x = softcap * tanh(x / softcap);  slopes: x -= slopes[head] * |p - t|
+ *   out_r = sum_t exp(x_t) v_t / sum_t exp(x_t),   lse_r = log sum_t exp(x_t)
+ * A row sees the keys [lo, hi) of its token's span: [0, p + 1) without `spans`, else spans[token] = {lo, hi} (clipped to the
+ * context); window > 0 further drops the keys t <= p - window.  Spans express the masks that are one interval a row: documents
+ * packed into one context ({start of the token's document, p + 1}), a prefix seen in both directions ({0, max(p + 1,
+ * prefix)}), a whole context ({0, length}).  A row that sees no key, or whose visible scores are all -inf, is 0 with lse =
+ * -inf.  Keys and values that a row does not see have no influence on it, whatever they hold (infinities and NaN
+ * included); slots behind a context's end are not read.
+ * q: heads contiguous, q_stride elements from token to token (a multiple of 8); out: dense [tokens][n_q_heads][head_dim];
+ * lse (may be NULL): [tokens][n_q_heads].  n_q may be NULL (one token each).  A context may be listed several times.
+ * workspace_dev: caller-owned scratch of aaf_kv_attend_workspace_bytes(pool) bytes, 16-byte aligned; one buffer serves all
+ * calls of a pool (they are ordered, whatever stream they name).  Results do not depend on timing: the same call gives the same bits.
+ * Errors: BAD_CTX, INVALID_ARG (n_q < 1 or longer than the context, pointers, strides, non-finite scale ...), INCOMPAT,
+ * DST_TOO_SMALL (workspace), TOO_MANY, TOO_LONG. */
+typedef struct aaf_kv_attn {
+    uint32_t struct_size; /* sizeof(aaf_kv_attn)                                  */
+    int32_t dtype;        /* AAF_DTYPE_*                                          */
+    int32_t n_q_heads;    /* a multiple of n_kv_heads                             */
+    int32_t window;       /* 0: none                                              */
+    float scale;
+    float softcap;        /* 0: none                                              */
+    const float *slopes;  /* (device) n_q_heads entries, or NULL                  */
+    const int32_t *spans; /* (device) two per query token, or NULL                */
+    int64_t q_stride;     /* elements                                             */
+} aaf_kv_attn;
+size_t aaf_kv_attend_workspace_bytes(const aaf_kv_pool *pool);
+int aaf_kv_attend(aaf_kv_pool *pool, int32_t layer, const aaf_kv_attn *a, int32_t n, const aaf_ctx_t *ctxs,
+                  const int32_t *n_q, const void *q_dev, void *out_dev, float *lse_dev, void *workspace_dev,
+                  size_t workspace_bytes, void *stream);
+
+/* attention mass -- mass[i][t] = prev[i][t] + sum over the query rows r of context i of exp(x_rt - lse_r), x and the visible keys as
+ * in aaf_kv_attend with the same arguments, lse as that call returned it (rows with lse = -inf add nothing).  Row i starts
+ * at i * mass_stride (>= the longest context, else DST_TOO_SMALL); entries behind a context's end are left as they are.
+ * prev may be NULL (zeros) or mass itself: one buffer then sums over layers and steps.  The order of every sum is fixed. */
+int aaf_kv_attn_mass(aaf_kv_pool *pool, int32_t layer, const aaf_kv_attn *a, int32_t n, const aaf_ctx_t *ctxs,
+                     const int32_t *n_q, const void *q_dev, const float *lse_dev, const float *prev_dev, float *mass_dev,
+                     int64_t mass_stride, void *stream);
+
+/* prune -- token-level eviction (Alg. "KV-Evict": drop what scores lowest): a new context of `budget` tokens of ctx, in
+ * their order: its first `sink`, its last `recent`, and of the others those with the largest scores (equal scores: the
+ * lower position; -0 equals 0; a NaN ranks below everything).  scores_dev: one float per token, e.g. a row of the
+ * attention mass.  Rows move in all layers, bytes verbatim (keys keep the rotation of their old positions: store later
+ * tokens with explicit positions).  kept_dev (budget entries) receives the kept positions in ascending order,
+ * kept_scores_dev (may be NULL) their scores.  ctx stays live; evict it to free its blocks.  *out_ctx (host): the
+ * smallest free handle; blocks come from the ring as for an import; lineage AAF_ORIGIN_PRUNE.  Errors: BAD_CTX,
+ * INVALID_ARG (budget outside [1, length], sink + recent > budget), OOM_CTX, OOM_BLOCKS. */
+int aaf_kv_prune(aaf_kv_pool *pool, aaf_ctx_t ctx, const float *scores_dev, int64_t budget, int64_t sink, int64_t recent,
+                 int32_t *kept_dev, float *kept_scores_dev, aaf_ctx_t *out_ctx, void *stream);
+
 /* Introspection (metadata catalog of App. A.2).  These synchronise the library's metadata stream and
  * the stream of the most recent call. */
 int aaf_kv_ctx_len(aaf_kv_pool *pool, aaf_ctx_t ctx, int64_t *n_tokens);
@@ -309,8 +436,8 @@ int aaf_kv_get_free_list(aaf_kv_pool *pool, int32_t *host_out /* n_blocks entrie
  * and list offsets, so a consumer on `stream` can wrap them without conversion.
  *   state rows, one per live context in ascending handle order (capacity max_ctx):
  *     state_id int32, n_tokens int64, reuse int64, last_access int64,
- *     lineage (Lambda of Sec. 3.2): origin int32 (AAF_ORIGIN_*), parent int32 (the fork parent or the
- *     first merged segment, -1 for none), born int64 (clock of the creating call), parent_born int64
+ *     lineage (Lambda of Sec. 3.2): origin int32 (AAF_ORIGIN_*), parent int32 (the fork parent, the
+ *     first merged segment or the pruned context, -1 for none), born int64 (clock of the creating call), parent_born int64
  *     (creation clock of that parent: handles are reused, (handle, born) names a state for good),
  *     block_offsets int32[n_states + 1]: list offsets into the block rows (exclusive prefix sum of
  *     the block-table lengths; capacity max_ctx + 1)
@@ -323,6 +450,7 @@ int aaf_kv_get_free_list(aaf_kv_pool *pool, int32_t *host_out /* n_blocks entrie
 #define AAF_ORIGIN_BUFFER 1 /* registered from a transfer buffer: prefill output or received state */
 #define AAF_ORIGIN_FORK 2
 #define AAF_ORIGIN_MERGE 3
+#define AAF_ORIGIN_PRUNE 4  /* tokens kept by aaf_kv_prune; parent = the context they were kept from */
 typedef struct aaf_kv_catalog_cols {
     int32_t *state_id;
     int64_t *n_tokens, *reuse, *last_access;

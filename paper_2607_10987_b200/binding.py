@@ -24,6 +24,8 @@ AAF_COMPOSE_SHARE, AAF_COMPOSE_COPY_ALL = 0, 1
 AAF_POLICY_REUSE, AAF_POLICY_TRANSFER, AAF_POLICY_RECOMPUTE = 0, 1, 2
 AAF_ENGINE_AUTO, AAF_ENGINE_VEC, AAF_ENGINE_BULK, AAF_ENGINE_WARP = 0, 1, 2, 3
 AAF_OP_MATERIALIZE, AAF_OP_IMPORT, AAF_OP_APPEND, AAF_OP_COMPOSE, AAF_OP_CLASSES = 0, 1, 2, 3, 4
+AAF_DTYPE_BF16, AAF_DTYPE_F16 = 0, 1
+AAF_ROPE_NONE, AAF_ROPE_LINEAR, AAF_ROPE_BASE, AAF_ROPE_WAVELENGTH, AAF_ROPE_RAMP = 0, 1, 2, 3, 4
 OP_NAMES = ("materialize", "import", "append", "compose")
 
 
@@ -64,6 +66,24 @@ class aaf_kv_catalog_cols(C.Structure):
                 ("pos_end", C.c_void_p), ("refcount", C.c_void_p), ("address", C.c_void_p)]
 
 
+class aaf_kv_store_desc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("mscale", C.c_float), ("inv_freq", C.c_void_p), ("pos", C.c_void_p),
+                ("q", C.c_void_p), ("q_out", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_stride", C.c_int64), ("q_out_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
+
+
+class aaf_kv_rope_scaling(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("reserved", C.c_uint32), ("factor", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("orig_context", C.c_double)]
+
+
+class aaf_kv_attn(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("window", C.c_int32),
+                ("scale", C.c_float), ("softcap", C.c_float), ("slopes", C.c_void_p), ("spans", C.c_void_p),
+                ("q_stride", C.c_int64)]
+
+
 # every symbol include/aaf_kv.h declares: name -> (restype, argtypes)
 _vp, _i32, _i64, _u32, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint32, C.c_size_t
 _p32 = C.POINTER(C.c_int32)
@@ -88,6 +108,14 @@ SYMBOLS = {
                                                   _i32, _p32, C.POINTER(aaf_kv_xfer_desc), _vp]),
     "aaf_kv_import_host_chunked": (C.c_int, [_vp, _vp, C.POINTER(aaf_kv_xfer_desc), _vp, _sz, _i32, _p32, _vp]),
     "aaf_kv_evict_to_budget": (C.c_int, [_vp, C.c_double, C.c_double, C.c_double, _i64, _p32, _i32, _p32, _vp]),
+    "aaf_kv_reserve": (C.c_int, [_vp, _i32, _p32, _p32, _vp]),
+    "aaf_kv_store": (C.c_int, [_vp, _i32, C.POINTER(aaf_kv_store_desc), _i32, _p32, _p32, _vp]),
+    "aaf_kv_rope_freqs": (C.c_int, [_i32, C.c_double, _i32, C.POINTER(aaf_kv_rope_scaling), C.POINTER(C.c_double),
+                                    C.POINTER(C.c_float)]),
+    "aaf_kv_attend_workspace_bytes": (_sz, [_vp]),
+    "aaf_kv_attend": (C.c_int, [_vp, _i32, C.POINTER(aaf_kv_attn), _i32, _p32, _p32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "aaf_kv_attn_mass": (C.c_int, [_vp, _i32, C.POINTER(aaf_kv_attn), _i32, _p32, _p32, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "aaf_kv_prune": (C.c_int, [_vp, _i32, _vp, _i64, _i64, _i64, _vp, _vp, _p32, _vp]),
     "aaf_kv_catalog_rows": (C.c_int, [_vp, _p32, C.POINTER(_i64)]),
     "aaf_kv_export_catalog": (C.c_int, [_vp, C.POINTER(aaf_kv_catalog_cols), _vp]),
     "aaf_kv_get_catalog": (C.c_int, [_vp, C.POINTER(_i64), C.POINTER(_i64), C.POINTER(_i64)]),
@@ -165,6 +193,18 @@ def aaf_kv_import_host_chunked(pool, src_host, desc, staging, staging_bytes, chu
     return _fn("aaf_kv_import_host_chunked")(pool, src_host, desc, staging, staging_bytes, chunk_tokens, out_ctx, stream)
 def aaf_kv_evict_to_budget(pool, alpha, beta, gamma, budget, out_victims, cap, n_victims, stream):
     return _fn("aaf_kv_evict_to_budget")(pool, alpha, beta, gamma, budget, out_victims, cap, n_victims, stream)
+def aaf_kv_reserve(pool, n, ctxs, n_new, stream): return _fn("aaf_kv_reserve")(pool, n, ctxs, n_new, stream)
+def aaf_kv_store(pool, layer, desc, n, ctxs, n_new, stream):
+    return _fn("aaf_kv_store")(pool, layer, desc, n, ctxs, n_new, stream)
+def aaf_kv_rope_freqs(rot_dim, base, scaling, params, inv_freq, mscale):
+    return _fn("aaf_kv_rope_freqs")(rot_dim, base, scaling, params, inv_freq, mscale)
+def aaf_kv_attend_workspace_bytes(pool): return _fn("aaf_kv_attend_workspace_bytes")(pool)
+def aaf_kv_attend(pool, layer, attn, n, ctxs, n_q, q, out, lse, workspace, workspace_bytes, stream):
+    return _fn("aaf_kv_attend")(pool, layer, attn, n, ctxs, n_q, q, out, lse, workspace, workspace_bytes, stream)
+def aaf_kv_attn_mass(pool, layer, attn, n, ctxs, n_q, q, lse, prev, mass, mass_stride, stream):
+    return _fn("aaf_kv_attn_mass")(pool, layer, attn, n, ctxs, n_q, q, lse, prev, mass, mass_stride, stream)
+def aaf_kv_prune(pool, ctx, scores, budget, sink, recent, kept, kept_scores, out_ctx, stream):
+    return _fn("aaf_kv_prune")(pool, ctx, scores, budget, sink, recent, kept, kept_scores, out_ctx, stream)
 def aaf_kv_catalog_rows(pool, n_states, n_rows): return _fn("aaf_kv_catalog_rows")(pool, n_states, n_rows)
 def aaf_kv_export_catalog(pool, cols, stream): return _fn("aaf_kv_export_catalog")(pool, cols, stream)
 def aaf_kv_get_catalog(pool, clock, reuse, last): return _fn("aaf_kv_get_catalog")(pool, clock, reuse, last)
@@ -206,6 +246,29 @@ def make_desc(n_layers, n_kv_heads, head_dim, block_size, elt_bytes, n_blocks, m
     return d
 
 
+def rope_freqs(rot_dim, base=10000.0, scaling=AAF_ROPE_NONE, factor=1.0, low=1.0, high=32.0, orig_context=0.0):
+    """Rotary frequencies as aaf_kv_rope_freqs defines them: (list of rot_dim / 2 doubles, mscale)."""
+    s = aaf_kv_rope_scaling(C.sizeof(aaf_kv_rope_scaling), 0, factor, low, high, orig_context)
+    out = (C.c_double * max(rot_dim // 2, 1))()
+    m = C.c_float(1.0)
+    st = aaf_kv_rope_freqs(rot_dim, base, scaling, C.byref(s), out, C.byref(m))
+    if st != AAF_OK:
+        raise ValueError(aaf_kv_strerror(st))
+    return list(out[: rot_dim // 2]), m.value
+
+
+class Rope:
+    """Rotary parameters of a model: leading dimensions of a head that turn, their frequencies (float64 device tensor
+    of rot_dim / 2 entries), pair layout and factor."""
+
+    def __init__(self, rot_dim, inv_freq, interleaved=False, mscale=1.0):
+        import torch
+
+        if inv_freq.dtype != torch.float64 or not inv_freq.is_cuda or not inv_freq.is_contiguous() or 2 * inv_freq.numel() != rot_dim:
+            raise ValueError("inv_freq: contiguous float64 CUDA tensor of rot_dim / 2 entries")
+        self.rot_dim, self.inv_freq, self.interleaved, self.mscale = rot_dim, inv_freq, interleaved, mscale
+
+
 class KVPool:
     """Holds the torch-allocated memory of one pool and forwards to the C ABI.
 
@@ -243,6 +306,7 @@ class KVPool:
             self._fo = np.ascontiguousarray(np.asarray(free_order, dtype=np.int32))
             d.free_order = self._fo.ctypes.data_as(_p32)
         self.desc = d
+        self._attend_ws = None  # scratch of attend, allocated by its first call
         self.h = C.c_void_p()
         st = aaf_kv_pool_create(d, self.h)
         if st != AAF_OK:
@@ -350,6 +414,119 @@ class KVPool:
         n = len(ctxs)
         a = (C.c_int32 * max(n, 1))(*ctxs)
         return aaf_kv_evict(self.h, n, a, self._stream()), None
+
+    # ------------------------------------------------------------------ operators that compute with the payload
+    # Tensors: q [tokens, q heads, head_dim], k and v [tokens, kv heads, head_dim], bf16 or f16, the heads of a token
+    # contiguous; tokens packed in the order of ctxs.
+    def _rows(self, t, tokens, heads, name, dtype=None):
+        """Device pointer and token stride of a packed per-token tensor."""
+        if t.device != self.device or t.dim() != 3 or t.shape != (tokens, heads, self.D) or (dtype is not None and t.dtype != dtype):
+            raise ValueError(f"{name}: expected a [{tokens}, {heads}, {self.D}] tensor of the pool's device and one dtype, "
+                             f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.D):
+            raise ValueError(f"{name}: the heads of a token must be contiguous")
+        return t.data_ptr(), (t.stride(0) if tokens > 1 else max(t.stride(0), heads * self.D))
+
+    def _flat(self, t, dtype, n, name):
+        if t is None:
+            return None
+        if t.device != self.device or t.dtype != dtype or not t.is_contiguous() or t.numel() != n:
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of {n} entries on the pool's device")
+        return t.data_ptr()
+
+    def _dtype(self, t):
+        code = {self.torch.bfloat16: AAF_DTYPE_BF16, self.torch.float16: AAF_DTYPE_F16}.get(t.dtype)
+        if code is None:
+            raise ValueError(f"bfloat16 or float16 expected, got {t.dtype}")
+        return code
+
+    def reserve(self, ctxs, n_new):
+        n = len(ctxs)
+        return aaf_kv_reserve(self.h, n, (C.c_int32 * max(n, 1))(*ctxs), (C.c_int32 * max(n, 1))(*n_new), self._stream()), None
+
+    def store(self, layer, ctxs, n_new, k, v, q=None, q_out=None, rope=None, pos=None):
+        """Rotates q (into q_out, default in place) and k, writes k and v into the slots of the contexts' last n_new tokens."""
+        n, tokens = len(ctxs), sum(n_new)
+        d = aaf_kv_store_desc()
+        d.struct_size, d.dtype = C.sizeof(d), self._dtype(k)
+        d.k, d.k_stride = self._rows(k, tokens, self.H, "k")
+        d.v, d.v_stride = self._rows(v, tokens, self.H, "v", k.dtype)
+        if q is not None:
+            d.n_q_heads = q.shape[1]
+            d.q, d.q_stride = self._rows(q, tokens, q.shape[1], "q", k.dtype)
+            d.q_out, d.q_out_stride = (d.q, d.q_stride) if q_out is None else self._rows(q_out, tokens, q.shape[1], "q_out", k.dtype)
+        d.mscale = 1.0
+        if rope is not None:
+            if rope.inv_freq.device != self.device:
+                raise ValueError("rope: frequencies on another device than the pool")
+            d.rot_dim, d.interleaved, d.mscale = rope.rot_dim, int(rope.interleaved), rope.mscale
+            d.inv_freq = rope.inv_freq.data_ptr()
+        d.pos = self._flat(pos, self.torch.int64, tokens, "pos")
+        return aaf_kv_store(self.h, layer, C.byref(d), n, (C.c_int32 * max(n, 1))(*ctxs), (C.c_int32 * max(n, 1))(*n_new),
+                            self._stream()), None
+
+    def _attn(self, q, tokens, scale, softcap, window, slopes, spans):
+        a = aaf_kv_attn()
+        a.struct_size, a.dtype, a.window = C.sizeof(a), self._dtype(q), window
+        a.n_q_heads = q.shape[1] if q.dim() == 3 else 0
+        ptr, a.q_stride = self._rows(q, tokens, a.n_q_heads, "q")
+        a.scale, a.softcap = self.D ** -0.5 if scale is None else scale, softcap
+        a.slopes = self._flat(slopes, self.torch.float32, a.n_q_heads, "slopes")
+        a.spans = self._flat(spans, self.torch.int32, 2 * tokens, "spans")
+        return a, ptr
+
+    def attend(self, layer, ctxs, n_q, q, out=None, lse=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):
+        """Attention of the contexts' last n_q tokens (None: one each); returns (status, (out, lse))."""
+        torch = self.torch
+        n = len(ctxs)
+        tokens = n if n_q is None else sum(n_q)
+        a, ptr = self._attn(q, tokens, scale, softcap, window, slopes, spans)
+        if out is None:
+            out = torch.empty(tokens, a.n_q_heads, self.D, dtype=q.dtype, device=self.device)
+        elif self._rows(out, tokens, a.n_q_heads, "out", q.dtype)[1] != a.n_q_heads * self.D:
+            raise ValueError("out: dense tensor expected")
+        if lse is None:
+            lse = torch.empty(tokens, a.n_q_heads, dtype=torch.float32, device=self.device)
+        if self._attend_ws is None:
+            self._attend_ws = torch.empty(aaf_kv_attend_workspace_bytes(self.h), dtype=torch.uint8, device=self.device)
+        st = aaf_kv_attend(self.h, layer, C.byref(a), n, (C.c_int32 * max(n, 1))(*ctxs),
+                           None if n_q is None else (C.c_int32 * max(n, 1))(*n_q), ptr, out.data_ptr(),
+                           self._flat(lse, torch.float32, tokens * a.n_q_heads, "lse"), self._attend_ws.data_ptr(),
+                           self._attend_ws.numel(), self._stream())
+        return st, ((out, lse) if st == AAF_OK else None)
+
+    def attn_mass(self, layer, ctxs, n_q, q, lse, mass, prev=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):
+        """mass[i, t] = prev[i, t] (default 0; may be mass itself) + what token t of context i received of this attention."""
+        n = len(ctxs)
+        tokens = n if n_q is None else sum(n_q)
+        a, ptr = self._attn(q, tokens, scale, softcap, window, slopes, spans)
+        for t in (mass,) if prev is None else (mass, prev):
+            if t.device != self.device or t.dtype != self.torch.float32 or t.dim() != 2 or t.shape != mass.shape or \
+                    t.shape[0] != n or t.stride(1) != 1 or (n > 1 and t.stride(0) != mass.stride(0)):
+                raise ValueError("mass, prev: float32 tensors of one row per context, equally strided, on the pool's device")
+        # a row's room: up to the next row, or the tensor's width where that is less
+        stride = mass.stride(0) if n > 1 else mass.shape[1]
+        if mass.shape[1] < stride and any((self.ctx_len(c) or 0) > mass.shape[1] for c in ctxs):
+            return AAF_ERR_DST_TOO_SMALL, None
+        st = aaf_kv_attn_mass(self.h, layer, C.byref(a), n, (C.c_int32 * max(n, 1))(*ctxs),
+                              None if n_q is None else (C.c_int32 * max(n, 1))(*n_q), ptr,
+                              self._flat(lse, self.torch.float32, tokens * a.n_q_heads, "lse"),
+                              None if prev is None else prev.data_ptr(), mass.data_ptr(),
+                              stride, self._stream())
+        return st, (mass if st == AAF_OK else None)
+
+    def prune(self, ctx, scores, budget, sink=0, recent=0, kept=None, kept_scores=None):
+        """New context of `budget` tokens of ctx; kept (int32) and kept_scores (float32) receive which ones.
+        Returns (status, handle)."""
+        torch = self.torch
+        n = self.ctx_len(ctx)
+        if kept is None:
+            kept = torch.empty(max(budget, 1), dtype=torch.int32, device=self.device)
+        out = C.c_int32(-1)
+        st = aaf_kv_prune(self.h, ctx, self._flat(scores, torch.float32, scores.numel() if n is None else n, "scores"), budget, sink, recent,
+                          self._flat(kept, torch.int32, max(budget, 1), "kept"),
+                          self._flat(kept_scores, torch.float32, max(budget, 1), "kept_scores"), C.byref(out), self._stream())
+        return st, (out.value if st == AAF_OK else None)
 
     def materialize_host(self, ctx, t0, t1, dst_host, staging):
         return aaf_kv_materialize_host(self.h, ctx, t0, t1, dst_host.data_ptr(),

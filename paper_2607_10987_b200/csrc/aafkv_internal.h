@@ -78,7 +78,7 @@ struct DevState {
 
 // ---- per-call argument records (written by the host into pinned memory, read by planners)
 struct AppendEntry {      // 32 bytes
-    const char *src;      // device payload [L][2][n_new][row]
+    const char *src;      // device payload [L][2][n_new][row]; null: slots only (reserve)
     long long T;          // tokens before the append
     int ctx;
     int n_new;
@@ -114,7 +114,7 @@ struct ImpEntry {         // 32 bytes; one transfer buffer registered as one new
     int ctx;              // handle of the new context
     int block_off;        // rank (from the ring head, over the batch) of its first block = its first piece slot
     int out_index;
-    int pad;
+    int parent;           // -1: registered from a buffer; else the handle of the context it is pruned from
 };
 struct EvictArgs {        // followed by int ctx[n], int ent_off[n + 1]
     int n;
@@ -152,7 +152,7 @@ cudaError_t launch_plan_materialize_batch(const Geom &g, const DevState &s, cons
 cudaError_t launch_plan_import_batch(const Geom &g, const DevState &s, const ImpEntry *ents_dev, const SmallImp &small,
                                      int n, int total_blocks, long long clock, cudaStream_t st);
 cudaError_t launch_plan_import(const Geom &g, const DevState &s, int ctx, long long n, const char *src,
-                               long long clock, cudaStream_t st);
+                               long long clock, cudaStream_t st, int parent = -1);
 // children_dev == nullptr: the k <= SMALL_ARGS children are in `small`
 cudaError_t launch_fork(const Geom &g, const DevState &s, int parent, long long T, int k, const int *children_dev,
                         const SmallInts &small, long long clock, cudaStream_t st);

@@ -1,0 +1,428 @@
+// Attention of a few query rows per kv head (one new token per sequence, or a handful) over paged keys and values.
+//
+//   s_rt = score(q_r . k_t),  o_r = sum_t exp(s_rt) v_t / sum_t exp(s_rt),  lse_r = log sum_t exp(s_rt)
+//
+// One pass over K and V with the running maximum m and sum l of every row; the key range of a sequence is cut into
+// parts, each part leaves (m, l, o) and attend_join adds them up in part order, so results do not depend on timing.
+//
+// Bound: every cached row is used by at most 8 * NT query rows, so the bytes of K and V decide.  A warp owns one kv
+// head of one part and shares nothing: each lane copies exactly the 16-byte pieces that its own matrix fragments need
+// (cp.async into slots of its own, several tiles of 16 tokens in flight), so there is no barrier and no bank conflict.
+// The tensor products take the tokens as the M side (16) and the query rows as the N side (8): S^T = K Q^T and
+// O^T = V^T P^T waste nothing for 8 rows, where rows as M would fill half a tile at best.  The order of the head
+// dimensions inside a product is free as long as both operands agree, and so is the order of the output rows: lane
+// (g, t) takes 8 consecutive dimensions of token g for K, and of tokens 2t, 2t+1, 2t+8, 2t+9 for V, whose pairs two
+// byte permutes bring together.
+//
+// P is split into two 16-bit parts (p = hi + lo) and multiplied twice: the tensor pipe is idle anyway and the result
+// then carries the output's own rounding only.
+#include "attend_device.cuh"
+
+namespace aafkv {
+
+template <int DP> struct FewShape {
+    static constexpr int KC = 2 * (DP / 32);        // 16-byte pieces of K per lane and tile of 16 tokens
+    static constexpr int VC = 4 * (DP / 64);        // of V
+    static constexpr int SLOTS = KC + VC;
+    static constexpr int STAGE_BYTES = SLOTS * 32 * 16;
+    static constexpr int WARPS = DP <= 128 ? 8 : 6;
+    static constexpr int STAGES = DP == 64 ? 6 : (DP == 128 ? 3 : 2);
+    static constexpr int SMEM = WARPS * STAGES * STAGE_BYTES;  // 192 KB: one CTA an SM
+    static_assert(SMEM <= 227 * 1024, "shared memory of a CTA");
+};
+
+template <typename T, int DP, int NT>
+__global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 1)
+    attend_few_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small) {
+    using S = FewShape<DP>;
+    extern __shared__ __align__(16) char smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int g = lane >> 2, t4 = lane & 3;
+    const long long task = (long long)blockIdx.x * S::WARPS + warp;
+    if (task >= (long long)p.total_units * p.H) return;
+    const int unit = (int)(task / p.H), head = (int)(task - (long long)unit * p.H);
+    const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
+    const AttnSeq sq = seqs[find_seq(seqs, p.n, unit)];
+    const int part = unit - sq.unit0;
+    const int R = sq.nq * p.G;
+
+    // rows of this lane: columns 2 t4, 2 t4 + 1 of every n-tile
+    RowSpan span[NT][2];
+    float slope[NT][2];
+    int lo_all = 0x7fffffff, hi_all = 0;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int r = nt * 8 + 2 * t4 + c;
+            span[nt][c] = row_span(p, sq, min(r, R - 1) / p.G);
+            slope[nt][c] = p.slopes ? p.slopes[head * p.G + min(r, R - 1) % p.G] : 0.0f;
+            if (span[nt][c].hi > span[nt][c].lo) {
+                lo_all = min(lo_all, span[nt][c].lo);
+                hi_all = max(hi_all, span[nt][c].hi);
+            }
+        }
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) {
+        lo_all = min(lo_all, __shfl_xor_sync(0xffffffffu, lo_all, d));
+        hi_all = max(hi_all, __shfl_xor_sync(0xffffffffu, hi_all, d));
+    }
+    // the part's keys: the host cut [first, len) into chunks, first being what the window leaves of the earliest row
+    const int first = p.window ? max(0, sq.len - sq.nq + 1 - p.window) : 0;
+    const long long c0 = first + (long long)part * sq.chunk;
+    int beg = (int)max((long long)lo_all, c0), end = (int)min((long long)hi_all, c0 + sq.chunk);
+    if (end <= beg) beg = end = 0;  // nothing to see in this part: no token index is formed from an empty range
+    const int tiles = (end - beg + 15) / 16;
+
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S::STAGES * S::STAGE_BYTES) + lane * 16;
+    const int *table = p.tables + (long long)sq.ctx * p.max_blk;
+    const char *kb = p.kbase + (long long)head * p.D * 2;
+
+    auto table_id = [&](int tile) -> int {  // lane l: block of the tile's token l % 16
+        const int t = beg + tile * 16 + (lane & 15);
+        return t < end ? __ldg(table + block_of(t, p.BS, p.bs_shift)) : 0;
+    };
+    auto issue = [&](int tile, int id) {
+        if (tile < tiles) {
+            const int tm = beg + tile * 16 + (lane & 15);
+            const int b = block_of(tm, p.BS, p.bs_shift);
+            const long long off = (long long)id * 2 * p.run + (long long)(tm - b * p.BS) * p.row;
+            const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const char *src = kb + __shfl_sync(0xffffffffu, off, g + 8 * i);
+                const bool ok = beg + tile * 16 + g + 8 * i < end;
+#pragma unroll
+                for (int kk = 0; kk < DP / 32; ++kk) {
+                    const int d = kk * 32 + t4 * 8;
+                    const bool in = ok && d < p.D;
+                    copy16(st + (i * (DP / 32) + kk) * 512, in ? src + d * 2 : kb, in ? 16 : 0);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int tk = 2 * t4 + (i & 1) + (i >> 1) * 8;
+                const char *src = kb + p.run + __shfl_sync(0xffffffffu, off, tk);
+                const bool ok = beg + tile * 16 + tk < end;
+#pragma unroll
+                for (int c = 0; c < DP / 64; ++c) {
+                    const int d = c * 64 + g * 8;
+                    const bool in = ok && d < p.D;
+                    copy16(st + (S::KC + i * (DP / 64) + c) * 512, in ? src + d * 2 : kb, in ? 16 : 0);
+                }
+            }
+        }
+        copy_commit();
+    };
+
+    int id = table_id(0);
+#pragma unroll
+    for (int s = 0; s < S::STAGES; ++s) {
+        const int nxt = table_id(s + 1);
+        issue(s, id);
+        id = nxt;
+    }
+
+    // query fragments: row nt * 8 + g, 8 dimensions at kk * 32 + t4 * 8
+    uint4 qf[NT][DP / 32];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int r = nt * 8 + g;
+        const T *q = static_cast<const T *>(p.q) + (long long)(sq.row0 + min(r, R - 1) / p.G) * p.q_stride +
+                     (long long)(head * p.G + min(r, R - 1) % p.G) * p.D;
+#pragma unroll
+        for (int kk = 0; kk < DP / 32; ++kk) {
+            const int d = kk * 32 + t4 * 8;
+            qf[nt][kk] = r < R && d < p.D ? __ldg(reinterpret_cast<const uint4 *>(q + d)) : make_uint4(0, 0, 0, 0);
+        }
+    }
+
+    float o[NT][DP / 16][4];
+    float m[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        m[nt][0] = m[nt][1] = -CUDART_INF_F;
+        l[nt][0] = l[nt][1] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.0f;
+    }
+
+    for (int tile = 0; tile < tiles; ++tile) {
+        copy_wait<S::STAGES - 1>();
+        const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
+        const int tb = beg + tile * 16;
+        float s[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
+#pragma unroll
+        for (int kk = 0; kk < DP / 32; ++kk) {
+            const uint4 w = lds16(st + kk * 512), x = lds16(st + (DP / 32 + kk) * 512);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                Elt<T>::mma(s[nt], w.x, x.x, w.y, x.y, qf[nt][kk].x, qf[nt][kk].y);
+                Elt<T>::mma(s[nt], w.z, x.z, w.w, x.w, qf[nt][kk].z, qf[nt][kk].w);
+            }
+        }
+        uint32_t ph[NT][2], pl[NT][2], vis[NT][2];
+        bool partial = false;  // some row misses a token of the tile that is within the part
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float mx[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const RowSpan &sp = span[nt][c];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int t = tb + g + 8 * h;
+                    const bool see = t >= sp.lo && t < sp.hi && t < end;
+                    partial |= !see && t < end;
+                    const float v = score2(p, s[nt][2 * h + c], slope[nt][c], sp, t);
+                    s[nt][2 * h + c] = see ? v : -CUDART_INF_F;
+                }
+                mx[c] = fmaxf(s[nt][c], s[nt][2 + c]);
+            }
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) {
+                mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], d));
+                mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], d));
+            }
+            const float n0 = fmaxf(m[nt][0], mx[0]), n1 = fmaxf(m[nt][1], mx[1]);
+            if (__any_sync(0xffffffffu, n0 > m[nt][0] || n1 > m[nt][1])) {  // a new maximum: rescale what is summed
+                const float a0 = n0 == -CUDART_INF_F ? 1.0f : ex2(m[nt][0] - n0);
+                const float a1 = n1 == -CUDART_INF_F ? 1.0f : ex2(m[nt][1] - n1);
+                l[nt][0] *= a0;
+                l[nt][1] *= a1;
+#pragma unroll
+                for (int i = 0; i < DP / 16; ++i) {
+                    o[nt][i][0] *= a0;
+                    o[nt][i][1] *= a1;
+                    o[nt][i][2] *= a0;
+                    o[nt][i][3] *= a1;
+                }
+                m[nt][0] = n0;
+                m[nt][1] = n1;
+            }
+            const float b0 = n0 == -CUDART_INF_F ? 0.0f : n0, b1 = n1 == -CUDART_INF_F ? 0.0f : n1;
+            const float p0 = ex2(s[nt][0] - b0), p1 = ex2(s[nt][1] - b1);
+            const float p2 = ex2(s[nt][2] - b0), p3 = ex2(s[nt][3] - b1);
+            l[nt][0] += p0 + p2;
+            l[nt][1] += p1 + p3;
+            const uint32_t h01 = Elt<T>::pack(p0, p1), h23 = Elt<T>::pack(p2, p3);
+            const uint32_t l01 = Elt<T>::pack(p0 - Elt<T>::lo(h01), p1 - Elt<T>::hi(h01));
+            const uint32_t l23 = Elt<T>::pack(p2 - Elt<T>::lo(h23), p3 - Elt<T>::hi(h23));
+            ph[nt][0] = transpose8x8(h01);
+            ph[nt][1] = transpose8x8(h23);
+            pl[nt][0] = transpose8x8(l01);
+            pl[nt][1] = transpose8x8(l23);
+            const uint32_t one = Elt<T>::ONE;
+            vis[nt][0] = (s[nt][0] != -CUDART_INF_F ? one : 0u) | (s[nt][1] != -CUDART_INF_F ? one << 16 : 0u);
+            vis[nt][1] = (s[nt][2] != -CUDART_INF_F ? one : 0u) | (s[nt][3] != -CUDART_INF_F ? one << 16 : 0u);
+        }
+        partial = __any_sync(0xffffffffu, partial);
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c) {
+            uint4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = lds16(st + (S::KC + i * (DP / 64) + c) * 512);
+            const uint32_t w0[4] = {v[0].x, v[0].y, v[0].z, v[0].w}, w1[4] = {v[1].x, v[1].y, v[1].z, v[1].w};
+            const uint32_t w2[4] = {v[2].x, v[2].y, v[2].z, v[2].w}, w3[4] = {v[3].x, v[3].y, v[3].z, v[3].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t a[4] = {prmt(w0[j], w1[j], 0x5410), prmt(w0[j], w1[j], 0x7632), prmt(w2[j], w3[j], 0x5410),
+                                 prmt(w2[j], w3[j], 0x7632)};
+                if (partial) {
+                    uint32_t f[4];
+                    bool odd = false;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        f[i] = finite_only<T>(a[i]);
+                        odd |= f[i] != a[i];
+                    }
+                    if (__any_sync(0xffffffffu, odd)) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            add4(o[nt][4 * c + j],
+                                 nonfinite_a<T>(a[0], a[1], a[2], a[3], transpose8x8(vis[nt][0]), transpose8x8(vis[nt][1])));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) a[i] = f[i];
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    Elt<T>::mma(o[nt][4 * c + j], a[0], a[1], a[2], a[3], ph[nt][0], ph[nt][1]);
+                    Elt<T>::mma(o[nt][4 * c + j], a[0], a[1], a[2], a[3], pl[nt][0], pl[nt][1]);
+                }
+            }
+        }
+        const int nxt = table_id(tile + S::STAGES + 1);
+        issue(tile + S::STAGES, id);
+        id = nxt;
+    }
+    copy_wait<0>();
+
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float sum = l[nt][c];
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            const int r = nt * 8 + 2 * t4 + c;
+            if (r >= R) continue;
+            if (sq.part0 >= 0) {  // a part of a longer range: (m, l, o) for the join
+                const long long pr = sq.part0 + ((long long)part * p.H + head) * R + r;
+#pragma unroll
+                for (int cc = 0; cc < DP / 64; ++cc) {
+                    const int d = cc * 64 + g * 8;
+                    if (d >= p.D) continue;
+                    float4 *dst = reinterpret_cast<float4 *>(p.part_o + pr * p.D + d);
+                    dst[0] = make_float4(o[nt][4 * cc][c], o[nt][4 * cc][2 + c], o[nt][4 * cc + 1][c], o[nt][4 * cc + 1][2 + c]);
+                    dst[1] = make_float4(o[nt][4 * cc + 2][c], o[nt][4 * cc + 2][2 + c], o[nt][4 * cc + 3][c], o[nt][4 * cc + 3][2 + c]);
+                }
+                if (g == 0) {
+                    p.part_ml[2 * pr] = m[nt][c];
+                    p.part_ml[2 * pr + 1] = sum;
+                }
+                continue;
+            }
+            const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;  // a row that sees nothing is zero
+            const long long qt = sq.row0 + r / p.G;
+            const int hq = head * p.G + r % p.G;
+            T *out = static_cast<T *>(p.out) + (qt * p.H * p.G + hq) * p.D;
+#pragma unroll
+            for (int cc = 0; cc < DP / 64; ++cc) {
+                const int d = cc * 64 + g * 8;
+                if (d >= p.D) continue;
+                uint4 w;
+                w.x = Elt<T>::pack(o[nt][4 * cc][c] * inv, o[nt][4 * cc][2 + c] * inv);
+                w.y = Elt<T>::pack(o[nt][4 * cc + 1][c] * inv, o[nt][4 * cc + 1][2 + c] * inv);
+                w.z = Elt<T>::pack(o[nt][4 * cc + 2][c] * inv, o[nt][4 * cc + 2][2 + c] * inv);
+                w.w = Elt<T>::pack(o[nt][4 * cc + 3][c] * inv, o[nt][4 * cc + 3][2 + c] * inv);
+                *reinterpret_cast<uint4 *>(out + d) = w;
+            }
+            if (p.lse && g == 0)
+                p.lse[qt * p.H * p.G + hq] =
+                    sum == 0.0f ? -CUDART_INF_F : (m[nt][c] + log2f(sum)) * LN2 - slope[nt][c] * (float)span[nt][c].near;
+        }
+}
+
+int few_rows_limit(int D) { return D <= 64 ? 32 : (D <= 128 ? 16 : 8); }
+
+template <typename T, int DP, int NT>
+static cudaError_t few_go(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
+    const cudaError_t e = cudaFuncSetAttribute(attend_few_kernel<T, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               FewShape<DP>::SMEM);
+    if (e != cudaSuccess) return e;
+    const long long tasks = (long long)p.total_units * p.H;
+    constexpr int W = FewShape<DP>::WARPS;
+    attend_few_kernel<T, DP, NT><<<(unsigned)((tasks + W - 1) / W), W * 32, FewShape<DP>::SMEM, st>>>(p, small);
+    return cudaGetLastError();
+}
+template <typename T> static cudaError_t few_pick(const AttnParams &p, const SmallSeqs &small, int max_rows, cudaStream_t st) {
+    if (p.D <= 64)
+        return max_rows <= 8 ? few_go<T, 64, 1>(p, small, st)
+                             : (max_rows <= 16 ? few_go<T, 64, 2>(p, small, st) : few_go<T, 64, 4>(p, small, st));
+    if (p.D <= 128) return max_rows <= 8 ? few_go<T, 128, 1>(p, small, st) : few_go<T, 128, 2>(p, small, st);
+    return few_go<T, 256, 1>(p, small, st);
+}
+cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, cudaStream_t st) {
+    return f16 ? few_pick<__half>(p, small, max_rows, st) : few_pick<__nv_bfloat16>(p, small, max_rows, st);
+}
+
+// ------------------------------------------------------------------------------------------ join
+// Adds up the parts of a split row: o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.  One CTA per query token and
+// query head; 8 warps take every eighth part, four dimensions a lane (DP / 128 passes), and meet in shared memory in
+// warp order.
+constexpr int JOIN_WARPS = 8;
+template <typename T>
+__global__ void __launch_bounds__(JOIN_WARPS * 32)
+    attend_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small, int tile_rows) {
+    __shared__ float4 acc_s[JOIN_WARPS][32];
+    __shared__ float sum_s[JOIN_WARPS], max_s[JOIN_WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
+    const int Hq = p.H * p.G;
+    const long long qt = blockIdx.x / Hq;
+    const int hq = (int)(blockIdx.x - qt * Hq), head = hq / p.G;
+    int lo = 0, hi = p.n - 1;  // sequence of the query token
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (seqs[mid].row0 <= qt) lo = mid; else hi = mid - 1;
+    }
+    const AttnSeq sq = seqs[lo];
+    if (sq.part0 < 0 || qt < sq.row0 || qt >= sq.row0 + sq.nq) return;  // not split, or of the batch's other kernel
+    const int j = (int)(qt - sq.row0), r = j * p.G + hq % p.G;
+    // partial rows of a sequence: [part][head][R] for the few-row kernel, [tile][part][head][tile_rows] for the tile kernel
+    long long row, step;
+    if (tile_rows) {
+        row = sq.part0 + ((long long)(r / tile_rows) * sq.nsplit * p.H + head) * tile_rows + r % tile_rows;
+        step = (long long)p.H * tile_rows;
+    } else {
+        const int R = sq.nq * p.G;
+        row = sq.part0 + (long long)head * R + r;
+        step = (long long)p.H * R;
+    }
+    float top = -CUDART_INF_F;
+    for (int s = threadIdx.x; s < sq.nsplit; s += JOIN_WARPS * 32) top = fmaxf(top, p.part_ml[2 * (row + s * step)]);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    if (lane == 0) max_s[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < JOIN_WARPS; ++w) top = fmaxf(top, max_s[w]);
+    const float base = top == -CUDART_INF_F ? 0.0f : top;
+    T *out = static_cast<T *>(p.out) + (qt * Hq + hq) * p.D;
+    for (int d0 = 0; d0 < p.D; d0 += 128) {
+        const int d = d0 + lane * 4;
+        float4 a = make_float4(0, 0, 0, 0);
+        float sum = 0.0f;
+#pragma unroll 4
+        for (int s = warp; s < sq.nsplit; s += JOIN_WARPS) {
+            const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * (row + s * step));
+            const float4 v = d < p.D ? *reinterpret_cast<const float4 *>(p.part_o + (row + s * step) * p.D + d)
+                                     : make_float4(0, 0, 0, 0);
+            const float w = ex2(ml.x - base);  // a part that saw nothing has m = -inf, l = 0, o = 0
+            sum += w * ml.y;
+            a.x += w * v.x;
+            a.y += w * v.y;
+            a.z += w * v.z;
+            a.w += w * v.w;
+        }
+        __syncthreads();
+        acc_s[warp][lane] = a;
+        if (lane == 0) sum_s[warp] = sum;
+        __syncthreads();
+        if (warp == 0) {
+#pragma unroll
+            for (int w = 1; w < JOIN_WARPS; ++w) {
+                const float4 v = acc_s[w][lane];
+                a.x += v.x;
+                a.y += v.y;
+                a.z += v.z;
+                a.w += v.w;
+                sum += sum_s[w];
+            }
+            const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+            if (d < p.D)
+                *reinterpret_cast<uint2 *>(out + d) =
+                    make_uint2(Elt<T>::pack(a.x * inv, a.y * inv), Elt<T>::pack(a.z * inv, a.w * inv));
+            if (d0 == 0 && lane == 0 && p.lse) {
+                const RowSpan sp = row_span(p, sq, j);
+                const float slope = p.slopes ? p.slopes[hq] : 0.0f;
+                p.lse[qt * Hq + hq] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * LN2 - slope * (float)sp.near;
+            }
+        }
+    }
+}
+
+cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int total_q,
+                               cudaStream_t st) {
+    const unsigned grid = (unsigned)((long long)total_q * p.H * p.G);
+    if (f16)
+        attend_join_kernel<__half><<<grid, JOIN_WARPS * 32, 0, st>>>(p, small, tile_rows);
+    else
+        attend_join_kernel<__nv_bfloat16><<<grid, JOIN_WARPS * 32, 0, st>>>(p, small, tile_rows);
+    return cudaGetLastError();
+}
+
+}  // namespace aafkv

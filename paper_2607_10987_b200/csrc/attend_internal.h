@@ -1,0 +1,97 @@
+// Declarations shared by the kernels that compute with the pool's bytes (attention over the block tables, the
+// attention mass of cached tokens, rotary stores, token pruning) and their host side in pool.cu.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "aafkv_internal.h"
+
+namespace aafkv {
+
+// One sequence of an attention batch.  Its queries are the last nq tokens of the context; row r of a kv head is
+// query token r / G, head r % G of the head's group.  Units are what the kernels are launched over; they are
+// numbered over the batch, unit0 is the sequence's first.
+struct AttnSeq {          // 32 bytes
+    int ctx;
+    int len;              // tokens of the context (an int: max_ctx * max_blk and the block size bound it, see pool.cu)
+    int nq;
+    int row0;             // first query token of the sequence in the packed batch
+    int unit0;            // first unit
+    int nsplit;           // parts that the key range of a row tile is cut into
+    int chunk;            // few-row kernel: keys of a part
+    int part0;            // first row of the sequence's partial results, -1: written straight to the output
+};
+static_assert(sizeof(AttnSeq) == 32, "AttnSeq layout");
+constexpr int SMALL_SEQS = 64;  // sequences that travel as kernel parameters
+struct SmallSeqs {
+    AttnSeq e[SMALL_SEQS];
+};
+
+struct AttnParams {
+    const void *q;
+    void *out;
+    float *lse;           // may be null
+    float *part_o;        // [partial rows][D]
+    float *part_ml;       // [partial rows][2]: running maximum (log2 domain) and sum
+    const AttnSeq *seqs;  // device records, null: the kernel parameter holds them
+    const int *tables;
+    const char *kbase;    // layer's first byte
+    const float *slopes;  // per query head, may be null
+    const int *spans;     // [query tokens][2], may be null
+    long long q_stride;   // elements between query tokens
+    long long run, row;   // bytes
+    int max_blk, BS, bs_shift;  // bs_shift: log2 of the block size, -1 if it is no power of two
+    int H, G, D, n, total_units;
+    int window;           // 0: none
+    float scale, softcap, inv_cap;  // softcap 0: none
+};
+
+struct MassParams {
+    AttnParams a;
+    const float *lse_in;
+    const float *prev;    // may be null
+    float *mass;
+    long long mass_stride;
+    int chunk;            // keys of one CTA
+};
+
+struct StoreSeq {         // 24 bytes
+    int ctx, len, n_new, row0, pad0, pad1;
+};
+struct SmallStores {
+    StoreSeq e[SMALL_SEQS];
+};
+struct StoreParams {
+    const void *q, *k, *v;
+    void *q_out;
+    long long q_stride, q_out_stride, k_stride, v_stride;  // elements between tokens
+    const double *inv_freq;
+    const long long *pos;
+    const StoreSeq *seqs;
+    const int *tables;
+    char *kbase;
+    long long run, row;
+    int max_blk, BS, bs_shift;
+    int Hq, H, D, rot, interleaved, n, total;
+    float mscale;
+};
+
+// ---- launchers (each returns cudaGetLastError() of its launches); f16: 1 = half, 0 = bfloat16
+constexpr int FEW_MAX_DIM = 256;
+int few_rows_limit(int D);                       // most rows of a kv head that the few-row kernel takes
+constexpr int TILE_ROWS = 64;                    // rows of a unit of the tile kernel
+constexpr int MASS_CHUNK = 64;                   // keys of a CTA of the mass kernel
+constexpr int MASS_MAX_HEADS = 512;              // its kv heads: chunk * heads floats of shared memory
+cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, cudaStream_t st);
+cudaError_t launch_attend_tile(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
+cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int total_q,
+                               cudaStream_t st);
+cudaError_t launch_attn_mass(const MassParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
+cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16, cudaStream_t st);
+// keep list of a pruned context: kept[budget] ascending, kept_scores (may be null); then the row gather
+cudaError_t launch_select(const float *scores, int len, int budget, int sink, int recent, int *kept, float *kept_scores,
+                          cudaStream_t st);
+cudaError_t launch_gather_rows(const Geom &g, const int *src_table, const int *dst_table, const int *kept, int budget,
+                               int sm_count, cudaStream_t st);
+
+}  // namespace aafkv

@@ -213,7 +213,14 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_import_kernel(Geom g, DevSt
     if (ok)
         for (int i = threadIdx.x; i < n; i += blockDim.x) {
             atomicAdd(&s.ctl->payload_bytes, (unsigned long long)(ent[i].n * 2 * g.L * g.row));
-            if (s.cat_len) catalog_born(s, ent[i].ctx, ent[i].n, clock + ent[i].out_index, 1, -1);
+            if (s.cat_len) {
+                const int parent = ent[i].parent;
+                catalog_born(s, ent[i].ctx, ent[i].n, clock + ent[i].out_index, parent >= 0 ? AAF_ORIGIN_PRUNE : AAF_ORIGIN_BUFFER, parent);
+                if (parent >= 0) {  // a pruned state reads the one it descends from
+                    s.cat_reuse[parent] += 1;
+                    s.cat_last[parent] = clock + ent[i].out_index;
+                }
+            }
         }
     __syncthreads();  // every thread has read head0 before it moves
     if (threadIdx.x == 0) {
@@ -382,6 +389,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_append_kernel(Geom g, DevSt
             table[jpos] = b;
         } else {  // the partial tail: the copy if there is one, else written in place
             b = cow ? ring_at(s.ring, first, g.NB) : tailb[i];
+        }
+        if (!e.src) {  // slots without a payload (reserve): nothing to copy
+            clear_piece(s.pieces[sl]);
+            continue;
         }
         const long long tlo = max(T, jpos * g.BS), thi = min(T + e.n_new, (jpos + 1) * g.BS);
         s.pieces[sl] = make_piece(e.src + (tlo - T) * g.row, 2ll * e.n_new * g.row, (long long)e.n_new * g.row,
@@ -872,9 +883,9 @@ cudaError_t launch_plan_import_batch(const Geom &g, const DevState &s, const Imp
     return cudaGetLastError();
 }
 cudaError_t launch_plan_import(const Geom &g, const DevState &s, int ctx, long long n, const char *src,
-                               long long clock, cudaStream_t st) {
+                               long long clock, cudaStream_t st, int parent) {
     SmallImp one{};
-    one.e[0].src = src; one.e[0].n = n; one.e[0].ctx = ctx;
+    one.e[0].src = src; one.e[0].n = n; one.e[0].ctx = ctx; one.e[0].parent = parent;
     return launch_plan_import_batch(g, s, nullptr, one, 1, (int)((n + g.BS - 1) / g.BS), clock, st);
 }
 cudaError_t launch_fork(const Geom &g, const DevState &s, int parent, long long T, int k, const int *children_dev,

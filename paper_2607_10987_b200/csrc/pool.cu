@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "aafkv_internal.h"
+#include "attend_internal.h"
 
 // Profiler ranges: built with -DAAFKV_NVTX every C-ABI operator call is an NVTX range named after the entry
 // point (header-only NVTX 3, no extra library); without the switch the macro is empty.
@@ -46,7 +47,7 @@ static_assert(sizeof(ComposeSeg) <= ARG_RECORD_BYTES && sizeof(AppendEntry) <= A
               "argument records must fit their room in the pinned ring");
 
 struct Layout {
-    size_t ctl, refcount, ring, last_pos, tables, pieces, scratch, cat_len, cat_reuse, cat_last, cat_score, cat_origin, cat_parent, cat_born, cat_parent_born, tile_count, total;
+    size_t ctl, refcount, ring, last_pos, tables, pieces, scratch, cat_len, cat_reuse, cat_last, cat_score, cat_origin, cat_parent, cat_born, cat_parent_born, tile_count, seq_records, total;
     int max_pieces, max_batch;
 };
 
@@ -85,6 +86,8 @@ Layout make_layout(const aaf_kv_pool_desc *d) {
     L.cat_parent_born = off; off = align_up(off + sizeof(long long) * (size_t)d->max_ctx, 256);
     L.tile_count = off;
     off = align_up(off + sizeof(int) * ((size_t)d->max_ctx * d->max_blocks_per_ctx / 8192 + 2), 256);
+    L.seq_records = off;  // sequence records of an attention / store batch too large for kernel parameters
+    off = align_up(off + sizeof(AttnSeq) * 2 * (size_t)L.max_batch, 256);
     L.total = off;
     return L;
 }
@@ -116,6 +119,9 @@ struct aaf_kv_pool {
     bool broken = false;  // a CUDA call failed after device state had changed: every later call returns AAF_ERR_CUDA
     CopyTuning tuning{};
     std::vector<long long> len;  // tokens per handle, -1 = free
+    // first token of a context whose slot no other context can share: what aaf_kv_store may write.  A fork or a sharing
+    // merge moves it to the context's end; tokens added later are in blocks that the append copied or took afresh.
+    std::vector<long long> own_from;
     int live_ctx = 0;
     long long free_lb = 0;       // guaranteed lower bound of the device's free-block count
     long long clock = 0;         // logical clock: successful state-touching calls so far
@@ -132,6 +138,12 @@ struct aaf_kv_pool {
     // copy launch, that stream is made to wait for the previous operator's last copy launch first.
     cudaStream_t last_copy_stream = nullptr;
     cudaEvent_t last_copy_event = nullptr;
+    // Kernels that compute with the pool (attention, stores, gathers of a prune) read block tables on the caller's
+    // stream: they wait for the metadata launched so far, and the next kernel that changes metadata waits for them.
+    cudaEvent_t meta_ev = nullptr, read_ev = nullptr;
+    long long meta_mark = -1;  // meta_launches when meta_ev was recorded
+    bool meta_drained = false; // meta_ev has been seen complete
+    bool read_pending = false;
     // pinned argument ring
     char *args = nullptr;
     size_t slot_bytes = 0;
@@ -245,7 +257,14 @@ struct PlanSlot {
 
 // Before a planner: pick the next piece buffer and make the metadata stream wait until the copy launch
 // that last read that buffer has finished.
+// Before any kernel that changes tables, reference counts or the ring: the readers on the caller's stream come first.
+void after_readers(aaf_kv_pool *p) {
+    if (!p->read_pending) return;
+    cudaStreamWaitEvent(p->meta_stream, p->read_ev, 0);
+    p->read_pending = false;
+}
 PlanSlot begin_plan(aaf_kv_pool *p) {
+    after_readers(p);
     PlanSlot ps;
     ps.buf = p->next_buf;
     ps.view = p->s;
@@ -264,6 +283,43 @@ void end_copy(aaf_kv_pool *p, const PlanSlot &ps, cudaStream_t st) {
     p->last_copy_stream = st;
     p->last_copy_event = p->copy_done[ps.buf];
     p->next_buf ^= 1;
+}
+
+// Before a kernel on `st` that reads block tables or payload: it comes after the pool's earlier payload work, whatever
+// stream that was on, and after the metadata launched so far.
+bool begin_read(aaf_kv_pool *p, cudaStream_t st) {
+    if (p->last_copy_event && cudaStreamWaitEvent(st, p->last_copy_event, 0) != cudaSuccess) return false;
+    if (p->meta_mark != p->meta_launches) {
+        if (cudaEventRecord(p->meta_ev, p->meta_stream) != cudaSuccess) return false;
+        p->meta_mark = p->meta_launches;
+        p->meta_drained = false;
+    }
+    if (!p->meta_drained) {
+        const cudaError_t e = cudaEventQuery(p->meta_ev);
+        if (e == cudaSuccess) {
+            p->meta_drained = true;
+        } else {
+            cudaGetLastError();
+            if (e != cudaErrorNotReady || cudaStreamWaitEvent(st, p->meta_ev, 0) != cudaSuccess) return false;
+        }
+    }
+    return true;
+}
+bool end_read(aaf_kv_pool *p, cudaStream_t st) {
+    if (cudaEventRecord(p->read_ev, st) != cudaSuccess) return false;
+    p->read_pending = true;
+    p->last_copy_stream = st;
+    p->last_copy_event = p->read_ev;
+    return true;
+}
+// A call reads host arrays and orders the pool's streams, neither of which a replayed graph would do again.
+bool capturing(cudaStream_t st) {
+    cudaStreamCaptureStatus s = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &s) != cudaSuccess) {
+        cudaGetLastError();
+        return true;
+    }
+    return s != cudaStreamCaptureStatusNone;
 }
 
 int run_copy(aaf_kv_pool *p, const PlanSlot &ps, int cls, int n_slots, long long payload_tokens, cudaStream_t st,
@@ -356,6 +412,7 @@ int import_impl(aaf_kv_pool *p, const void *src_dev, const aaf_kv_xfer_desc *des
     p->meta_launches += 1;
     p->free_lb -= nb;
     p->len[c] = n;
+    p->own_from[c] = 0;
     p->live_ctx += 1;
     *out_ctx = c;
     const int rc = run_copy(p, ps, AAF_OP_IMPORT, (int)nb, n, st);
@@ -467,6 +524,7 @@ int aaf_kv_pool_create(const aaf_kv_pool_desc *desc, aaf_kv_pool **out) {
     p->s.cat_parent_born = reinterpret_cast<long long *>(ws + lay.cat_parent_born);
     p->s.tile_count = reinterpret_cast<int *>(ws + lay.tile_count);
     p->len.assign((size_t)desc->max_ctx, -1);
+    p->own_from.assign((size_t)desc->max_ctx, 0);
     p->free_lb = desc->n_blocks;
 
     bool ok = cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device) == cudaSuccess;
@@ -480,6 +538,8 @@ int aaf_kv_pool_create(const aaf_kv_pool_desc *desc, aaf_kv_pool **out) {
     for (int i = 0; ok && i < 2; ++i)
         ok = cudaEventCreateWithFlags(&p->plan_done[i], cudaEventDisableTiming) == cudaSuccess &&
              cudaEventCreateWithFlags(&p->copy_done[i], cudaEventDisableTiming) == cudaSuccess;
+    ok = ok && cudaEventCreateWithFlags(&p->meta_ev, cudaEventDisableTiming) == cudaSuccess &&
+         cudaEventCreateWithFlags(&p->read_ev, cudaEventDisableTiming) == cudaSuccess;
     ok = ok && cudaHostAlloc(reinterpret_cast<void **>(&p->result), sizeof(int) * ((size_t)desc->max_ctx + 2),
                              cudaHostAllocMapped) == cudaSuccess;
     // device state: counters, reference counts 0, ring, evict scratch -1
@@ -527,6 +587,8 @@ int aaf_kv_pool_destroy(aaf_kv_pool *p) {
         if (p->plan_done[i]) cudaEventDestroy(p->plan_done[i]);
         if (p->copy_done[i]) cudaEventDestroy(p->copy_done[i]);
     }
+    if (p->meta_ev) cudaEventDestroy(p->meta_ev);
+    if (p->read_ev) cudaEventDestroy(p->read_ev);
     if (p->meta_stream) cudaStreamDestroy(p->meta_stream);
     for (int i = 0; i < ARG_SLOTS; ++i)
         if (p->slot_ev[i]) cudaEventDestroy(p->slot_ev[i]);
@@ -650,7 +712,7 @@ int aaf_kv_import_batch(aaf_kv_pool *p, int32_t n, const void *const *src_dev, c
         ImpEntry &e = ent[i];
         e.src = static_cast<const char *>(src_dev[i]);
         e.n = descs[i].n_tokens;
-        e.ctx = c; e.block_off = off; e.out_index = i; e.pad = 0;
+        e.ctx = c; e.block_off = off; e.out_index = i; e.parent = -1;
         off += (int)nblk_of(p, e.n);
     }
     const PlanSlot ps = begin_plan(p);
@@ -663,7 +725,10 @@ int aaf_kv_import_batch(aaf_kv_pool *p, int32_t n, const void *const *src_dev, c
     p->clock += n;
     p->meta_launches += 1;
     p->free_lb -= blocks;
-    for (int i = 0; i < n; ++i) p->len[out_ctxs[i]] = descs[i].n_tokens;
+    for (int i = 0; i < n; ++i) {
+        p->len[out_ctxs[i]] = descs[i].n_tokens;
+        p->own_from[out_ctxs[i]] = 0;
+    }
     p->live_ctx += n;
     const int rc = run_copy(p, ps, AAF_OP_IMPORT, (int)blocks, tokens, st);
     end_copy(p, ps, st);
@@ -771,6 +836,7 @@ int aaf_kv_import_host_chunked(aaf_kv_pool *p, const void *src_host, const aaf_k
     p->meta_launches += 1;
     p->free_lb -= nb;
     p->len[c] = n;
+    p->own_from[c] = 0;
     p->live_ctx += 1;
     *out_ctx = c;
     const int BS = p->g.BS, per_chunk = chunk_tokens / BS;
@@ -812,6 +878,7 @@ int aaf_kv_fork(aaf_kv_pool *p, aaf_ctx_t parent, int32_t k, aaf_ctx_t *out_chil
         children[j] = c;
     }
     const long long T = p->len[parent];
+    after_readers(p);
     const cudaError_t e = launch_fork(p->g, p->s, parent, T, k, by_value ? nullptr : children, small, p->clock + 1,
                                       p->meta_stream);
     if (!by_value) release_args(p, p->meta_stream);
@@ -820,8 +887,10 @@ int aaf_kv_fork(aaf_kv_pool *p, aaf_ctx_t parent, int32_t k, aaf_ctx_t *out_chil
     p->meta_launches += 1;
     for (int j = 0; j < k; ++j) {
         p->len[children[j]] = T;
+        p->own_from[children[j]] = T;
         out_children[j] = children[j];
     }
+    p->own_from[parent] = T;
     p->live_ctx += k;
     return AAF_OK;
 }
@@ -841,22 +910,25 @@ static int append_check(const aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, 
     return AAF_OK;
 }
 
-int aaf_kv_append(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_new,
-                  const void *const *src_dev, void *stream) {
-    AAF_RANGE("aaf_kv_append");
-    if (!p || n < 1 || !ctxs || !n_new || !src_dev) return AAF_ERR_INVALID_ARG;
+// src_dev == nullptr: the new slots get no payload (aaf_kv_reserve)
+static int append_impl(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_new,
+                       const void *const *src_dev, void *stream) {
     if (p->broken) return AAF_ERR_CUDA;
     {
         const int rc = append_check(p, n, ctxs, n_new);
         if (rc != AAF_OK) return rc;
     }
-    for (int i = 0; i < n; ++i)
-        if (!aligned16(src_dev[i])) return AAF_ERR_INVALID_ARG;
+    bool copies = src_dev != nullptr;  // a shared partial tail is copied, whatever the payload
+    for (int i = 0; i < n; ++i) {
+        if (src_dev && !aligned16(src_dev[i])) return AAF_ERR_INVALID_ARG;
+        const long long T = p->len[ctxs[i]];
+        copies |= T % p->g.BS != 0 && p->own_from[ctxs[i]] > T / p->g.BS * p->g.BS;
+    }
     const int BS = p->g.BS;
     long long worst = 0, slots = 0, append_tokens = 0;  // append_tokens: new tokens plus the copy-on-write worst case
     for (int i = 0; i < n; ++i) {
         const long long T = p->len[ctxs[i]];
-        append_tokens += n_new[i] + T % BS;
+        append_tokens += (src_dev ? n_new[i] : 0) + T % BS;
         worst += (T % BS ? 1 : 0) + nblk_of(p, T + n_new[i]) - nblk_of(p, T);
         slots += 1 + nblk_of(p, T + n_new[i]) - T / BS;
     }
@@ -873,7 +945,7 @@ int aaf_kv_append(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const int32_
     int off = 0;
     for (int i = 0; i < n; ++i) {
         const long long T = p->len[ctxs[i]];
-        ent[i].src = static_cast<const char *>(src_dev[i]);
+        ent[i].src = src_dev ? static_cast<const char *>(src_dev[i]) : nullptr;
         ent[i].T = T;
         ent[i].ctx = ctxs[i];
         ent[i].n_new = n_new[i];
@@ -912,9 +984,22 @@ int aaf_kv_append(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const int32_
     p->meta_launches += 1;
     p->free_lb -= charge;
     for (int i = 0; i < n; ++i) p->len[ctxs[i]] += n_new[i];
-    const int rc_copy = run_copy(p, ps, AAF_OP_APPEND, (int)slots, append_tokens, st);
+    const int rc_copy = copies ? run_copy(p, ps, AAF_OP_APPEND, (int)slots, append_tokens, st) : AAF_OK;
     end_copy(p, ps, st);
     return rc_copy;
+}
+
+int aaf_kv_append(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_new,
+                  const void *const *src_dev, void *stream) {
+    AAF_RANGE("aaf_kv_append");
+    if (!p || n < 1 || !ctxs || !n_new || !src_dev) return AAF_ERR_INVALID_ARG;
+    return append_impl(p, n, ctxs, n_new, src_dev, stream);
+}
+
+int aaf_kv_reserve(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_new, void *stream) {
+    AAF_RANGE("aaf_kv_reserve");
+    if (!p || n < 1 || !ctxs || !n_new) return AAF_ERR_INVALID_ARG;
+    return append_impl(p, n, ctxs, n_new, nullptr, stream);
 }
 
 int aaf_kv_append_host(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_new,
@@ -1030,8 +1115,11 @@ static int compose_impl(aaf_kv_pool *p, int32_t n_out, const int32_t *seg_off, c
     p->free_lb -= fresh;
     for (int o = 0; o < n_out; ++o) {
         p->len[handles[(size_t)o]] = out_len[(size_t)o];
+        p->own_from[handles[(size_t)o]] = copy_all ? 0 : out_len[(size_t)o];
         out_ctxs[o] = handles[(size_t)o];
     }
+    if (!copy_all)
+        for (int i = 0; i < m; ++i) p->own_from[segs[i]] = p->len[segs[i]];
     p->live_ctx += n_out;
     const int rc_copy = run_copy(p, ps, AAF_OP_COMPOSE, (int)slots, copied_tokens, st);
     end_copy(p, ps, st);
@@ -1095,6 +1183,7 @@ int aaf_kv_evict(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, void *stream)
         a->total = (int)total;
     }
     int n_launches = 0;
+    after_readers(p);
     const cudaError_t e = launch_evict(p->g, p->s, a, small, n, (int)total, p->clock + 1, &n_launches, p->meta_stream);
     if (a) release_args(p, p->meta_stream);
     if (e != cudaSuccess) return broke(p);
@@ -1124,6 +1213,7 @@ int aaf_kv_evict_to_budget(aaf_kv_pool *p, double alpha, double beta, double gam
     DeviceGuard guard(p->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     p->last_stream = st;
+    after_readers(p);
     if (launch_evict_to_budget(p->g, p->s, alpha, beta, gamma, budget_blocks, p->clock + 1, p->result,
                                p->meta_stream) != cudaSuccess)
         return broke(p);
@@ -1140,6 +1230,361 @@ int aaf_kv_evict_to_budget(aaf_kv_pool *p, double alpha, double beta, double gam
     p->live_ctx -= nv;
     p->free_lb = p->result[1];  // exact
     *n_victims = nv;
+    return AAF_OK;
+}
+
+// ---- operators that compute with the payload: checks, the cut of the work into units, launches ----------------------
+}  // extern "C"
+namespace {
+
+constexpr long long PART_ROWS = 65536;  // rows of partial results that a workspace holds
+
+size_t attend_ws_bytes(const aaf_kv_pool *p) { return (size_t)PART_ROWS * ((size_t)p->g.D + 2) * sizeof(float); }
+
+bool dtype_ok(int dtype) { return dtype == AAF_DTYPE_BF16 || dtype == AAF_DTYPE_F16; }
+bool is_finite(float x) { return x - x == 0.0f; }
+int log2_of(int v) {
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return (1 << s) == v ? s : -1;
+}
+
+// what attention and attention mass have in common; *total_q, *max_rows describe the batch
+int attn_check(const aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n, const aaf_ctx_t *ctxs,
+               const int32_t *n_q, const void *q, long long *total_q) {
+    if (!a || a->struct_size != sizeof(aaf_kv_attn) || n < 1 || !ctxs || !aligned16(q)) return AAF_ERR_INVALID_ARG;
+    if (layer < 0 || layer >= p->g.L || !dtype_ok(a->dtype)) return AAF_ERR_INVALID_ARG;
+    if (p->g.E != 2 || p->g.D % 8 != 0 || p->g.D > AAF_ATTN_MAX_HEAD_DIM) return AAF_ERR_INCOMPAT;
+    if (a->n_q_heads < 1 || a->n_q_heads % p->g.H != 0 || a->window < 0) return AAF_ERR_INVALID_ARG;
+    if (!is_finite(a->scale) || !is_finite(a->softcap) || a->softcap < 0.0f) return AAF_ERR_INVALID_ARG;
+    if (a->q_stride % 8 != 0 || a->q_stride < (long long)a->n_q_heads * p->g.D) return AAF_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(a->slopes) & 3u) || (reinterpret_cast<uintptr_t>(a->spans) & 3u)) return AAF_ERR_INVALID_ARG;
+    if (n > p->lay.max_batch) return AAF_ERR_TOO_MANY;
+    long long total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (!is_live(p, ctxs[i])) return AAF_ERR_BAD_CTX;
+        const int nq = n_q ? n_q[i] : 1;
+        if (nq < 1 || nq > p->len[ctxs[i]]) return AAF_ERR_INVALID_ARG;
+        if (p->len[ctxs[i]] > (1ll << 30)) return AAF_ERR_TOO_LONG;  // token indices are ints in the kernels
+        if ((long long)nq * (a->n_q_heads / p->g.H) > (1ll << 30)) return AAF_ERR_TOO_LONG;
+        total += nq;
+    }
+    if (total * a->n_q_heads > (1ll << 31) - 1) return AAF_ERR_TOO_MANY;  // one CTA of the join per token and head
+    *total_q = total;
+    return AAF_OK;
+}
+
+AttnParams attn_params(const aaf_kv_pool *p, int layer, const aaf_kv_attn *a, const void *q) {
+    AttnParams k{};
+    k.q = q;
+    k.tables = p->s.tables;
+    k.kbase = p->g.pool + (long long)layer * p->g.layer_stride;
+    k.slopes = a->slopes;
+    k.spans = a->spans;
+    k.q_stride = a->q_stride;
+    k.run = p->g.run; k.row = p->g.row;
+    k.max_blk = p->g.max_blk; k.BS = p->g.BS; k.bs_shift = log2_of(p->g.BS);
+    k.H = p->g.H; k.G = a->n_q_heads / p->g.H; k.D = p->g.D;
+    k.window = a->window;
+    k.scale = a->scale; k.softcap = a->softcap;
+    k.inv_cap = a->softcap > 0.0f ? 1.0f / a->softcap : 0.0f;
+    return k;
+}
+
+// Records of a batch: kernel parameters while they fit, else through the pinned ring into the pool's workspace on `st`
+// (the copies and their readers of all calls are ordered by begin_read / end_read).
+template <typename Rec, typename Small>
+bool place_records(aaf_kv_pool *p, const std::vector<Rec> &rec, Small &small, const Rec **dev, int which, cudaStream_t st) {
+    static_assert(sizeof(Rec) <= sizeof(AttnSeq), "records share the workspace of the attention records");
+    *dev = nullptr;
+    if (rec.size() <= (size_t)SMALL_SEQS) {
+        std::copy(rec.begin(), rec.end(), small.e);
+        return true;
+    }
+    char *pinned = acquire_args(p);
+    const size_t bytes = sizeof(Rec) * rec.size();
+    memcpy(pinned, rec.data(), bytes);
+    char *dst = reinterpret_cast<char *>(p->desc.workspace) + p->lay.seq_records + sizeof(AttnSeq) * (size_t)p->lay.max_batch * which;
+    const bool ok = cudaMemcpyAsync(dst, pinned, bytes, cudaMemcpyHostToDevice, st) == cudaSuccess;
+    release_args(p, st);
+    *dev = reinterpret_cast<const Rec *>(dst);
+    return ok;
+}
+
+}  // namespace
+extern "C" {
+
+size_t aaf_kv_attend_workspace_bytes(const aaf_kv_pool *p) { return p ? attend_ws_bytes(p) : 0; }
+
+int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n, const aaf_ctx_t *ctxs,
+                  const int32_t *n_q, const void *q_dev, void *out_dev, float *lse_dev, void *workspace_dev,
+                  size_t workspace_bytes, void *stream) {
+    AAF_RANGE("aaf_kv_attend");
+    if (!p) return AAF_ERR_INVALID_ARG;
+    if (p->broken) return AAF_ERR_CUDA;
+    long long total_q = 0;
+    const int rc = attn_check(p, layer, a, n, ctxs, n_q, q_dev, &total_q);
+    if (rc != AAF_OK) return rc;
+    if (!aligned16(out_dev) || (reinterpret_cast<uintptr_t>(lse_dev) & 3u) || !aligned16(workspace_dev)) return AAF_ERR_INVALID_ARG;
+    if (workspace_bytes < attend_ws_bytes(p)) return AAF_ERR_DST_TOO_SMALL;
+    DeviceGuard guard(p->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (capturing(st)) return AAF_ERR_INVALID_ARG;
+    AttnParams k = attn_params(p, layer, a, q_dev);
+    k.out = out_dev;
+    k.lse = lse_dev;
+    k.part_o = static_cast<float *>(workspace_dev);
+    k.part_ml = k.part_o + PART_ROWS * p->g.D;
+    const int G = k.G, H = k.H, limit = few_rows_limit(p->g.D);
+    // sequences with few query rows per kv head and those with many go to kernels of their own
+    std::vector<AttnSeq> few, many;
+    int row0 = 0, few_rows = 1;
+    long long keys = 0;  // keys that the few-row kernel reads
+    for (int i = 0; i < n; ++i) {
+        AttnSeq s{};
+        s.ctx = ctxs[i];
+        s.len = (int)p->len[ctxs[i]];
+        s.nq = n_q ? n_q[i] : 1;
+        s.row0 = row0;
+        s.nsplit = 1;
+        s.part0 = -1;
+        row0 += s.nq;
+        if (s.nq * G <= limit) {
+            few.push_back(s);
+            few_rows = std::max(few_rows, s.nq * G);
+            keys += s.len - (k.window ? std::max(0, s.len - s.nq + 1 - k.window) : 0);
+        } else {
+            many.push_back(s);
+        }
+    }
+    long long part_rows = 0;
+    bool few_joined = false, many_joined = false;
+    int few_units = 0, many_units = 0;
+    if (!few.empty()) {
+        // Parts of equal length over the batch, so many that every warp the GPU holds has about three, at least 64 keys
+        // each: a part costs a row of partial results, an SM that gets ahead takes more of them.
+        const long long warps = 3ll * p->sm_count * 8;
+        long long chunk = std::max<long long>(64, (keys * H + warps - 1) / warps);
+        for (;;) {
+            chunk = (chunk + 15) / 16 * 16;
+            long long rows = 0;
+            for (const AttnSeq &s : few) {
+                const long long range = s.len - (k.window ? std::max(0, s.len - s.nq + 1 - k.window) : 0);
+                const long long parts = (range + chunk - 1) / chunk;
+                if (parts > 1) rows += parts * H * s.nq * G;
+            }
+            if (rows <= PART_ROWS / 2) break;
+            chunk *= 2;
+        }
+        for (AttnSeq &s : few) {
+            const long long range = s.len - (k.window ? std::max(0, s.len - s.nq + 1 - k.window) : 0);
+            s.nsplit = (int)((range + chunk - 1) / chunk);
+            s.chunk = (int)(((range + s.nsplit - 1) / s.nsplit + 15) / 16 * 16);
+            s.unit0 = few_units;
+            few_units += s.nsplit;
+            if (s.nsplit > 1) {
+                s.part0 = (int)part_rows;
+                part_rows += (long long)s.nsplit * H * s.nq * G;
+                few_joined = true;
+            }
+        }
+    }
+    if (!many.empty()) {
+        long long ctas = 0;
+        for (const AttnSeq &s : many) ctas += ((long long)s.nq * G + TILE_ROWS - 1) / TILE_ROWS * H;
+        // few row tiles: the keys are cut so that each SM has two CTAs, at least 256 keys a part
+        const long long want = std::max<long long>(1, 2ll * p->sm_count / ctas);
+        for (AttnSeq &s : many) {
+            const long long tiles = ((long long)s.nq * G + TILE_ROWS - 1) / TILE_ROWS;
+            const long long range = s.len - (k.window ? std::max(0, s.len - s.nq + 1 - k.window) : 0);
+            long long parts = std::min(want, (range + 255) / 256);
+            while (parts > 1 && part_rows + tiles * parts * H * TILE_ROWS > PART_ROWS) --parts;
+            s.nsplit = (int)parts;
+            s.unit0 = many_units;
+            if ((long long)many_units + tiles * parts > (1ll << 30) / H) return AAF_ERR_TOO_MANY;
+            many_units += (int)(tiles * parts);
+            if (parts > 1) {
+                s.part0 = (int)part_rows;
+                part_rows += tiles * parts * H * TILE_ROWS;
+                many_joined = true;
+            }
+        }
+    }
+    p->last_stream = st;
+    if (!begin_read(p, st)) return broke(p);
+    const int f16 = a->dtype == AAF_DTYPE_F16;
+    bool ok = true;
+    if (!few.empty()) {
+        SmallSeqs small;
+        AttnParams kf = k;
+        kf.n = (int)few.size();
+        kf.total_units = few_units;
+        ok = place_records(p, few, small, &kf.seqs, 0, st) && launch_attend_few(kf, small, f16, few_rows, st) == cudaSuccess;
+        if (ok && few_joined) ok = launch_attend_join(kf, small, f16, 0, (int)total_q, st) == cudaSuccess;
+    }
+    if (ok && !many.empty()) {
+        SmallSeqs small;
+        AttnParams km = k;
+        km.n = (int)many.size();
+        km.total_units = many_units;
+        ok = place_records(p, many, small, &km.seqs, 1, st) && launch_attend_tile(km, small, f16, st) == cudaSuccess;
+        if (ok && many_joined) ok = launch_attend_join(km, small, f16, TILE_ROWS, (int)total_q, st) == cudaSuccess;
+    }
+    return ok && end_read(p, st) ? AAF_OK : broke(p);
+}
+
+int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n, const aaf_ctx_t *ctxs,
+                     const int32_t *n_q, const void *q_dev, const float *lse_dev, const float *prev_dev, float *mass_dev,
+                     int64_t mass_stride, void *stream) {
+    AAF_RANGE("aaf_kv_attn_mass");
+    if (!p) return AAF_ERR_INVALID_ARG;
+    if (p->broken) return AAF_ERR_CUDA;
+    long long total_q = 0;
+    const int rc = attn_check(p, layer, a, n, ctxs, n_q, q_dev, &total_q);
+    if (rc != AAF_OK) return rc;
+    if (!lse_dev || !mass_dev || ((reinterpret_cast<uintptr_t>(lse_dev) | reinterpret_cast<uintptr_t>(prev_dev) |
+                                   reinterpret_cast<uintptr_t>(mass_dev)) & 3u))
+        return AAF_ERR_INVALID_ARG;
+    for (int i = 0; i < n; ++i)
+        if (mass_stride < p->len[ctxs[i]]) return AAF_ERR_DST_TOO_SMALL;
+    if (p->g.H > MASS_MAX_HEADS) return AAF_ERR_INCOMPAT;
+    DeviceGuard guard(p->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (capturing(st)) return AAF_ERR_INVALID_ARG;
+    MassParams k{};
+    k.a = attn_params(p, layer, a, q_dev);
+    k.lse_in = lse_dev;
+    k.prev = prev_dev;
+    k.mass = mass_dev;
+    k.mass_stride = mass_stride;
+    k.chunk = MASS_CHUNK;
+    std::vector<AttnSeq> rec((size_t)n);
+    long long units = 0;
+    int row0 = 0;
+    for (int i = 0; i < n; ++i) {
+        AttnSeq &s = rec[(size_t)i];
+        s = AttnSeq{};
+        s.ctx = ctxs[i];
+        s.len = (int)p->len[ctxs[i]];
+        s.nq = n_q ? n_q[i] : 1;
+        s.row0 = row0;
+        s.unit0 = (int)units;
+        s.nsplit = (s.len + k.chunk - 1) / k.chunk;
+        row0 += s.nq;
+        units += s.nsplit;
+        if (units > (1ll << 30)) return AAF_ERR_TOO_MANY;
+    }
+    k.a.n = n;
+    k.a.total_units = (int)units;
+    p->last_stream = st;
+    if (!begin_read(p, st)) return broke(p);
+    SmallSeqs small;
+    const bool ok = place_records(p, rec, small, &k.a.seqs, 0, st) &&
+                    launch_attn_mass(k, small, a->dtype == AAF_DTYPE_F16, st) == cudaSuccess && end_read(p, st);
+    return ok ? AAF_OK : broke(p);
+}
+
+int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int32_t n, const aaf_ctx_t *ctxs,
+                 const int32_t *n_new, void *stream) {
+    AAF_RANGE("aaf_kv_store");
+    if (!p || !d || d->struct_size != sizeof(aaf_kv_store_desc) || n < 1 || !ctxs || !n_new) return AAF_ERR_INVALID_ARG;
+    if (p->broken) return AAF_ERR_CUDA;
+    if (layer < 0 || layer >= p->g.L || !dtype_ok(d->dtype)) return AAF_ERR_INVALID_ARG;
+    if (p->g.E != 2 || p->g.D % 8 != 0) return AAF_ERR_INCOMPAT;
+    if (!aligned16(d->k) || !aligned16(d->v) || d->n_q_heads < 0) return AAF_ERR_INVALID_ARG;
+    if (d->n_q_heads > 0 && (!aligned16(d->q) || !aligned16(d->q_out))) return AAF_ERR_INVALID_ARG;
+    const long long kv_min = (long long)p->g.H * p->g.D, q_min = (long long)d->n_q_heads * p->g.D;
+    if (d->k_stride < kv_min || d->v_stride < kv_min || d->k_stride % 8 || d->v_stride % 8) return AAF_ERR_INVALID_ARG;
+    if (d->n_q_heads > 0 && (d->q_stride < q_min || d->q_out_stride < q_min || d->q_stride % 8 || d->q_out_stride % 8))
+        return AAF_ERR_INVALID_ARG;
+    if (d->rot_dim < 0 || d->rot_dim % 2 || d->rot_dim > p->g.D || d->rot_dim > AAF_ROPE_MAX_DIM || !is_finite(d->mscale))
+        return AAF_ERR_INVALID_ARG;
+    if (d->rot_dim > 0 && (!d->inv_freq || (reinterpret_cast<uintptr_t>(d->inv_freq) & 7u))) return AAF_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(d->pos) & 7u) return AAF_ERR_INVALID_ARG;
+    if (n > p->lay.max_batch) return AAF_ERR_TOO_MANY;
+    std::vector<StoreSeq> rec((size_t)n);
+    std::vector<int> sorted(ctxs, ctxs + n);
+    std::sort(sorted.begin(), sorted.end());
+    long long total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (!is_live(p, ctxs[i])) return AAF_ERR_BAD_CTX;
+        const long long T = p->len[ctxs[i]];
+        if (n_new[i] < 1 || n_new[i] > T) return AAF_ERR_INVALID_ARG;
+        if (T > (1ll << 30)) return AAF_ERR_TOO_LONG;
+        if (T - n_new[i] < p->own_from[ctxs[i]]) return AAF_ERR_INVALID_ARG;  // slots that other contexts may share
+        StoreSeq &s = rec[(size_t)i];
+        s = StoreSeq{};
+        s.ctx = ctxs[i];
+        s.len = (int)T;
+        s.n_new = n_new[i];
+        s.row0 = (int)total;
+        total += n_new[i];
+        if (total > (1ll << 30)) return AAF_ERR_TOO_MANY;
+    }
+    if (std::adjacent_find(sorted.begin(), sorted.end()) != sorted.end()) return AAF_ERR_INVALID_ARG;
+    DeviceGuard guard(p->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (capturing(st)) return AAF_ERR_INVALID_ARG;
+    StoreParams k{};
+    k.q = d->n_q_heads ? d->q : nullptr;
+    k.q_out = d->q_out; k.k = d->k; k.v = d->v;
+    k.q_stride = d->q_stride; k.q_out_stride = d->q_out_stride; k.k_stride = d->k_stride; k.v_stride = d->v_stride;
+    k.inv_freq = d->inv_freq;
+    k.pos = reinterpret_cast<const long long *>(d->pos);
+    k.tables = p->s.tables;
+    k.kbase = p->g.pool + (long long)layer * p->g.layer_stride;
+    k.run = p->g.run; k.row = p->g.row;
+    k.max_blk = p->g.max_blk; k.BS = p->g.BS; k.bs_shift = log2_of(p->g.BS);
+    k.Hq = d->n_q_heads; k.H = p->g.H; k.D = p->g.D; k.rot = d->rot_dim; k.interleaved = d->interleaved != 0;
+    k.n = n; k.total = (int)total; k.mscale = d->mscale;
+    p->last_stream = st;
+    if (!begin_read(p, st)) return broke(p);
+    SmallStores small;
+    const bool ok = place_records(p, rec, small, &k.seqs, 0, st) &&
+                    launch_store(k, small, d->dtype == AAF_DTYPE_F16, st) == cudaSuccess && end_read(p, st);
+    return ok ? AAF_OK : broke(p);
+}
+
+int aaf_kv_prune(aaf_kv_pool *p, aaf_ctx_t ctx, const float *scores_dev, int64_t budget, int64_t sink, int64_t recent,
+                 int32_t *kept_dev, float *kept_scores_dev, aaf_ctx_t *out_ctx, void *stream) {
+    AAF_RANGE("aaf_kv_prune");
+    if (!p || !scores_dev || !kept_dev || !out_ctx) return AAF_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(scores_dev) | reinterpret_cast<uintptr_t>(kept_dev) |
+         reinterpret_cast<uintptr_t>(kept_scores_dev)) & 3u)
+        return AAF_ERR_INVALID_ARG;
+    if (p->broken) return AAF_ERR_CUDA;
+    if (!is_live(p, ctx)) return AAF_ERR_BAD_CTX;
+    const long long T = p->len[ctx];
+    if (T > (1ll << 30)) return AAF_ERR_TOO_LONG;
+    if (budget < 1 || budget > T || sink < 0 || recent < 0 || sink > budget || recent > budget - sink) return AAF_ERR_INVALID_ARG;
+    const int c = smallest_free_ctx(p);
+    if (c < 0) return AAF_ERR_OOM_CTX;
+    DeviceGuard guard(p->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (capturing(st)) return AAF_ERR_INVALID_ARG;
+    const long long nb = nblk_of(p, budget);
+    const int rc0 = ensure_free(p, nb, st);
+    if (rc0 != AAF_OK) return rc0;
+    p->last_stream = st;
+    const PlanSlot ps = begin_plan(p);
+    // the new context's table, blocks and catalog entry; its piece list (no buffer behind it) is not run
+    if (launch_plan_import(p->g, ps.view, c, budget, nullptr, p->clock + 1, p->meta_stream, ctx) != cudaSuccess ||
+        !end_plan(p, ps, st))
+        return broke(p);
+    p->clock += 1;
+    p->meta_launches += 1;
+    p->free_lb -= nb;
+    p->len[c] = budget;
+    p->own_from[c] = 0;
+    p->live_ctx += 1;
+    const int *tables = p->s.tables;
+    const bool ok = begin_read(p, st) &&
+                    launch_select(scores_dev, (int)T, (int)budget, (int)sink, (int)recent, kept_dev, kept_scores_dev, st) == cudaSuccess &&
+                    launch_gather_rows(p->g, tables + (long long)ctx * p->g.max_blk, tables + (long long)c * p->g.max_blk, kept_dev,
+                                       (int)budget, p->sm_count, st) == cudaSuccess;
+    end_copy(p, ps, st);
+    if (!ok || !end_read(p, st)) return broke(p);
+    *out_ctx = c;
     return AAF_OK;
 }
 
