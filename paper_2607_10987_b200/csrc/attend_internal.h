@@ -43,6 +43,9 @@ struct AttnParams {
     int max_blk, BS, bs_shift;  // bs_shift: log2 of the block size, -1 if it is no power of two
     int H, G, D, n, total_units;
     int window;           // 0: none
+    int epoch;            // what `flag` holds when a CTA of the wide kernel has met values it cannot keep apart
+    int *flag;            // wide kernel: written; tile kernel: run only if it holds `epoch` (null: always)
+    int *status;          // sticky device status of the pool
     float scale, softcap, inv_cap;  // softcap 0: none
 };
 
@@ -84,6 +87,14 @@ constexpr int MASS_CHUNK = 64;                   // keys of a CTA of the mass ke
 constexpr int MASS_MAX_HEADS = 512;              // its kv heads: chunk * heads floats of shared memory
 cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, cudaStream_t st);
 cudaError_t launch_attend_tile(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
+constexpr int WIDE_ROWS = 256;                   // rows of a unit of the wide kernel
+bool wide_takes(int D, int BS);                  // pool geometries of the wide kernel
+cudaError_t launch_attend_wide(const AttnParams &p, const SmallSeqs &small, int f16, const void *map, int layer,
+                               cudaStream_t st);
+struct alignas(64) PoolMap {                     // a tensor map, opaque to the host side
+    unsigned char bytes[128];
+};
+bool encode_pool_map(const Geom &g, PoolMap *out);
 cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int total_q,
                                cudaStream_t st);
 cudaError_t launch_attn_mass(const MassParams &p, const SmallSeqs &small, int f16, cudaStream_t st);

@@ -32,7 +32,9 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
     using S = TileShape<DP>;
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t4 = lane & 3;
-    const int unit = blockIdx.x / p.H, head = blockIdx.x - unit * p.H;
+    if (p.flag && *p.flag != p.epoch) return;  // a second run that is not needed
+    for (long long cta = blockIdx.x; cta < (long long)p.total_units * p.H; cta += gridDim.x) {
+    const int unit = (int)(cta / p.H), head = (int)(cta - (long long)unit * p.H);
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
     const AttnSeq sq = seqs[find_seq(seqs, p.n, unit)];
     const int R = sq.nq * p.G, n_tiles = (R + TILE_ROWS - 1) / TILE_ROWS;
@@ -261,13 +263,17 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
             p.lse[qt * p.H * p.G + hq] =
                 sum == 0.0f ? -CUDART_INF_F : (m[h] + log2f(sum)) * LN2 - slope[h] * (float)span[h].near;
     }
+    __syncthreads();  // the next unit loads over this one's tiles
+    }
 }
 
 template <typename T, int DP> static cudaError_t tile_go(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
     const cudaError_t e =
         cudaFuncSetAttribute(attend_tile_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<DP>::SMEM);
     if (e != cudaSuccess) return e;
-    attend_tile_kernel<T, DP><<<(unsigned)((long long)p.total_units * p.H), TILE_WARPS * 32, TileShape<DP>::SMEM, st>>>(p, small);
+    long long ctas = (long long)p.total_units * p.H;
+    if (p.flag && ctas > 296) ctas = 296;
+    attend_tile_kernel<T, DP><<<(unsigned)ctas, TILE_WARPS * 32, TileShape<DP>::SMEM, st>>>(p, small);
     return cudaGetLastError();
 }
 template <typename T> static cudaError_t tile_pick(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {

@@ -87,7 +87,7 @@ Layout make_layout(const aaf_kv_pool_desc *d) {
     L.tile_count = off;
     off = align_up(off + sizeof(int) * ((size_t)d->max_ctx * d->max_blocks_per_ctx / 8192 + 2), 256);
     L.seq_records = off;  // sequence records of an attention / store batch too large for kernel parameters
-    off = align_up(off + sizeof(AttnSeq) * 2 * (size_t)L.max_batch, 256);
+    off = align_up(off + sizeof(AttnSeq) * 3 * (size_t)L.max_batch, 256);
     L.total = off;
     return L;
 }
@@ -144,6 +144,9 @@ struct aaf_kv_pool {
     long long meta_mark = -1;  // meta_launches when meta_ev was recorded
     bool meta_drained = false; // meta_ev has been seen complete
     bool read_pending = false;
+    PoolMap map;               // tensor map of the pool memory (wide attention kernel)
+    bool map_ok = false;
+    int epoch = 0;             // counts calls of the wide kernel
     // pinned argument ring
     char *args = nullptr;
     size_t slot_bytes = 0;
@@ -529,6 +532,7 @@ int aaf_kv_pool_create(const aaf_kv_pool_desc *desc, aaf_kv_pool **out) {
 
     bool ok = cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device) == cudaSuccess;
     ok = ok && copy_tuning_init(p->g.run, &p->tuning) == cudaSuccess;
+    p->map_ok = p->g.E == 2 && wide_takes(p->g.D, p->g.BS) && encode_pool_map(p->g, &p->map);
     p->slot_bytes = align_up(ARG_RECORD_BYTES * (size_t)lay.max_batch + 256, 256);
     ok = ok && cudaHostAlloc(reinterpret_cast<void **>(&p->args), p->slot_bytes * ARG_SLOTS, cudaHostAllocMapped) ==
                    cudaSuccess;
@@ -1239,7 +1243,7 @@ namespace {
 
 constexpr long long PART_ROWS = 65536;  // rows of partial results that a workspace holds
 
-size_t attend_ws_bytes(const aaf_kv_pool *p) { return (size_t)PART_ROWS * ((size_t)p->g.D + 2) * sizeof(float); }
+size_t attend_ws_bytes(const aaf_kv_pool *p) { return (size_t)PART_ROWS * ((size_t)p->g.D + 2) * sizeof(float) + 16; }
 
 bool dtype_ok(int dtype) { return dtype == AAF_DTYPE_BF16 || dtype == AAF_DTYPE_F16; }
 bool is_finite(float x) { return x - x == 0.0f; }
@@ -1389,23 +1393,30 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
             }
         }
     }
+    const bool wide = !many.empty() && p->map_ok;
+    const int rows_of = wide ? WIDE_ROWS : TILE_ROWS;
+    std::vector<AttnSeq> again;  // the batch for the 64-row kernel, should the wide one meet values it cannot keep apart
+    int again_units = 0;
     if (!many.empty()) {
         long long ctas = 0;
-        for (const AttnSeq &s : many) ctas += ((long long)s.nq * G + TILE_ROWS - 1) / TILE_ROWS * H;
-        // few row tiles: the keys are cut so that each SM has two CTAs, at least 256 keys a part
-        const long long want = std::max<long long>(1, 2ll * p->sm_count / ctas);
+        for (const AttnSeq &s : many) ctas += ((long long)s.nq * G + rows_of - 1) / rows_of * H;
+        // few row tiles: the keys are cut so that each SM has a CTA (two of the 64-row kernel), at least 256 keys a part
+        const long long want = std::max<long long>(1, (wide ? 1ll : 2ll) * p->sm_count / ctas);
         for (AttnSeq &s : many) {
-            const long long tiles = ((long long)s.nq * G + TILE_ROWS - 1) / TILE_ROWS;
+            const long long tiles = ((long long)s.nq * G + rows_of - 1) / rows_of;
             const long long range = s.len - (k.window ? std::max(0, s.len - s.nq + 1 - k.window) : 0);
             long long parts = std::min(want, (range + 255) / 256);
-            while (parts > 1 && part_rows + tiles * parts * H * TILE_ROWS > PART_ROWS) --parts;
+            while (parts > 1 && part_rows + tiles * parts * H * rows_of > PART_ROWS) --parts;
+            s.unit0 = again_units;
+            if (wide) again.push_back(s);
+            again_units += (int)(((long long)s.nq * G + TILE_ROWS - 1) / TILE_ROWS);
             s.nsplit = (int)parts;
             s.unit0 = many_units;
-            if ((long long)many_units + tiles * parts > (1ll << 30) / H) return AAF_ERR_TOO_MANY;
+            if ((long long)many_units + tiles * parts > (1ll << 30) / H || again_units > (1 << 30) / H) return AAF_ERR_TOO_MANY;
             many_units += (int)(tiles * parts);
             if (parts > 1) {
                 s.part0 = (int)part_rows;
-                part_rows += tiles * parts * H * TILE_ROWS;
+                part_rows += tiles * parts * H * rows_of;
                 many_joined = true;
             }
         }
@@ -1427,8 +1438,24 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
         AttnParams km = k;
         km.n = (int)many.size();
         km.total_units = many_units;
-        ok = place_records(p, many, small, &km.seqs, 1, st) && launch_attend_tile(km, small, f16, st) == cudaSuccess;
-        if (ok && many_joined) ok = launch_attend_join(km, small, f16, TILE_ROWS, (int)total_q, st) == cudaSuccess;
+        km.status = &p->s.ctl->status;
+        ok = place_records(p, many, small, &km.seqs, 1, st);
+        if (wide) {
+            km.flag = reinterpret_cast<int *>(k.part_ml + 2 * PART_ROWS);
+            km.epoch = p->epoch = p->epoch % 0x7fffffff + 1;
+            ok = ok && launch_attend_wide(km, small, f16, &p->map, layer, st) == cudaSuccess;
+        } else {
+            ok = ok && launch_attend_tile(km, small, f16, st) == cudaSuccess;
+        }
+        if (ok && many_joined) {
+            AttnParams kj = km;
+            kj.flag = nullptr;
+            ok = launch_attend_join(kj, small, f16, rows_of, (int)total_q, st) == cudaSuccess;
+        }
+        if (ok && wide) {
+            km.total_units = again_units;
+            ok = place_records(p, again, small, &km.seqs, 2, st) && launch_attend_tile(km, small, f16, st) == cudaSuccess;
+        }
     }
     return ok && end_read(p, st) ? AAF_OK : broke(p);
 }

@@ -112,6 +112,47 @@ def test_masks_as_spans(dim):
     assert (out[3::7] == 0).all() and (lse[3::7] == -math.inf).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("block", [8, 16, 32, 64, 128])
+def test_extend_long_prompts(block, dim, dtype):
+    # several 256-row units, keys cut into parts for the short ones, block sizes that divide a key tile differently
+    case(2, 4, dim, block, [1500, 777, 5000, 130], n_q=[700, 777, 30, 129], dtype=dtype)
+
+
+@pytest.mark.parametrize("group,n_q,lens", [(1, [256, 257, 100], [256, 3000, 129]), (3, [86, 43], [2000, 43]), (7, [300], [301]),
+                                            (32, [4, 33], [1000, 1000]), (128, [2, 3], [400, 128])])
+def test_extend_groups_that_do_not_divide_the_tile(group, n_q, lens):
+    case(1, group, 128, 16, lens, n_q=n_q)
+    case(2, group, 64, 16, lens, n_q=n_q)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("scale", [-0.1, 0.0, 2.0])
+def test_extend_scales(scale, dim):
+    case(1, 2, dim, 16, [900, 400], n_q=[400, 90], scale=scale)
+    case(1, 2, dim, 16, [900, 400], scale=scale)
+
+
+@pytest.mark.parametrize("n_q", [1, 4, 300])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_scores_that_keep_growing_along_the_keys(dim, n_q):
+    # every few tiles the running maximum outgrows what has been summed by far more than a rescale's threshold
+    t = 2000
+    pool = R.make_pool(1, 1, dim, 16, 256)
+    q = R.rand((n_q, 2, dim), 3)
+    rows = R.rand((1, 2, t, 1, dim), 4)
+    ramp = torch.linspace(0, 6, t, device="cuda")[:, None, None]
+    rows[0, 0] = (rows[0, 0].float() * 0.1 + ramp * q[0, :1].float().sign()).to(torch.bfloat16)
+    c = R.add_ctx(pool, t, 0, rows)
+    got = run_attend(pool, [c], [n_q], q)
+    R.check_attend(got, R.attend_ref([c], [n_q], q), torch.bfloat16, dim, p_rounded=n_q > 4)
+
+
+def test_extend_many_sequences():
+    case(1, 4, 64, 16, [20 + 9 * i for i in range(80)], n_q=[10 + i % 11 for i in range(80)])
+
+
 def test_empty_span_of_single_tokens():
     spans = torch.tensor([[5, 5], [0, 40], [100, 7]], dtype=torch.int32, device="cuda")
     _, _, _, (out, lse) = case(2, 4, 64, 16, [80, 40, 900], spans=spans)
