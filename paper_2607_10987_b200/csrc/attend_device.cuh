@@ -190,6 +190,8 @@ __device__ __forceinline__ int find_seq(const AttnSeq *s, int n, int unit) {
     return lo;
 }
 
+// query token of a row
+__device__ __forceinline__ int token_of(const AttnParams &p, int row) { return p.g_shift >= 0 ? row >> p.g_shift : row / p.G; }
 __device__ __forceinline__ int block_of(int t, int BS, int shift) { return shift >= 0 ? t >> shift : t / BS; }
 
 }  // namespace aafkv

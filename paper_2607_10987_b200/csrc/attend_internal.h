@@ -41,7 +41,7 @@ struct AttnParams {
     long long q_stride;   // elements between query tokens
     long long run, row;   // bytes
     int max_blk, BS, bs_shift;  // bs_shift: log2 of the block size, -1 if it is no power of two
-    int H, G, D, n, total_units;
+    int H, G, D, g_shift, n, total_units;  // g_shift as bs_shift, of G
     int window;           // 0: none
     int epoch;            // what `flag` holds when a CTA of the wide kernel has met values it cannot keep apart
     int *flag;            // wide kernel: written; tile kernel: run only if it holds `epoch` (null: always)

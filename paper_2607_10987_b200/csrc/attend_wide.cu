@@ -10,8 +10,9 @@
 //   - a thread owns a row: its maximum and sum need no exchange.  O is rescaled only when a row's maximum has grown by
 //     more than 2^8 since the last time, which costs nothing in accuracy (all sums are in 32 bits, a weight of up to 2^8
 //     keeps its digits) and leaves the outputs alone in almost every tile;
-//   - one warp copies pages with tiled bulk copies (one per page and 64 dimensions, 128-byte swizzle, five stages), one
-//     issues the products, two look at V tiles before they are multiplied.
+//   - a warp for K and one for V copy blocks with tiled bulk copies (one per block and 64 dimensions, 128-byte swizzle, five
+//     stages; a copy takes about 85 cycles to issue, one warp for both would be as slow as the products), two warps issue
+//     the products, one for each row tile.
 // Key tiles start on a block boundary, so a copied box is always a whole block; rows of V outside the keys that the
 // CTA's rows see are set to zero (0 * garbage is not 0), and a value that is not finite in a tile that some rows see and
 // others do not raises `flag`: the caller then runs the 64-row kernel over the batch, which keeps such rows apart.
@@ -20,19 +21,22 @@
 // Every wait is bounded; one that gives up records AAF_ERR_TIMEOUT and ends the kernel.
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "attend_device.cuh"
 
 namespace aafkv {
 
 constexpr int WIDE_TILE = 128, WIDE_KEYS = 128;
-constexpr int WIDE_THREADS = 384;
+constexpr int WIDE_THREADS = 384;  // 8 warps for the weights, 4 for copies, products and the look at V
 constexpr int WAIT_LIMIT = 1 << 20;
 
 template <int D> struct WideShape {
     static constexpr int HALVES = D / 64;
     static constexpr int TILE_BYTES = HALVES * 128 * 128;  // 128 rows of D 16-bit elements, 64 dims a half
     static constexpr int STAGES = D == 128 ? 5 : 10;
-    static constexpr int SMEM = 1024 + (2 + STAGES) * TILE_BYTES + 512;
+    static constexpr int BARS = (2 + STAGES) * TILE_BYTES, WORDS = BARS + 512;
+    static constexpr int SMEM = WORDS + 64;
     static_assert(SMEM <= 227 * 1024, "shared memory of a CTA");
 };
 
@@ -54,23 +58,31 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 }
 // false: gave up, here or elsewhere in the CTA
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status) {
-    for (int i = 0; i < WAIT_LIMIT; ++i) {
-        if (bar_try(bar, parity)) return true;
+    int left = WAIT_LIMIT;
+#pragma unroll 1
+    while (!bar_try(bar, parity)) {
+        if (--left == 0) {
+            *abort_flag = 1;
+            atomicCAS(status, 0, AAF_ERR_TIMEOUT);
+        }
         if (*abort_flag) return false;
     }
-    *abort_flag = 1;
-    atomicCAS(status, 0, AAF_ERR_TIMEOUT);
-    return false;
+    return true;
 }
 // the same for a whole warp: all lanes agree
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status) {
     return __all_sync(0xffffffffu, bar_wait(bar, parity, abort_flag, status));
 }
+__device__ __forceinline__ bool elected() {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok));
+    return ok != 0;
+}
 
-__device__ __forceinline__ void page_copy(uint32_t dst, const CUtensorMap *map, uint32_t bar, int d, int head, int plane, int layer) {
+__device__ __forceinline__ void page_copy(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int slot, int layer) {
     asm volatile(
-        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
-        ::"r"(dst), "l"(map), "r"(bar), "r"(d), "r"(head), "r"(0), "r"(plane), "r"(layer) : "memory");
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(slot), "r"(layer) : "memory");
 }
 
 // shared-memory matrix descriptor, 128-byte swizzle: start, leading and stride byte offsets in 16-byte units
@@ -116,25 +128,113 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t *u) {
           "r"(u[30]), "r"(u[31])
         : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float *r) {
+    uint32_t *u = reinterpret_cast<uint32_t *>(r);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+          "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+        : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *u) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(addr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]), "r"(u[9]),
+          "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15])
+        : "memory");
+}
 
+// two 32-bit values in one 64-bit register: one instruction does both
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pair(float a, float b) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(f2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {  // a NaN wins
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// cap * tanh(s k) * log2(e) as s * (c0 + z (c1 + z (c2 + z (c3 + z c4)))), z = s^2, for |s k| <= 0.5: tanh(y) / y as a polynomial
+// in y^2 (least maximal relative error, 1.3e-8, fitted by reweighted least squares), k and the cap folded into its
+// coefficients.  The last one is positive, so a masked score, -inf, stays -inf.
+constexpr float TANH_POLY_MAX = 0.5f;
+struct CapPoly {
+    float c[5];
+    __device__ __forceinline__ CapPoly(float times, float k) {  // times = cap * k * log2(e)
+        const float z = k * k;
+        c[0] = 0.99999999f * times;
+        c[1] = -0.33333069f * times * z;
+        c[2] = 0.13324779f * times * z * z;
+        c[3] = -0.052986075f * times * z * z * z;
+        c[4] = 0.017135007f * times * z * z * z * z;
+    }
+    __device__ __forceinline__ f2 operator()(f2 s, f2 add) const {
+        const f2 z = mul2(s, s);
+        f2 q = fma2(z, pair(c[4], c[4]), pair(c[3], c[3]));
+        q = fma2(z, q, pair(c[2], c[2]));
+        q = fma2(z, q, pair(c[1], c[1]));
+        q = fma2(z, q, pair(c[0], c[0]));
+        return fma2(s, q, add);
+    }
+};
+
+// element format in an instruction descriptor; the larger magnitude of two pairs of elements, a NaN above all
 template <typename T> struct WideFormat;
-template <> struct WideFormat<__half> { static constexpr uint32_t F = 0; };
-template <> struct WideFormat<__nv_bfloat16> { static constexpr uint32_t F = 1; };
+template <> struct WideFormat<__half> {
+    static constexpr uint32_t F = 0;
+    static __device__ __forceinline__ uint32_t larger(uint32_t m, uint32_t v) {
+        uint32_t r;
+        asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(v & 0x7fff7fffu));
+        return r;
+    }
+};
+template <> struct WideFormat<__nv_bfloat16> {
+    static constexpr uint32_t F = 1;
+    static __device__ __forceinline__ uint32_t larger(uint32_t m, uint32_t v) {
+        uint32_t r;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(v & 0x7fff7fffu));
+        return r;
+    }
+};
 
-template <typename T, int D, bool FANCY>
+// MODE: what a score is.  0: a multiple of the product; 1: capped; 2: anything (with a distance bias, or a scale of zero)
+template <typename T, int D, int MODE>
 __global__ void __launch_bounds__(WIDE_THREADS, 1)
     attend_wide_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small,
                        const __grid_constant__ CUtensorMap map, int layer) {
     using S = WideShape<D>;
-    extern __shared__ char smem_raw[];
-    __shared__ uint32_t sh_tmem;
-    __shared__ volatile int sh_abort;
-    __shared__ int sh_lo[2], sh_hi[2], sh_lo_max[2], sh_hi_min[2];
+    // all shared memory is dynamic, so that its start is that of the CTA's window and the swizzled tiles are aligned
+    extern __shared__ __align__(1024) char smem_raw[];
+    uint32_t &sh_tmem = *reinterpret_cast<uint32_t *>(smem_raw + S::WORDS);
+    volatile int &sh_abort = *reinterpret_cast<volatile int *>(smem_raw + S::WORDS + 4);
+    int *sh_lo = reinterpret_cast<int *>(smem_raw + S::WORDS + 8), *sh_hi = sh_lo + 2, *sh_lo_max = sh_lo + 4, *sh_hi_min = sh_lo + 6;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t raw = (uint32_t)__cvta_generic_to_shared(smem_raw);
-    const uint32_t sQ = (raw + 1023) & ~1023u, sKV = sQ + 2 * S::TILE_BYTES, bars = sKV + S::STAGES * S::TILE_BYTES;
+    const uint32_t sQ = raw, sKV = sQ + 2 * S::TILE_BYTES, bars = raw + S::BARS;
+    if (raw & 1023) {  // never: the swizzle goes by address bits
+        if (threadIdx.x == 0) atomicCAS(p.status, 0, AAF_ERR_CORRUPT);
+        return;
+    }
     const uint32_t full = bars, guarded = full + 8 * S::STAGES, empty = guarded + 8 * S::STAGES, q_ready = empty + 8 * S::STAGES,
-                   s_full = q_ready + 8, p_ready = s_full + 16, o_done = p_ready + 16, drain = o_done + 16;
+                   s_full = q_ready + 8, p_ready = s_full + 16, o_done = p_ready + 16, drain = o_done + 16, p_rest = drain + 16, turn = p_rest + 16;
 
     const int unit = blockIdx.x / p.H, head = blockIdx.x - unit * p.H;
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
@@ -149,14 +249,18 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
         if (lane == 0) {
             for (int i = 0; i < S::STAGES; ++i) {
                 bar_init(full + 8 * i, 1);
-                bar_init(guarded + 8 * i, 2);
-                bar_init(empty + 8 * i, 1);
+                bar_init(guarded + 8 * i, 1);
+                bar_init(empty + 8 * i, two ? 2 : 1);
             }
             bar_init(q_ready, 256);
             bar_init(drain, 1);
+            bar_init(turn, 1);
+            bar_init(turn + 8, 1);
+            bar_init(drain + 8, 1);
             for (int w = 0; w < 2; ++w) {
                 bar_init(s_full + 8 * w, 1);
-                bar_init(p_ready + 8 * w, 128);
+                bar_init(p_ready + 8 * w, 4);
+                bar_init(p_rest + 8 * w, 4);
                 bar_init(o_done + 8 * w, 1);
             }
             sh_abort = 0;
@@ -197,7 +301,8 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
     tmem_before();
     __syncthreads();
     tmem_after();
-    const uint32_t tmem = sh_tmem;
+    constexpr uint32_t tmem = 0;  // all 512 columns are this CTA's, so they start at column 0
+    if (sh_tmem != 0 && threadIdx.x == 0) atomicCAS(p.status, 0, AAF_ERR_CORRUPT);  // never
     int lo = min(sh_lo[0], sh_lo[1]), hi = max(sh_hi[0], sh_hi[1]);
     const int lo_max = max(sh_lo_max[0], sh_lo_max[1]), hi_min = min(sh_hi_min[0], sh_hi_min[1]);
     if (hi <= lo) lo = hi = 0;
@@ -217,25 +322,30 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int w = warp >> 2, rl = (warp & 3) * 32 + lane, rr = r0 + w * WIDE_TILE + rl;
         const int rc = min(rr, R - 1);
-        {   // the row's queries into the swizzled tile (rows behind the last: zeros); a negative scale moves into their sign
-            const T *q = static_cast<const T *>(p.q) + (long long)(sq.row0 + rc / p.G) * p.q_stride + (long long)(head * p.G + rc % p.G) * D;
-            const uint32_t flip = !FANCY && p.scale < 0.0f ? 0x80008000u : 0u;
-            const uint32_t dst = sQ + w * S::TILE_BYTES + rl * 128;
+        {   // the warp's 32 rows of queries into the swizzled tile, D / 8 lanes a row (rows behind the last: zeros); a negative
+            // scale moves into their sign
+            constexpr int PIECES = D / 8, AT_ONCE = 32 / PIECES;
+            const uint32_t flip = MODE < 2 && p.scale < 0.0f ? 0x80008000u : 0u;
+            const int ch = lane % PIECES;
+            uint4 v[PIECES];
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
-                uint4 v = rr < R ? __ldg(reinterpret_cast<const uint4 *>(q + c * 8)) : make_uint4(0, 0, 0, 0);
-                v.x ^= flip;
-                v.y ^= flip;
-                v.z ^= flip;
-                v.w ^= flip;
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst + (c >> 3) * 16384 + (((c & 7) ^ (rl & 7)) << 4)),
-                             "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+            for (int i = 0; i < PIECES; ++i) {
+                const int rq = r0 + w * WIDE_TILE + (warp & 3) * 32 + i * AT_ONCE + lane / PIECES, rn = min(rq, R - 1), rt = token_of(p, rn);
+                const T *q = static_cast<const T *>(p.q) + (long long)(sq.row0 + rt) * p.q_stride + (long long)(head * p.G + rn - rt * p.G) * D;
+                v[i] = rq < R ? __ldg(reinterpret_cast<const uint4 *>(q + ch * 8)) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {  // all loads are under way before the first result is stored
+                const int r = (warp & 3) * 32 + i * AT_ONCE + lane / PIECES;
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(sQ + w * S::TILE_BYTES + r * 128 + (ch >> 3) * 16384 +
+                                                                         (((ch & 7) ^ (r & 7)) << 4)),
+                             "r"(v[i].x ^ flip), "r"(v[i].y ^ flip), "r"(v[i].z ^ flip), "r"(v[i].w ^ flip) : "memory");
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             bar_arrive(q_ready);
         }
         const RowSpan span = row_span(p, sq, rc / p.G);
-        const float slope = p.slopes ? p.slopes[head * p.G + rc % p.G] : 0.0f;
+        const float slope = MODE == 2 && p.slopes ? p.slopes[head * p.G + rc % p.G] : 0.0f;
         int w_lo_max = span.lo, w_hi_min = span.hi;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -244,10 +354,29 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
         }
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tS = tmem + lanes + w * 128, tP = tS + 64, tO = tmem + lanes + 256 + w * D;
-        const float c = fabsf(p.scale) * LOG2E;
+        const float c = fabsf(p.scale) * LOG2E, k1 = fabsf(p.scale) * p.inv_cap, cap2 = p.softcap * LOG2E;
+        const CapPoly capped(c, k1);
         float m = -CUDART_INF_F, l = 0.0f;
         const bool active = w == 0 || two;
         bool ok = true;
+        // weights of two keys: scores are multiples of the products, or, with a cap and all of them small, a polynomial
+        auto pair_of = [&](float s0, float s1, float times, float base, auto poly) -> f2 {
+            f2 x;
+            if (poly.value)
+                x = capped(pair(s0, s1), pair(-base, -base));
+            else
+                x = fma2(pair(s0, s1), pair(times, times), pair(-base, -base));
+            float a, b;
+            unpair(x, a, b);
+            return pair(ex2(a), ex2(b));
+        };
+        auto done_half = [&](int h, const uint32_t *pk) {  // 64 keys' weights: the product may start on them
+            tmem_st32(tP + 32 * h, pk);
+            tmem_wait_st();
+            tmem_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive((h ? p_rest : p_ready) + 8 * w);
+        };
         for (int j = 0; active && j < tiles; ++j) {
             if (!(ok = warp_wait(s_full + 8 * w, j & 1, &sh_abort, p.status))) break;
             tmem_after();
@@ -256,68 +385,102 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             for (int i = 0; i < 4; ++i) tmem_ld32(tS + 32 * i, s + 32 * i);
             tmem_wait_ld();
             const int tb = t0 + j * WIDE_KEYS;
-            if (FANCY) {
+            const bool edge = tb < w_lo_max || tb + WIDE_KEYS > w_hi_min || tb + WIDE_KEYS > hi;
+            const int a0 = span.lo - tb, b0 = min(span.hi, hi) - tb;  // the tile's keys that this row sees
+            float times = 1.0f;
+            bool small = false;
+            if (MODE == 1) {
+                float mx[4];
 #pragma unroll
-                for (int i = 0; i < 128; ++i) s[i] = score2(p, s[i], slope, span, tb + i);
+                for (int k = 0; k < 4; ++k) mx[k] = fabsf(s[k]);
+#pragma unroll
+                for (int i = 4; i < 124; i += 8)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], fabsf(s[i + 2 * k]), fabsf(s[i + 2 * k + 1]));
+                const float most = max3(max3(mx[0], fabsf(s[124]), fabsf(s[125])), max3(mx[1], fabsf(s[126]), fabsf(s[127])), max3(mx[2], mx[3], mx[3]));
+                small = __all_sync(0xffffffffu, most * k1 <= TANH_POLY_MAX) && capped.c[4] > 0.0f;  // false for a NaN
             }
-            if (tb < w_lo_max || tb + WIDE_KEYS > w_hi_min || tb + WIDE_KEYS > hi) {
-                const int a = span.lo - tb, b = min(span.hi, hi) - tb;
+            if (MODE == 0 || small) {
+                times = c;
+            } else if (MODE == 2 && p.softcap == 0.0f) {
+                // distances are whole numbers, measured from the nearest visible key (see RowSpan)
+                const float d0 = (float)(span.pos - tb), slope2 = slope * LOG2E, c2 = p.scale * LOG2E, near = (float)span.near;
 #pragma unroll
-                for (int i = 0; i < 128; ++i) s[i] = i >= a && i < b ? s[i] : -CUDART_INF_F;
+                for (int i = 0; i < 128; ++i) s[i] = fmaf(-slope2, fabsf(d0 - (float)i) - near, s[i] * c2);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 128; ++i) s[i] = score2(p, MODE == 1 && p.scale < 0.0f ? -s[i] : s[i], slope, span, tb + i);
             }
-            float mx[4] = {s[0], s[1], s[2], s[3]};
+            if (edge) {
+                if (__any_sync(0xffffffffu, a0 > 0))
 #pragma unroll
-            for (int i = 4; i < 128; i += 4) {
-                mx[0] = fmaxf(mx[0], s[i]);
-                mx[1] = fmaxf(mx[1], s[i + 1]);
-                mx[2] = fmaxf(mx[2], s[i + 2]);
-                mx[3] = fmaxf(mx[3], s[i + 3]);
+                    for (int i = 0; i < 128; ++i) s[i] = i < a0 ? -CUDART_INF_F : s[i];
+                if (__any_sync(0xffffffffu, b0 < 128))
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) s[i] = i >= b0 ? -CUDART_INF_F : s[i];
             }
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * (FANCY ? 1.0f : c);
-            // the first maximum, or one that outgrew the one in use by more than 2^8
-            const bool grow = top > m + 8.0f || (m == -CUDART_INF_F && top > m);
-            if (__any_sync(0xffffffffu, grow)) {
-                const float f = grow && m != -CUDART_INF_F ? ex2(m - top) : 1.0f;
-                if (grow) m = top;
-                l *= f;
-                if (j > 0 && __any_sync(0xffffffffu, f != 1.0f)) {
-                    if (!(ok = warp_wait(o_done + 8 * w, (j - 1) & 1, &sh_abort, p.status))) break;
-                    tmem_after();
-#pragma unroll
-                    for (int d = 0; d < D; d += 32) {
-                        float o[32];
-                        tmem_ld32(tO + d, o);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] *= f;
-                        tmem_st32(tO + d, reinterpret_cast<const uint32_t *>(o));
-                    }
-                    tmem_wait_st();
-                }
-            }
-            const float base = m == -CUDART_INF_F ? 0.0f : m;
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            auto weights = [&](auto poly) -> bool {
                 uint32_t pk[32];
+                f2 sums[2];
+                // The maximum in use serves this tile too unless a score outgrows it by 2^8, so the first half of the weights is
+                // computed beside the tile's maximum, not behind it, and once more in the tiles where it was too small.
+                for (;;) {
+                    const float base = m == -CUDART_INF_F ? 0.0f : m;
+                    float mx[4] = {s[0], s[1], s[2], s[3]};
+                    sums[0] = sums[1] = 0;
 #pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    const int e = h * 64 + 2 * i;
-                    float x[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        x[k] = ex2(FANCY ? s[e + k] - base : fmaf(s[e + k], c, -base));
-                        sum[k] += x[k];
+                    for (int i = 0; i < 32; ++i) {
+                        const f2 x = pair_of(s[2 * i], s[2 * i + 1], times, base, poly);
+                        sums[i & 1] = add2(sums[i & 1], x);
+                        float a, b;
+                        unpair(x, a, b);
+                        pk[i] = Elt<T>::pack(a, b);
+                        mx[i & 3] = fmaxf(fmaxf(fmaxf(mx[i & 3], s[4 * i]), fmaxf(s[4 * i + 1], s[4 * i + 2])), s[4 * i + 3]);
                     }
-                    pk[i] = Elt<T>::pack(x[0], x[1]);
-                    pk[i + 1] = Elt<T>::pack(x[2], x[3]);
+                    const float most = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    const float top = poly.value && most > -CUDART_INF_F ? cap2 * tanh_f32(most * k1) : most * times;
+                    // the first maximum, or one that outgrew the one in use
+                    const bool grow = top > m + 8.0f || (m == -CUDART_INF_F && top > m);
+                    if (!__any_sync(0xffffffffu, grow)) break;
+                    const float f = grow && m != -CUDART_INF_F ? ex2(m - top) : 1.0f;
+                    if (grow) m = top;
+                    l *= f;
+                    if (j > 0 && __any_sync(0xffffffffu, f != 1.0f)) {
+                        if (!warp_wait(o_done + 8 * w, (j - 1) & 1, &sh_abort, p.status)) return false;
+                        tmem_after();
+#pragma unroll 1
+                        for (int d = 0; d < D; d += 16) {
+                            float o[16];
+                            tmem_ld16(tO + d, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] *= f;
+                            tmem_st16(tO + d, reinterpret_cast<const uint32_t *>(o));
+                        }
+                        tmem_wait_st();
+                    }
                 }
-                tmem_st32(tP + 32 * h, pk);
-            }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            tmem_wait_st();
-            tmem_before();
-            bar_arrive(p_ready + 8 * w);
+                done_half(0, pk);
+                const float base = m == -CUDART_INF_F ? 0.0f : m;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const f2 x = pair_of(s[64 + 2 * i], s[65 + 2 * i], times, base, poly);
+                    sums[i & 1] = add2(sums[i & 1], x);
+                    float a, b;
+                    unpair(x, a, b);
+                    pk[i] = Elt<T>::pack(a, b);
+                }
+                done_half(1, pk);
+                float a, b;
+                unpair(add2(sums[0], sums[1]), a, b);
+                l += a + b;
+                return true;
+            };
+            if (MODE == 1 && small)
+                ok = weights(std::true_type{});
+            else
+                ok = weights(std::false_type{});
+            if (!ok) break;
         }
         if (ok && active && tiles > 0) {
             ok = warp_wait(o_done + 8 * w, (tiles - 1) & 1, &sh_abort, p.status);
@@ -331,7 +494,8 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             const long long pr = sq.part0 + (((long long)tile * sq.nsplit + part) * p.H + head) * WIDE_ROWS + w * WIDE_TILE + rl;
             const float inv = part_out ? 1.0f : (l > 0.0f || l != l ? 1.0f / l : 0.0f);  // a row that sees nothing is zero
             T *out = static_cast<T *>(p.out) + (qt * p.H * p.G + hq) * D;
-#pragma unroll
+            float *part_o = p.part_o + pr * D;
+#pragma unroll 1
             for (int d = 0; d < D; d += 32) {
                 float o[32];
                 __syncwarp();
@@ -344,7 +508,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                 if (live && part_out) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 4)
-                        *reinterpret_cast<float4 *>(p.part_o + pr * D + d + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                        *reinterpret_cast<float4 *>(part_o + d + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                 } else if (live) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 8)
@@ -363,18 +527,46 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         const int loads = 2 * tiles;  // K0 V0 K1 V1 ...
-        if (warp == 8) {
-            // ------------------------------------------------------------ pages of K and V into the stages
+        if (warp == 8 || warp == 10) {
+            // ------------------------------------------------------------ blocks of keys (values) into the stages
             const int *table = p.tables + (long long)sq.ctx * p.max_blk;
-            const int pages = WIDE_KEYS / p.BS;  // per tile, at most 16
+            const int pages = WIDE_KEYS / p.BS, which = warp == 8 ? 0 : 1;
             bool ok = true;
-            int id = 0, done = 0;
-            for (int n = 0; ok && n < loads; ++n) {
+            int at_end = 0;
+            uint32_t largest = 0;
+            // V tiles that not every row sees whole: rows that none sees become zeros, values that are not finite are noticed
+            auto look = [&](int n) -> bool {
+                const int stage = n % S::STAGES, tb = t0 + (n >> 1) * WIDE_KEYS;
+                if (tb >= lo_max && tb + WIDE_KEYS <= hi_min && tb + WIDE_KEYS <= hi) return true;
+                if (!warp_wait(full + 8 * stage, (n / S::STAGES) & 1, &sh_abort, p.status)) return false;
+                const uint32_t v = sKV + stage * S::TILE_BYTES + lane * 16;
+#pragma unroll 1
+                for (int i = 0; i < S::TILE_BYTES / 16; i += 256) {  // eight pieces at a time, 32 token rows
+                    const int ta = tb + ((i >> 3) & 127);
+                    if (ta >= lo_max && ta + 32 <= hi_min) continue;  // every row sees these tokens
+                    uint4 x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = lds16(v + (i + 32 * e) * 16);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int t = ta + e * 4 + (lane >> 3);
+                        if (t < lo || t >= hi)
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v + (i + 32 * e) * 16), "r"(0) : "memory");
+                        else
+                            largest = WideFormat<T>::larger(WideFormat<T>::larger(WideFormat<T>::larger(
+                                WideFormat<T>::larger(largest, x[e].x), x[e].y), x[e].z), x[e].w);
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(guarded + 8 * stage);
+                return true;
+            };
+            for (int n = which; n < loads; n += 2) {
                 const int stage = n % S::STAGES, tb = t0 + (n >> 1) * WIDE_KEYS, at = tb + lane * p.BS;
                 const bool mine = lane < pages && at < hi && at + p.BS > lo;
-                if (!(n & 1)) id = mine ? __ldg(table + at / p.BS) : 0;
-                if (n >= S::STAGES) ok = warp_wait(empty + 8 * stage, (n / S::STAGES - 1) & 1, &sh_abort, p.status);
-                if (!ok) break;
+                const int slot = mine ? (2 * __ldg(table + block_of(at, p.BS, p.bs_shift)) + which) * p.BS : 0;
+                if (n >= S::STAGES && !(ok = warp_wait(empty + 8 * stage, (n / S::STAGES - 1) & 1, &sh_abort, p.status))) break;
                 const int count = __popc(__ballot_sync(0xffffffffu, mine));
                 if (lane == 0) bar_expect(full + 8 * stage, (uint32_t)(count * p.BS * D * 2));
                 __syncwarp();
@@ -382,123 +574,120 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                     const uint32_t dst = sKV + stage * S::TILE_BYTES + lane * p.BS * 128;
 #pragma unroll
                     for (int h = 0; h < S::HALVES; ++h)
-                        page_copy(dst + h * 16384, &map, full + 8 * stage, h * 64, head, 2 * id + (n & 1), layer);
+                        page_copy(dst + h * 16384, &map, full + 8 * stage, head * D + h * 64, slot, layer);
                 }
-                done = n + 1;
+                at_end = n + 2;
+                if (which && n > 1 && !(ok = look(n - 2))) break;  // the tile before: it has had time to land
             }
+            if (ok && which && loads > 0) ok = look(loads - 1);
+            if (finite_only<T>(largest) != largest) *p.flag = p.epoch;
             // nothing may be in flight when the CTA ends early: wait for what was issued
             if (!ok)
-                for (int n = max(0, done - S::STAGES); n < done; ++n)
+                for (int n = max(which, at_end - 2 * S::STAGES); n < at_end; n += 2)
                     for (int i = 0; i < WAIT_LIMIT && !bar_try(full + 8 * (n % S::STAGES), (n / S::STAGES) & 1); ++i) {}
-        } else if (warp == 9) {
-            // ------------------------------------------------------------ products
-            if (lane == 0) {
-                constexpr uint32_t F = WideFormat<T>::F;
-                constexpr uint32_t QK = 1u << 4 | F << 7 | F << 10 | (WIDE_KEYS / 8) << 17 | (WIDE_TILE / 16) << 24;
-                constexpr uint32_t PV = 1u << 4 | F << 7 | F << 10 | 1u << 16 | (D / 8) << 17 | (WIDE_TILE / 16) << 24;
-                bool ok = bar_wait(q_ready, 0, &sh_abort, p.status);
-                auto ready = [&](int n) {  // load n has landed and been looked at
-                    const int stage = n % S::STAGES, parity = (n / S::STAGES) & 1;
-                    return bar_wait(full + 8 * stage, parity, &sh_abort, p.status) && bar_wait(guarded + 8 * stage, parity, &sh_abort, p.status);
-                };
-                auto scores = [&](int w, int n) {
-                    const uint32_t a = sQ + w * S::TILE_BYTES, b = sKV + (n % S::STAGES) * S::TILE_BYTES;
+        } else if (warp == 9 || two) {
+            // ------------------------------------------------------------ products, a warp for each row tile
+            // The whole warp keeps the loop, one lane issues: addresses and descriptors are then the same in all lanes and
+            // stay in uniform registers.  A wait costs some 300 cycles even where there is nothing to wait for, so the row tiles
+            // do not share a warp.
+            constexpr uint32_t F = WideFormat<T>::F;
+            constexpr uint32_t QK = 1u << 4 | F << 7 | F << 10 | (WIDE_KEYS / 8) << 17 | (WIDE_TILE / 16) << 24;
+            constexpr uint32_t PV = 1u << 4 | F << 7 | F << 10 | 1u << 16 | (D / 8) << 17 | (WIDE_TILE / 16) << 24;
+            const int n_tile = __shfl_sync(0xffffffffu, tiles, 0), w = __shfl_sync(0xffffffffu, warp == 9 ? 0 : 1, 0);
+            const uint64_t dQ = smem_desc(sQ, 16, 1024) + w * (S::TILE_BYTES >> 4), dK = smem_desc(sKV, 16, 1024), dV = smem_desc(sKV, 16384, 1024);
+            const uint32_t tS = w * 128, tO = 256 + w * D;
+            auto scores = [&](int stage, bool release) {
+                if (elected()) {
+                    uint64_t a = dQ, b = dK + stage * (S::TILE_BYTES >> 4);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off = (k >> 2) * 16384 + (k & 3) * 32;
-                        mma_ss(tmem + w * 128, smem_desc(a + off, 16, 1024), smem_desc(b + off, 16, 1024), QK, k > 0);
-                    }
+                    for (int h = 0; h < S::HALVES; ++h, a += 16384 >> 4, b += 16384 >> 4)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) mma_ss(tS, a + 2 * k, b + 2 * k, QK, h + k > 0);
                     mma_commit(s_full + 8 * w);
-                };
-                if (ok && tiles > 0 && (ok = ready(0))) {
-                    tmem_after();
-                    scores(0, 0);
-                    if (two) scores(1, 0);
-                    if (S::STAGES < loads) mma_commit(empty);  // an arrival is asked for only where someone waits for it
-                }
-                for (int j = 0; ok && j < tiles; ++j) {
-                    const int nv = 2 * j + 1, nk = 2 * j + 2;
-                    const bool more = j + 1 < tiles;
-                    if (!(ok = ready(nv))) break;
-                    for (int w = 0; w < (two ? 2 : 1); ++w) {
-                        if (!(ok = bar_wait(p_ready + 8 * w, j & 1, &sh_abort, p.status))) break;
-                        tmem_after();
-                        const uint32_t b = sKV + (nv % S::STAGES) * S::TILE_BYTES;
-#pragma unroll
-                        for (int k = 0; k < WIDE_KEYS / 16; ++k)
-                            mma_ts(tmem + 256 + w * D, tmem + w * 128 + 64 + k * 8, smem_desc(b + k * 2048, 16384, 1024), PV, j > 0 || k > 0);
-                        mma_commit(o_done + 8 * w);
-                        if (more) {  // in order behind the product that still reads P from these columns
-                            if (w == 0 && !(ok = ready(nk))) break;
-                            scores(w, nk);
-                        }
-                    }
-                    if (!ok) break;
-                    if (nv + S::STAGES < loads) mma_commit(empty + 8 * (nv % S::STAGES));
-                    if (nk + S::STAGES < loads) mma_commit(empty + 8 * (nk % S::STAGES));
-                }
-            }
-            __syncwarp();
-        } else {
-            // ------------------------------------------------------------ V tiles that not every row sees whole
-            const int tid = threadIdx.x - 320;
-            bool odd = false, ok = true;
-            for (int n = 0; n < loads; ++n) {
-                const int stage = n % S::STAGES;
-                if (!(ok = warp_wait(full + 8 * stage, (n / S::STAGES) & 1, &sh_abort, p.status))) break;
-                const int tb = t0 + (n >> 1) * WIDE_KEYS;
-                if ((n & 1) && (tb < lo_max || tb + WIDE_KEYS > hi_min || tb + WIDE_KEYS > hi)) {
-                    const uint32_t v = sKV + stage * S::TILE_BYTES;
-                    for (int i = tid; i < S::TILE_BYTES / 16; i += 64) {
-                        const int t = tb + ((i >> 3) & 127);
-                        const uint32_t at = v + i * 16;
-                        if (t < lo || t >= hi) {
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at), "r"(0) : "memory");
-                        } else {
-                            const uint4 x = lds16(at);
-                            odd |= finite_only<T>(x.x) != x.x || finite_only<T>(x.y) != x.y || finite_only<T>(x.z) != x.z ||
-                                   finite_only<T>(x.w) != x.w;
-                        }
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    if (release) mma_commit(empty + 8 * stage);  // an arrival is asked for only where someone waits for it
                 }
                 __syncwarp();
-                if (lane == 0) bar_arrive(guarded + 8 * stage);
+            };
+            bool ok = warp_wait(q_ready, 0, &sh_abort, p.status);
+            uint32_t looked = 0;  // parity of every stage's `guarded`
+            int sv = 1 % S::STAGES, pv = 0, sk = 2 % S::STAGES, pk = 0;  // stage and parity of V_j and of K_j+1
+            if (ok && n_tile > 0 && (ok = warp_wait(full, 0, &sh_abort, p.status))) {
+                tmem_after();
+                scores(0, S::STAGES < loads);
             }
-            if (odd) *p.flag = p.epoch;
+            for (int j = 0; ok && j < n_tile; ++j) {
+                const bool more = j + 1 < n_tile;
+                const int tb = t0 + j * WIDE_KEYS;
+                if (!(ok = warp_wait(full + 8 * sv, pv, &sh_abort, p.status))) break;
+                if (more && !(ok = warp_wait(full + 8 * sk, pk, &sh_abort, p.status))) break;
+                if (tb < lo_max || tb + WIDE_KEYS > hi_min || tb + WIDE_KEYS > hi) {
+                    if (!(ok = warp_wait(guarded + 8 * sv, looked >> sv & 1, &sh_abort, p.status))) break;
+                    looked ^= 1u << sv;
+                }
+                const uint64_t b = dV + sv * (S::TILE_BYTES >> 4);
+                // the row tiles take turns, else both would exponentiate, then both multiply at the same time
+                if (two && (w || j) && !(ok = warp_wait(turn + 8 * w, w ? j & 1 : (j - 1) & 1, &sh_abort, p.status))) break;
+                if (!(ok = warp_wait(p_ready + 8 * w, j & 1, &sh_abort, p.status))) break;
+                tmem_after();
+                if (elected()) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_ts(tO, tS + 64 + 8 * k, b + k * (2048 >> 4), PV, j > 0 || k > 0);
+                }
+                __syncwarp();
+                if (!(ok = warp_wait(p_rest + 8 * w, j & 1, &sh_abort, p.status))) break;
+                tmem_after();
+                if (elected()) {
+#pragma unroll
+                    for (int k = 4; k < 8; ++k) mma_ts(tO, tS + 64 + 8 * k, b + k * (2048 >> 4), PV, 1);
+                    mma_commit(o_done + 8 * w);
+                    if (2 * j + 1 + S::STAGES < loads) mma_commit(empty + 8 * sv);
+                }
+                __syncwarp();
+                if (more) scores(sk, 2 * j + 2 + S::STAGES < loads);  // in order behind the product that still reads P from these columns
+                if (two && lane == 0) bar_arrive(turn + 8 * (w ^ 1));
+                sv += 2;
+                if (sv >= S::STAGES) sv -= S::STAGES, pv ^= 1;
+                sk += 2;
+                if (sk >= S::STAGES) sk -= S::STAGES, pk ^= 1;
+            }
         }
     }
     __syncthreads();
-    if (sh_abort && threadIdx.x == 288) {
+    if (sh_abort && (warp == 9 || warp == 11) && lane == 0) {
         // a wait gave up: let the products that were issued finish before tensor memory is given back
-        mma_commit(drain);
-        for (int i = 0; i < WAIT_LIMIT && !bar_try(drain, 0); ++i) {}
+        const uint32_t bar = drain + (warp == 11 ? 8 : 0);
+        mma_commit(bar);
+        for (int i = 0; i < WAIT_LIMIT && !bar_try(bar, 0); ++i) {}
     }
     __syncthreads();
-    if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh_tmem));
 }
 
 bool wide_takes(int D, int BS) { return (D == 64 || D == 128) && BS >= 8 && BS <= WIDE_KEYS && (BS & (BS - 1)) == 0; }
 
-template <typename T, int D, bool FANCY>
+template <typename T, int D, int MODE>
 static cudaError_t wide_go(const AttnParams &p, const SmallSeqs &small, const void *map, int layer, cudaStream_t st) {
     const cudaError_t e =
-        cudaFuncSetAttribute(attend_wide_kernel<T, D, FANCY>, cudaFuncAttributeMaxDynamicSharedMemorySize, WideShape<D>::SMEM);
+        cudaFuncSetAttribute(attend_wide_kernel<T, D, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, WideShape<D>::SMEM);
     if (e != cudaSuccess) return e;
-    attend_wide_kernel<T, D, FANCY><<<(unsigned)((long long)p.total_units * p.H), WIDE_THREADS, WideShape<D>::SMEM, st>>>(
+    attend_wide_kernel<T, D, MODE><<<(unsigned)((long long)p.total_units * p.H), WIDE_THREADS, WideShape<D>::SMEM, st>>>(
         p, small, *static_cast<const CUtensorMap *>(map), layer);
     return cudaGetLastError();
 }
 template <typename T> static cudaError_t wide_pick(const AttnParams &p, const SmallSeqs &small, const void *map, int layer, cudaStream_t st) {
-    const bool fancy = p.softcap != 0.0f || p.slopes || p.scale == 0.0f;  // 0 * -inf would undo a mask
-    if (p.D == 64) return fancy ? wide_go<T, 64, true>(p, small, map, layer, st) : wide_go<T, 64, false>(p, small, map, layer, st);
-    return fancy ? wide_go<T, 128, true>(p, small, map, layer, st) : wide_go<T, 128, false>(p, small, map, layer, st);
+    // a scale of zero would undo a mask (0 * -inf) where scores are multiples of the product
+    const int mode = p.slopes || p.scale == 0.0f ? 2 : (p.softcap != 0.0f ? 1 : 0);
+    if (p.D == 64)
+        return mode == 0 ? wide_go<T, 64, 0>(p, small, map, layer, st)
+                         : (mode == 1 ? wide_go<T, 64, 1>(p, small, map, layer, st) : wide_go<T, 64, 2>(p, small, map, layer, st));
+    return mode == 0 ? wide_go<T, 128, 0>(p, small, map, layer, st)
+                     : (mode == 1 ? wide_go<T, 128, 1>(p, small, map, layer, st) : wide_go<T, 128, 2>(p, small, map, layer, st));
 }
 cudaError_t launch_attend_wide(const AttnParams &p, const SmallSeqs &small, int f16, const void *map, int layer, cudaStream_t st) {
     return f16 ? wide_pick<__half>(p, small, map, layer, st) : wide_pick<__nv_bfloat16>(p, small, map, layer, st);
 }
 
-// Tensor map of a whole pool: [layer][block * 2 + (K, V)][slot][kv head][dim], boxes of one block's slots of one head, 64 dims.
+// Tensor map of a whole pool: [layer][slot of a block's keys or values][kv head and dim], boxes of a block's slots, 64 dims.
 // The encoder is the driver's, found through the runtime (nothing links against the driver library).
 static_assert(sizeof(CUtensorMap) == sizeof(PoolMap), "room for a tensor map");
 bool encode_pool_map(const Geom &g, PoolMap *out) {
@@ -512,10 +701,11 @@ bool encode_pool_map(const Geom &g, PoolMap *out) {
         cudaGetLastError();
         return false;
     }
-    const cuuint64_t dims[5] = {(cuuint64_t)g.D, (cuuint64_t)g.H, (cuuint64_t)g.BS, 2 * (cuuint64_t)g.NB, (cuuint64_t)g.L};
-    const cuuint64_t strides[4] = {2 * (cuuint64_t)g.D, (cuuint64_t)g.row, (cuuint64_t)g.run, (cuuint64_t)g.layer_stride};
-    const cuuint32_t box[5] = {64, 1, (cuuint32_t)g.BS, 1, 1}, step[5] = {1, 1, 1, 1, 1};
-    return reinterpret_cast<Encode>(fn)(reinterpret_cast<CUtensorMap *>(out), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, g.pool, dims, strides,
+    const cuuint64_t dims[3] = {(cuuint64_t)g.H * g.D, 2 * (cuuint64_t)g.NB * g.BS, (cuuint64_t)g.L};
+    const cuuint64_t strides[2] = {(cuuint64_t)g.row, (cuuint64_t)g.layer_stride};
+    const cuuint32_t box[3] = {64, (cuuint32_t)g.BS, 1}, step[3] = {1, 1, 1};
+    if (dims[1] >= (1ull << 31)) return false;
+    return reinterpret_cast<Encode>(fn)(reinterpret_cast<CUtensorMap *>(out), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, g.pool, dims, strides,
                                         box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

@@ -1289,6 +1289,7 @@ AttnParams attn_params(const aaf_kv_pool *p, int layer, const aaf_kv_attn *a, co
     k.run = p->g.run; k.row = p->g.row;
     k.max_blk = p->g.max_blk; k.BS = p->g.BS; k.bs_shift = log2_of(p->g.BS);
     k.H = p->g.H; k.G = a->n_q_heads / p->g.H; k.D = p->g.D;
+    k.g_shift = log2_of(k.G);
     k.window = a->window;
     k.scale = a->scale; k.softcap = a->softcap;
     k.inv_cap = a->softcap > 0.0f ? 1.0f / a->softcap : 0.0f;
