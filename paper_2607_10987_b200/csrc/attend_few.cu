@@ -25,14 +25,14 @@ template <int DP> struct FewShape {
     static constexpr int VC = 4 * (DP / 64);        // of V
     static constexpr int SLOTS = KC + VC;
     static constexpr int STAGE_BYTES = SLOTS * 32 * 16;
-    static constexpr int WARPS = DP <= 128 ? 8 : 6;
+    static constexpr int WARPS = DP <= 128 ? 4 : 3;
     static constexpr int STAGES = DP == 64 ? 6 : (DP == 128 ? 3 : 2);
-    static constexpr int SMEM = WARPS * STAGES * STAGE_BYTES;  // 192 KB: one CTA an SM
-    static_assert(SMEM <= 227 * 1024, "shared memory of a CTA");
+    static constexpr int SMEM = WARPS * STAGES * STAGE_BYTES;  // 96 KB: two CTAs an SM, one starts while the other streams
+    static_assert(2 * (SMEM + 1024) <= 228 * 1024, "shared memory of a CTA");
 };
 
 template <typename T, int DP, int NT>
-__global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 1)
+__global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
     attend_few_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small) {
     using S = FewShape<DP>;
     extern __shared__ __align__(16) char smem[];
@@ -41,6 +41,7 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 1)
     const long long task = (long long)blockIdx.x * S::WARPS + warp;
     if (task >= (long long)p.total_units * p.H) return;
     const int unit = (int)(task / p.H), head = (int)(task - (long long)unit * p.H);
+    asm volatile("griddepcontrol.launch_dependents;");  // the join may be brought up beside this kernel
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
     const AttnSeq sq = seqs[find_seq(seqs, p.n, unit)];
     const int part = unit - sq.unit0;
@@ -67,9 +68,8 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 1)
         lo_all = min(lo_all, __shfl_xor_sync(0xffffffffu, lo_all, d));
         hi_all = max(hi_all, __shfl_xor_sync(0xffffffffu, hi_all, d));
     }
-    // the part's keys: the host cut [first, len) into chunks, first being what the window leaves of the earliest row
-    const int first = p.window ? max(0, sq.len - sq.nq + 1 - p.window) : 0;
-    const long long c0 = first + (long long)part * sq.chunk;
+    // the part's keys: the host cut [key0, len) into chunks
+    const long long c0 = sq.key0 + (long long)part * sq.chunk;
     int beg = (int)max((long long)lo_all, c0), end = (int)min((long long)hi_all, c0 + sq.chunk);
     if (end <= beg) beg = end = 0;  // nothing to see in this part: no token index is formed from an empty range
     const int tiles = (end - beg + 15) / 16;
@@ -304,29 +304,41 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 1)
                 p.lse[qt * p.H * p.G + hq] =
                     sum == 0.0f ? -CUDART_INF_F : (m[nt][c] + log2f(sum)) * LN2 - slope[nt][c] * (float)span[nt][c].near;
         }
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // what it ran beside is done before it is
 }
 
 int few_rows_limit(int D) { return D <= 64 ? 32 : (D <= 128 ? 16 : 8); }
 
 template <typename T, int DP, int NT>
-static cudaError_t few_go(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
-    const cudaError_t e = cudaFuncSetAttribute(attend_few_kernel<T, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               FewShape<DP>::SMEM);
+static cudaError_t few_go(const AttnParams &p, const SmallSeqs &small, bool beside, cudaStream_t st) {
+    cudaError_t e = cudaFuncSetAttribute(attend_few_kernel<T, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         FewShape<DP>::SMEM);
     if (e != cudaSuccess) return e;
-    const long long tasks = (long long)p.total_units * p.H;
     constexpr int W = FewShape<DP>::WARPS;
-    attend_few_kernel<T, DP, NT><<<(unsigned)((tasks + W - 1) / W), W * 32, FewShape<DP>::SMEM, st>>>(p, small);
-    return cudaGetLastError();
+    const long long tasks = (long long)p.total_units * p.H;
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((tasks + W - 1) / W));
+    cfg.blockDim = dim3(W * 32);
+    cfg.dynamicSmemBytes = FewShape<DP>::SMEM;
+    cfg.stream = st;
+    cfg.attrs = &early;
+    cfg.numAttrs = beside ? 1 : 0;
+    e = cudaLaunchKernelEx(&cfg, attend_few_kernel<T, DP, NT>, p, small);
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
-template <typename T> static cudaError_t few_pick(const AttnParams &p, const SmallSeqs &small, int max_rows, cudaStream_t st) {
+template <typename T>
+static cudaError_t few_pick(const AttnParams &p, const SmallSeqs &small, int max_rows, bool beside, cudaStream_t st) {
     if (p.D <= 64)
-        return max_rows <= 8 ? few_go<T, 64, 1>(p, small, st)
-                             : (max_rows <= 16 ? few_go<T, 64, 2>(p, small, st) : few_go<T, 64, 4>(p, small, st));
-    if (p.D <= 128) return max_rows <= 8 ? few_go<T, 128, 1>(p, small, st) : few_go<T, 128, 2>(p, small, st);
-    return few_go<T, 256, 1>(p, small, st);
+        return max_rows <= 8 ? few_go<T, 64, 1>(p, small, beside, st)
+                             : (max_rows <= 16 ? few_go<T, 64, 2>(p, small, beside, st) : few_go<T, 64, 4>(p, small, beside, st));
+    if (p.D <= 128) return max_rows <= 8 ? few_go<T, 128, 1>(p, small, beside, st) : few_go<T, 128, 2>(p, small, beside, st);
+    return few_go<T, 256, 1>(p, small, beside, st);
 }
-cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, cudaStream_t st) {
-    return f16 ? few_pick<__half>(p, small, max_rows, st) : few_pick<__nv_bfloat16>(p, small, max_rows, st);
+cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, bool beside, cudaStream_t st) {
+    return f16 ? few_pick<__half>(p, small, max_rows, beside, st) : few_pick<__nv_bfloat16>(p, small, max_rows, beside, st);
 }
 
 // ------------------------------------------------------------------------------------------ join
@@ -342,18 +354,19 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
     const int Hq = p.H * p.G;
-    const long long qt = blockIdx.x / Hq;
-    const int hq = (int)(blockIdx.x - qt * Hq), head = hq / p.G;
-    int lo = 0, hi = p.n - 1;  // sequence of the query token
+    const int tok = (int)(blockIdx.x / Hq), hq = (int)(blockIdx.x - (long long)tok * Hq), head = hq / p.G;
+    int lo = 0, hi = p.n - 1;  // record of the query token
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (seqs[mid].row0 <= qt) lo = mid; else hi = mid - 1;
+        if (seqs[mid].tok0 <= tok) lo = mid; else hi = mid - 1;
     }
     const AttnSeq sq = seqs[lo];
-    if (sq.part0 < 0 || qt < sq.row0 || qt >= sq.row0 + sq.nq) return;  // not split, or of the batch's other kernel
+    if (sq.part0 < 0) return;
+    const long long qt = sq.row0 + (tok - sq.tok0);
     const int j = (int)(qt - sq.row0), r = j * p.G + hq % p.G;
-    // partial rows of a sequence: [part][head][R] for the few-row kernel, [tile][part][head][tile_rows] for the tile kernel
-    long long row, step;
+    // partial rows of a sequence: [part][head][R] for the few-row kernel, [tile][part][head][tile_rows] for the others; behind
+    // them in order the parts of the keys that its group shares
+    long long row, step, grow = 0, gstep = 0;
     if (tile_rows) {
         row = sq.part0 + ((long long)(r / tile_rows) * sq.nsplit * p.H + head) * tile_rows + r % tile_rows;
         step = (long long)p.H * tile_rows;
@@ -361,9 +374,15 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32)
         const int R = sq.nq * p.G;
         row = sq.part0 + (long long)head * R + r;
         step = (long long)p.H * R;
+        const int gr = sq.grow + r;
+        grow = sq.gpart0 + ((long long)(gr / WIDE_ROWS) * sq.gsplit * p.H + head) * WIDE_ROWS + gr % WIDE_ROWS;
+        gstep = (long long)p.H * WIDE_ROWS;
     }
+    const int parts = sq.nsplit + sq.gsplit;
+    auto at = [&](int s) { return s < sq.nsplit ? row + s * step : grow + (s - sq.nsplit) * gstep; };
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the parts are written
     float top = -CUDART_INF_F;
-    for (int s = threadIdx.x; s < sq.nsplit; s += JOIN_WARPS * 32) top = fmaxf(top, p.part_ml[2 * (row + s * step)]);
+    for (int s = threadIdx.x; s < parts; s += JOIN_WARPS * 32) top = fmaxf(top, p.part_ml[2 * at(s)]);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
     if (lane == 0) max_s[warp] = top;
@@ -377,10 +396,10 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32)
         float4 a = make_float4(0, 0, 0, 0);
         float sum = 0.0f;
 #pragma unroll 4
-        for (int s = warp; s < sq.nsplit; s += JOIN_WARPS) {
-            const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * (row + s * step));
-            const float4 v = d < p.D ? *reinterpret_cast<const float4 *>(p.part_o + (row + s * step) * p.D + d)
-                                     : make_float4(0, 0, 0, 0);
+        for (int s = warp; s < parts; s += JOIN_WARPS) {
+            const long long pr = at(s);
+            const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * pr);
+            const float4 v = d < p.D ? *reinterpret_cast<const float4 *>(p.part_o + pr * p.D + d) : make_float4(0, 0, 0, 0);
             const float w = ex2(ml.x - base);  // a part that saw nothing has m = -inf, l = 0, o = 0
             sum += w * ml.y;
             a.x += w * v.x;
@@ -415,14 +434,21 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32)
     }
 }
 
-cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int total_q,
+cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int tokens,
                                cudaStream_t st) {
-    const unsigned grid = (unsigned)((long long)total_q * p.H * p.G);
-    if (f16)
-        attend_join_kernel<__half><<<grid, JOIN_WARPS * 32, 0, st>>>(p, small, tile_rows);
-    else
-        attend_join_kernel<__nv_bfloat16><<<grid, JOIN_WARPS * 32, 0, st>>>(p, small, tile_rows);
-    return cudaGetLastError();
+    // launched so that its CTAs come up while the parts are still being computed; it waits for them itself
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)((long long)tokens * p.H * p.G));
+    cfg.blockDim = dim3(JOIN_WARPS * 32);
+    cfg.stream = st;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    const cudaError_t e = f16 ? cudaLaunchKernelEx(&cfg, attend_join_kernel<__half>, p, small, tile_rows)
+                              : cudaLaunchKernelEx(&cfg, attend_join_kernel<__nv_bfloat16>, p, small, tile_rows);
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace aafkv

@@ -11,17 +11,26 @@ namespace aafkv {
 // One sequence of an attention batch.  Its queries are the last nq tokens of the context; row r of a kv head is
 // query token r / G, head r % G of the head's group.  Units are what the kernels are launched over; they are
 // numbered over the batch, unit0 is the sequence's first.
-struct AttnSeq {          // 32 bytes
+struct AttnSeq {          // 56 bytes
     int ctx;
     int len;              // tokens of the context (an int: max_ctx * max_blk and the block size bound it, see pool.cu)
     int nq;
     int row0;             // first query token of the sequence in the packed batch
     int unit0;            // first unit
     int nsplit;           // parts that the key range of a row tile is cut into
-    int chunk;            // few-row kernel: keys of a part
+    int chunk;            // few-row kernel: keys of a part; wide kernel: query tokens of each member of a group, 0: a sequence
     int part0;            // first row of the sequence's partial results, -1: written straight to the output
+    int key0;             // few-row kernel: first key
+    int gpart0;           // parts of the keys before key0, which a group of sequences shares (wide kernel's rows)
+    int gsplit;           // how many, 0: none
+    int grow;             // the sequence's first row within the group
+    int tok0;             // query tokens of the records before this one
+    int pad;
 };
-static_assert(sizeof(AttnSeq) == 32, "AttnSeq layout");
+static_assert(sizeof(AttnSeq) == 56, "AttnSeq layout");
+// Sequences forked from one context hold the same blocks up to where they were forked.  A group record of the wide kernel stands
+// for several of them: the rows of all of them over the shared keys [0, len); row0 is then the first member's place
+// in the record array, members are consecutive there.
 constexpr int SMALL_SEQS = 64;  // sequences that travel as kernel parameters
 struct SmallSeqs {
     AttnSeq e[SMALL_SEQS];
@@ -41,7 +50,7 @@ struct AttnParams {
     long long q_stride;   // elements between query tokens
     long long run, row;   // bytes
     int max_blk, BS, bs_shift;  // bs_shift: log2 of the block size, -1 if it is no power of two
-    int H, G, D, g_shift, n, total_units;  // g_shift as bs_shift, of G
+    int H, G, D, g_shift, n, total_units, first;  // records [first, first + n) are launched over  // g_shift as bs_shift, of G
     int window;           // 0: none
     int epoch;            // what `flag` holds when a CTA of the wide kernel has met values it cannot keep apart
     int *flag;            // wide kernel: written; tile kernel: run only if it holds `epoch` (null: always)
@@ -85,7 +94,9 @@ int few_rows_limit(int D);                       // most rows of a kv head that 
 constexpr int TILE_ROWS = 64;                    // rows of a unit of the tile kernel
 constexpr int MASS_CHUNK = 64;                   // keys of a CTA of the mass kernel
 constexpr int MASS_MAX_HEADS = 512;              // its kv heads: chunk * heads floats of shared memory
-cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, cudaStream_t st);
+// beside: brought up beside the kernel launched before it, which it does not depend on
+cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, bool beside,
+                              cudaStream_t st);
 cudaError_t launch_attend_tile(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
 constexpr int WIDE_ROWS = 256;                   // rows of a unit of the wide kernel
 bool wide_takes(int D, int BS);                  // pool geometries of the wide kernel
@@ -95,7 +106,7 @@ struct alignas(64) PoolMap {                     // a tensor map, opaque to the 
     unsigned char bytes[128];
 };
 bool encode_pool_map(const Geom &g, PoolMap *out);
-cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int total_q,
+cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int tokens,
                                cudaStream_t st);
 cudaError_t launch_attn_mass(const MassParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
 cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16, cudaStream_t st);

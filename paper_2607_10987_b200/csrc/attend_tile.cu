@@ -32,6 +32,7 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
     using S = TileShape<DP>;
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t4 = lane & 3;
+    asm volatile("griddepcontrol.launch_dependents;");
     if (p.flag && *p.flag != p.epoch) return;  // a second run that is not needed
     for (long long cta = blockIdx.x; cta < (long long)p.total_units * p.H; cta += gridDim.x) {
     const int unit = (int)(cta / p.H), head = (int)(cta - (long long)unit * p.H);

@@ -226,6 +226,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
     uint32_t &sh_tmem = *reinterpret_cast<uint32_t *>(smem_raw + S::WORDS);
     volatile int &sh_abort = *reinterpret_cast<volatile int *>(smem_raw + S::WORDS + 4);
     int *sh_lo = reinterpret_cast<int *>(smem_raw + S::WORDS + 8), *sh_hi = sh_lo + 2, *sh_lo_max = sh_lo + 4, *sh_hi_min = sh_lo + 6;
+    asm volatile("griddepcontrol.launch_dependents;");  // the join may be brought up beside this kernel
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t raw = (uint32_t)__cvta_generic_to_shared(smem_raw);
     const uint32_t sQ = raw, sKV = sQ + 2 * S::TILE_BYTES, bars = raw + S::BARS;
@@ -238,7 +239,23 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
 
     const int unit = blockIdx.x / p.H, head = blockIdx.x - unit * p.H;
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
-    const AttnSeq sq = seqs[find_seq(seqs, p.n, unit)];
+    const AttnSeq sq = seqs[p.first + find_seq(seqs + p.first, p.n, unit)];
+    // query token j of the record, its place in the packed batch and the keys it sees
+    auto token = [&](int j, int &packed) -> RowSpan {
+        if (sq.chunk == 0) {
+            packed = sq.row0 + j;
+            return row_span(p, sq, j);
+        }
+        const int member = j / sq.chunk, jj = j - member * sq.chunk;
+        const AttnSeq &ms = seqs[sq.row0 + member];
+        packed = ms.row0 + jj;
+        RowSpan r;  // no mask but the causal one; the nearest key is the token itself, in the member's own part
+        r.pos = ms.len - ms.nq + jj;
+        r.lo = 0;
+        r.hi = min(r.pos + 1, sq.len);
+        r.near = 0;
+        return r;
+    };
     const int R = sq.nq * p.G, n_tiles = (R + WIDE_ROWS - 1) / WIDE_ROWS;
     const int u = unit - sq.unit0, part = u % sq.nsplit;
     const int tile = n_tiles - 1 - u / sq.nsplit;  // the latest rows see the most keys: they start first
@@ -276,7 +293,8 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
         const int w = warp - 10, a = min(r0 + w * WIDE_TILE, R - 1), b = min(r0 + w * WIDE_TILE + WIDE_TILE - 1, R - 1);
         int lo = 0x7fffffff, hi = 0, lo_max = 0, hi_min = 0x7fffffff;
         for (int j = a / p.G + lane; j <= b / p.G; j += 32) {
-            const RowSpan sp = row_span(p, sq, j);
+            int packed;
+            const RowSpan sp = token(j, packed);
             if (sp.hi > sp.lo) {
                 lo = min(lo, sp.lo);
                 hi = max(hi, sp.hi);
@@ -321,7 +339,9 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
         // ---------------------------------------------------------------- a thread per row: weights
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const int w = warp >> 2, rl = (warp & 3) * 32 + lane, rr = r0 + w * WIDE_TILE + rl;
-        const int rc = min(rr, R - 1);
+        const int rc = min(rr, R - 1), rj = token_of(p, rc), hq = head * p.G + rc - rj * p.G;
+        int packed;
+        const RowSpan span = token(rj, packed);
         {   // the warp's 32 rows of queries into the swizzled tile, D / 8 lanes a row (rows behind the last: zeros); a negative
             // scale moves into their sign
             constexpr int PIECES = D / 8, AT_ONCE = 32 / PIECES;
@@ -331,7 +351,9 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const int rq = r0 + w * WIDE_TILE + (warp & 3) * 32 + i * AT_ONCE + lane / PIECES, rn = min(rq, R - 1), rt = token_of(p, rn);
-                const T *q = static_cast<const T *>(p.q) + (long long)(sq.row0 + rt) * p.q_stride + (long long)(head * p.G + rn - rt * p.G) * D;
+                int at;
+                token(rt, at);
+                const T *q = static_cast<const T *>(p.q) + (long long)at * p.q_stride + (long long)(head * p.G + rn - rt * p.G) * D;
                 v[i] = rq < R ? __ldg(reinterpret_cast<const uint4 *>(q + ch * 8)) : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
@@ -344,8 +366,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             bar_arrive(q_ready);
         }
-        const RowSpan span = row_span(p, sq, rc / p.G);
-        const float slope = MODE == 2 && p.slopes ? p.slopes[head * p.G + rc % p.G] : 0.0f;
+        const float slope = MODE == 2 && p.slopes ? p.slopes[hq] : 0.0f;
         int w_lo_max = span.lo, w_hi_min = span.hi;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -389,7 +410,16 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             const int a0 = span.lo - tb, b0 = min(span.hi, hi) - tb;  // the tile's keys that this row sees
             float times = 1.0f;
             bool small = false;
+            auto mask = [&](float with) {
+                if (__any_sync(0xffffffffu, a0 > 0))
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) s[i] = i < a0 ? with : s[i];
+                if (__any_sync(0xffffffffu, b0 < 128))
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) s[i] = i >= b0 ? with : s[i];
+            };
             if (MODE == 1) {
+                if (edge) mask(0.0f);  // what a masked key holds decides nothing
                 float mx[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) mx[k] = fabsf(s[k]);
@@ -411,14 +441,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
 #pragma unroll
                 for (int i = 0; i < 128; ++i) s[i] = score2(p, MODE == 1 && p.scale < 0.0f ? -s[i] : s[i], slope, span, tb + i);
             }
-            if (edge) {
-                if (__any_sync(0xffffffffu, a0 > 0))
-#pragma unroll
-                    for (int i = 0; i < 128; ++i) s[i] = i < a0 ? -CUDART_INF_F : s[i];
-                if (__any_sync(0xffffffffu, b0 < 128))
-#pragma unroll
-                    for (int i = 0; i < 128; ++i) s[i] = i >= b0 ? -CUDART_INF_F : s[i];
-            }
+            if (edge) mask(-CUDART_INF_F);
             auto weights = [&](auto poly) -> bool {
                 uint32_t pk[32];
                 f2 sums[2];
@@ -489,8 +512,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
         if (ok && active) {
             const bool live = rr < R;
             const bool part_out = sq.part0 >= 0;
-            const long long qt = sq.row0 + rc / p.G;
-            const int hq = head * p.G + rc % p.G;
+            const long long qt = packed;
             const long long pr = sq.part0 + (((long long)tile * sq.nsplit + part) * p.H + head) * WIDE_ROWS + w * WIDE_TILE + rl;
             const float inv = part_out ? 1.0f : (l > 0.0f || l != l ? 1.0f / l : 0.0f);  // a row that sees nothing is zero
             T *out = static_cast<T *>(p.out) + (qt * p.H * p.G + hq) * D;

@@ -41,7 +41,7 @@ using namespace aafkv;
 namespace {
 
 constexpr int ARG_SLOTS = 16;
-constexpr size_t ARG_RECORD_BYTES = 64;  // per-record room in a slot of the pinned argument ring
+constexpr size_t ARG_RECORD_BYTES = 96;  // per-record room in a slot of the pinned argument ring
 static_assert(sizeof(ComposeSeg) <= ARG_RECORD_BYTES && sizeof(AppendEntry) <= ARG_RECORD_BYTES &&
                   sizeof(MatEntry) <= ARG_RECORD_BYTES && sizeof(ImpEntry) <= ARG_RECORD_BYTES,
               "argument records must fit their room in the pinned ring");
@@ -87,7 +87,7 @@ Layout make_layout(const aaf_kv_pool_desc *d) {
     L.tile_count = off;
     off = align_up(off + sizeof(int) * ((size_t)d->max_ctx * d->max_blocks_per_ctx / 8192 + 2), 256);
     L.seq_records = off;  // sequence records of an attention / store batch too large for kernel parameters
-    off = align_up(off + sizeof(AttnSeq) * 3 * (size_t)L.max_batch, 256);
+    off = align_up(off + sizeof(AttnSeq) * 4 * (size_t)L.max_batch, 256);
     L.total = off;
     return L;
 }
@@ -122,6 +122,10 @@ struct aaf_kv_pool {
     // first token of a context whose slot no other context can share: what aaf_kv_store may write.  A fork or a sharing
     // merge moves it to the context's end; tokens added later are in blocks that the append copied or took afresh.
     std::vector<long long> own_from;
+    // Contexts with the same non-zero fork id hold the same blocks for their first fork_len tokens (whole blocks): set by a
+    // fork, in parent and children.  Shared blocks are never written again, so this stays true while both live.
+    std::vector<long long> fork_id, fork_len;
+    long long last_fork_id = 0;
     int live_ctx = 0;
     long long free_lb = 0;       // guaranteed lower bound of the device's free-block count
     long long clock = 0;         // logical clock: successful state-touching calls so far
@@ -416,6 +420,7 @@ int import_impl(aaf_kv_pool *p, const void *src_dev, const aaf_kv_xfer_desc *des
     p->free_lb -= nb;
     p->len[c] = n;
     p->own_from[c] = 0;
+    p->fork_id[c] = 0;
     p->live_ctx += 1;
     *out_ctx = c;
     const int rc = run_copy(p, ps, AAF_OP_IMPORT, (int)nb, n, st);
@@ -528,6 +533,8 @@ int aaf_kv_pool_create(const aaf_kv_pool_desc *desc, aaf_kv_pool **out) {
     p->s.tile_count = reinterpret_cast<int *>(ws + lay.tile_count);
     p->len.assign((size_t)desc->max_ctx, -1);
     p->own_from.assign((size_t)desc->max_ctx, 0);
+    p->fork_id.assign((size_t)desc->max_ctx, 0);
+    p->fork_len.assign((size_t)desc->max_ctx, 0);
     p->free_lb = desc->n_blocks;
 
     bool ok = cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device) == cudaSuccess;
@@ -732,6 +739,7 @@ int aaf_kv_import_batch(aaf_kv_pool *p, int32_t n, const void *const *src_dev, c
     for (int i = 0; i < n; ++i) {
         p->len[out_ctxs[i]] = descs[i].n_tokens;
         p->own_from[out_ctxs[i]] = 0;
+        p->fork_id[out_ctxs[i]] = 0;
     }
     p->live_ctx += n;
     const int rc = run_copy(p, ps, AAF_OP_IMPORT, (int)blocks, tokens, st);
@@ -841,6 +849,7 @@ int aaf_kv_import_host_chunked(aaf_kv_pool *p, const void *src_host, const aaf_k
     p->free_lb -= nb;
     p->len[c] = n;
     p->own_from[c] = 0;
+    p->fork_id[c] = 0;
     p->live_ctx += 1;
     *out_ctx = c;
     const int BS = p->g.BS, per_chunk = chunk_tokens / BS;
@@ -889,9 +898,16 @@ int aaf_kv_fork(aaf_kv_pool *p, aaf_ctx_t parent, int32_t k, aaf_ctx_t *out_chil
     if (e != cudaSuccess) return broke(p);
     p->clock += 1;
     p->meta_launches += 1;
+    const long long whole = T / p->g.BS * p->g.BS;
+    if (p->fork_id[parent] == 0 || p->fork_len[parent] != whole) {
+        p->fork_id[parent] = ++p->last_fork_id;
+        p->fork_len[parent] = whole;
+    }
     for (int j = 0; j < k; ++j) {
         p->len[children[j]] = T;
         p->own_from[children[j]] = T;
+        p->fork_id[children[j]] = p->fork_id[parent];
+        p->fork_len[children[j]] = p->fork_len[parent];
         out_children[j] = children[j];
     }
     p->own_from[parent] = T;
@@ -1120,6 +1136,7 @@ static int compose_impl(aaf_kv_pool *p, int32_t n_out, const int32_t *seg_off, c
     for (int o = 0; o < n_out; ++o) {
         p->len[handles[(size_t)o]] = out_len[(size_t)o];
         p->own_from[handles[(size_t)o]] = copy_all ? 0 : out_len[(size_t)o];
+        p->fork_id[handles[(size_t)o]] = 0;
         out_ctxs[o] = handles[(size_t)o];
     }
     if (!copy_all)
@@ -1242,6 +1259,7 @@ int aaf_kv_evict_to_budget(aaf_kv_pool *p, double alpha, double beta, double gam
 namespace {
 
 constexpr long long PART_ROWS = 65536;  // rows of partial results that a workspace holds
+constexpr long long SHARED_MIN = 16ll << 20;
 
 size_t attend_ws_bytes(const aaf_kv_pool *p) { return (size_t)PART_ROWS * ((size_t)p->g.D + 2) * sizeof(float) + 16; }
 
@@ -1344,7 +1362,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
     // sequences with few query rows per kv head and those with many go to kernels of their own
     std::vector<AttnSeq> few, many;
     int row0 = 0, few_rows = 1;
-    long long keys = 0;  // keys that the few-row kernel reads
+    bool forked = false;
     for (int i = 0; i < n; ++i) {
         AttnSeq s{};
         s.ctx = ctxs[i];
@@ -1355,39 +1373,109 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
         s.part0 = -1;
         row0 += s.nq;
         if (s.nq * G <= limit) {
+            s.key0 = k.window ? std::max(0, s.len - s.nq + 1 - k.window) : 0;  // what the window leaves of the earliest row
             few.push_back(s);
             few_rows = std::max(few_rows, s.nq * G);
-            keys += s.len - (k.window ? std::max(0, s.len - s.nq + 1 - k.window) : 0);
+            forked |= p->fork_id[ctxs[i]] != 0;
         } else {
             many.push_back(s);
         }
     }
     long long part_rows = 0;
     bool few_joined = false, many_joined = false;
-    int few_units = 0, many_units = 0;
-    if (!few.empty()) {
-        // Parts of equal length over the batch, so many that every warp the GPU holds has about three, at least 64 keys
-        // each: a part costs a row of partial results, an SM that gets ahead takes more of them.
-        const long long warps = 3ll * p->sm_count * 8;
-        long long chunk = std::max<long long>(64, (keys * H + warps - 1) / warps);
-        for (;;) {
-            chunk = (chunk + 15) / 16 * 16;
-            long long rows = 0;
-            for (const AttnSeq &s : few) {
-                const long long range = s.len - (k.window ? std::max(0, s.len - s.nq + 1 - k.window) : 0);
-                const long long parts = (range + chunk - 1) / chunk;
-                if (parts > 1) rows += parts * H * s.nq * G;
+    long long own_rows = 0;
+    int few_tokens = 0, many_tokens = 0;
+    int few_units = 0, many_units = 0, group_units = 0;
+    const size_t n_few = few.size();
+    if (forked && p->map_ok && !k.window && !k.spans) {
+        // Forked contexts: the blocks they share are read once for all of them (the wide kernel takes the members' rows together),
+        // each reads what is its own.  Worth a launch more and a longer join from about SHARED_MIN bytes that are not
+        // read again.
+        // Only queries behind the shared keys: every row of a group then sees all of them.
+        auto group_of = [&](const AttnSeq &x) {
+            return (long long)x.len - x.nq + 1 >= p->fork_len[x.ctx] ? p->fork_id[x.ctx] : 0;
+        };
+        std::stable_sort(few.begin(), few.end(), [&](const AttnSeq &x, const AttnSeq &y) {
+            const long long a = group_of(x), b = group_of(y);
+            return a != b ? a < b : x.nq < y.nq;
+        });
+        for (size_t i = 0, e; i < n_few; i = e) {
+            const long long id = group_of(few[i]), shared = p->fork_len[few[i].ctx];
+            for (e = i + 1; e < n_few && group_of(few[e]) == id && few[e].nq == few[i].nq; ++e) {}
+            const long long members = (long long)(e - i);
+            if (id == 0 || (members - 1) * shared * 2 * p->g.row < SHARED_MIN) continue;
+            AttnSeq g{};
+            g.ctx = few[i].ctx;
+            g.len = (int)shared;
+            g.chunk = few[i].nq;
+            g.nq = (int)(members * g.chunk);
+            g.row0 = (int)i;
+            const long long tiles = ((long long)g.nq * G + WIDE_ROWS - 1) / WIDE_ROWS;
+            long long parts = std::max<long long>(1, std::min(p->sm_count / (tiles * H), (shared + 255) / 256));
+            // its partial results, and one part of each member's own keys, have to fit into half of the workspace
+            const long long room = PART_ROWS / 2 - part_rows - own_rows - members * H * g.chunk * G;
+            while (parts > 1 && tiles * parts * H * WIDE_ROWS > room) --parts;
+            if (tiles * parts * H * WIDE_ROWS > room) continue;
+            own_rows += members * H * g.chunk * G;
+            g.nsplit = (int)parts;
+            g.unit0 = group_units;
+            g.part0 = (int)part_rows;
+            part_rows += tiles * parts * H * WIDE_ROWS;
+            group_units += (int)(tiles * parts);
+            for (size_t m = i; m < e; ++m) {
+                few[m].key0 = (int)shared;
+                few[m].gpart0 = g.part0;
+                few[m].gsplit = g.nsplit;
+                few[m].grow = (int)(m - i) * g.chunk * G;
             }
-            if (rows <= PART_ROWS / 2) break;
-            chunk *= 2;
+            few.push_back(g);
         }
-        for (AttnSeq &s : few) {
-            const long long range = s.len - (k.window ? std::max(0, s.len - s.nq + 1 - k.window) : 0);
-            s.nsplit = (int)((range + chunk - 1) / chunk);
-            s.chunk = (int)(((range + s.nsplit - 1) / s.nsplit + 15) / 16 * 16);
+    }
+    if (n_few) {
+        // Parts of about equal length over the batch, so many that the warps the GPU holds are filled a whole number of times:
+        // the cost of `waves` rounds is their number times a part's keys and a start's (about 24 keys' time).
+        const long long warps = 8ll * p->sm_count;
+        auto tasks = [&](long long chunk) {
+            long long t = 0;
+            for (size_t i = 0; i < n_few; ++i) t += (few[i].len - few[i].key0 + chunk - 1) / chunk;
+            return t * H;
+        };
+        long long keys = 0, longest = 1;
+        for (size_t i = 0; i < n_few; ++i) {
+            keys += few[i].len - few[i].key0;
+            longest = std::max<long long>(longest, few[i].len - few[i].key0);
+        }
+        long long chunk = longest, best = 1ll << 62;
+        for (int waves = 1; waves <= 4; ++waves) {
+            long long lo = std::max<long long>(2, keys * H / (waves * warps) / 16), hi = std::max(lo, (longest + 15) / 16);  // in 16 keys
+            while (lo < hi) {
+                const long long mid = (lo + hi) / 2;
+                if (tasks(16 * mid) <= waves * warps) hi = mid; else lo = mid + 1;
+            }
+            const long long rounds = (tasks(16 * lo) + warps - 1) / warps, cost = rounds * (16 * lo + 24);
+            if (cost < best) {
+                best = cost;
+                chunk = 16 * lo;
+            }
+        }
+        for (;; chunk *= 2) {  // partial results have to fit
+            long long rows = part_rows;
+            for (size_t i = 0; i < n_few; ++i) {
+                const long long parts = (few[i].len - few[i].key0 + chunk - 1) / chunk;
+                if (parts > 1 || few[i].gsplit) rows += parts * H * few[i].nq * G;
+            }
+            if (rows <= PART_ROWS || chunk > longest) break;
+        }
+        for (size_t i = 0; i < n_few; ++i) {
+            AttnSeq &s = few[i];
+            const long long range = s.len - s.key0;
+            s.nsplit = (int)((range + chunk - 1) / chunk);  // 0: a member of a group without tokens of its own
+            s.chunk = s.nsplit ? (int)(((range + s.nsplit - 1) / s.nsplit + 15) / 16 * 16) : 0;
             s.unit0 = few_units;
             few_units += s.nsplit;
-            if (s.nsplit > 1) {
+            s.tok0 = few_tokens;
+            few_tokens += s.nq;
+            if (s.nsplit > 1 || s.gsplit) {
                 s.part0 = (int)part_rows;
                 part_rows += (long long)s.nsplit * H * s.nq * G;
                 few_joined = true;
@@ -1413,6 +1501,8 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
             again_units += (int)(((long long)s.nq * G + TILE_ROWS - 1) / TILE_ROWS);
             s.nsplit = (int)parts;
             s.unit0 = many_units;
+            s.tok0 = many_tokens;
+            many_tokens += s.nq;
             if ((long long)many_units + tiles * parts > (1ll << 30) / H || again_units > (1 << 30) / H) return AAF_ERR_TOO_MANY;
             many_units += (int)(tiles * parts);
             if (parts > 1) {
@@ -1426,13 +1516,24 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
     if (!begin_read(p, st)) return broke(p);
     const int f16 = a->dtype == AAF_DTYPE_F16;
     bool ok = true;
-    if (!few.empty()) {
+    if (n_few) {
         SmallSeqs small;
         AttnParams kf = k;
-        kf.n = (int)few.size();
+        kf.n = (int)n_few;
         kf.total_units = few_units;
-        ok = place_records(p, few, small, &kf.seqs, 0, st) && launch_attend_few(kf, small, f16, few_rows, st) == cudaSuccess;
-        if (ok && few_joined) ok = launch_attend_join(kf, small, f16, 0, (int)total_q, st) == cudaSuccess;
+        kf.status = &p->s.ctl->status;
+        kf.flag = reinterpret_cast<int *>(k.part_ml + 2 * PART_ROWS);
+        ok = place_records(p, few, small, &kf.seqs, 0, st);
+        if (ok && group_units) {
+            // no key of a group is masked for one row and seen by another but the last ones, which the rows' own tokens are among
+            AttnParams kg = kf;
+            kg.first = (int)n_few;
+            kg.n = (int)(few.size() - n_few);
+            kg.total_units = group_units;
+            ok = launch_attend_wide(kg, small, f16, &p->map, layer, st) == cudaSuccess;
+        }
+        if (ok && few_units) ok = launch_attend_few(kf, small, f16, few_rows, group_units > 0, st) == cudaSuccess;
+        if (ok && few_joined) ok = launch_attend_join(kf, small, f16, 0, few_tokens, st) == cudaSuccess;
     }
     if (ok && !many.empty()) {
         SmallSeqs small;
@@ -1440,7 +1541,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
         km.n = (int)many.size();
         km.total_units = many_units;
         km.status = &p->s.ctl->status;
-        ok = place_records(p, many, small, &km.seqs, 1, st);
+        ok = place_records(p, many, small, &km.seqs, 2, st);
         if (wide) {
             km.flag = reinterpret_cast<int *>(k.part_ml + 2 * PART_ROWS);
             km.epoch = p->epoch = p->epoch % 0x7fffffff + 1;
@@ -1451,11 +1552,11 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
         if (ok && many_joined) {
             AttnParams kj = km;
             kj.flag = nullptr;
-            ok = launch_attend_join(kj, small, f16, rows_of, (int)total_q, st) == cudaSuccess;
+            ok = launch_attend_join(kj, small, f16, rows_of, many_tokens, st) == cudaSuccess;
         }
         if (ok && wide) {
             km.total_units = again_units;
-            ok = place_records(p, again, small, &km.seqs, 2, st) && launch_attend_tile(km, small, f16, st) == cudaSuccess;
+            ok = place_records(p, again, small, &km.seqs, 3, st) && launch_attend_tile(km, small, f16, st) == cudaSuccess;
         }
     }
     return ok && end_read(p, st) ? AAF_OK : broke(p);
@@ -1604,6 +1705,7 @@ int aaf_kv_prune(aaf_kv_pool *p, aaf_ctx_t ctx, const float *scores_dev, int64_t
     p->free_lb -= nb;
     p->len[c] = budget;
     p->own_from[c] = 0;
+    p->fork_id[c] = 0;
     p->live_ctx += 1;
     const int *tables = p->s.tables;
     const bool ok = begin_read(p, st) &&

@@ -209,6 +209,68 @@ def test_layers_blocks_shared_by_forks_and_repeated_contexts():
         R.check_attend(got, R.attend_ref(ctxs, n_q, q, layer=layer), torch.bfloat16, 64, True)
 
 
+@pytest.mark.parametrize("opts", [{}, dict(softcap=20.0), dict(slopes=True), dict(window=700)])
+@pytest.mark.parametrize("dim,heads,group", [(128, 8, 4), (64, 8, 2)])
+def test_forked_contexts_read_their_shared_blocks_together(dim, heads, group, opts):
+    if opts.get("slopes"):
+        opts = dict(opts, slopes=2.0 ** (-8.0 * torch.arange(1, heads * group + 1, device="cuda") / (heads * group)))
+    pool = R.make_pool(1, heads, dim, 16, 1200, max_ctx=64)
+    root = R.add_ctx(pool, 2100, 1)
+    alone = R.add_ctx(pool, 777, 2)
+    st, kids = pool.fork(root.handle, 9)
+    assert st == 0
+    own = [1, 2, 5, 16, 17, 300, 33, 64, 4]
+    tails = [R.rand((1, 2, t, heads, dim), 60 + i) for i, t in enumerate(own)]
+    assert pool.append(kids[:9], own, tails)[0] == 0
+    ctxs = [R.Ctx(h, torch.cat((root.rows, t), 2)) for h, t in zip(kids, tails)]
+    st, more = pool.fork(ctxs[5].handle, 7)  # a second generation, without tokens of its own
+    assert st == 0
+    ctxs += [R.Ctx(h, ctxs[5].rows) for h in more] + [alone, root]
+    order = [3, 17, 0, 9, 10, 16, 11, 1, 2, 4, 12, 5, 13, 6, 7, 14, 8, 15, 3]
+    batch = [ctxs[i] for i in order]
+    for n_q in ([1] * len(batch), [1 + i % 2 for i in range(len(batch))], [1] * 10 + [40] + [1] * (len(batch) - 11)):
+        n_q = [min(a, len(c)) for a, c in zip(n_q, batch)]
+        q = R.rand((sum(n_q), heads * group, dim), sum(n_q), scale=2.0)
+        got = run_attend(pool, batch, n_q, q, **opts)
+        R.check_attend(got, R.attend_ref(batch, n_q, q, **opts), torch.bfloat16, dim, True)
+        again = run_attend(pool, batch, n_q, q, **opts)
+        assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+def test_forked_contexts_more_than_kernel_parameters_hold():
+    pool = R.make_pool(1, 8, 64, 16, 800, max_ctx=120)
+    root = R.add_ctx(pool, 1030, 1)
+    st, kids = pool.fork(root.handle, 100)
+    tails = [R.rand((1, 2, 1 + i % 7, 8, 64), 60 + i) for i in range(100)]
+    assert pool.append(kids, [1 + i % 7 for i in range(100)], tails)[0] == 0
+    ctxs = [R.Ctx(h, torch.cat((root.rows, t), 2)) for h, t in zip(kids, tails)]
+    q = R.rand((100, 16, 64), 3, scale=2.0)
+    got = run_attend(pool, ctxs, [1] * 100, q)
+    R.check_attend(got, R.attend_ref(ctxs, [1] * 100, q), torch.bfloat16, 64, True)
+
+
+def test_nonfinite_values_of_shared_blocks_reach_the_forks():
+    pool = R.make_pool(1, 8, 128, 16, 400)
+    rows = R.rand((1, 2, 1600, 8, 128), 5)
+    rows[0, 1, 1599, 0, 3] = math.inf
+    rows[0, 1, 700, 1, 4] = math.nan
+    root = R.add_ctx(pool, 1600, 0, rows)
+    st, kids = pool.fork(root.handle, 6)
+    assert pool.reserve(kids[:3], [1, 1, 1])[0] == 0
+    kv = torch.zeros(3, 8, 128, dtype=torch.bfloat16, device="cuda")
+    assert pool.store(0, kids[:3], [1, 1, 1], kv, kv)[0] == 0
+    q = R.rand((6, 32, 128), 6, scale=2.0)
+    st, (out, lse) = pool.attend(0, kids, None, q)
+    assert st == 0
+    assert (out[:, :4, 3] == math.inf).all() and torch.isnan(out[:, 4:8, 4]).all() and torch.isfinite(lse).all()
+    rest = out.clone()
+    rest[:, :4, 3], rest[:, 4:8, 4] = 0, 0
+    assert torch.isfinite(rest).all()
+    # two queries each, the first of them before the last shared token
+    st, (out, lse) = pool.attend(0, kids[3:], [2, 2, 2], q)
+    assert st == 0 and torch.isfinite(out[0::2, :4, 3]).all() and (out[1::2, :4, 3] == math.inf).all()
+
+
 def test_strided_queries_and_same_bits_again():
     pool = R.make_pool(1, 2, 64, 16, 256)
     ctxs = [R.add_ctx(pool, t, t) for t in (100, 901)]
