@@ -283,6 +283,9 @@ class KVPool:
 
         self.torch = torch
         self.device = torch.device("cuda", device)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
+        self._codes = {torch.bfloat16: AAF_DTYPE_BF16, torch.float16: AAF_DTYPE_F16}
         self.L, self.H, self.D, self.BS, self.E, self.NB = n_layers, n_kv_heads, head_dim, block_size, elt_bytes, n_blocks
         self.max_ctx, self.max_blk = max_ctx, max_blocks_per_ctx
         self.row = n_kv_heads * head_dim * elt_bytes
@@ -315,6 +318,10 @@ class KVPool:
     # ------------------------------------------------------------------ helpers
     def _stream(self):
         return C.c_void_p(self.torch.cuda.current_stream(self.device).cuda_stream)
+
+    def _stream_handle(self):
+        """The current stream as an integer (what the latency-critical calls pass)."""
+        return self._raw_stream(self.device.index)
 
     def xfer_desc(self, n_tokens, pos_start=0) -> aaf_kv_xfer_desc:
         x = aaf_kv_xfer_desc()
@@ -417,89 +424,91 @@ class KVPool:
 
     # ------------------------------------------------------------------ operators that compute with the payload
     # Tensors: q [tokens, q heads, head_dim], k and v [tokens, kv heads, head_dim], bf16 or f16, the heads of a token
-    # contiguous; tokens packed in the order of ctxs.
-    def _rows(self, t, tokens, heads, name, dtype=None):
-        """Device pointer and token stride of a packed per-token tensor."""
-        if t.device != self.device or t.dim() != 3 or t.shape != (tokens, heads, self.D) or (dtype is not None and t.dtype != dtype):
-            raise ValueError(f"{name}: expected a [{tokens}, {heads}, {self.D}] tensor of the pool's device and one dtype, "
+    # contiguous; tokens packed in the order of ctxs.  These calls are made once per layer and step: the checks are few
+    # and cheap, the library checks the rest.
+    def _rows(self, t, tokens, heads, name, dtype):
+        """Token stride of a packed per-token tensor."""
+        d = self.D
+        if t.shape != (tokens, heads, d) or t.dtype != dtype or t.device != self.device:
+            raise ValueError(f"{name}: expected a [{tokens}, {heads}, {d}] tensor of {dtype} on {self.device}, "
                              f"got {tuple(t.shape)} {t.dtype} on {t.device}")
-        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.D):
+        st = t.stride()
+        if st[2] != 1 or (heads > 1 and st[1] != d):
             raise ValueError(f"{name}: the heads of a token must be contiguous")
-        return t.data_ptr(), (t.stride(0) if tokens > 1 else max(t.stride(0), heads * self.D))
+        return st[0] if tokens > 1 else max(st[0], heads * d)
 
     def _flat(self, t, dtype, n, name):
-        if t is None:
-            return None
-        if t.device != self.device or t.dtype != dtype or not t.is_contiguous() or t.numel() != n:
+        if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device:
             raise ValueError(f"{name}: expected a contiguous {dtype} tensor of {n} entries on the pool's device")
         return t.data_ptr()
 
-    def _dtype(self, t):
-        code = {self.torch.bfloat16: AAF_DTYPE_BF16, self.torch.float16: AAF_DTYPE_F16}.get(t.dtype)
+    def _code(self, t):
+        code = self._codes.get(t.dtype)
         if code is None:
             raise ValueError(f"bfloat16 or float16 expected, got {t.dtype}")
         return code
 
     def reserve(self, ctxs, n_new):
         n = len(ctxs)
-        return aaf_kv_reserve(self.h, n, (C.c_int32 * max(n, 1))(*ctxs), (C.c_int32 * max(n, 1))(*n_new), self._stream()), None
+        return load().aaf_kv_reserve(self.h, n, (C.c_int32 * (n or 1))(*ctxs), (C.c_int32 * (n or 1))(*n_new),
+                                     self._stream_handle()), None
 
     def store(self, layer, ctxs, n_new, k, v, q=None, q_out=None, rope=None, pos=None):
         """Rotates q (into q_out, default in place) and k, writes k and v into the slots of the contexts' last n_new tokens."""
-        n, tokens = len(ctxs), sum(n_new)
-        d = aaf_kv_store_desc()
-        d.struct_size, d.dtype = C.sizeof(d), self._dtype(k)
-        d.k, d.k_stride = self._rows(k, tokens, self.H, "k")
-        d.v, d.v_stride = self._rows(v, tokens, self.H, "v", k.dtype)
+        n, tokens, dtype = len(ctxs), sum(n_new), k.dtype
+        code = self._code(k)
+        ks, vs = self._rows(k, tokens, self.H, "k", dtype), self._rows(v, tokens, self.H, "v", dtype)
+        heads = qp = op = qs = os = 0
         if q is not None:
-            d.n_q_heads = q.shape[1]
-            d.q, d.q_stride = self._rows(q, tokens, q.shape[1], "q", k.dtype)
-            d.q_out, d.q_out_stride = (d.q, d.q_stride) if q_out is None else self._rows(q_out, tokens, q.shape[1], "q_out", k.dtype)
-        d.mscale = 1.0
+            heads = q.shape[1] if q.dim() == 3 else 0
+            qs, qp = self._rows(q, tokens, heads, "q", dtype), q.data_ptr()
+            os, op = (qs, qp) if q_out is None else (self._rows(q_out, tokens, heads, "q_out", dtype), q_out.data_ptr())
+        rot, inter, mscale, inv = 0, 0, 1.0, 0
         if rope is not None:
             if rope.inv_freq.device != self.device:
                 raise ValueError("rope: frequencies on another device than the pool")
-            d.rot_dim, d.interleaved, d.mscale = rope.rot_dim, int(rope.interleaved), rope.mscale
-            d.inv_freq = rope.inv_freq.data_ptr()
-        d.pos = self._flat(pos, self.torch.int64, tokens, "pos")
-        return aaf_kv_store(self.h, layer, C.byref(d), n, (C.c_int32 * max(n, 1))(*ctxs), (C.c_int32 * max(n, 1))(*n_new),
-                            self._stream()), None
+            rot, inter, mscale, inv = rope.rot_dim, int(rope.interleaved), rope.mscale, rope.inv_freq.data_ptr()
+        d = aaf_kv_store_desc(C.sizeof(aaf_kv_store_desc), code, heads, rot, inter, mscale, inv,
+                              None if pos is None else self._flat(pos, self.torch.int64, tokens, "pos"),
+                              qp, op, k.data_ptr(), v.data_ptr(), qs, os, ks, vs)
+        return load().aaf_kv_store(self.h, layer, d, n, (C.c_int32 * (n or 1))(*ctxs), (C.c_int32 * (n or 1))(*n_new),
+                                   self._stream_handle()), None
 
     def _attn(self, q, tokens, scale, softcap, window, slopes, spans):
-        a = aaf_kv_attn()
-        a.struct_size, a.dtype, a.window = C.sizeof(a), self._dtype(q), window
-        a.n_q_heads = q.shape[1] if q.dim() == 3 else 0
-        ptr, a.q_stride = self._rows(q, tokens, a.n_q_heads, "q")
-        a.scale, a.softcap = self.D ** -0.5 if scale is None else scale, softcap
-        a.slopes = self._flat(slopes, self.torch.float32, a.n_q_heads, "slopes")
-        a.spans = self._flat(spans, self.torch.int32, 2 * tokens, "spans")
-        return a, ptr
+        heads = q.shape[1] if q.dim() == 3 else 0
+        stride = self._rows(q, tokens, heads, "q", q.dtype)
+        return aaf_kv_attn(C.sizeof(aaf_kv_attn), self._code(q), heads, window, self.D ** -0.5 if scale is None else scale, softcap,
+                           None if slopes is None else self._flat(slopes, self.torch.float32, heads, "slopes"),
+                           None if spans is None else self._flat(spans, self.torch.int32, 2 * tokens, "spans"), stride)
 
     def attend(self, layer, ctxs, n_q, q, out=None, lse=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):
         """Attention of the contexts' last n_q tokens (None: one each); returns (status, (out, lse))."""
         torch = self.torch
         n = len(ctxs)
         tokens = n if n_q is None else sum(n_q)
-        a, ptr = self._attn(q, tokens, scale, softcap, window, slopes, spans)
+        a = self._attn(q, tokens, scale, softcap, window, slopes, spans)
+        heads = a.n_q_heads
         if out is None:
-            out = torch.empty(tokens, a.n_q_heads, self.D, dtype=q.dtype, device=self.device)
-        elif self._rows(out, tokens, a.n_q_heads, "out", q.dtype)[1] != a.n_q_heads * self.D:
+            out = torch.empty((tokens, heads, self.D), dtype=q.dtype, device=self.device)
+        elif self._rows(out, tokens, heads, "out", q.dtype) != heads * self.D:
             raise ValueError("out: dense tensor expected")
         if lse is None:
-            lse = torch.empty(tokens, a.n_q_heads, dtype=torch.float32, device=self.device)
-        if self._attend_ws is None:
-            self._attend_ws = torch.empty(aaf_kv_attend_workspace_bytes(self.h), dtype=torch.uint8, device=self.device)
-        st = aaf_kv_attend(self.h, layer, C.byref(a), n, (C.c_int32 * max(n, 1))(*ctxs),
-                           None if n_q is None else (C.c_int32 * max(n, 1))(*n_q), ptr, out.data_ptr(),
-                           self._flat(lse, torch.float32, tokens * a.n_q_heads, "lse"), self._attend_ws.data_ptr(),
-                           self._attend_ws.numel(), self._stream())
+            lse = torch.empty((tokens, heads), dtype=torch.float32, device=self.device)
+        else:
+            self._flat(lse, torch.float32, tokens * heads, "lse")
+        ws = self._attend_ws
+        if ws is None:
+            ws = self._attend_ws = torch.empty(aaf_kv_attend_workspace_bytes(self.h), dtype=torch.uint8, device=self.device)
+        st = load().aaf_kv_attend(self.h, layer, a, n, (C.c_int32 * (n or 1))(*ctxs),
+                                  None if n_q is None else (C.c_int32 * (n or 1))(*n_q), q.data_ptr(), out.data_ptr(),
+                                  lse.data_ptr(), ws.data_ptr(), ws.numel(), self._stream_handle())
         return st, ((out, lse) if st == AAF_OK else None)
 
     def attn_mass(self, layer, ctxs, n_q, q, lse, mass, prev=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):
         """mass[i, t] = prev[i, t] (default 0; may be mass itself) + what token t of context i received of this attention."""
         n = len(ctxs)
         tokens = n if n_q is None else sum(n_q)
-        a, ptr = self._attn(q, tokens, scale, softcap, window, slopes, spans)
+        a = self._attn(q, tokens, scale, softcap, window, slopes, spans)
         for t in (mass,) if prev is None else (mass, prev):
             if t.device != self.device or t.dtype != self.torch.float32 or t.dim() != 2 or t.shape != mass.shape or \
                     t.shape[0] != n or t.stride(1) != 1 or (n > 1 and t.stride(0) != mass.stride(0)):
@@ -508,11 +517,10 @@ class KVPool:
         stride = mass.stride(0) if n > 1 else mass.shape[1]
         if mass.shape[1] < stride and any((self.ctx_len(c) or 0) > mass.shape[1] for c in ctxs):
             return AAF_ERR_DST_TOO_SMALL, None
-        st = aaf_kv_attn_mass(self.h, layer, C.byref(a), n, (C.c_int32 * max(n, 1))(*ctxs),
-                              None if n_q is None else (C.c_int32 * max(n, 1))(*n_q), ptr,
-                              self._flat(lse, self.torch.float32, tokens * a.n_q_heads, "lse"),
-                              None if prev is None else prev.data_ptr(), mass.data_ptr(),
-                              stride, self._stream())
+        st = load().aaf_kv_attn_mass(self.h, layer, a, n, (C.c_int32 * (n or 1))(*ctxs),
+                                     None if n_q is None else (C.c_int32 * (n or 1))(*n_q), q.data_ptr(),
+                                     self._flat(lse, self.torch.float32, tokens * a.n_q_heads, "lse"),
+                                     None if prev is None else prev.data_ptr(), mass.data_ptr(), stride, self._stream_handle())
         return st, (mass if st == AAF_OK else None)
 
     def prune(self, ctx, scores, budget, sink=0, recent=0, kept=None, kept_scores=None):
@@ -523,9 +531,10 @@ class KVPool:
         if kept is None:
             kept = torch.empty(max(budget, 1), dtype=torch.int32, device=self.device)
         out = C.c_int32(-1)
-        st = aaf_kv_prune(self.h, ctx, self._flat(scores, torch.float32, scores.numel() if n is None else n, "scores"), budget, sink, recent,
-                          self._flat(kept, torch.int32, max(budget, 1), "kept"),
-                          self._flat(kept_scores, torch.float32, max(budget, 1), "kept_scores"), C.byref(out), self._stream())
+        st = load().aaf_kv_prune(self.h, ctx, self._flat(scores, torch.float32, scores.numel() if n is None else n, "scores"), budget,
+                                 sink, recent, self._flat(kept, torch.int32, max(budget, 1), "kept"),
+                                 None if kept_scores is None else self._flat(kept_scores, torch.float32, max(budget, 1), "kept_scores"),
+                                 C.byref(out), self._stream_handle())
         return st, (out.value if st == AAF_OK else None)
 
     def materialize_host(self, ctx, t0, t1, dst_host, staging):

@@ -6,13 +6,13 @@
 // parts, each part leaves (m, l, o) and attend_join adds them up in part order, so results do not depend on timing.
 //
 // Bound: every cached row is used by at most 8 * NT query rows, so the bytes of K and V decide.  A warp owns one kv
-// head of one part and shares nothing: each lane copies exactly the 16-byte pieces that its own matrix fragments need
-// (cp.async into slots of its own, several tiles of 16 tokens in flight), so there is no barrier and no bank conflict.
+// head of one part and shares nothing with the others: no barrier, only warps that wait for their own copies (cp.async,
+// several tiles of 16 tokens in flight; a copy instruction covers whole rows, 256 contiguous bytes at 128 dims).
 // The tensor products take the tokens as the M side (16) and the query rows as the N side (8): S^T = K Q^T and
 // O^T = V^T P^T waste nothing for 8 rows, where rows as M would fill half a tile at best.  The order of the head
 // dimensions inside a product is free as long as both operands agree, and so is the order of the output rows: lane
 // (g, t) takes 8 consecutive dimensions of token g for K, and of tokens 2t, 2t+1, 2t+8, 2t+9 for V, whose pairs two
-// byte permutes bring together.
+// byte permutes bring together; the 16-byte pieces of a row are stored so that neither pattern meets a bank twice.
 //
 // P is split into two 16-bit parts (p = hi + lo) and multiplied twice: the tensor pipe is idle anyway and the result
 // then carries the output's own rounding only.
@@ -21,10 +21,9 @@
 namespace aafkv {
 
 template <int DP> struct FewShape {
-    static constexpr int KC = 2 * (DP / 32);        // 16-byte pieces of K per lane and tile of 16 tokens
-    static constexpr int VC = 4 * (DP / 64);        // of V
-    static constexpr int SLOTS = KC + VC;
-    static constexpr int STAGE_BYTES = SLOTS * 32 * 16;
+    static constexpr int PIECES = DP / 8;           // 16-byte pieces of a row
+    static constexpr int ROW = DP * 2, HALF = 16 * ROW;  // bytes of a row, of a tile of 16 keys (or values)
+    static constexpr int STAGE_BYTES = 2 * HALF;
     static constexpr int WARPS = DP <= 128 ? 4 : 3;
     static constexpr int STAGES = DP == 64 ? 6 : (DP == 128 ? 3 : 2);
     static constexpr int SMEM = WARPS * STAGES * STAGE_BYTES;  // 96 KB: two CTAs an SM, one starts while the other streams
@@ -74,7 +73,11 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
     if (end <= beg) beg = end = 0;  // nothing to see in this part: no token index is formed from an empty range
     const int tiles = (end - beg + 15) / 16;
 
-    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S::STAGES * S::STAGE_BYTES) + lane * 16;
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S::STAGES * S::STAGE_BYTES);
+    // where piece c of row r lies: lanes that read together have two rows and four pieces of K, four even (odd) rows and two
+    // pieces of V
+    auto k_at = [](int r, int c) { return (uint32_t)(r * S::ROW + ((c ^ ((r & 1) << 2)) << 4)); };
+    auto v_at = [](int r, int c) { return (uint32_t)(S::HALF + r * S::ROW + ((c ^ (r & 6)) << 4)); };
     const int *table = p.tables + (long long)sq.ctx * p.max_blk;
     const char *kb = p.kbase + (long long)head * p.D * 2;
 
@@ -88,28 +91,15 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
             const int b = block_of(tm, p.BS, p.bs_shift);
             const long long off = (long long)id * 2 * p.run + (long long)(tm - b * p.BS) * p.row;
             const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
+            constexpr int AT_ONCE = 32 / S::PIECES;  // rows of one copy instruction
+            const int c = lane % S::PIECES;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const char *src = kb + __shfl_sync(0xffffffffu, off, g + 8 * i);
-                const bool ok = beg + tile * 16 + g + 8 * i < end;
-#pragma unroll
-                for (int kk = 0; kk < DP / 32; ++kk) {
-                    const int d = kk * 32 + t4 * 8;
-                    const bool in = ok && d < p.D;
-                    copy16(st + (i * (DP / 32) + kk) * 512, in ? src + d * 2 : kb, in ? 16 : 0);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int tk = 2 * t4 + (i & 1) + (i >> 1) * 8;
-                const char *src = kb + p.run + __shfl_sync(0xffffffffu, off, tk);
-                const bool ok = beg + tile * 16 + tk < end;
-#pragma unroll
-                for (int c = 0; c < DP / 64; ++c) {
-                    const int d = c * 64 + g * 8;
-                    const bool in = ok && d < p.D;
-                    copy16(st + (S::KC + i * (DP / 64) + c) * 512, in ? src + d * 2 : kb, in ? 16 : 0);
-                }
+            for (int i = 0; i < 16 / AT_ONCE; ++i) {
+                const int r = i * AT_ONCE + lane / S::PIECES;
+                const char *src = kb + __shfl_sync(0xffffffffu, off, r) + c * 16;
+                const bool in = beg + tile * 16 + r < end && c * 8 < p.D;
+                copy16(st + k_at(r, c), in ? src : kb, in ? 16 : 0);
+                copy16(st + v_at(r, c), in ? src + p.run : kb, in ? 16 : 0);
             }
         }
         copy_commit();
@@ -149,6 +139,7 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
 
     for (int tile = 0; tile < tiles; ++tile) {
         copy_wait<S::STAGES - 1>();
+        __syncwarp();  // every lane's pieces have landed
         const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
         const int tb = beg + tile * 16;
         float s[NT][4];
@@ -156,7 +147,7 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
         for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
 #pragma unroll
         for (int kk = 0; kk < DP / 32; ++kk) {
-            const uint4 w = lds16(st + kk * 512), x = lds16(st + (DP / 32 + kk) * 512);
+            const uint4 w = lds16(st + k_at(g, kk * 4 + t4)), x = lds16(st + k_at(g + 8, kk * 4 + t4));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 Elt<T>::mma(s[nt], w.x, x.x, w.y, x.y, qf[nt][kk].x, qf[nt][kk].y);
@@ -223,7 +214,7 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
         for (int c = 0; c < DP / 64; ++c) {
             uint4 v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = lds16(st + (S::KC + i * (DP / 64) + c) * 512);
+            for (int i = 0; i < 4; ++i) v[i] = lds16(st + v_at(2 * t4 + (i & 1) + (i >> 1) * 8, c * 8 + g));
             const uint32_t w0[4] = {v[0].x, v[0].y, v[0].z, v[0].w}, w1[4] = {v[1].x, v[1].y, v[1].z, v[1].w};
             const uint32_t w2[4] = {v[2].x, v[2].y, v[2].z, v[2].w}, w3[4] = {v[3].x, v[3].y, v[3].z, v[3].w};
 #pragma unroll
@@ -255,6 +246,7 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
             }
         }
         const int nxt = table_id(tile + S::STAGES + 1);
+        __syncwarp();  // every lane has read this stage
         issue(tile + S::STAGES, id);
         id = nxt;
     }
@@ -311,8 +303,8 @@ int few_rows_limit(int D) { return D <= 64 ? 32 : (D <= 128 ? 16 : 8); }
 
 template <typename T, int DP, int NT>
 static cudaError_t few_go(const AttnParams &p, const SmallSeqs &small, bool beside, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(attend_few_kernel<T, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         FewShape<DP>::SMEM);
+    static unsigned long long seen = 0;
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_few_kernel<T, DP, NT>), FewShape<DP>::SMEM, &seen);
     if (e != cudaSuccess) return e;
     constexpr int W = FewShape<DP>::WARPS;
     const long long tasks = (long long)p.total_units * p.H;
@@ -342,19 +334,21 @@ cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f
 }
 
 // ------------------------------------------------------------------------------------------ join
-// Adds up the parts of a split row: o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.  One CTA per query token and
-// query head; 8 warps take every eighth part, four dimensions a lane (DP / 128 passes), and meet in shared memory in
-// warp order.
-constexpr int JOIN_WARPS = 8;
-template <typename T>
+// Adds up the parts of a split row: o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s, in part order.  SPREAD warps work on a
+// query token's head, four dimensions a lane: one while there are few parts, a whole CTA's eight, each with every eighth
+// part, when there are many and few rows to share them out over; then they meet in shared memory in warp order.
+constexpr int JOIN_WARPS = 8, JOIN_AHEAD = 8;
+template <typename T, int SPREAD>
 __global__ void __launch_bounds__(JOIN_WARPS * 32)
-    attend_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small, int tile_rows) {
+    attend_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small, int tile_rows, int rows) {
     __shared__ float4 acc_s[JOIN_WARPS][32];
     __shared__ float sum_s[JOIN_WARPS], max_s[JOIN_WARPS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % SPREAD;
+    const int out_row = blockIdx.x * (JOIN_WARPS / SPREAD) + (threadIdx.x >> 5) / SPREAD;
+    if (out_row >= rows) return;  // SPREAD == 1 only: nobody waits for this warp
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
     const int Hq = p.H * p.G;
-    const int tok = (int)(blockIdx.x / Hq), hq = (int)(blockIdx.x - (long long)tok * Hq), head = hq / p.G;
+    const int tok = out_row / Hq, hq = out_row - tok * Hq, head = hq / p.G;
     int lo = 0, hi = p.n - 1;  // record of the query token
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -378,77 +372,99 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32)
         grow = sq.gpart0 + ((long long)(gr / WIDE_ROWS) * sq.gsplit * p.H + head) * WIDE_ROWS + gr % WIDE_ROWS;
         gstep = (long long)p.H * WIDE_ROWS;
     }
-    const int parts = sq.nsplit + sq.gsplit;
+    const int parts = sq.nsplit + sq.gsplit, dims = p.D;
     auto at = [&](int s) { return s < sq.nsplit ? row + s * step : grow + (s - sq.nsplit) * gstep; };
+    auto load = [&](int s, int d) {
+        return s < parts && d < dims ? __ldcg(reinterpret_cast<const float4 *>(p.part_o + at(s) * dims + d)) : make_float4(0, 0, 0, 0);
+    };
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the parts are written
+    float4 first[JOIN_AHEAD];  // the first parts' outputs are on their way while the weights are worked out
+#pragma unroll
+    for (int i = 0; i < JOIN_AHEAD; ++i) first[i] = load(warp + i * SPREAD, lane * 4);
     float top = -CUDART_INF_F;
-    for (int s = threadIdx.x; s < parts; s += JOIN_WARPS * 32) top = fmaxf(top, p.part_ml[2 * at(s)]);
+    for (int s = warp * 32 + lane; s < parts; s += SPREAD * 32) top = fmaxf(top, p.part_ml[2 * at(s)]);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    if (lane == 0) max_s[warp] = top;
-    __syncthreads();
+    if (SPREAD > 1) {
+        if (lane == 0) max_s[warp] = top;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < JOIN_WARPS; ++w) top = fmaxf(top, max_s[w]);
+        for (int w = 0; w < SPREAD; ++w) top = fmaxf(top, max_s[w]);
+    }
     const float base = top == -CUDART_INF_F ? 0.0f : top;
-    T *out = static_cast<T *>(p.out) + (qt * Hq + hq) * p.D;
-    for (int d0 = 0; d0 < p.D; d0 += 128) {
+    auto weight = [&](int s) { return s < parts ? ex2(p.part_ml[2 * at(s)] - base) : 0.0f; };  // a part that saw nothing: m = -inf
+    float sum = 0.0f;
+    for (int s = warp + lane * SPREAD; s < parts; s += 32 * SPREAD) sum += weight(s) * p.part_ml[2 * at(s) + 1];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (SPREAD > 1 && lane == 0) sum_s[warp] = sum;
+    T *out = static_cast<T *>(p.out) + (qt * Hq + hq) * dims;
+    for (int d0 = 0; d0 < dims; d0 += 128) {
         const int d = d0 + lane * 4;
         float4 a = make_float4(0, 0, 0, 0);
-        float sum = 0.0f;
-#pragma unroll 4
-        for (int s = warp; s < parts; s += JOIN_WARPS) {
-            const long long pr = at(s);
-            const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + 2 * pr);
-            const float4 v = d < p.D ? *reinterpret_cast<const float4 *>(p.part_o + pr * p.D + d) : make_float4(0, 0, 0, 0);
-            const float w = ex2(ml.x - base);  // a part that saw nothing has m = -inf, l = 0, o = 0
-            sum += w * ml.y;
-            a.x += w * v.x;
-            a.y += w * v.y;
-            a.z += w * v.z;
-            a.w += w * v.w;
-        }
-        __syncthreads();
-        acc_s[warp][lane] = a;
-        if (lane == 0) sum_s[warp] = sum;
-        __syncthreads();
-        if (warp == 0) {
+        for (int s0 = warp; s0 < parts; s0 += JOIN_AHEAD * SPREAD) {
+            float4 v[JOIN_AHEAD];
 #pragma unroll
-            for (int w = 1; w < JOIN_WARPS; ++w) {
+            for (int i = 0; i < JOIN_AHEAD; ++i) v[i] = d0 == 0 && s0 == warp ? first[i] : load(s0 + i * SPREAD, d);
+#pragma unroll
+            for (int i = 0; i < JOIN_AHEAD; ++i) {
+                const float w = weight(s0 + i * SPREAD);
+                a.x += w * v[i].x;
+                a.y += w * v[i].y;
+                a.z += w * v[i].z;
+                a.w += w * v[i].w;
+            }
+        }
+        float all = sum;
+        if (SPREAD > 1) {
+            __syncthreads();
+            acc_s[warp][lane] = a;
+            __syncthreads();
+            all = sum_s[0];
+            if (warp) continue;
+#pragma unroll
+            for (int w = 1; w < SPREAD; ++w) {
                 const float4 v = acc_s[w][lane];
                 a.x += v.x;
                 a.y += v.y;
                 a.z += v.z;
                 a.w += v.w;
-                sum += sum_s[w];
+                all += sum_s[w];
             }
-            const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-            if (d < p.D)
-                *reinterpret_cast<uint2 *>(out + d) =
-                    make_uint2(Elt<T>::pack(a.x * inv, a.y * inv), Elt<T>::pack(a.z * inv, a.w * inv));
-            if (d0 == 0 && lane == 0 && p.lse) {
-                const RowSpan sp = row_span(p, sq, j);
-                const float slope = p.slopes ? p.slopes[hq] : 0.0f;
-                p.lse[qt * Hq + hq] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * LN2 - slope * (float)sp.near;
-            }
+        }
+        const float inv = all > 0.0f || all != all ? 1.0f / all : 0.0f;
+        if (d < dims)
+            *reinterpret_cast<uint2 *>(out + d) = make_uint2(Elt<T>::pack(a.x * inv, a.y * inv), Elt<T>::pack(a.z * inv, a.w * inv));
+        if (d0 == 0 && lane == 0 && p.lse) {
+            const RowSpan sp = row_span(p, sq, j);
+            const float slope = p.slopes ? p.slopes[hq] : 0.0f;
+            p.lse[qt * Hq + hq] = all == 0.0f ? -CUDART_INF_F : (top + log2f(all)) * LN2 - slope * (float)sp.near;
         }
     }
 }
 
-cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int tokens,
-                               cudaStream_t st) {
+template <typename T, int SPREAD>
+static cudaError_t join_go(const AttnParams &p, const SmallSeqs &small, int tile_rows, int rows, cudaStream_t st) {
     // launched so that its CTAs come up while the parts are still being computed; it waits for them itself
     cudaLaunchAttribute early;
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)((long long)tokens * p.H * p.G));
+    cfg.gridDim = dim3((unsigned)((rows + JOIN_WARPS / SPREAD - 1) / (JOIN_WARPS / SPREAD)));
     cfg.blockDim = dim3(JOIN_WARPS * 32);
     cfg.stream = st;
     cfg.attrs = &early;
     cfg.numAttrs = 1;
-    const cudaError_t e = f16 ? cudaLaunchKernelEx(&cfg, attend_join_kernel<__half>, p, small, tile_rows)
-                              : cudaLaunchKernelEx(&cfg, attend_join_kernel<__nv_bfloat16>, p, small, tile_rows);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, attend_join_kernel<T, SPREAD>, p, small, tile_rows, rows);
     return e != cudaSuccess ? e : cudaGetLastError();
+}
+cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int tokens, int max_parts,
+                               int sm_count, cudaStream_t st) {
+    const int rows = tokens * p.H * p.G;
+    if (max_parts <= 2 * JOIN_AHEAD || rows > 2 * sm_count)
+        return f16 ? join_go<__half, 1>(p, small, tile_rows, rows, st) : join_go<__nv_bfloat16, 1>(p, small, tile_rows, rows, st);
+    return f16 ? join_go<__half, JOIN_WARPS>(p, small, tile_rows, rows, st)
+               : join_go<__nv_bfloat16, JOIN_WARPS>(p, small, tile_rows, rows, st);
 }
 
 }  // namespace aafkv

@@ -64,7 +64,6 @@ struct MassParams {
     const float *prev;    // may be null
     float *mass;
     long long mass_stride;
-    int chunk;            // keys of one CTA
 };
 
 struct StoreSeq {         // 24 bytes
@@ -88,12 +87,21 @@ struct StoreParams {
     float mscale;
 };
 
+// Shared memory beyond 48 KB is allowed once per kernel and device; `seen` is the kernel's own.
+inline cudaError_t allow_smem(const void *kernel, int bytes, unsigned long long *seen) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < 64 && (*seen >> dev & 1))) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) *seen |= 1ull << dev;
+    return e;
+}
+
 // ---- launchers (each returns cudaGetLastError() of its launches); f16: 1 = half, 0 = bfloat16
 constexpr int FEW_MAX_DIM = 256;
 int few_rows_limit(int D);                       // most rows of a kv head that the few-row kernel takes
 constexpr int TILE_ROWS = 64;                    // rows of a unit of the tile kernel
 constexpr int MASS_CHUNK = 64;                   // keys of a CTA of the mass kernel
-constexpr int MASS_MAX_HEADS = 512;              // its kv heads: chunk * heads floats of shared memory
 // beside: brought up beside the kernel launched before it, which it does not depend on
 cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, bool beside,
                               cudaStream_t st);
@@ -106,9 +114,9 @@ struct alignas(64) PoolMap {                     // a tensor map, opaque to the 
     unsigned char bytes[128];
 };
 bool encode_pool_map(const Geom &g, PoolMap *out);
-cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int tokens,
-                               cudaStream_t st);
-cudaError_t launch_attn_mass(const MassParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
+cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int tokens, int max_parts,
+                               int sm_count, cudaStream_t st);
+cudaError_t launch_attn_mass(const MassParams &p, const SmallSeqs &small, int f16, int max_rows, cudaStream_t st);
 cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16, cudaStream_t st);
 // keep list of a pruned context: kept[budget] ascending, kept_scores (may be null); then the row gather
 cudaError_t launch_select(const float *scores, int len, int budget, int sink, int recent, int *kept, float *kept_scores,

@@ -1,114 +1,206 @@
 // Attention mass of cached tokens: mass_t = prev_t + sum over query rows r of exp(score_rt - lse_r).
 //
-// One pass over the keys; with the rows' log-sums given, every token is independent of the others.  A CTA takes a
-// chunk of tokens of one sequence and all kv heads, so the sum over heads stays inside it and is taken in a fixed
-// order (head by head, row block by row block): no atomics, the same bits every time.  Bound: the bytes of K.  A
-// warp holds the keys of 32 tokens of one head in registers, in the layout of the products' first operand, straight
-// from global memory (lane (g, t): 8 consecutive dimensions of tokens g, g + 8, g + 16, g + 24), and runs the rows
-// past them eight at a time.
+// One pass over the keys; with the rows' log-sums given, every token is independent of the others.  A warp owns 16
+// tokens and walks over all kv heads and query rows, so a token's sum stays in one lane quad and is taken in a fixed order
+// (row block by row block, head by head, eight rows at a time): no atomics, the same bits every time.  Bound: the bytes of
+// K while there are few rows, the exponentials' surroundings (masks, sums) from about a hundred rows on.  Keys come through
+// the block table into stages of the warp's own, two heads ahead; the queries of as many heads as fit (64 rows) are shared by the
+// CTA's four warps.  CTAs are small, four an SM: while one waits for its first keys or its next queries, the others work.  Products as in attend_few.cu: tokens
+// as the M side, eight query rows as the N side.
 #include "attend_device.cuh"
 
 namespace aafkv {
 
-constexpr int MASS_WARPS = 8, MASS_TOKENS = 32;  // tokens of a warp's task
+constexpr int MASS_WARPS = 4, MASS_TOKENS = 16;  // tokens of a warp
+static_assert(MASS_WARPS * MASS_TOKENS == MASS_CHUNK, "tokens of a CTA");
+
+template <int DP> struct MassShape {
+    static constexpr int ROW = DP * 2, PIECES = DP / 8, ROWS = DP <= 128 ? 64 : 32;  // rows of a batch of queries
+    static constexpr int TILE_BYTES = MASS_TOKENS * ROW, STAGES = 2;
+    static constexpr int K_BYTES = MASS_WARPS * STAGES * TILE_BYTES;
+};
+constexpr int MASS_AT_ONCE = 4;  // groups of eight rows in flight
+struct MassRow {  // what a query row of any head sees
+    int lo, hi, pos, near;
+};
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(MASS_WARPS * 32, DP <= 128 ? 2 : 1)
+__global__ void __launch_bounds__(MASS_WARPS * 32, DP <= 128 ? 4 : 2)
     attn_mass_kernel(const __grid_constant__ MassParams p, const __grid_constant__ SmallSeqs small) {
-    extern __shared__ float part[];  // [head][chunk]
+    using S = MassShape<DP>;
+    extern __shared__ __align__(16) char smem[];
+    __shared__ MassRow row_info[S::ROWS];
+    __shared__ float row_lse[S::ROWS], row_slope[S::ROWS];
     const AttnParams &a = p.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t4 = lane & 3;
     const AttnSeq *seqs = a.seqs ? a.seqs : small.e;
     const int unit = blockIdx.x, si = find_seq(seqs, a.n, unit);
     const AttnSeq sq = seqs[si];
-    const int c0 = (unit - sq.unit0) * p.chunk, cn = min(p.chunk, sq.len - c0);
+    const int tb = (unit - sq.unit0) * MASS_CHUNK + warp * MASS_TOKENS;  // the warp's tokens
     const int R = sq.nq * a.G, Hq = a.H * a.G;
-    const int *table = a.tables + (long long)sq.ctx * a.max_blk;
-    const int subs = (cn + MASS_TOKENS - 1) / MASS_TOKENS;
+    const int block_rows = min((R + 7) / 8 * 8, S::ROWS), batch_heads = min(a.H, S::ROWS / block_rows);
+    const int row_blocks = (R + block_rows - 1) / block_rows, batches = (a.H + batch_heads - 1) / batch_heads;
+    const uint32_t sK = (uint32_t)__cvta_generic_to_shared(smem) + warp * S::STAGES * S::TILE_BYTES;
+    const uint32_t sQ = (uint32_t)__cvta_generic_to_shared(smem) + S::K_BYTES;
+    auto at = [](int r, int c) { return (uint32_t)(r * S::ROW + ((c ^ ((r & 1) << 2)) << 4)); };
 
-    for (int task = warp; task < subs * a.H; task += MASS_WARPS) {
-        const int sub = task / a.H, head = task - sub * a.H, tb = c0 + sub * MASS_TOKENS;
-        uint4 kf[4][DP / 32];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int t = tb + g + 8 * i;
-            const char *src = a.kbase;
-            if (t < c0 + cn) {
-                const int b = block_of(t, a.BS, a.bs_shift);
-                src += (long long)__ldg(table + b) * 2 * a.run + (long long)(t - b * a.BS) * a.row + (long long)head * a.D * 2;
-            }
-#pragma unroll
-            for (int kk = 0; kk < DP / 32; ++kk) {
-                const int d = kk * 32 + t4 * 8;
-                kf[i][kk] = t < c0 + cn && d < a.D ? __ldg(reinterpret_cast<const uint4 *>(src + d * 2)) : make_uint4(0, 0, 0, 0);
-            }
-        }
-        float w[4] = {0, 0, 0, 0};  // tokens g, g + 8, g + 16, g + 24, rows of this lane's columns
-        for (int rb = 0; rb < R; rb += 8) {
-            float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-            const int rq = min(rb + g, R - 1);
-            const T *q = static_cast<const T *>(a.q) + (long long)(sq.row0 + rq / a.G) * a.q_stride +
-                         (long long)(head * a.G + rq % a.G) * a.D;
-#pragma unroll
-            for (int kk = 0; kk < DP / 32; ++kk) {
-                const int d = kk * 32 + t4 * 8;
-                const uint4 qf = d < a.D ? __ldg(reinterpret_cast<const uint4 *>(q + d)) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint4 x = kf[2 * i][kk], y = kf[2 * i + 1][kk];
-                    Elt<T>::mma(s[i], x.x, y.x, x.y, y.y, qf.x, qf.y);
-                    Elt<T>::mma(s[i], x.z, y.z, x.w, y.w, qf.z, qf.w);
-                }
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int r = rb + 2 * t4 + c;
-                if (r >= R) continue;
-                const RowSpan sp = row_span(a, sq, r / a.G);
-                const int hq = head * a.G + r % a.G;
-                const float slope = a.slopes ? a.slopes[hq] : 0.0f;
-                // the scores are measured from the nearest visible key, so is the log-sum
-                const float lse = (p.lse_in[(long long)(sq.row0 + r / a.G) * Hq + hq] + slope * (float)sp.near) * LOG2E;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = tb + g + 8 * i;
-                    const float x = score2(a, s[i >> 1][2 * (i & 1) + c], slope, sp, t);
-                    if (t >= sp.lo && t < sp.hi && lse != -CUDART_INF_F) w[i] += ex2(x - lse);
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            w[i] += __shfl_xor_sync(0xffffffffu, w[i], 1);
-            w[i] += __shfl_xor_sync(0xffffffffu, w[i], 2);
-        }
-        const int t = sub * MASS_TOKENS + g + 8 * t4;  // lane (g, t4) writes token g + 8 t4 of the task
-        const float mine = t4 == 0 ? w[0] : (t4 == 1 ? w[1] : (t4 == 2 ? w[2] : w[3]));
-        if (t < cn) part[head * p.chunk + t] = mine;
+    // keys: lane l knows where the warp's token l % 16 is
+    long long off = 0;
+    {
+        const int t = tb + (lane & 15), b = block_of(t, a.BS, a.bs_shift);
+        if (t < sq.len)
+            off = (long long)__ldg(a.tables + (long long)sq.ctx * a.max_blk + b) * 2 * a.run + (long long)(t - b * a.BS) * a.row;
     }
-    __syncthreads();
-    for (int t = threadIdx.x; t < cn; t += MASS_WARPS * 32) {
-        float sum = 0.0f;
-        for (int h = 0; h < a.H; ++h) sum += part[h * p.chunk + t];
-        const long long at = si * p.mass_stride + c0 + t;
-        p.mass[at] = (p.prev ? p.prev[at] : 0.0f) + sum;
+    const int steps = tb < sq.len ? row_blocks * a.H : 0;  // one head of one row block each
+    auto load_keys = [&](int step) {
+        if (step < steps) {
+            constexpr int AT_ONCE = 32 / S::PIECES;
+            const int head = step % a.H, c = lane % S::PIECES;
+            const uint32_t dst = sK + (step % S::STAGES) * S::TILE_BYTES;
+#pragma unroll
+            for (int i = 0; i < MASS_TOKENS / AT_ONCE; ++i) {
+                const int r = i * AT_ONCE + lane / S::PIECES;
+                const char *src = a.kbase + __shfl_sync(0xffffffffu, off, r) + (long long)head * a.D * 2 + c * 16;
+                const bool in = tb + r < sq.len && c * 8 < a.D;
+                copy16(dst + at(r, c), in ? src : a.kbase, in ? 16 : 0);
+            }
+        }
+        copy_commit();
+    };
+    // queries of a batch of heads: row hh * block_rows + r
+    auto load_queries = [&](int batch) {
+        if (batch < row_blocks * batches) {
+            const int rb = batch / batches * block_rows, h0 = batch % batches * batch_heads, heads = min(batch_heads, a.H - h0);
+            const uint32_t dst = sQ;
+            for (int i = threadIdx.x; i < heads * block_rows * S::PIECES; i += MASS_WARPS * 32) {
+                const int c = i % S::PIECES, r = i / S::PIECES, hh = r / block_rows, rq = rb + r - hh * block_rows;
+                const int j = min(rq, R - 1) / a.G;
+                const T *src = static_cast<const T *>(a.q) + (sq.row0 + j) * a.q_stride +
+                               (long long)((h0 + hh) * a.G + min(rq, R - 1) - j * a.G) * a.D + c * 8;
+                const bool in = rq < R && c * 8 < a.D;
+                copy16(dst + at(r, c), in ? src : static_cast<const T *>(a.q), in ? 16 : 0);
+            }
+            for (int r = threadIdx.x; r < heads * block_rows; r += MASS_WARPS * 32) {
+                const int hh = r / block_rows, rq = min(rb + r - hh * block_rows, R - 1), j = rq / a.G, hq = (h0 + hh) * a.G + rq - j * a.G;
+                const RowSpan sp = row_span(a, sq, j);
+                const float slope = a.slopes ? a.slopes[hq] : 0.0f;
+                // scores are measured from the nearest visible key, so is the log-sum; a row without a sum adds nothing
+                const float lse = (p.lse_in[(long long)(sq.row0 + j) * Hq + hq] + slope * (float)sp.near) * LOG2E;
+                row_slope[r] = slope;
+                row_lse[r] = lse == -CUDART_INF_F ? CUDART_INF_F : lse;
+            }
+        }
+        copy_commit();
+    };
+
+    load_queries(0);
+#pragma unroll
+    for (int i = 0; i < S::STAGES - 1; ++i) load_keys(i);
+    float w[2] = {0.0f, 0.0f};  // tokens g, g + 8, rows of this lane's columns
+    const float c2 = a.scale * LOG2E;
+    const bool plain = a.softcap == 0.0f && !a.slopes;
+    int step = 0;
+    for (int batch = 0; batch < row_blocks * batches; ++batch) {
+        const int rb = batch / batches * block_rows, h0 = batch % batches * batch_heads, heads = min(batch_heads, a.H - h0);
+        copy_wait<0>();   // this batch's queries (and the keys asked for so far)
+        __syncthreads();  // everyone's part of them; everyone is done with the batch before
+        if (batch % batches == 0) {  // a new block of rows
+            for (int r = threadIdx.x; r < block_rows; r += MASS_WARPS * 32) {
+                const RowSpan sp = row_span(a, sq, min(rb + r, R - 1) / a.G);
+                row_info[r] = MassRow{sp.lo, rb + r < R ? sp.hi : 0, sp.pos, sp.near};
+            }
+            __syncthreads();
+        }
+        for (int hh = 0; hh < heads && steps; ++hh, ++step) {
+            load_keys(step + S::STAGES - 1);
+            copy_wait<S::STAGES - 1>();
+            __syncwarp();
+            const uint32_t k = sK + (step % S::STAGES) * S::TILE_BYTES;
+            uint4 kf[2][DP / 32];
+#pragma unroll
+            for (int kk = 0; kk < DP / 32; ++kk) {
+                kf[0][kk] = lds16(k + at(g, kk * 4 + t4));
+                kf[1][kk] = lds16(k + at(g + 8, kk * 4 + t4));
+            }
+            __syncwarp();
+            const uint32_t q = sQ + hh * block_rows * S::ROW;
+            for (int r0 = 0; r0 < block_rows; r0 += 8 * MASS_AT_ONCE) {
+                float s[MASS_AT_ONCE][4];  // independent products, one would wait for itself at every step
+#pragma unroll
+                for (int u = 0; u < MASS_AT_ONCE; ++u) s[u][0] = s[u][1] = s[u][2] = s[u][3] = 0.0f;
+#pragma unroll
+                for (int kk = 0; kk < DP / 32; ++kk)
+#pragma unroll
+                    for (int u = 0; u < MASS_AT_ONCE; ++u) {
+                        if (r0 + 8 * u >= block_rows) continue;
+                        const uint4 qf = lds16(q + at(r0 + 8 * u + g, kk * 4 + t4));
+                        Elt<T>::mma(s[u], kf[0][kk].x, kf[1][kk].x, kf[0][kk].y, kf[1][kk].y, qf.x, qf.y);
+                        Elt<T>::mma(s[u], kf[0][kk].z, kf[1][kk].z, kf[0][kk].w, kf[1][kk].w, qf.z, qf.w);
+                    }
+#pragma unroll
+                for (int u = 0; u < MASS_AT_ONCE; ++u) {
+                    const int r8 = r0 + 8 * u;
+                    if (r8 >= block_rows) continue;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int r = r8 + 2 * t4 + c;
+                    const MassRow ri = row_info[r];
+                    const float lse = row_lse[hh * block_rows + r];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int t = tb + g + 8 * h;
+                        float x = s[u][2 * h + c];
+                        if (plain) {
+                            x = fmaf(x, c2, -lse);
+                        } else {
+                            RowSpan sp;
+                            sp.lo = ri.lo;
+                            sp.hi = ri.hi;
+                            sp.pos = ri.pos;
+                            sp.near = ri.near;
+                            x = score2(a, x, row_slope[hh * block_rows + r], sp, t) - lse;
+                        }
+                        w[h] += t >= ri.lo && t < ri.hi ? ex2(x) : 0.0f;
+                    }
+                }
+                }
+            }
+        }
+        if (batch + 1 < row_blocks * batches) {
+            __syncthreads();
+            load_queries(batch + 1);
+        }
+    }
+    copy_wait<0>();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        w[h] += __shfl_xor_sync(0xffffffffu, w[h], 1);
+        w[h] += __shfl_xor_sync(0xffffffffu, w[h], 2);
+        const int t = tb + g + 8 * h;
+        if (t4 == 0 && t < sq.len) {
+            const long long o = si * p.mass_stride + t;
+            p.mass[o] = (p.prev ? p.prev[o] : 0.0f) + w[h];
+        }
     }
 }
 
-template <typename T, int DP> static cudaError_t mass_go(const MassParams &p, const SmallSeqs &small, cudaStream_t st) {
-    const size_t smem = sizeof(float) * (size_t)p.a.H * p.chunk;
-    const cudaError_t e = cudaFuncSetAttribute(attn_mass_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+template <typename T, int DP> static cudaError_t mass_go(const MassParams &p, const SmallSeqs &small, int max_rows, cudaStream_t st) {
+    using S = MassShape<DP>;
+    const int block = min((max_rows + 7) / 8 * 8, S::ROWS), rows = (int)min((long long)S::ROWS, (long long)block * p.a.H);
+    const int smem = S::K_BYTES + rows * S::ROW;
+    static unsigned long long seen = 0;
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(attn_mass_kernel<T, DP>), S::K_BYTES + S::ROWS * S::ROW, &seen);
     if (e != cudaSuccess) return e;
     attn_mass_kernel<T, DP><<<(unsigned)p.a.total_units, MASS_WARPS * 32, smem, st>>>(p, small);
     return cudaGetLastError();
 }
-template <typename T> static cudaError_t mass_pick(const MassParams &p, const SmallSeqs &small, cudaStream_t st) {
-    if (p.a.D <= 64) return mass_go<T, 64>(p, small, st);
-    if (p.a.D <= 128) return mass_go<T, 128>(p, small, st);
-    return mass_go<T, 256>(p, small, st);
+template <typename T> static cudaError_t mass_pick(const MassParams &p, const SmallSeqs &small, int max_rows, cudaStream_t st) {
+    if (p.a.D <= 64) return mass_go<T, 64>(p, small, max_rows, st);
+    if (p.a.D <= 128) return mass_go<T, 128>(p, small, max_rows, st);
+    return mass_go<T, 256>(p, small, max_rows, st);
 }
-cudaError_t launch_attn_mass(const MassParams &p, const SmallSeqs &small, int f16, cudaStream_t st) {
-    return f16 ? mass_pick<__half>(p, small, st) : mass_pick<__nv_bfloat16>(p, small, st);
+cudaError_t launch_attn_mass(const MassParams &p, const SmallSeqs &small, int f16, int max_rows, cudaStream_t st) {
+    return f16 ? mass_pick<__half>(p, small, max_rows, st) : mass_pick<__nv_bfloat16>(p, small, max_rows, st);
 }
 
 }  // namespace aafkv

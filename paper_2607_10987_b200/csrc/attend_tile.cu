@@ -269,8 +269,8 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
 }
 
 template <typename T, int DP> static cudaError_t tile_go(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(attend_tile_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileShape<DP>::SMEM);
+    static unsigned long long seen = 0;
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_tile_kernel<T, DP>), TileShape<DP>::SMEM, &seen);
     if (e != cudaSuccess) return e;
     long long ctas = (long long)p.total_units * p.H;
     if (p.flag && ctas > 296) ctas = 296;

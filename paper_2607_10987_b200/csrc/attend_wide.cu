@@ -689,8 +689,8 @@ bool wide_takes(int D, int BS) { return (D == 64 || D == 128) && BS >= 8 && BS <
 
 template <typename T, int D, int MODE>
 static cudaError_t wide_go(const AttnParams &p, const SmallSeqs &small, const void *map, int layer, cudaStream_t st) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(attend_wide_kernel<T, D, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, WideShape<D>::SMEM);
+    static unsigned long long seen = 0;
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_wide_kernel<T, D, MODE>), WideShape<D>::SMEM, &seen);
     if (e != cudaSuccess) return e;
     attend_wide_kernel<T, D, MODE><<<(unsigned)((long long)p.total_units * p.H), WIDE_THREADS, WideShape<D>::SMEM, st>>>(
         p, small, *static_cast<const CUtensorMap *>(map), layer);

@@ -143,11 +143,14 @@ struct aaf_kv_pool {
     cudaStream_t last_copy_stream = nullptr;
     cudaEvent_t last_copy_event = nullptr;
     // Kernels that compute with the pool (attention, stores, gathers of a prune) read block tables on the caller's
-    // stream: they wait for the metadata launched so far, and the next kernel that changes metadata waits for them.
+    // stream: they wait for the metadata launched so far, and the next kernel that changes metadata waits for them.  Streams
+    // are told apart by their ids, which are never reused.  read_ev is recorded when someone has to wait.
     cudaEvent_t meta_ev = nullptr, read_ev = nullptr;
     long long meta_mark = -1;  // meta_launches when meta_ev was recorded
     bool meta_drained = false; // meta_ev has been seen complete
-    bool read_pending = false;
+    bool read_pending = false; // work on read_stream that the metadata stream has not been ordered behind
+    cudaStream_t read_stream = nullptr;
+    unsigned long long read_id = 0, copy_id = 0;  // streams of the last reader and of the last copy launch
     PoolMap map;               // tensor map of the pool memory (wide attention kernel)
     bool map_ok = false;
     int epoch = 0;             // counts calls of the wide kernel
@@ -267,8 +270,22 @@ struct PlanSlot {
 // Before any kernel that changes tables, reference counts or the ring: the readers on the caller's stream come first.
 void after_readers(aaf_kv_pool *p) {
     if (!p->read_pending) return;
+    cudaEventRecord(p->read_ev, p->read_stream);
     cudaStreamWaitEvent(p->meta_stream, p->read_ev, 0);
     p->read_pending = false;
+}
+unsigned long long stream_id(cudaStream_t st) {
+    unsigned long long id = 0;
+    if (cudaStreamGetId(st, &id) != cudaSuccess) {
+        cudaGetLastError();
+        return ~0ull;
+    }
+    return id;
+}
+// Before payload work on `st`: readers on another stream come first.
+bool after_readers_on(aaf_kv_pool *p, cudaStream_t st, unsigned long long id) {
+    if (!p->read_id || id == p->read_id) return true;
+    return cudaEventRecord(p->read_ev, p->read_stream) == cudaSuccess && cudaStreamWaitEvent(st, p->read_ev, 0) == cudaSuccess;
 }
 PlanSlot begin_plan(aaf_kv_pool *p) {
     after_readers(p);
@@ -288,6 +305,7 @@ bool end_plan(aaf_kv_pool *p, const PlanSlot &ps, cudaStream_t st) {
 void end_copy(aaf_kv_pool *p, const PlanSlot &ps, cudaStream_t st) {
     cudaEventRecord(p->copy_done[ps.buf], st);
     p->last_copy_stream = st;
+    p->copy_id = stream_id(st);
     p->last_copy_event = p->copy_done[ps.buf];
     p->next_buf ^= 1;
 }
@@ -295,7 +313,12 @@ void end_copy(aaf_kv_pool *p, const PlanSlot &ps, cudaStream_t st) {
 // Before a kernel on `st` that reads block tables or payload: it comes after the pool's earlier payload work, whatever
 // stream that was on, and after the metadata launched so far.
 bool begin_read(aaf_kv_pool *p, cudaStream_t st) {
-    if (p->last_copy_event && cudaStreamWaitEvent(st, p->last_copy_event, 0) != cudaSuccess) return false;
+    const unsigned long long id = stream_id(st);
+    if (!after_readers_on(p, st, id)) return false;
+    if (p->last_copy_event && id != p->copy_id && cudaStreamWaitEvent(st, p->last_copy_event, 0) != cudaSuccess) return false;
+    p->read_id = id;
+    p->read_stream = st;
+    p->read_pending = true;
     if (p->meta_mark != p->meta_launches) {
         if (cudaEventRecord(p->meta_ev, p->meta_stream) != cudaSuccess) return false;
         p->meta_mark = p->meta_launches;
@@ -310,13 +333,6 @@ bool begin_read(aaf_kv_pool *p, cudaStream_t st) {
             if (e != cudaErrorNotReady || cudaStreamWaitEvent(st, p->meta_ev, 0) != cudaSuccess) return false;
         }
     }
-    return true;
-}
-bool end_read(aaf_kv_pool *p, cudaStream_t st) {
-    if (cudaEventRecord(p->read_ev, st) != cudaSuccess) return false;
-    p->read_pending = true;
-    p->last_copy_stream = st;
-    p->last_copy_event = p->read_ev;
     return true;
 }
 // A call reads host arrays and orders the pool's streams, neither of which a replayed graph would do again.
@@ -336,6 +352,7 @@ int run_copy(aaf_kv_pool *p, const PlanSlot &ps, int cls, int n_slots, long long
     view.pieces += piece0;  // a launch may cover a sub-range of the planned pieces (chunked transfers)
     const long long avg_piece = n_slots > 0 ? payload_tokens * p->g.row / n_slots : 0;
     if (n_slots <= 0) return AAF_OK;
+    if (!after_readers_on(p, st, stream_id(st))) return broke(p);
     if (p->last_copy_event && st != p->last_copy_stream) {  // a different stream: serialise behind the last copy launch
         if (cudaStreamWaitEvent(st, p->last_copy_event, 0) != cudaSuccess) return broke(p);
         p->last_copy_stream = st;  // the wait is queued; later launches of this operator need not repeat it
@@ -1315,7 +1332,7 @@ AttnParams attn_params(const aaf_kv_pool *p, int layer, const aaf_kv_attn *a, co
 }
 
 // Records of a batch: kernel parameters while they fit, else through the pinned ring into the pool's workspace on `st`
-// (the copies and their readers of all calls are ordered by begin_read / end_read).
+// (the copies and their readers of all calls are ordered by begin_read).
 template <typename Rec, typename Small>
 bool place_records(aaf_kv_pool *p, const std::vector<Rec> &rec, Small &small, const Rec **dev, int which, cudaStream_t st) {
     static_assert(sizeof(Rec) <= sizeof(AttnSeq), "records share the workspace of the attention records");
@@ -1384,7 +1401,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
     long long part_rows = 0;
     bool few_joined = false, many_joined = false;
     long long own_rows = 0;
-    int few_tokens = 0, many_tokens = 0;
+    int few_tokens = 0, many_tokens = 0, few_parts = 0, many_parts = 0;  // parts: the most of a sequence
     int few_units = 0, many_units = 0, group_units = 0;
     const size_t n_few = few.size();
     if (forked && p->map_ok && !k.window && !k.spans) {
@@ -1474,6 +1491,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
             s.unit0 = few_units;
             few_units += s.nsplit;
             s.tok0 = few_tokens;
+            few_parts = std::max(few_parts, s.nsplit + s.gsplit);
             few_tokens += s.nq;
             if (s.nsplit > 1 || s.gsplit) {
                 s.part0 = (int)part_rows;
@@ -1502,6 +1520,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
             s.nsplit = (int)parts;
             s.unit0 = many_units;
             s.tok0 = many_tokens;
+            many_parts = std::max(many_parts, s.nsplit);
             many_tokens += s.nq;
             if ((long long)many_units + tiles * parts > (1ll << 30) / H || again_units > (1 << 30) / H) return AAF_ERR_TOO_MANY;
             many_units += (int)(tiles * parts);
@@ -1533,7 +1552,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
             ok = launch_attend_wide(kg, small, f16, &p->map, layer, st) == cudaSuccess;
         }
         if (ok && few_units) ok = launch_attend_few(kf, small, f16, few_rows, group_units > 0, st) == cudaSuccess;
-        if (ok && few_joined) ok = launch_attend_join(kf, small, f16, 0, few_tokens, st) == cudaSuccess;
+        if (ok && few_joined) ok = launch_attend_join(kf, small, f16, 0, few_tokens, few_parts, p->sm_count, st) == cudaSuccess;
     }
     if (ok && !many.empty()) {
         SmallSeqs small;
@@ -1552,14 +1571,14 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
         if (ok && many_joined) {
             AttnParams kj = km;
             kj.flag = nullptr;
-            ok = launch_attend_join(kj, small, f16, rows_of, many_tokens, st) == cudaSuccess;
+            ok = launch_attend_join(kj, small, f16, rows_of, many_tokens, many_parts, p->sm_count, st) == cudaSuccess;
         }
         if (ok && wide) {
             km.total_units = again_units;
             ok = place_records(p, again, small, &km.seqs, 3, st) && launch_attend_tile(km, small, f16, st) == cudaSuccess;
         }
     }
-    return ok && end_read(p, st) ? AAF_OK : broke(p);
+    return ok ? AAF_OK : broke(p);
 }
 
 int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n, const aaf_ctx_t *ctxs,
@@ -1576,7 +1595,6 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
         return AAF_ERR_INVALID_ARG;
     for (int i = 0; i < n; ++i)
         if (mass_stride < p->len[ctxs[i]]) return AAF_ERR_DST_TOO_SMALL;
-    if (p->g.H > MASS_MAX_HEADS) return AAF_ERR_INCOMPAT;
     DeviceGuard guard(p->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (capturing(st)) return AAF_ERR_INVALID_ARG;
@@ -1586,10 +1604,9 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
     k.prev = prev_dev;
     k.mass = mass_dev;
     k.mass_stride = mass_stride;
-    k.chunk = MASS_CHUNK;
     std::vector<AttnSeq> rec((size_t)n);
     long long units = 0;
-    int row0 = 0;
+    int row0 = 0, max_rows = 1;
     for (int i = 0; i < n; ++i) {
         AttnSeq &s = rec[(size_t)i];
         s = AttnSeq{};
@@ -1598,7 +1615,8 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
         s.nq = n_q ? n_q[i] : 1;
         s.row0 = row0;
         s.unit0 = (int)units;
-        s.nsplit = (s.len + k.chunk - 1) / k.chunk;
+        s.nsplit = (s.len + MASS_CHUNK - 1) / MASS_CHUNK;
+        max_rows = std::max(max_rows, s.nq * k.a.G);
         row0 += s.nq;
         units += s.nsplit;
         if (units > (1ll << 30)) return AAF_ERR_TOO_MANY;
@@ -1609,7 +1627,7 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
     if (!begin_read(p, st)) return broke(p);
     SmallSeqs small;
     const bool ok = place_records(p, rec, small, &k.a.seqs, 0, st) &&
-                    launch_attn_mass(k, small, a->dtype == AAF_DTYPE_F16, st) == cudaSuccess && end_read(p, st);
+                    launch_attn_mass(k, small, a->dtype == AAF_DTYPE_F16, max_rows, st) == cudaSuccess;
     return ok ? AAF_OK : broke(p);
 }
 
@@ -1670,7 +1688,7 @@ int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int3
     if (!begin_read(p, st)) return broke(p);
     SmallStores small;
     const bool ok = place_records(p, rec, small, &k.seqs, 0, st) &&
-                    launch_store(k, small, d->dtype == AAF_DTYPE_F16, st) == cudaSuccess && end_read(p, st);
+                    launch_store(k, small, d->dtype == AAF_DTYPE_F16, st) == cudaSuccess;
     return ok ? AAF_OK : broke(p);
 }
 
@@ -1713,7 +1731,7 @@ int aaf_kv_prune(aaf_kv_pool *p, aaf_ctx_t ctx, const float *scores_dev, int64_t
                     launch_gather_rows(p->g, tables + (long long)ctx * p->g.max_blk, tables + (long long)c * p->g.max_blk, kept_dev,
                                        (int)budget, p->sm_count, st) == cudaSuccess;
     end_copy(p, ps, st);
-    if (!ok || !end_read(p, st)) return broke(p);
+    if (!ok) return broke(p);
     *out_ctx = c;
     return AAF_OK;
 }
