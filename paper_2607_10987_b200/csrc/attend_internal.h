@@ -121,7 +121,7 @@ cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16
 // keep list of a pruned context: kept[budget] ascending, kept_scores (may be null); then the row gather
 cudaError_t launch_select(const float *scores, int len, int budget, int sink, int recent, int *kept, float *kept_scores,
                           cudaStream_t st);
-cudaError_t launch_gather_rows(const Geom &g, const int *src_table, const int *dst_table, const int *kept, int budget,
+cudaError_t launch_gather_rows(const Geom &g, const int *src_table, const Piece *dst_blocks, const int *kept, int budget,
                                int sm_count, cudaStream_t st);
 
 }  // namespace aafkv

@@ -7,6 +7,8 @@
 // the block table into stages of the warp's own, two heads ahead; the queries of as many heads as fit (64 rows) are shared by the
 // CTA's four warps.  CTAs are small, four an SM: while one waits for its first keys or its next queries, the others work.  Products as in attend_few.cu: tokens
 // as the M side, eight query rows as the N side.
+#include <type_traits>
+
 #include "attend_device.cuh"
 
 namespace aafkv {
@@ -19,7 +21,6 @@ template <int DP> struct MassShape {
     static constexpr int TILE_BYTES = MASS_TOKENS * ROW, STAGES = 2;
     static constexpr int K_BYTES = MASS_WARPS * STAGES * TILE_BYTES;
 };
-constexpr int MASS_AT_ONCE = 4;  // groups of eight rows in flight
 struct MassRow {  // what a query row of any head sees
     int lo, hi, pos, near;
 };
@@ -30,7 +31,8 @@ __global__ void __launch_bounds__(MASS_WARPS * 32, DP <= 128 ? 4 : 2)
     using S = MassShape<DP>;
     extern __shared__ __align__(16) char smem[];
     __shared__ MassRow row_info[S::ROWS];
-    __shared__ float row_lse[S::ROWS], row_slope[S::ROWS];
+    __shared__ __align__(8) float row_lse[S::ROWS];
+    __shared__ float row_slope[S::ROWS];
     const AttnParams &a = p.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t4 = lane & 3;
     const AttnSeq *seqs = a.seqs ? a.seqs : small.e;
@@ -72,22 +74,30 @@ __global__ void __launch_bounds__(MASS_WARPS * 32, DP <= 128 ? 4 : 2)
         if (batch < row_blocks * batches) {
             const int rb = batch / batches * block_rows, h0 = batch % batches * batch_heads, heads = min(batch_heads, a.H - h0);
             const uint32_t dst = sQ;
-            for (int i = threadIdx.x; i < heads * block_rows * S::PIECES; i += MASS_WARPS * 32) {
-                const int c = i % S::PIECES, r = i / S::PIECES, hh = r / block_rows, rq = rb + r - hh * block_rows;
-                const int j = min(rq, R - 1) / a.G;
-                const T *src = static_cast<const T *>(a.q) + (sq.row0 + j) * a.q_stride +
-                               (long long)((h0 + hh) * a.G + min(rq, R - 1) - j * a.G) * a.D + c * 8;
+            constexpr int AT_ONCE = MASS_WARPS * 32 / S::PIECES;
+            const int c = threadIdx.x % S::PIECES;
+            auto row_of = [&](int r, int &hh) {  // row of the sequence, capped at the last
+                hh = batch_heads == 1 ? 0 : r / block_rows;
+                return rb + r - hh * block_rows;
+            };
+#pragma unroll 4
+            for (int r = threadIdx.x / S::PIECES; r < heads * block_rows; r += AT_ONCE) {
+                int hh;
+                const int rq = row_of(r, hh), rc = min(rq, R - 1), j = token_of(a, rc);
+                const T *src = static_cast<const T *>(a.q) + (sq.row0 + j) * a.q_stride + ((h0 + hh) * a.G + rc - j * a.G) * a.D + c * 8;
                 const bool in = rq < R && c * 8 < a.D;
                 copy16(dst + at(r, c), in ? src : static_cast<const T *>(a.q), in ? 16 : 0);
             }
             for (int r = threadIdx.x; r < heads * block_rows; r += MASS_WARPS * 32) {
-                const int hh = r / block_rows, rq = min(rb + r - hh * block_rows, R - 1), j = rq / a.G, hq = (h0 + hh) * a.G + rq - j * a.G;
-                const RowSpan sp = row_span(a, sq, j);
-                const float slope = a.slopes ? a.slopes[hq] : 0.0f;
-                // scores are measured from the nearest visible key, so is the log-sum; a row without a sum adds nothing
-                const float lse = (p.lse_in[(long long)(sq.row0 + j) * Hq + hq] + slope * (float)sp.near) * LOG2E;
-                row_slope[r] = slope;
-                row_lse[r] = lse == -CUDART_INF_F ? CUDART_INF_F : lse;
+                int hh;
+                const int rc = min(row_of(r, hh), R - 1), j = token_of(a, rc), hq = (h0 + hh) * a.G + rc - j * a.G;
+                float lse = p.lse_in[(long long)(sq.row0 + j) * Hq + hq];
+                if (a.slopes) {  // scores are measured from the nearest visible key, so is the log-sum
+                    row_slope[r] = a.slopes[hq];
+                    lse += a.slopes[hq] * (float)row_span(a, sq, j).near;
+                }
+                // a row without a sum adds nothing, nor does one behind the last
+                row_lse[r] = lse == -CUDART_INF_F || row_of(r, hh) >= R ? CUDART_INF_F : lse * LOG2E;
             }
         }
         copy_commit();
@@ -100,16 +110,28 @@ __global__ void __launch_bounds__(MASS_WARPS * 32, DP <= 128 ? 4 : 2)
     const float c2 = a.scale * LOG2E;
     const bool plain = a.softcap == 0.0f && !a.slopes;
     int step = 0;
+    bool quick = false;  // no score of the warp's tokens is masked, and scores are multiples of the products
     for (int batch = 0; batch < row_blocks * batches; ++batch) {
         const int rb = batch / batches * block_rows, h0 = batch % batches * batch_heads, heads = min(batch_heads, a.H - h0);
         copy_wait<0>();   // this batch's queries (and the keys asked for so far)
         __syncthreads();  // everyone's part of them; everyone is done with the batch before
         if (batch % batches == 0) {  // a new block of rows
             for (int r = threadIdx.x; r < block_rows; r += MASS_WARPS * 32) {
-                const RowSpan sp = row_span(a, sq, min(rb + r, R - 1) / a.G);
+                const RowSpan sp = row_span(a, sq, token_of(a, min(rb + r, R - 1)));
                 row_info[r] = MassRow{sp.lo, rb + r < R ? sp.hi : 0, sp.pos, sp.near};
             }
             __syncthreads();
+            int lo = 0, hi = 0x7fffffff;  // tokens that every row of the block sees
+            for (int r = lane; r < block_rows && rb + r < R; r += 32) {
+                lo = max(lo, row_info[r].lo);
+                hi = min(hi, row_info[r].hi);
+            }
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                lo = max(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+                hi = min(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+            }
+            quick = plain && tb >= lo && tb + MASS_TOKENS <= hi;
         }
         for (int hh = 0; hh < heads && steps; ++hh, ++step) {
             load_keys(step + S::STAGES - 1);
@@ -124,47 +146,50 @@ __global__ void __launch_bounds__(MASS_WARPS * 32, DP <= 128 ? 4 : 2)
             }
             __syncwarp();
             const uint32_t q = sQ + hh * block_rows * S::ROW;
-            for (int r0 = 0; r0 < block_rows; r0 += 8 * MASS_AT_ONCE) {
-                float s[MASS_AT_ONCE][4];  // independent products, one would wait for itself at every step
+            // weights of UNITS groups of eight rows: independent products, one would wait for itself at every step
+            auto rows = [&](int r0, auto units) {
+                constexpr int U = decltype(units)::value;
+                float s[U][4];
 #pragma unroll
-                for (int u = 0; u < MASS_AT_ONCE; ++u) s[u][0] = s[u][1] = s[u][2] = s[u][3] = 0.0f;
+                for (int u = 0; u < U; ++u) s[u][0] = s[u][1] = s[u][2] = s[u][3] = 0.0f;
 #pragma unroll
                 for (int kk = 0; kk < DP / 32; ++kk)
 #pragma unroll
-                    for (int u = 0; u < MASS_AT_ONCE; ++u) {
-                        if (r0 + 8 * u >= block_rows) continue;
+                    for (int u = 0; u < U; ++u) {
                         const uint4 qf = lds16(q + at(r0 + 8 * u + g, kk * 4 + t4));
                         Elt<T>::mma(s[u], kf[0][kk].x, kf[1][kk].x, kf[0][kk].y, kf[1][kk].y, qf.x, qf.y);
                         Elt<T>::mma(s[u], kf[0][kk].z, kf[1][kk].z, kf[0][kk].w, kf[1][kk].w, qf.z, qf.w);
                     }
 #pragma unroll
-                for (int u = 0; u < MASS_AT_ONCE; ++u) {
-                    const int r8 = r0 + 8 * u;
-                    if (r8 >= block_rows) continue;
+                for (int u = 0; u < U; ++u) {
+                    const int r = r0 + 8 * u + 2 * t4;
+                    const float2 lse = *reinterpret_cast<const float2 *>(&row_lse[hh * block_rows + r]);
+                    if (quick) {
+                        w[0] += ex2(fmaf(s[u][0], c2, -lse.x)) + ex2(fmaf(s[u][1], c2, -lse.y));
+                        w[1] += ex2(fmaf(s[u][2], c2, -lse.x)) + ex2(fmaf(s[u][3], c2, -lse.y));
+                        continue;
+                    }
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int r = r8 + 2 * t4 + c;
-                    const MassRow ri = row_info[r];
-                    const float lse = row_lse[hh * block_rows + r];
+                    for (int c = 0; c < 2; ++c) {
+                        const MassRow ri = row_info[r + c];
+                        RowSpan sp;
+                        sp.lo = ri.lo;
+                        sp.hi = ri.hi;
+                        sp.pos = ri.pos;
+                        sp.near = ri.near;
+                        const float slope = a.slopes ? row_slope[hh * block_rows + r + c] : 0.0f;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int t = tb + g + 8 * h;
-                        float x = s[u][2 * h + c];
-                        if (plain) {
-                            x = fmaf(x, c2, -lse);
-                        } else {
-                            RowSpan sp;
-                            sp.lo = ri.lo;
-                            sp.hi = ri.hi;
-                            sp.pos = ri.pos;
-                            sp.near = ri.near;
-                            x = score2(a, x, row_slope[hh * block_rows + r], sp, t) - lse;
+                        for (int h = 0; h < 2; ++h) {
+                            const int t = tb + g + 8 * h;
+                            const float x = score2(a, s[u][2 * h + c], slope, sp, t) - (c ? lse.y : lse.x);
+                            w[h] += t >= ri.lo && t < ri.hi ? ex2(x) : 0.0f;
                         }
-                        w[h] += t >= ri.lo && t < ri.hi ? ex2(x) : 0.0f;
                     }
                 }
-                }
-            }
+            };
+            int r0 = 0;
+            for (; r0 + 32 <= block_rows; r0 += 32) rows(r0, std::integral_constant<int, 4>{});
+            for (; r0 < block_rows; r0 += 8) rows(r0, std::integral_constant<int, 1>{});
         }
         if (batch + 1 < row_blocks * batches) {
             __syncthreads();

@@ -148,7 +148,8 @@ struct aaf_kv_pool {
     cudaEvent_t meta_ev = nullptr, read_ev = nullptr;
     long long meta_mark = -1;  // meta_launches when meta_ev was recorded
     bool meta_drained = false; // meta_ev has been seen complete
-    bool read_pending = false; // work on read_stream that the metadata stream has not been ordered behind
+    bool read_pending = false; // work on read_stream that the metadata stream has not been ordered behind,
+    std::vector<char> row_read; // and the handles whose table rows it may read
     cudaStream_t read_stream = nullptr;
     unsigned long long read_id = 0, copy_id = 0;  // streams of the last reader and of the last copy launch
     PoolMap map;               // tensor map of the pool memory (wide attention kernel)
@@ -267,12 +268,17 @@ struct PlanSlot {
 
 // Before a planner: pick the next piece buffer and make the metadata stream wait until the copy launch
 // that last read that buffer has finished.
-// Before any kernel that changes tables, reference counts or the ring: the readers on the caller's stream come first.
-void after_readers(aaf_kv_pool *p) {
+// Before a kernel that writes the table rows of n handles: readers of those rows on the caller's stream come first.
+// (Reference counts and the ring are the metadata stream's own.)
+void after_readers(aaf_kv_pool *p, const int *handles, int n) {
     if (!p->read_pending) return;
+    bool read = false;
+    for (int i = 0; i < n && !read; ++i) read = p->row_read[(size_t)handles[i]] != 0;
+    if (!read) return;
     cudaEventRecord(p->read_ev, p->read_stream);
     cudaStreamWaitEvent(p->meta_stream, p->read_ev, 0);
     p->read_pending = false;
+    std::fill(p->row_read.begin(), p->row_read.end(), 0);
 }
 unsigned long long stream_id(cudaStream_t st) {
     unsigned long long id = 0;
@@ -288,7 +294,6 @@ bool after_readers_on(aaf_kv_pool *p, cudaStream_t st, unsigned long long id) {
     return cudaEventRecord(p->read_ev, p->read_stream) == cudaSuccess && cudaStreamWaitEvent(st, p->read_ev, 0) == cudaSuccess;
 }
 PlanSlot begin_plan(aaf_kv_pool *p) {
-    after_readers(p);
     PlanSlot ps;
     ps.buf = p->next_buf;
     ps.view = p->s;
@@ -312,13 +317,14 @@ void end_copy(aaf_kv_pool *p, const PlanSlot &ps, cudaStream_t st) {
 
 // Before a kernel on `st` that reads block tables or payload: it comes after the pool's earlier payload work, whatever
 // stream that was on, and after the metadata launched so far.
-bool begin_read(aaf_kv_pool *p, cudaStream_t st) {
+bool begin_read(aaf_kv_pool *p, const int *handles, int n, cudaStream_t st) {
     const unsigned long long id = stream_id(st);
     if (!after_readers_on(p, st, id)) return false;
     if (p->last_copy_event && id != p->copy_id && cudaStreamWaitEvent(st, p->last_copy_event, 0) != cudaSuccess) return false;
     p->read_id = id;
     p->read_stream = st;
     p->read_pending = true;
+    for (int i = 0; i < n; ++i) p->row_read[(size_t)handles[i]] = 1;
     if (p->meta_mark != p->meta_launches) {
         if (cudaEventRecord(p->meta_ev, p->meta_stream) != cudaSuccess) return false;
         p->meta_mark = p->meta_launches;
@@ -427,6 +433,7 @@ int import_impl(aaf_kv_pool *p, const void *src_dev, const aaf_kv_xfer_desc *des
                             st) != cudaSuccess)
             return broke(p);
     }
+    after_readers(p, &c, 1);
     const PlanSlot ps = begin_plan(p);
     if (launch_plan_import(p->g, ps.view, c, n, static_cast<const char *>(src_dev), p->clock + 1, p->meta_stream) !=
             cudaSuccess ||
@@ -550,6 +557,7 @@ int aaf_kv_pool_create(const aaf_kv_pool_desc *desc, aaf_kv_pool **out) {
     p->s.tile_count = reinterpret_cast<int *>(ws + lay.tile_count);
     p->len.assign((size_t)desc->max_ctx, -1);
     p->own_from.assign((size_t)desc->max_ctx, 0);
+    p->row_read.assign((size_t)desc->max_ctx, 0);
     p->fork_id.assign((size_t)desc->max_ctx, 0);
     p->fork_len.assign((size_t)desc->max_ctx, 0);
     p->free_lb = desc->n_blocks;
@@ -743,6 +751,7 @@ int aaf_kv_import_batch(aaf_kv_pool *p, int32_t n, const void *const *src_dev, c
         e.ctx = c; e.block_off = off; e.out_index = i; e.parent = -1;
         off += (int)nblk_of(p, e.n);
     }
+    for (int i = 0; i < n; ++i) after_readers(p, &ent[i].ctx, 1);
     const PlanSlot ps = begin_plan(p);
     const cudaError_t e = launch_plan_import_batch(p->g, ps.view, by_value ? nullptr : ent, small, n, (int)blocks,
                                                    p->clock + 1, p->meta_stream);
@@ -856,6 +865,7 @@ int aaf_kv_import_host_chunked(aaf_kv_pool *p, const void *src_host, const aaf_k
     // previous aaf_kv_import_host_chunked, so the upload waits for that and for nothing else on `stream`
     bool ok = !p->import_reader_pending ||
               cudaStreamWaitEvent(p->upload_stream, p->import_reader_done, 0) == cudaSuccess;
+    after_readers(p, &c, 1);
     const PlanSlot ps = begin_plan(p);
     ok = ok && launch_plan_import(p->g, ps.view, c, n, static_cast<const char *>(staging_dev), p->clock + 1,
                                   p->meta_stream) == cudaSuccess &&
@@ -908,7 +918,7 @@ int aaf_kv_fork(aaf_kv_pool *p, aaf_ctx_t parent, int32_t k, aaf_ctx_t *out_chil
         children[j] = c;
     }
     const long long T = p->len[parent];
-    after_readers(p);
+    after_readers(p, children, k);
     const cudaError_t e = launch_fork(p->g, p->s, parent, T, k, by_value ? nullptr : children, small, p->clock + 1,
                                       p->meta_stream);
     if (!by_value) release_args(p, p->meta_stream);
@@ -1012,6 +1022,7 @@ static int append_impl(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const i
             return rc;
         }
     }
+    after_readers(p, ctxs, n);
     const PlanSlot ps = begin_plan(p);
     const cudaError_t e = launch_plan_append(p->g, ps.view, ent_dev, small, n, (int)slots, p->lay.max_batch, 0,
                                              p->clock + 1, p->meta_stream);
@@ -1142,6 +1153,7 @@ static int compose_impl(aaf_kv_pool *p, int32_t n_out, const int32_t *seg_off, c
     const bool by_value = m <= SMALL_RECORDS;
     ComposeSeg *dev_rec = by_value ? nullptr : reinterpret_cast<ComposeSeg *>(acquire_args(p));
     memcpy(by_value ? small.s : dev_rec, rec.data(), sizeof(ComposeSeg) * (size_t)m);
+    after_readers(p, handles.data(), n_out);
     const PlanSlot ps = begin_plan(p);
     const cudaError_t e = launch_plan_compose(p->g, ps.view, dev_rec, small, m, (int)work, (int)fresh, (int)slots,
                                               p->clock + 1, p->meta_stream);
@@ -1221,7 +1233,6 @@ int aaf_kv_evict(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, void *stream)
         a->total = (int)total;
     }
     int n_launches = 0;
-    after_readers(p);
     const cudaError_t e = launch_evict(p->g, p->s, a, small, n, (int)total, p->clock + 1, &n_launches, p->meta_stream);
     if (a) release_args(p, p->meta_stream);
     if (e != cudaSuccess) return broke(p);
@@ -1251,7 +1262,6 @@ int aaf_kv_evict_to_budget(aaf_kv_pool *p, double alpha, double beta, double gam
     DeviceGuard guard(p->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     p->last_stream = st;
-    after_readers(p);
     if (launch_evict_to_budget(p->g, p->s, alpha, beta, gamma, budget_blocks, p->clock + 1, p->result,
                                p->meta_stream) != cudaSuccess)
         return broke(p);
@@ -1532,7 +1542,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
         }
     }
     p->last_stream = st;
-    if (!begin_read(p, st)) return broke(p);
+    if (!begin_read(p, ctxs, n, st)) return broke(p);
     const int f16 = a->dtype == AAF_DTYPE_F16;
     bool ok = true;
     if (n_few) {
@@ -1624,7 +1634,7 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
     k.a.n = n;
     k.a.total_units = (int)units;
     p->last_stream = st;
-    if (!begin_read(p, st)) return broke(p);
+    if (!begin_read(p, ctxs, n, st)) return broke(p);
     SmallSeqs small;
     const bool ok = place_records(p, rec, small, &k.a.seqs, 0, st) &&
                     launch_attn_mass(k, small, a->dtype == AAF_DTYPE_F16, max_rows, st) == cudaSuccess;
@@ -1685,7 +1695,7 @@ int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int3
     k.Hq = d->n_q_heads; k.H = p->g.H; k.D = p->g.D; k.rot = d->rot_dim; k.interleaved = d->interleaved != 0;
     k.n = n; k.total = (int)total; k.mscale = d->mscale;
     p->last_stream = st;
-    if (!begin_read(p, st)) return broke(p);
+    if (!begin_read(p, ctxs, n, st)) return broke(p);
     SmallStores small;
     const bool ok = place_records(p, rec, small, &k.seqs, 0, st) &&
                     launch_store(k, small, d->dtype == AAF_DTYPE_F16, st) == cudaSuccess;
@@ -1713,11 +1723,13 @@ int aaf_kv_prune(aaf_kv_pool *p, aaf_ctx_t ctx, const float *scores_dev, int64_t
     const int rc0 = ensure_free(p, nb, st);
     if (rc0 != AAF_OK) return rc0;
     p->last_stream = st;
+    after_readers(p, &c, 1);
     const PlanSlot ps = begin_plan(p);
     // the new context's table, blocks and catalog entry; its piece list (no buffer behind it) is not run
-    if (launch_plan_import(p->g, ps.view, c, budget, nullptr, p->clock + 1, p->meta_stream, ctx) != cudaSuccess ||
-        !end_plan(p, ps, st))
-        return broke(p);
+    bool ok = launch_plan_import(p->g, ps.view, c, budget, nullptr, p->clock + 1, p->meta_stream, ctx) == cudaSuccess;
+    // the selection needs none of that: it runs beside the planner (and beside an eviction still under way)
+    ok = ok && launch_select(scores_dev, (int)T, (int)budget, (int)sink, (int)recent, kept_dev, kept_scores_dev, st) == cudaSuccess;
+    if (!ok || !end_plan(p, ps, st)) return broke(p);
     p->clock += 1;
     p->meta_launches += 1;
     p->free_lb -= nb;
@@ -1726,10 +1738,7 @@ int aaf_kv_prune(aaf_kv_pool *p, aaf_ctx_t ctx, const float *scores_dev, int64_t
     p->fork_id[c] = 0;
     p->live_ctx += 1;
     const int *tables = p->s.tables;
-    const bool ok = begin_read(p, st) &&
-                    launch_select(scores_dev, (int)T, (int)budget, (int)sink, (int)recent, kept_dev, kept_scores_dev, st) == cudaSuccess &&
-                    launch_gather_rows(p->g, tables + (long long)ctx * p->g.max_blk, tables + (long long)c * p->g.max_blk, kept_dev,
-                                       (int)budget, p->sm_count, st) == cudaSuccess;
+    ok = begin_read(p, &ctx, 1, st) && launch_gather_rows(p->g, tables + (long long)ctx * p->g.max_blk, ps.view.pieces, kept_dev, (int)budget, p->sm_count, st) == cudaSuccess;
     end_copy(p, ps, st);
     if (!ok) return broke(p);
     *out_ctx = c;
