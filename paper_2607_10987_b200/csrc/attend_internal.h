@@ -117,6 +117,9 @@ bool encode_pool_map(const Geom &g, PoolMap *out);
 cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int tokens, int max_parts,
                                int sm_count, cudaStream_t st);
 cudaError_t launch_attn_mass(const MassParams &p, const SmallSeqs &small, int f16, int max_rows, cudaStream_t st);
+constexpr int MASS_WIDE_CHUNK = 256;             // keys of a CTA of the mass kernel for many rows
+cudaError_t launch_attn_mass_wide(const MassParams &p, const SmallSeqs &small, int f16, const void *map, int layer,
+                                  cudaStream_t st);
 cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16, cudaStream_t st);
 // keep list of a pruned context: kept[budget] ascending, kept_scores (may be null); then the row gather
 cudaError_t launch_select(const float *scores, int len, int budget, int sink, int recent, int *kept, float *kept_scores,

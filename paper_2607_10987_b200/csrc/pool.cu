@@ -1614,9 +1614,16 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
     k.prev = prev_dev;
     k.mass = mass_dev;
     k.mass_stride = mass_stride;
+    int max_rows = 1;
+    for (int i = 0; i < n; ++i) max_rows = std::max(max_rows, (n_q ? n_q[i] : 1) * k.a.G);
+    // Many query rows go to the tensor cores (up to 16 rows the bytes of the keys decide either way, and the kernel that
+    // streams them has less to set up; 32763 tokens, 128 rows: 76 us there, 29 here).
+    const bool wide = p->map_ok && max_rows > 16;
+    const int chunk = wide ? MASS_WIDE_CHUNK : MASS_CHUNK;
+    k.a.status = &p->s.ctl->status;
     std::vector<AttnSeq> rec((size_t)n);
     long long units = 0;
-    int row0 = 0, max_rows = 1;
+    int row0 = 0;
     for (int i = 0; i < n; ++i) {
         AttnSeq &s = rec[(size_t)i];
         s = AttnSeq{};
@@ -1625,8 +1632,7 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
         s.nq = n_q ? n_q[i] : 1;
         s.row0 = row0;
         s.unit0 = (int)units;
-        s.nsplit = (s.len + MASS_CHUNK - 1) / MASS_CHUNK;
-        max_rows = std::max(max_rows, s.nq * k.a.G);
+        s.nsplit = (s.len + chunk - 1) / chunk;
         row0 += s.nq;
         units += s.nsplit;
         if (units > (1ll << 30)) return AAF_ERR_TOO_MANY;
@@ -1637,7 +1643,8 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
     if (!begin_read(p, ctxs, n, st)) return broke(p);
     SmallSeqs small;
     const bool ok = place_records(p, rec, small, &k.a.seqs, 0, st) &&
-                    launch_attn_mass(k, small, a->dtype == AAF_DTYPE_F16, max_rows, st) == cudaSuccess;
+                    (wide ? launch_attn_mass_wide(k, small, a->dtype == AAF_DTYPE_F16, &p->map, layer, st)
+                          : launch_attn_mass(k, small, a->dtype == AAF_DTYPE_F16, max_rows, st)) == cudaSuccess;
     return ok ? AAF_OK : broke(p);
 }
 

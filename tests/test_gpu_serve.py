@@ -487,6 +487,35 @@ def test_mass(heads, group, dim, block, n_q, opts):
         assert abs(float(again[i, :t].double().sum()) - n_q[i] * heads * group) < 1e-3 * n_q[i] * heads * group  # each row gives one
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim,heads,group,block,n_q", [(128, 8, 4, 16, [32, 5, 100]), (64, 2, 3, 8, [43, 6, 131]), (128, 1, 32, 64, [1, 3, 9]),
+                                                       (64, 4, 1, 128, [17, 128, 1])])
+@pytest.mark.parametrize("opts", [{}, dict(softcap=20.0), dict(window=300, slopes=True)])
+def test_mass_of_many_rows(dim, heads, group, block, n_q, opts, dtype):
+    if opts.get("slopes"):
+        opts = dict(opts, slopes=2.0 ** (-8.0 * torch.arange(1, heads * group + 1, device="cuda") / (heads * group)))
+    lens = [1501, 300, 140]
+    pool = R.make_pool(2, heads, dim, block, sum(-(-t // block) for t in lens) + 2, dtype=dtype)
+    ctxs = [R.add_ctx(pool, t, t) for t in lens]
+    hs = [c.handle for c in ctxs]
+    q = R.rand((sum(n_q), heads * group, dim), 3, dtype, 2.0)
+    _, lse, _, big = R.attend_ref(ctxs, n_q, q, layer=1, **opts)
+    lse = lse.float()
+    lse[1] = -math.inf  # a row that is said to have seen nothing
+    prev = torch.rand(3, 1600, device="cuda")
+    want = R.mass_ref(ctxs, n_q, q, lse, prev, layer=1, **opts)
+    ds = dim * 2.0 ** -23 * big + 16 * 2.0 ** -24 * (big + 16)
+    mass, again = torch.full_like(prev, -7.0), torch.full_like(prev, -7.0)
+    assert pool.attn_mass(1, hs, n_q, q, lse, mass, prev=prev, **opts)[0] == 0
+    assert pool.attn_mass(1, hs, n_q, q, lse, again, prev=prev, **opts)[0] == 0
+    torch.cuda.synchronize()
+    assert pool.sync_status() == 0 and torch.equal(mass, again)
+    for i, t in enumerate(lens):
+        lim = (ds + 2.0 ** -22 + n_q[i] * heads * group * 2.0 ** -24) * want[i] + 1e-30
+        assert ((mass[i, :t].double() - want[i]).abs() <= lim).all()
+        assert (mass[i, t:] == -7.0).all()
+
+
 def test_mass_with_spans_and_rows_that_see_nothing():
     pool = R.make_pool(1, 2, 64, 16, 64)
     c = R.add_ctx(pool, 300, 1)
