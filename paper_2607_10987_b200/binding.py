@@ -317,10 +317,7 @@ class KVPool:
 
     # ------------------------------------------------------------------ helpers
     def _stream(self):
-        return C.c_void_p(self.torch.cuda.current_stream(self.device).cuda_stream)
-
-    def _stream_handle(self):
-        """The current stream as an integer (what the latency-critical calls pass)."""
+        """Handle of the current stream of the pool's device."""
         return self._raw_stream(self.device.index)
 
     def xfer_desc(self, n_tokens, pos_start=0) -> aaf_kv_xfer_desc:
@@ -451,7 +448,7 @@ class KVPool:
     def reserve(self, ctxs, n_new):
         n = len(ctxs)
         return load().aaf_kv_reserve(self.h, n, (C.c_int32 * (n or 1))(*ctxs), (C.c_int32 * (n or 1))(*n_new),
-                                     self._stream_handle()), None
+                                     self._stream()), None
 
     def store(self, layer, ctxs, n_new, k, v, q=None, q_out=None, rope=None, pos=None):
         """Rotates q (into q_out, default in place) and k, writes k and v into the slots of the contexts' last n_new tokens."""
@@ -472,7 +469,7 @@ class KVPool:
                               None if pos is None else self._flat(pos, self.torch.int64, tokens, "pos"),
                               qp, op, k.data_ptr(), v.data_ptr(), qs, os, ks, vs)
         return load().aaf_kv_store(self.h, layer, d, n, (C.c_int32 * (n or 1))(*ctxs), (C.c_int32 * (n or 1))(*n_new),
-                                   self._stream_handle()), None
+                                   self._stream()), None
 
     def _attn(self, q, tokens, scale, softcap, window, slopes, spans):
         heads = q.shape[1] if q.dim() == 3 else 0
@@ -489,11 +486,11 @@ class KVPool:
         a = self._attn(q, tokens, scale, softcap, window, slopes, spans)
         heads = a.n_q_heads
         if out is None:
-            out = torch.empty((tokens, heads, self.D), dtype=q.dtype, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif self._rows(out, tokens, heads, "out", q.dtype) != heads * self.D:
             raise ValueError("out: dense tensor expected")
         if lse is None:
-            lse = torch.empty((tokens, heads), dtype=torch.float32, device=self.device)
+            lse = q.new_empty((tokens, heads), dtype=torch.float32)
         else:
             self._flat(lse, torch.float32, tokens * heads, "lse")
         ws = self._attend_ws
@@ -501,7 +498,7 @@ class KVPool:
             ws = self._attend_ws = torch.empty(aaf_kv_attend_workspace_bytes(self.h), dtype=torch.uint8, device=self.device)
         st = load().aaf_kv_attend(self.h, layer, a, n, (C.c_int32 * (n or 1))(*ctxs),
                                   None if n_q is None else (C.c_int32 * (n or 1))(*n_q), q.data_ptr(), out.data_ptr(),
-                                  lse.data_ptr(), ws.data_ptr(), ws.numel(), self._stream_handle())
+                                  lse.data_ptr(), ws.data_ptr(), ws.numel(), self._stream())
         return st, ((out, lse) if st == AAF_OK else None)
 
     def attn_mass(self, layer, ctxs, n_q, q, lse, mass, prev=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):
@@ -520,7 +517,7 @@ class KVPool:
         st = load().aaf_kv_attn_mass(self.h, layer, a, n, (C.c_int32 * (n or 1))(*ctxs),
                                      None if n_q is None else (C.c_int32 * (n or 1))(*n_q), q.data_ptr(),
                                      self._flat(lse, self.torch.float32, tokens * a.n_q_heads, "lse"),
-                                     None if prev is None else prev.data_ptr(), mass.data_ptr(), stride, self._stream_handle())
+                                     None if prev is None else prev.data_ptr(), mass.data_ptr(), stride, self._stream())
         return st, (mass if st == AAF_OK else None)
 
     def prune(self, ctx, scores, budget, sink=0, recent=0, kept=None, kept_scores=None):
@@ -534,7 +531,7 @@ class KVPool:
         st = load().aaf_kv_prune(self.h, ctx, self._flat(scores, torch.float32, scores.numel() if n is None else n, "scores"), budget,
                                  sink, recent, self._flat(kept, torch.int32, max(budget, 1), "kept"),
                                  None if kept_scores is None else self._flat(kept_scores, torch.float32, max(budget, 1), "kept_scores"),
-                                 C.byref(out), self._stream_handle())
+                                 C.byref(out), self._stream())
         return st, (out.value if st == AAF_OK else None)
 
     def materialize_host(self, ctx, t0, t1, dst_host, staging):
