@@ -334,18 +334,19 @@ cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f
 }
 
 // ------------------------------------------------------------------------------------------ join
-// Adds up the parts of a split row: o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s, in part order.  SPREAD warps work on a
-// query token's head, four dimensions a lane: one while there are few parts, a whole CTA's eight, each with every eighth
-// part, when there are many and few rows to share them out over; then they meet in shared memory in warp order.
+// Adds up the parts of a split row: o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.  SPREAD warps work on a query token's
+// head, each with every SPREAD-th part, four dimensions a lane; a warp keeps its own running maximum and sum, and the
+// warps meet once, in shared memory, in warp order.  Bound: latency (a trip to L2 for the parts' maxima and outputs, both asked for
+// at once), which is why there are as many warps a row as fill the GPU.
 constexpr int JOIN_WARPS = 8, JOIN_AHEAD = 8;
 template <typename T, int SPREAD>
 __global__ void __launch_bounds__(JOIN_WARPS * 32)
     attend_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small, int tile_rows, int rows) {
-    __shared__ float4 acc_s[JOIN_WARPS][32];
+    __shared__ float4 acc_s[JOIN_WARPS][2][32];
     __shared__ float sum_s[JOIN_WARPS], max_s[JOIN_WARPS];
-    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % SPREAD;
-    const int out_row = blockIdx.x * (JOIN_WARPS / SPREAD) + (threadIdx.x >> 5) / SPREAD;
-    if (out_row >= rows) return;  // SPREAD == 1 only: nobody waits for this warp
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % SPREAD, team = (threadIdx.x >> 5) / SPREAD;
+    const int out_row = blockIdx.x * (JOIN_WARPS / SPREAD) + team;
+    if (out_row >= rows) return;  // a whole team: only its own warps meet
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
     const int Hq = p.H * p.G;
     const int tok = out_row / Hq, hq = out_row - tok * Hq, head = hq / p.G;
@@ -378,68 +379,88 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32)
         return s < parts && d < dims ? __ldcg(reinterpret_cast<const float4 *>(p.part_o + at(s) * dims + d)) : make_float4(0, 0, 0, 0);
     };
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the parts are written
-    float4 first[JOIN_AHEAD];  // the first parts' outputs are on their way while the weights are worked out
+    float m = -CUDART_INF_F, sum = 0.0f;
+    float4 acc[2] = {make_float4(0, 0, 0, 0), make_float4(0, 0, 0, 0)};  // dimensions lane * 4 and 128 + lane * 4
+    auto add = [&](int half, float w, const float4 &v) {
+        acc[half].x += w * v.x;
+        acc[half].y += w * v.y;
+        acc[half].z += w * v.z;
+        acc[half].w += w * v.w;
+    };
+    for (int c0 = warp; c0 < parts; c0 += 32 * SPREAD) {  // 32 parts, a lane looks after the weight of one
+        const int count = min(32, (parts - c0 + SPREAD - 1) / SPREAD);
+        float4 v[JOIN_AHEAD];
 #pragma unroll
-    for (int i = 0; i < JOIN_AHEAD; ++i) first[i] = load(warp + i * SPREAD, lane * 4);
-    float top = -CUDART_INF_F;
-    for (int s = warp * 32 + lane; s < parts; s += SPREAD * 32) top = fmaxf(top, p.part_ml[2 * at(s)]);
+        for (int k = 0; k < JOIN_AHEAD; ++k) v[k] = load(c0 + k * SPREAD, lane * 4);
+        const float2 ml = lane < count ? __ldcg(reinterpret_cast<const float2 *>(p.part_ml + 2 * at(c0 + lane * SPREAD)))
+                                       : make_float2(-CUDART_INF_F, 0.0f);
+        float top = ml.x;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    if (SPREAD > 1) {
-        if (lane == 0) max_s[warp] = top;
-        __syncthreads();
+        for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        top = fmaxf(top, m);
+        const float base = top == -CUDART_INF_F ? 0.0f : top, old = top == -CUDART_INF_F ? 1.0f : ex2(m - top);
+        const float w = ex2(ml.x - base);  // a part that saw nothing: m = -inf
+        sum = sum * old + w * ml.y;
+        m = top;
 #pragma unroll
-        for (int w = 0; w < SPREAD; ++w) top = fmaxf(top, max_s[w]);
+        for (int half = 0; half < 2; ++half) {
+            acc[half].x *= old;
+            acc[half].y *= old;
+            acc[half].z *= old;
+            acc[half].w *= old;
+        }
+        for (int i = 0; i < count; i += JOIN_AHEAD) {
+            if (i)
+#pragma unroll
+                for (int k = 0; k < JOIN_AHEAD; ++k) v[k] = load(i + k < count ? c0 + (i + k) * SPREAD : parts, lane * 4);
+#pragma unroll
+            for (int k = 0; k < JOIN_AHEAD; ++k) add(0, __shfl_sync(0xffffffffu, w, (i + k) & 31), v[k]);
+            if (dims > 128)
+#pragma unroll
+                for (int k = 0; k < JOIN_AHEAD; ++k)
+                    add(1, __shfl_sync(0xffffffffu, w, (i + k) & 31), load(i + k < count ? c0 + (i + k) * SPREAD : parts, 128 + lane * 4));
+        }
     }
-    const float base = top == -CUDART_INF_F ? 0.0f : top;
-    auto weight = [&](int s) { return s < parts ? ex2(p.part_ml[2 * at(s)] - base) : 0.0f; };  // a part that saw nothing: m = -inf
-    float sum = 0.0f;
-    for (int s = warp + lane * SPREAD; s < parts; s += 32 * SPREAD) sum += weight(s) * p.part_ml[2 * at(s) + 1];
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (SPREAD > 1 && lane == 0) sum_s[warp] = sum;
+    if (SPREAD > 1) {
+        const int at_s = team * SPREAD;
+        acc_s[at_s + warp][0][lane] = acc[0];
+        acc_s[at_s + warp][1][lane] = acc[1];
+        if (lane == 0) {
+            sum_s[at_s + warp] = sum;
+            max_s[at_s + warp] = m;
+        }
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(SPREAD * 32) : "memory");
+        if (warp) return;
+        float top = m;
+#pragma unroll
+        for (int w = 1; w < SPREAD; ++w) top = fmaxf(top, max_s[at_s + w]);
+        const float base = top == -CUDART_INF_F ? 0.0f : top;
+        sum = 0.0f;
+        acc[0] = acc[1] = make_float4(0, 0, 0, 0);
+#pragma unroll
+        for (int w = 0; w < SPREAD; ++w) {
+            const float f = ex2(max_s[at_s + w] - base);
+            sum += f * sum_s[at_s + w];
+            add(0, f, acc_s[at_s + w][0][lane]);
+            add(1, f, acc_s[at_s + w][1][lane]);
+        }
+        m = top;
+    }
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     T *out = static_cast<T *>(p.out) + (qt * Hq + hq) * dims;
-    for (int d0 = 0; d0 < dims; d0 += 128) {
-        const int d = d0 + lane * 4;
-        float4 a = make_float4(0, 0, 0, 0);
-        for (int s0 = warp; s0 < parts; s0 += JOIN_AHEAD * SPREAD) {
-            float4 v[JOIN_AHEAD];
 #pragma unroll
-            for (int i = 0; i < JOIN_AHEAD; ++i) v[i] = d0 == 0 && s0 == warp ? first[i] : load(s0 + i * SPREAD, d);
-#pragma unroll
-            for (int i = 0; i < JOIN_AHEAD; ++i) {
-                const float w = weight(s0 + i * SPREAD);
-                a.x += w * v[i].x;
-                a.y += w * v[i].y;
-                a.z += w * v[i].z;
-                a.w += w * v[i].w;
-            }
-        }
-        float all = sum;
-        if (SPREAD > 1) {
-            __syncthreads();
-            acc_s[warp][lane] = a;
-            __syncthreads();
-            all = sum_s[0];
-            if (warp) continue;
-#pragma unroll
-            for (int w = 1; w < SPREAD; ++w) {
-                const float4 v = acc_s[w][lane];
-                a.x += v.x;
-                a.y += v.y;
-                a.z += v.z;
-                a.w += v.w;
-                all += sum_s[w];
-            }
-        }
-        const float inv = all > 0.0f || all != all ? 1.0f / all : 0.0f;
+    for (int half = 0; half < 2; ++half) {
+        const int d = half * 128 + lane * 4;
         if (d < dims)
-            *reinterpret_cast<uint2 *>(out + d) = make_uint2(Elt<T>::pack(a.x * inv, a.y * inv), Elt<T>::pack(a.z * inv, a.w * inv));
-        if (d0 == 0 && lane == 0 && p.lse) {
-            const RowSpan sp = row_span(p, sq, j);
-            const float slope = p.slopes ? p.slopes[hq] : 0.0f;
-            p.lse[qt * Hq + hq] = all == 0.0f ? -CUDART_INF_F : (top + log2f(all)) * LN2 - slope * (float)sp.near;
-        }
+            *reinterpret_cast<uint2 *>(out + d) = make_uint2(Elt<T>::pack(acc[half].x * inv, acc[half].y * inv),
+                                                             Elt<T>::pack(acc[half].z * inv, acc[half].w * inv));
+    }
+    if (lane == 0 && p.lse) {
+        const RowSpan sp = row_span(p, sq, j);
+        const float slope = p.slopes ? p.slopes[hq] : 0.0f;
+        p.lse[qt * Hq + hq] = sum == 0.0f ? -CUDART_INF_F : (m + log2f(sum)) * LN2 - slope * (float)sp.near;
     }
 }
 
@@ -461,10 +482,15 @@ static cudaError_t join_go(const AttnParams &p, const SmallSeqs &small, int tile
 cudaError_t launch_attend_join(const AttnParams &p, const SmallSeqs &small, int f16, int tile_rows, int tokens, int max_parts,
                                int sm_count, cudaStream_t st) {
     const int rows = tokens * p.H * p.G;
-    if (max_parts <= 2 * JOIN_AHEAD || rows > 2 * sm_count)
-        return f16 ? join_go<__half, 1>(p, small, tile_rows, rows, st) : join_go<__nv_bfloat16, 1>(p, small, tile_rows, rows, st);
-    return f16 ? join_go<__half, JOIN_WARPS>(p, small, tile_rows, rows, st)
-               : join_go<__nv_bfloat16, JOIN_WARPS>(p, small, tile_rows, rows, st);
+    // warps a row: no more than its parts keep busy, nor than the GPU holds at once
+    int spread = 1;
+    while (spread < JOIN_WARPS && spread * JOIN_AHEAD < max_parts && (long long)rows * spread < 8ll * sm_count) spread *= 2;
+    switch (spread) {
+        case 1: return f16 ? join_go<__half, 1>(p, small, tile_rows, rows, st) : join_go<__nv_bfloat16, 1>(p, small, tile_rows, rows, st);
+        case 2: return f16 ? join_go<__half, 2>(p, small, tile_rows, rows, st) : join_go<__nv_bfloat16, 2>(p, small, tile_rows, rows, st);
+        case 4: return f16 ? join_go<__half, 4>(p, small, tile_rows, rows, st) : join_go<__nv_bfloat16, 4>(p, small, tile_rows, rows, st);
+        default: return f16 ? join_go<__half, 8>(p, small, tile_rows, rows, st) : join_go<__nv_bfloat16, 8>(p, small, tile_rows, rows, st);
+    }
 }
 
 }  // namespace aafkv

@@ -1368,7 +1368,7 @@ size_t aaf_kv_attend_workspace_bytes(const aaf_kv_pool *p) { return p ? attend_w
 
 int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n, const aaf_ctx_t *ctxs,
                   const int32_t *n_q, const void *q_dev, void *out_dev, float *lse_dev, void *workspace_dev,
-                  size_t workspace_bytes, void *stream) {
+                  size_t workspace_bytes, void *stream) try {
     AAF_RANGE("aaf_kv_attend");
     if (!p) return AAF_ERR_INVALID_ARG;
     if (p->broken) return AAF_ERR_CUDA;
@@ -1589,11 +1589,13 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
         }
     }
     return ok ? AAF_OK : broke(p);
+} catch (const std::bad_alloc &) {
+    return AAF_ERR_INVALID_ARG;  // the host has no memory for the records; nothing was launched
 }
 
 int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n, const aaf_ctx_t *ctxs,
                      const int32_t *n_q, const void *q_dev, const float *lse_dev, const float *prev_dev, float *mass_dev,
-                     int64_t mass_stride, void *stream) {
+                     int64_t mass_stride, void *stream) try {
     AAF_RANGE("aaf_kv_attn_mass");
     if (!p) return AAF_ERR_INVALID_ARG;
     if (p->broken) return AAF_ERR_CUDA;
@@ -1646,10 +1648,12 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
                     (wide ? launch_attn_mass_wide(k, small, a->dtype == AAF_DTYPE_F16, &p->map, layer, st)
                           : launch_attn_mass(k, small, a->dtype == AAF_DTYPE_F16, max_rows, st)) == cudaSuccess;
     return ok ? AAF_OK : broke(p);
+} catch (const std::bad_alloc &) {
+    return AAF_ERR_INVALID_ARG;  // the host has no memory for the records; nothing was launched
 }
 
 int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int32_t n, const aaf_ctx_t *ctxs,
-                 const int32_t *n_new, void *stream) {
+                 const int32_t *n_new, void *stream) try {
     AAF_RANGE("aaf_kv_store");
     if (!p || !d || d->struct_size != sizeof(aaf_kv_store_desc) || n < 1 || !ctxs || !n_new) return AAF_ERR_INVALID_ARG;
     if (p->broken) return AAF_ERR_CUDA;
@@ -1707,6 +1711,8 @@ int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int3
     const bool ok = place_records(p, rec, small, &k.seqs, 0, st) &&
                     launch_store(k, small, d->dtype == AAF_DTYPE_F16, st) == cudaSuccess;
     return ok ? AAF_OK : broke(p);
+} catch (const std::bad_alloc &) {
+    return AAF_ERR_INVALID_ARG;  // the host has no memory for the records; nothing was launched
 }
 
 int aaf_kv_prune(aaf_kv_pool *p, aaf_ctx_t ctx, const float *scores_dev, int64_t budget, int64_t sink, int64_t recent,

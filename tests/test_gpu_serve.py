@@ -193,6 +193,26 @@ def test_nonfinite_values_reach_only_the_rows_that_see_them(dim, n_q):
     R.check_attend(part, (ref[0][:-2, :, keep], ref[1][:-2], ref[2][:-2, :, keep], ref[3]), torch.bfloat16, dim, p_rounded=n_q[0] > 16)
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("opts", [{}, dict(softcap=30.0)])
+def test_nonfinite_values_in_split_ranges(dim, opts):
+    t, n_q = 3000, 70
+    pool = R.make_pool(1, 1, dim, 16, 200)
+    rows = R.rand((1, 2, t, 1, dim), 5)
+    rows[0, 1, t - 1, 0, 3] = math.nan
+    rows[0, 1, t - 40, 0, 7] = math.inf
+    c = R.add_ctx(pool, t, 0, rows)
+    q = R.rand((n_q, 2, dim), 6, scale=2.0)
+    out, lse = run_attend(pool, [c], [n_q], q, **opts)
+    assert torch.isfinite(out[:-1, :, 3]).all() and torch.isnan(out[-1, :, 3]).all()
+    assert torch.isfinite(out[:n_q - 40, :, 7]).all() and (out[n_q - 40:, :, 7] == math.inf).all()
+    clean = rows.clone()
+    clean[0, 1, t - 1, 0, 3] = clean[0, 1, t - 40, 0, 7] = 0
+    keep = [i for i in range(dim) if i not in (3, 7)]
+    ref = R.attend_ref([R.Ctx(0, clean)], [n_q], q, **opts)
+    R.check_attend((out[:, :, keep], lse), (ref[0][:, :, keep], ref[1], ref[2][:, :, keep], ref[3]), torch.bfloat16, dim, True)
+
+
 def test_layers_blocks_shared_by_forks_and_repeated_contexts():
     pool = R.make_pool(3, 2, 64, 16, 256)
     root = R.add_ctx(pool, 333, 1)
