@@ -30,7 +30,9 @@ template <int DP> struct FewShape {
     static_assert(2 * (SMEM + 1024) <= 228 * 1024, "shared memory of a CTA");
 };
 
-template <typename T, int DP, int NT>
+// SIMPLE: one query token a sequence, no cap, bias or spans: every row sees every key of its part, a score is a multiple of the
+// product.  Two in five instructions of a tile go into the general case (486 at 128 dims).
+template <typename T, int DP, int NT, bool SIMPLE>
 __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
     attend_few_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small) {
     using S = FewShape<DP>;
@@ -47,25 +49,28 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
     const int R = sq.nq * p.G;
 
     // rows of this lane: columns 2 t4, 2 t4 + 1 of every n-tile
-    RowSpan span[NT][2];
-    float slope[NT][2];
-    int lo_all = 0x7fffffff, hi_all = 0;
+    RowSpan span[SIMPLE ? 1 : NT][2];
+    float slope[SIMPLE ? 1 : NT][2];
+    int lo_all = SIMPLE ? 0 : 0x7fffffff, hi_all = SIMPLE ? sq.len : 0;
+    if (!SIMPLE) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int r = nt * 8 + 2 * t4 + c;
-            span[nt][c] = row_span(p, sq, min(r, R - 1) / p.G);
-            slope[nt][c] = p.slopes ? p.slopes[head * p.G + min(r, R - 1) % p.G] : 0.0f;
-            if (span[nt][c].hi > span[nt][c].lo) {
-                lo_all = min(lo_all, span[nt][c].lo);
-                hi_all = max(hi_all, span[nt][c].hi);
+            RowSpan &sp = span[SIMPLE ? 0 : nt][c];
+            sp = row_span(p, sq, min(r, R - 1) / p.G);
+            slope[SIMPLE ? 0 : nt][c] = p.slopes ? p.slopes[head * p.G + min(r, R - 1) % p.G] : 0.0f;
+            if (sp.hi > sp.lo) {
+                lo_all = min(lo_all, sp.lo);
+                hi_all = max(hi_all, sp.hi);
             }
         }
 #pragma unroll
     for (int d = 1; d < 4; d <<= 1) {
         lo_all = min(lo_all, __shfl_xor_sync(0xffffffffu, lo_all, d));
         hi_all = max(hi_all, __shfl_xor_sync(0xffffffffu, hi_all, d));
+    }
     }
     // the part's keys: the host cut [key0, len) into chunks
     const long long c0 = sq.key0 + (long long)part * sq.chunk;
@@ -127,6 +132,7 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
         }
     }
 
+    const float c2 = p.scale * LOG2E;
     float o[NT][DP / 16][4];
     float m[NT][2], l[NT][2];
 #pragma unroll
@@ -161,14 +167,18 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
             float mx[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const RowSpan &sp = span[nt][c];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int t = tb + g + 8 * h;
-                    const bool see = t >= sp.lo && t < sp.hi && t < end;
-                    partial |= !see && t < end;
-                    const float v = score2(p, s[nt][2 * h + c], slope[nt][c], sp, t);
-                    s[nt][2 * h + c] = see ? v : -CUDART_INF_F;
+                    float &x = s[nt][2 * h + c];
+                    if (SIMPLE) {
+                        x = t < end ? x * c2 : -CUDART_INF_F;
+                    } else {
+                        const RowSpan &sp = span[SIMPLE ? 0 : nt][c];
+                        const bool see = t >= sp.lo && t < sp.hi && t < end;
+                        partial |= !see && t < end;
+                        x = see ? score2(p, x, slope[SIMPLE ? 0 : nt][c], sp, t) : -CUDART_INF_F;
+                    }
                 }
                 mx[c] = fmaxf(s[nt][c], s[nt][2 + c]);
             }
@@ -205,11 +215,12 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
             ph[nt][1] = transpose8x8(h23);
             pl[nt][0] = transpose8x8(l01);
             pl[nt][1] = transpose8x8(l23);
+            if (SIMPLE) continue;
             const uint32_t one = Elt<T>::ONE;
             vis[nt][0] = (s[nt][0] != -CUDART_INF_F ? one : 0u) | (s[nt][1] != -CUDART_INF_F ? one << 16 : 0u);
             vis[nt][1] = (s[nt][2] != -CUDART_INF_F ? one : 0u) | (s[nt][3] != -CUDART_INF_F ? one << 16 : 0u);
         }
-        partial = __any_sync(0xffffffffu, partial);
+        partial = !SIMPLE && __any_sync(0xffffffffu, partial);
 #pragma unroll
         for (int c = 0; c < DP / 64; ++c) {
             uint4 v[4];
@@ -294,17 +305,18 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
             }
             if (p.lse && g == 0)
                 p.lse[qt * p.H * p.G + hq] =
-                    sum == 0.0f ? -CUDART_INF_F : (m[nt][c] + log2f(sum)) * LN2 - slope[nt][c] * (float)span[nt][c].near;
+                    sum == 0.0f ? -CUDART_INF_F
+                                : (m[nt][c] + log2f(sum)) * LN2 - (SIMPLE ? 0.0f : slope[SIMPLE ? 0 : nt][c] * (float)span[SIMPLE ? 0 : nt][c].near);
         }
     asm volatile("griddepcontrol.wait;" ::: "memory");  // what it ran beside is done before it is
 }
 
 int few_rows_limit(int D) { return D <= 64 ? 32 : (D <= 128 ? 16 : 8); }
 
-template <typename T, int DP, int NT>
+template <typename T, int DP, int NT, bool SIMPLE>
 static cudaError_t few_go(const AttnParams &p, const SmallSeqs &small, bool beside, cudaStream_t st) {
     static unsigned long long seen = 0;
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_few_kernel<T, DP, NT>), FewShape<DP>::SMEM, &seen);
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_few_kernel<T, DP, NT, SIMPLE>), FewShape<DP>::SMEM, &seen);
     if (e != cudaSuccess) return e;
     constexpr int W = FewShape<DP>::WARPS;
     const long long tasks = (long long)p.total_units * p.H;
@@ -318,19 +330,25 @@ static cudaError_t few_go(const AttnParams &p, const SmallSeqs &small, bool besi
     cfg.stream = st;
     cfg.attrs = &early;
     cfg.numAttrs = beside ? 1 : 0;
-    e = cudaLaunchKernelEx(&cfg, attend_few_kernel<T, DP, NT>, p, small);
+    e = cudaLaunchKernelEx(&cfg, attend_few_kernel<T, DP, NT, SIMPLE>, p, small);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
-template <typename T>
-static cudaError_t few_pick(const AttnParams &p, const SmallSeqs &small, int max_rows, bool beside, cudaStream_t st) {
-    if (p.D <= 64)
-        return max_rows <= 8 ? few_go<T, 64, 1>(p, small, beside, st)
-                             : (max_rows <= 16 ? few_go<T, 64, 2>(p, small, beside, st) : few_go<T, 64, 4>(p, small, beside, st));
-    if (p.D <= 128) return max_rows <= 8 ? few_go<T, 128, 1>(p, small, beside, st) : few_go<T, 128, 2>(p, small, beside, st);
-    return few_go<T, 256, 1>(p, small, beside, st);
+template <typename T, int DP, int NT>
+static cudaError_t few_kind(const AttnParams &p, const SmallSeqs &small, bool simple, bool beside, cudaStream_t st) {
+    return simple ? few_go<T, DP, NT, true>(p, small, beside, st) : few_go<T, DP, NT, false>(p, small, beside, st);
 }
-cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, bool beside, cudaStream_t st) {
-    return f16 ? few_pick<__half>(p, small, max_rows, beside, st) : few_pick<__nv_bfloat16>(p, small, max_rows, beside, st);
+template <typename T>
+static cudaError_t few_pick(const AttnParams &p, const SmallSeqs &small, int max_rows, bool single, bool beside, cudaStream_t st) {
+    const bool simple = single && p.softcap == 0.0f && !p.slopes && !p.spans;
+    if (p.D <= 64)
+        return max_rows <= 8 ? few_kind<T, 64, 1>(p, small, simple, beside, st)
+                             : (max_rows <= 16 ? few_kind<T, 64, 2>(p, small, simple, beside, st) : few_kind<T, 64, 4>(p, small, simple, beside, st));
+    if (p.D <= 128) return max_rows <= 8 ? few_kind<T, 128, 1>(p, small, simple, beside, st) : few_kind<T, 128, 2>(p, small, simple, beside, st);
+    return few_kind<T, 256, 1>(p, small, simple, beside, st);
+}
+cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, bool single, bool beside,
+                              cudaStream_t st) {
+    return f16 ? few_pick<__half>(p, small, max_rows, single, beside, st) : few_pick<__nv_bfloat16>(p, small, max_rows, single, beside, st);
 }
 
 // ------------------------------------------------------------------------------------------ join

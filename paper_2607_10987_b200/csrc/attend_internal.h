@@ -102,8 +102,8 @@ constexpr int FEW_MAX_DIM = 256;
 int few_rows_limit(int D);                       // most rows of a kv head that the few-row kernel takes
 constexpr int TILE_ROWS = 64;                    // rows of a unit of the tile kernel
 constexpr int MASS_CHUNK = 64;                   // keys of a CTA of the mass kernel
-// beside: brought up beside the kernel launched before it, which it does not depend on
-cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, bool beside,
+// single: one query token each; beside: brought up beside the kernel launched before it, which it does not depend on
+cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, bool single, bool beside,
                               cudaStream_t st);
 cudaError_t launch_attend_tile(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
 constexpr int WIDE_ROWS = 256;                   // rows of a unit of the wide kernel

@@ -1561,7 +1561,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
             kg.total_units = group_units;
             ok = launch_attend_wide(kg, small, f16, &p->map, layer, st) == cudaSuccess;
         }
-        if (ok && few_units) ok = launch_attend_few(kf, small, f16, few_rows, group_units > 0, st) == cudaSuccess;
+        if (ok && few_units) ok = launch_attend_few(kf, small, f16, few_rows, few_tokens == (int)n_few, group_units > 0, st) == cudaSuccess;
         if (ok && few_joined) ok = launch_attend_join(kf, small, f16, 0, few_tokens, few_parts, p->sm_count, st) == cudaSuccess;
     }
     if (ok && !many.empty()) {
