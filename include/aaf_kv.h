@@ -382,7 +382,8 @@ int aaf_kv_rope_freqs(int32_t rot_dim, double base, int32_t scaling, const aaf_k
  * packed into one context ({start of the token's document, p + 1}), a prefix seen in both directions ({0, max(p + 1,
  * prefix)}), a whole context ({0, length}).  A row that sees no key, or whose visible scores are all -inf, is 0 with lse =
  * -inf.  Keys and values that a row does not see have no influence on it, whatever they hold (infinities and NaN
- * included); slots behind a context's end are not read.
+ * included); slots behind a context's end are not read.  An infinite value that a row sees makes that element of the row
+ * infinite; NaN if its weight is too small for the type.
  * q: heads contiguous, q_stride elements from token to token (a multiple of 8); out: dense [tokens][n_q_heads][head_dim];
  * lse (may be NULL): [tokens][n_q_heads].  n_q may be NULL (one token each).  A context may be listed several times.
  * workspace_dev: caller-owned scratch of aaf_kv_attend_workspace_bytes(pool) bytes, 16-byte aligned; one buffer serves all

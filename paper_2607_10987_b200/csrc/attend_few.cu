@@ -110,13 +110,17 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
         copy_commit();
     };
 
-    int id = table_id(0);
+    int id;
+    auto start = [&] {
+        id = table_id(0);
 #pragma unroll
-    for (int s = 0; s < S::STAGES; ++s) {
-        const int nxt = table_id(s + 1);
-        issue(s, id);
-        id = nxt;
-    }
+        for (int s = 0; s < S::STAGES; ++s) {
+            const int nxt = table_id(s + 1);
+            issue(s, id);
+            id = nxt;
+        }
+    };
+    start();
 
     // query fragments: row nt * 8 + g, 8 dimensions at kk * 32 + t4 * 8
     uint4 qf[NT][DP / 32];
@@ -135,6 +139,11 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
     const float c2 = p.scale * LOG2E;
     float o[NT][DP / 16][4];
     float m[NT][2], l[NT][2];
+    // An infinite value times one part of its weight is infinite, times the other NaN (the low part may be zero or negative).  So a
+    // warp that ends with a NaN takes its keys once more with such values kept out of the products, as tiles that only
+    // some rows see do.
+    bool careful = false;
+again:
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         m[nt][0] = m[nt][1] = -CUDART_INF_F;
@@ -215,12 +224,12 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
             ph[nt][1] = transpose8x8(h23);
             pl[nt][0] = transpose8x8(l01);
             pl[nt][1] = transpose8x8(l23);
-            if (SIMPLE) continue;
+            if (SIMPLE && !careful) continue;
             const uint32_t one = Elt<T>::ONE;
             vis[nt][0] = (s[nt][0] != -CUDART_INF_F ? one : 0u) | (s[nt][1] != -CUDART_INF_F ? one << 16 : 0u);
             vis[nt][1] = (s[nt][2] != -CUDART_INF_F ? one : 0u) | (s[nt][3] != -CUDART_INF_F ? one << 16 : 0u);
         }
-        partial = !SIMPLE && __any_sync(0xffffffffu, partial);
+        partial = careful || (!SIMPLE && __any_sync(0xffffffffu, partial));
 #pragma unroll
         for (int c = 0; c < DP / 64; ++c) {
             uint4 v[4];
@@ -262,6 +271,20 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
         id = nxt;
     }
     copy_wait<0>();
+    if (!careful) {
+        bool odd = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) odd |= o[nt][i][k] != o[nt][i][k];
+        if (__any_sync(0xffffffffu, odd)) {
+            careful = true;
+            start();
+            goto again;
+        }
+    }
 
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)

@@ -193,6 +193,22 @@ def test_nonfinite_values_reach_only_the_rows_that_see_them(dim, n_q):
     R.check_attend(part, (ref[0][:-2, :, keep], ref[1][:-2], ref[2][:-2, :, keep], ref[3]), torch.bfloat16, dim, p_rounded=n_q[0] > 16)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim,n_q,t,opts", [(64, 1, 40, {}), (128, 1, 40, {}), (128, 1, 5000, {}), (256, 1, 40, {}), (128, 4, 300, {}),
+                                            (128, 1, 300, dict(softcap=20.0)), (64, 90, 300, {}), (96, 90, 300, {})])
+def test_an_infinite_value_that_is_seen_is_infinite(dim, n_q, t, opts, dtype):
+    pool = R.make_pool(1, 2, dim, 16, 400, dtype=dtype)
+    rows = R.rand((1, 2, t, 2, dim), 5, dtype)
+    rows[0, 1, 3, 0, 3] = math.inf
+    rows[0, 1, 20, 1, 5] = -math.inf
+    rows[0, 1, 21, 1, 6], rows[0, 1, 22, 1, 6] = -math.inf, math.inf
+    c = R.add_ctx(pool, t, 0, rows)
+    q = R.rand((n_q, 4, dim), 6, dtype, 0.5)
+    out, lse = run_attend(pool, [c], [n_q], q, **opts)
+    assert (out[:, :2, 3] == math.inf).all() and (out[:, 2:, 5] == -math.inf).all() and torch.isnan(out[:, 2:, 6]).all()
+    R.check_attend((out, lse), R.attend_ref([c], [n_q], q, **opts), dtype, dim, p_rounded=n_q * 2 > 8)
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("opts", [{}, dict(softcap=30.0)])
 def test_nonfinite_values_in_split_ranges(dim, opts):
