@@ -180,6 +180,9 @@ __device__ __forceinline__ float score2(const AttnParams &p, float x, float slop
     return x * LOG2E;
 }
 
+// an output from its weighted sum; a row without weights is zero, whatever it multiplied by zero
+__device__ __forceinline__ float scaled(float o, float inv) { return inv == 0.0f ? 0.0f : o * inv; }
+
 // sequence that a unit belongs to: the last one whose first unit is not behind it
 __device__ __forceinline__ int find_seq(const AttnSeq *s, int n, int unit) {
     int lo = 0, hi = n - 1;

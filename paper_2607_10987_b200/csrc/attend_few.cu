@@ -296,14 +296,15 @@ again:
             const int r = nt * 8 + 2 * t4 + c;
             if (r >= R) continue;
             if (sq.part0 >= 0) {  // a part of a longer range: (m, l, o) for the join
+                const float some = sum == 0.0f ? 0.0f : 1.0f;
                 const long long pr = sq.part0 + ((long long)part * p.H + head) * R + r;
 #pragma unroll
                 for (int cc = 0; cc < DP / 64; ++cc) {
                     const int d = cc * 64 + g * 8;
                     if (d >= p.D) continue;
                     float4 *dst = reinterpret_cast<float4 *>(p.part_o + pr * p.D + d);
-                    dst[0] = make_float4(o[nt][4 * cc][c], o[nt][4 * cc][2 + c], o[nt][4 * cc + 1][c], o[nt][4 * cc + 1][2 + c]);
-                    dst[1] = make_float4(o[nt][4 * cc + 2][c], o[nt][4 * cc + 2][2 + c], o[nt][4 * cc + 3][c], o[nt][4 * cc + 3][2 + c]);
+                    dst[0] = make_float4(scaled(o[nt][4 * cc][c], some), scaled(o[nt][4 * cc][2 + c], some), scaled(o[nt][4 * cc + 1][c], some), scaled(o[nt][4 * cc + 1][2 + c], some));
+                    dst[1] = make_float4(scaled(o[nt][4 * cc + 2][c], some), scaled(o[nt][4 * cc + 2][2 + c], some), scaled(o[nt][4 * cc + 3][c], some), scaled(o[nt][4 * cc + 3][2 + c], some));
                 }
                 if (g == 0) {
                     p.part_ml[2 * pr] = m[nt][c];
@@ -495,8 +496,8 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32)
     for (int half = 0; half < 2; ++half) {
         const int d = half * 128 + lane * 4;
         if (d < dims)
-            *reinterpret_cast<uint2 *>(out + d) = make_uint2(Elt<T>::pack(acc[half].x * inv, acc[half].y * inv),
-                                                             Elt<T>::pack(acc[half].z * inv, acc[half].w * inv));
+            *reinterpret_cast<uint2 *>(out + d) = make_uint2(Elt<T>::pack(scaled(acc[half].x, inv), scaled(acc[half].y, inv)),
+                                                             Elt<T>::pack(scaled(acc[half].z, inv), scaled(acc[half].w, inv)));
     }
     if (lane == 0 && p.lse) {
         const RowSpan sp = row_span(p, sq, j);

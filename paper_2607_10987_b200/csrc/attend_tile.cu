@@ -240,10 +240,12 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
         if (rr >= R) continue;
         if (sq.part0 >= 0) {
             const long long pr = sq.part0 + (((long long)tile * sq.nsplit + part) * p.H + head) * TILE_ROWS + rl;
+            const float some = sum == 0.0f ? 0.0f : 1.0f;
 #pragma unroll
             for (int i = 0; i < DP / 8; ++i) {
                 const int d = i * 8 + 2 * t4;
-                if (d < p.D) *reinterpret_cast<float2 *>(p.part_o + pr * p.D + d) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
+                if (d < p.D)
+                    *reinterpret_cast<float2 *>(p.part_o + pr * p.D + d) = make_float2(scaled(o[i][2 * h], some), scaled(o[i][2 * h + 1], some));
             }
             if (t4 == 0) {
                 p.part_ml[2 * pr] = m[h];
@@ -258,7 +260,7 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
 #pragma unroll
         for (int i = 0; i < DP / 8; ++i) {
             const int d = i * 8 + 2 * t4;
-            if (d < p.D) *reinterpret_cast<uint32_t *>(out + d) = Elt<T>::pack(o[i][2 * h] * inv, o[i][2 * h + 1] * inv);
+            if (d < p.D) *reinterpret_cast<uint32_t *>(out + d) = Elt<T>::pack(scaled(o[i][2 * h], inv), scaled(o[i][2 * h + 1], inv));
         }
         if (p.lse && t4 == 0)
             p.lse[qt * p.H * p.G + hq] =

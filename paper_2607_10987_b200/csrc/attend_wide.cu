@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             const bool part_out = sq.part0 >= 0;
             const long long qt = packed;
             const long long pr = sq.part0 + (((long long)tile * sq.nsplit + part) * p.H + head) * WIDE_ROWS + w * WIDE_TILE + rl;
-            const float inv = part_out ? 1.0f : (l > 0.0f || l != l ? 1.0f / l : 0.0f);  // a row that sees nothing is zero
+            const float inv = l > 0.0f || l != l ? (part_out ? 1.0f : 1.0f / l) : 0.0f;  // a row that sees nothing is zero
             T *out = static_cast<T *>(p.out) + (qt * p.H * p.G + hq) * D;
             float *part_o = p.part_o + pr * D;
 #pragma unroll 1
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                     tmem_wait_ld();
                 }
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = tiles > 0 ? o[i] * inv : 0.0f;
+                for (int i = 0; i < 32; ++i) o[i] = tiles > 0 ? scaled(o[i], inv) : 0.0f;
                 if (live && part_out) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 4)

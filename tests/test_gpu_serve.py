@@ -209,6 +209,22 @@ def test_an_infinite_value_that_is_seen_is_infinite(dim, n_q, t, opts, dtype):
     R.check_attend((out, lse), R.attend_ref([c], [n_q], q, **opts), dtype, dim, p_rounded=n_q * 2 > 8)
 
 
+@pytest.mark.parametrize("dim,n_q,t", [(64, 1, 40), (128, 1, 40), (128, 1, 5000), (256, 1, 40), (128, 4, 300), (64, 90, 300), (128, 90, 3000),
+                                       (96, 90, 300), (96, 90, 3000)])
+def test_a_row_of_scores_of_minus_infinity_is_zero(dim, n_q, t):
+    """Also where values are infinite: no weight is left to multiply them."""
+    pool = R.make_pool(1, 2, dim, 16, 400)
+    rows = R.rand((1, 2, t, 2, dim), 5)
+    rows[0, 0, :, 0, 0] = -math.inf
+    rows[0, 1, 3:40:7, 0, 2] = math.inf
+    c = R.add_ctx(pool, t, 0, rows)
+    q = R.rand((n_q, 4, dim), 6)
+    q[:, :, 0] = q[:, :, 0].abs() + 0.5
+    out, lse = run_attend(pool, [c], [n_q], q)
+    assert (out[:, :2] == 0).all() and (lse[:, :2] == -math.inf).all()
+    assert torch.isfinite(out[:, 2:]).all() and torch.isfinite(lse[:, 2:]).all()
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("opts", [{}, dict(softcap=30.0)])
 def test_nonfinite_values_in_split_ranges(dim, opts):
