@@ -303,8 +303,10 @@ again:
                     const int d = cc * 64 + g * 8;
                     if (d >= p.D) continue;
                     float4 *dst = reinterpret_cast<float4 *>(p.part_o + pr * p.D + d);
-                    dst[0] = make_float4(scaled(o[nt][4 * cc][c], some), scaled(o[nt][4 * cc][2 + c], some), scaled(o[nt][4 * cc + 1][c], some), scaled(o[nt][4 * cc + 1][2 + c], some));
-                    dst[1] = make_float4(scaled(o[nt][4 * cc + 2][c], some), scaled(o[nt][4 * cc + 2][2 + c], some), scaled(o[nt][4 * cc + 3][c], some), scaled(o[nt][4 * cc + 3][2 + c], some));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        dst[i] = make_float4(scaled(o[nt][4 * cc + 2 * i][c], some), scaled(o[nt][4 * cc + 2 * i][2 + c], some),
+                                             scaled(o[nt][4 * cc + 2 * i + 1][c], some), scaled(o[nt][4 * cc + 2 * i + 1][2 + c], some));
                 }
                 if (g == 0) {
                     p.part_ml[2 * pr] = m[nt][c];
@@ -321,10 +323,10 @@ again:
                 const int d = cc * 64 + g * 8;
                 if (d >= p.D) continue;
                 uint4 w;
-                w.x = Elt<T>::pack(o[nt][4 * cc][c] * inv, o[nt][4 * cc][2 + c] * inv);
-                w.y = Elt<T>::pack(o[nt][4 * cc + 1][c] * inv, o[nt][4 * cc + 1][2 + c] * inv);
-                w.z = Elt<T>::pack(o[nt][4 * cc + 2][c] * inv, o[nt][4 * cc + 2][2 + c] * inv);
-                w.w = Elt<T>::pack(o[nt][4 * cc + 3][c] * inv, o[nt][4 * cc + 3][2 + c] * inv);
+                w.x = Elt<T>::pack(scaled(o[nt][4 * cc][c], inv), scaled(o[nt][4 * cc][2 + c], inv));
+                w.y = Elt<T>::pack(scaled(o[nt][4 * cc + 1][c], inv), scaled(o[nt][4 * cc + 1][2 + c], inv));
+                w.z = Elt<T>::pack(scaled(o[nt][4 * cc + 2][c], inv), scaled(o[nt][4 * cc + 2][2 + c], inv));
+                w.w = Elt<T>::pack(scaled(o[nt][4 * cc + 3][c], inv), scaled(o[nt][4 * cc + 3][2 + c], inv));
                 *reinterpret_cast<uint4 *>(out + d) = w;
             }
             if (p.lse && g == 0)
