@@ -69,7 +69,8 @@ __global__ void __launch_bounds__(MASS_WARPS * 32, DP <= 128 ? 4 : 2)
         }
         copy_commit();
     };
-    // queries of a batch of heads: row hh * block_rows + r
+    // Queries of a batch of heads: row hh * block_rows + r.  A row behind the last repeats the last one, with a log-sum of
+    // infinity: it adds nothing unless the last row itself adds a NaN (zeros would make a NaN of an infinite key).
     auto load_queries = [&](int batch) {
         if (batch < row_blocks * batches) {
             const int rb = batch / batches * block_rows, h0 = batch % batches * batch_heads, heads = min(batch_heads, a.H - h0);
@@ -83,9 +84,9 @@ __global__ void __launch_bounds__(MASS_WARPS * 32, DP <= 128 ? 4 : 2)
 #pragma unroll 4
             for (int r = threadIdx.x / S::PIECES; r < heads * block_rows; r += AT_ONCE) {
                 int hh;
-                const int rq = row_of(r, hh), rc = min(rq, R - 1), j = token_of(a, rc);
+                const int rc = min(row_of(r, hh), R - 1), j = token_of(a, rc);
                 const T *src = static_cast<const T *>(a.q) + (sq.row0 + j) * a.q_stride + ((h0 + hh) * a.G + rc - j * a.G) * a.D + c * 8;
-                const bool in = rq < R && c * 8 < a.D;
+                const bool in = c * 8 < a.D;
                 copy16(dst + at(r, c), in ? src : static_cast<const T *>(a.q), in ? 16 : 0);
             }
             for (int r = threadIdx.x; r < heads * block_rows; r += MASS_WARPS * 32) {

@@ -148,10 +148,10 @@ __global__ void __launch_bounds__(MW_THREADS, 1)
             if (s >= MW_Q && !warp_wait(q_free + 8 * e, s / MW_Q - 1 & 1, &sh_abort, a.status)) break;
 #pragma unroll
             for (int i = 0; i < MW_ROWS / AT_ONCE; ++i) {
-                const int r = i * AT_ONCE + tid / PIECES, rq = rb + r, rc = min(rq, R - 1), j = token_of(a, rc);
+                const int r = i * AT_ONCE + tid / PIECES, rc = min(rb + r, R - 1), j = token_of(a, rc);  // behind the last: the last again
                 const T *src = static_cast<const T *>(a.q) + (sq.row0 + j) * a.q_stride + (head * a.G + rc - j * a.G) * D + c * 8;
                 copy16(sQ + e * S::Q_BYTES + r * 128 + (c >> 3) * (MW_ROWS * 128) + (((c & 7) ^ (r & 7)) << 4),
-                       rq < R ? src : static_cast<const T *>(a.q), rq < R ? 16 : 0);
+                       src, 16);
             }
             copy_commit();
             if (tid < MW_ROWS) {

@@ -568,6 +568,23 @@ def test_mass_of_many_rows(dim, heads, group, block, n_q, opts, dtype):
         assert (mass[i, t:] == -7.0).all()
 
 
+@pytest.mark.parametrize("dim,group,n_q", [(64, 4, 1), (128, 4, 1), (256, 3, 1), (128, 4, 5), (64, 3, 50)])
+def test_mass_of_a_key_of_minus_infinity(dim, group, n_q):
+    """Every row's score is -inf there: the key gets nothing, also where rows do not fill a tile."""
+    pool = R.make_pool(1, 2, dim, 16, 64)
+    rows = R.rand((1, 2, 700, 2, dim), 5)
+    rows[0, 0, 7, :, 0] = -math.inf
+    c = R.add_ctx(pool, 700, 0, rows)
+    q = R.rand((n_q, 2 * group, dim), 6)
+    q[:, :, 0] = q[:, :, 0].abs() + 0.5
+    out, lse = run_attend(pool, [c], [n_q], q)
+    mass = torch.full((1, 700), 3.0, device="cuda")
+    assert pool.attn_mass(0, [c.handle], [n_q], q, lse, mass)[0] == 0
+    torch.cuda.synchronize()
+    total = 2 * group * n_q
+    assert torch.isfinite(out).all() and float(mass[0, 7]) == 0.0 and abs(float(mass.double().sum()) - total) < 1e-3 * total
+
+
 def test_mass_with_spans_and_rows_that_see_nothing():
     pool = R.make_pool(1, 2, 64, 16, 64)
     c = R.add_ctx(pool, 300, 1)
