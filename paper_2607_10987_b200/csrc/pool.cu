@@ -1047,6 +1047,9 @@ int aaf_kv_append(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const int32_
 int aaf_kv_reserve(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_new, void *stream) {
     AAF_RANGE("aaf_kv_reserve");
     if (!p || n < 1 || !ctxs || !n_new) return AAF_ERR_INVALID_ARG;
+    if (p->broken) return AAF_ERR_CUDA;
+    DeviceGuard guard(p->device);
+    if (capturing(static_cast<cudaStream_t>(stream))) return AAF_ERR_INVALID_ARG;
     return append_impl(p, n, ctxs, n_new, nullptr, stream);
 }
 

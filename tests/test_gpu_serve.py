@@ -745,6 +745,21 @@ def test_calls_during_capture_are_refused():
     run_attend(pool, [c], [1], q)
 
 
+def test_reserve_during_capture_is_refused():
+    pool = R.make_pool(1, 2, 64, 16, 32)
+    c = R.add_ctx(pool, 20, 1)
+    x = torch.zeros(1, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.add_(1.0)
+        st = pool.reserve([c.handle], [1])[0]
+    assert st == B.AAF_ERR_INVALID_ARG and pool.ctx_len(c.handle) == 20
+    graph.replay()
+    assert pool.reserve([c.handle], [1])[0] == 0 and pool.ctx_len(c.handle) == 21
+    torch.cuda.synchronize()
+    assert float(x) == 1 and pool.sync_status() == 0
+
+
 def test_an_unusable_pool_refuses():
     pool = R.make_pool(1, 2, 64, 16, 32)
     c = R.add_ctx(pool, 20, 1)
