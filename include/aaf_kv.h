@@ -396,7 +396,7 @@ typedef struct aaf_kv_attn {
     int32_t n_q_heads;    /* a multiple of n_kv_heads                             */
     int32_t window;       /* 0: none                                              */
     float scale;
-    float softcap;        /* 0: none                                              */
+    float softcap;        /* 0: none; its reciprocal must be finite               */
     const float *slopes;  /* (device) n_q_heads entries, or NULL                  */
     const int32_t *spans; /* (device) two per query token, or NULL                */
     int64_t q_stride;     /* elements                                             */

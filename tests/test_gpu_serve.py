@@ -705,6 +705,18 @@ def test_attend_refusals():
     torch.cuda.synchronize()
 
 
+def test_a_cap_without_a_reciprocal_is_refused():
+    pool = R.make_pool(1, 2, 64, 16, 32)
+    c = R.add_ctx(pool, 20, 1)
+    q = R.rand((1, 4, 64), 1)
+    lse, mass = torch.zeros(1, 4, device="cuda"), torch.zeros(1, 20, device="cuda")
+    for cap in (1e-40, 1e-45):
+        assert pool.attend(0, [c.handle], None, q, softcap=cap)[0] == B.AAF_ERR_INVALID_ARG
+        assert pool.attn_mass(0, [c.handle], None, q, lse, mass, softcap=cap)[0] == B.AAF_ERR_INVALID_ARG
+    out, _ = run_attend(pool, [c], [1], q, softcap=1e-37)  # every key alike
+    assert torch.isfinite(out).all()
+
+
 def test_store_refusals():
     pool = R.make_pool(2, 2, 64, 16, 32)
     c = R.add_ctx(pool, 20, 1)
