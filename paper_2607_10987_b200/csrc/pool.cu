@@ -15,6 +15,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <new>
 #include <vector>
 
@@ -154,7 +155,6 @@ struct aaf_kv_pool {
     unsigned long long read_id = 0, copy_id = 0;  // streams of the last reader and of the last copy launch
     PoolMap map;               // tensor map of the pool memory (wide attention kernel)
     bool map_ok = false;
-    int epoch = 0;             // counts calls of the wide kernel
     // pinned argument ring
     char *args = nullptr;
     size_t slot_bytes = 0;
@@ -1293,6 +1293,12 @@ constexpr long long SHARED_MIN = 16ll << 20;
 
 size_t attend_ws_bytes(const aaf_kv_pool *p) { return (size_t)PART_ROWS * ((size_t)p->g.D + 2) * sizeof(float) + 16; }
 
+// Number of a call of the wide kernel, over all pools: a workspace that another pool has used holds no number to come.
+int next_epoch() {
+    static std::atomic<unsigned> calls{0};
+    return (int)(calls.fetch_add(1, std::memory_order_relaxed) % 0x7fffffffu) + 1;
+}
+
 bool dtype_ok(int dtype) { return dtype == AAF_DTYPE_BF16 || dtype == AAF_DTYPE_F16; }
 bool is_finite(float x) { return x - x == 0.0f; }
 int log2_of(int v) {
@@ -1577,7 +1583,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
         ok = place_records(p, many, small, &km.seqs, 2, st);
         if (wide) {
             km.flag = reinterpret_cast<int *>(k.part_ml + 2 * PART_ROWS);
-            km.epoch = p->epoch = p->epoch % 0x7fffffff + 1;
+            km.epoch = next_epoch();
             ok = ok && launch_attend_wide(km, small, f16, &p->map, layer, st) == cudaSuccess;
         } else {
             ok = ok && launch_attend_tile(km, small, f16, st) == cudaSuccess;

@@ -335,6 +335,28 @@ def test_strided_queries_and_same_bits_again():
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+def test_a_workspace_that_another_pool_has_used():
+    """The first call of a pool meets values that the 256-row kernel cannot keep apart and leaves its mark in the workspace:
+    the first call of the next pool with the same workspace does not take it for its own."""
+    dim, t, n_q = 64, 300, 90
+    q = R.rand((n_q, 4, dim), 6, scale=2.0)
+    pools, ctxs = [], []
+    for i in range(2):
+        pool = R.make_pool(1, 2, dim, 16, 64)
+        rows = R.rand((1, 2, t, 2, dim), 5 + i)
+        if i == 0:
+            rows[0, 1, t - 1, 0, 3] = math.inf
+        pools.append(pool)
+        ctxs.append(R.add_ctx(pool, t, 0, rows))
+    ws = torch.zeros(B.aaf_kv_attend_workspace_bytes(pools[0].h), dtype=torch.uint8, device="cuda")
+    fresh = R.make_pool(1, 2, dim, 16, 64)
+    want = run_attend(fresh, [R.add_ctx(fresh, t, 0, ctxs[1].rows)], [n_q], q)
+    for i in range(2):
+        pools[i]._attend_ws = ws
+        got = run_attend(pools[i], [ctxs[i]], [n_q], q)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_calls_on_two_streams_share_the_workspace():
     pool = R.make_pool(1, 8, 128, 16, 700)
     ctxs = [R.add_ctx(pool, 5000, 1), R.add_ctx(pool, 4100, 2)]
