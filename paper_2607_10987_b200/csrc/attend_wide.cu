@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], fabsf(s[i + 2 * k]), fabsf(s[i + 2 * k + 1]));
                 const float most = max3(max3(mx[0], fabsf(s[124]), fabsf(s[125])), max3(mx[1], fabsf(s[126]), fabsf(s[127])), max3(mx[2], mx[3], mx[3]));
-                small = __all_sync(0xffffffffu, most * k1 <= TANH_POLY_MAX) && capped.c[4] > 0.0f;  // false for a NaN
+                small = __all_sync(0xffffffffu, most * k1 <= TANH_POLY_MAX) && capped.c[4] > 0.0f && capped.c[4] < CUDART_INF_F;  // false for a NaN
             }
             if (MODE == 0 || small) {
                 times = c;

@@ -739,6 +739,16 @@ def test_a_cap_without_a_reciprocal_is_refused():
     assert torch.isfinite(out).all()
 
 
+def test_a_tiny_cap_over_many_rows():
+    """Scores of zero under a cap so small that powers of its reciprocal overflow: every visible key weighs the same."""
+    pool = R.make_pool(1, 2, 64, 16, 64)
+    c = R.add_ctx(pool, 300, 1)
+    q = torch.zeros(90, 4, 64, dtype=torch.bfloat16, device="cuda")
+    got = run_attend(pool, [c], [90], q, softcap=1e-37)
+    R.check_attend(got, R.attend_ref([c], [90], q), torch.bfloat16, 64, True)
+    assert pool.attend(0, [c.handle], [90], q, scale=3e38)[0] == B.AAF_ERR_INVALID_ARG  # scale * log2(e) is not finite
+
+
 def test_store_refusals():
     pool = R.make_pool(2, 2, 64, 16, 32)
     c = R.add_ctx(pool, 20, 1)
