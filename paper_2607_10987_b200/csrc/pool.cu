@@ -331,7 +331,11 @@ bool begin_read(aaf_kv_pool *p, const int *handles, int n, cudaStream_t st) {
         p->meta_drained = false;
     }
     if (!p->meta_drained) {
+        // another stream of this thread may be capturing, which a query would end unless it is allowed to pass
+        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+        cudaThreadExchangeStreamCaptureMode(&mode);
         const cudaError_t e = cudaEventQuery(p->meta_ev);
+        cudaThreadExchangeStreamCaptureMode(&mode);
         if (e == cudaSuccess) {
             p->meta_drained = true;
         } else {

@@ -804,6 +804,24 @@ def test_reserve_during_capture_is_refused():
     assert float(x) == 1 and pool.sync_status() == 0
 
 
+def test_calls_beside_a_capture_on_another_stream():
+    pool = R.make_pool(1, 2, 64, 16, 32)
+    c = R.add_ctx(pool, 20, 1)
+    q = R.rand((1, 4, 64), 1, scale=2.0)
+    out, lse = run_attend(pool, [c], [1], q)
+    want = out.clone()
+    x = torch.zeros(1, device="cuda")
+    other = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.add_(1.0)
+        with torch.cuda.stream(other):
+            st = pool.attend(0, [c.handle], None, q, out=out, lse=lse)[0]
+    graph.replay()
+    torch.cuda.synchronize()
+    assert st == 0 and float(x) == 1 and torch.equal(out, want) and pool.sync_status() == 0
+
+
 def test_an_unusable_pool_refuses():
     pool = R.make_pool(1, 2, 64, 16, 32)
     c = R.add_ctx(pool, 20, 1)
