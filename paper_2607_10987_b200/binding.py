@@ -432,7 +432,7 @@ class KVPool:
         st = t.stride()
         if st[2] != 1 or (heads > 1 and st[1] != d):
             raise ValueError(f"{name}: the heads of a token must be contiguous")
-        return st[0] if tokens > 1 else max(st[0], heads * d)
+        return st[0] if tokens > 1 else heads * d  # one token: whatever stride the tensor names is not used
 
     def _flat(self, t, dtype, n, name):
         if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device:

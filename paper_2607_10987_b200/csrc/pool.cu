@@ -266,8 +266,6 @@ struct PlanSlot {
     int buf;
 };
 
-// Before a planner: pick the next piece buffer and make the metadata stream wait until the copy launch
-// that last read that buffer has finished.
 // Before a kernel that writes the table rows of n handles: readers of those rows on the caller's stream come first.
 // (Reference counts and the ring are the metadata stream's own.)
 void after_readers(aaf_kv_pool *p, const int *handles, int n) {
@@ -275,8 +273,8 @@ void after_readers(aaf_kv_pool *p, const int *handles, int n) {
     bool read = false;
     for (int i = 0; i < n && !read; ++i) read = p->row_read[(size_t)handles[i]] != 0;
     if (!read) return;
-    cudaEventRecord(p->read_ev, p->read_stream);
-    cudaStreamWaitEvent(p->meta_stream, p->read_ev, 0);
+    if (cudaEventRecord(p->read_ev, p->read_stream) != cudaSuccess || cudaStreamWaitEvent(p->meta_stream, p->read_ev, 0) != cudaSuccess)
+        p->broken = true;
     p->read_pending = false;
     std::fill(p->row_read.begin(), p->row_read.end(), 0);
 }
@@ -293,6 +291,8 @@ bool after_readers_on(aaf_kv_pool *p, cudaStream_t st, unsigned long long id) {
     if (!p->read_id || id == p->read_id) return true;
     return cudaEventRecord(p->read_ev, p->read_stream) == cudaSuccess && cudaStreamWaitEvent(st, p->read_ev, 0) == cudaSuccess;
 }
+// Before a planner: pick the next piece buffer and make the metadata stream wait until the copy launch
+// that last read that buffer has finished.
 PlanSlot begin_plan(aaf_kv_pool *p) {
     PlanSlot ps;
     ps.buf = p->next_buf;
@@ -1673,6 +1673,7 @@ int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int3
     if (p->broken) return AAF_ERR_CUDA;
     if (layer < 0 || layer >= p->g.L || !dtype_ok(d->dtype)) return AAF_ERR_INVALID_ARG;
     if (p->g.E != 2 || p->g.D % 8 != 0) return AAF_ERR_INCOMPAT;
+    if ((long long)std::max(d->n_q_heads, p->g.H) * p->g.D > (1ll << 30)) return AAF_ERR_INVALID_ARG;  // 32-bit places within a token
     if (!aligned16(d->k) || !aligned16(d->v) || d->n_q_heads < 0) return AAF_ERR_INVALID_ARG;
     if (d->n_q_heads > 0 && (!aligned16(d->q) || !aligned16(d->q_out))) return AAF_ERR_INVALID_ARG;
     const long long kv_min = (long long)p->g.H * p->g.D, q_min = (long long)d->n_q_heads * p->g.D;

@@ -14,6 +14,7 @@ namespace aafkv {
 constexpr int STORE_THREADS = 256;
 constexpr int STORE_ANGLES = 2048;  // (token, frequency) pairs of a CTA
 constexpr int STORE_AHEAD = 4;
+constexpr int STORE_TOKENS = 8;     // tokens of a CTA at most
 
 template <typename T> __device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -31,7 +32,7 @@ template <typename T>
 __global__ void __launch_bounds__(STORE_THREADS)
     store_kernel(const __grid_constant__ StoreParams p, const __grid_constant__ SmallStores small, int tokens) {
     __shared__ float2 turn[STORE_ANGLES];
-    __shared__ char *slot_of[64];
+    __shared__ char *slot_of[STORE_TOKENS];
     const StoreSeq *seqs = p.seqs ? p.seqs : small.e;
     const int t0 = blockIdx.x * tokens, cnt = min(tokens, p.total - t0);
     const int half = p.rot / 2;
@@ -74,9 +75,11 @@ __global__ void __launch_bounds__(STORE_THREADS)
     auto copy_heads = [&](const T *src, long long src_stride, int heads, int which) {
         const bool rotate = which < 2 && p.rot > 0;
         const int units = rotate ? (paired ? pieces - turned : pieces) : pieces;
-        const unsigned per_unit = 0xffffffffu / (unsigned)units + 1;  // i / units = high word of i * per_unit
+        // i / units = high word of i * per_unit, exact while i * units < 2^32
+        const unsigned per_unit = 0xffffffffu / (unsigned)units + 1;
+        const bool by_word = units > 1 && (long long)heads * units * units < 1ll << 32;
         for (int i = threadIdx.x; i < heads * units; i += STORE_THREADS) {  // the same unit of all the CTA's tokens
-            const int h = units == 1 ? i : (int)__umulhi((unsigned)i, per_unit), u = i - h * units;
+            const int h = by_word ? (int)__umulhi((unsigned)i, per_unit) : i / units, u = i - h * units;
             const int d = (rotate && paired && u >= turned ? u + turned : u) * 8;
             const bool two = rotate && paired && u < turned;
             const T *s = src + t0 * src_stride + (long long)h * p.D;
@@ -145,8 +148,8 @@ __global__ void __launch_bounds__(STORE_THREADS)
 }
 
 cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16, cudaStream_t st) {
-    // tokens of a CTA: enough CTAs for every SM while there are few tokens, at most 64 and the angle table's room
-    int tokens = max(1, min(8, p.total / 1184));
+    // tokens of a CTA: enough CTAs for every SM while there are few tokens, at most 8 and the angle table's room
+    int tokens = max(1, min(STORE_TOKENS, p.total / 1184));
     if (p.rot) tokens = max(1, min(tokens, STORE_ANGLES / (p.rot / 2)));
     const unsigned grid = (unsigned)((p.total + tokens - 1) / tokens);
     if (f16)

@@ -457,6 +457,30 @@ def test_store_rotates_and_writes_only_its_slots(dim, rot, inter, dtype):
     assert torch.equal(fk, k) and torch.equal(fv, v)
 
 
+def test_store_odd_shapes_of_tokens():
+    """Wide heads, many of them, and a single token whose stride is never used."""
+    pool = R.make_pool(1, 2, 1032, 8, 16, fill=0.0)
+    c = R.add_ctx(pool, 9, 1)
+    q, k, v = R.rand((1, 700, 1032), 2), R.rand((1, 2, 1032), 3), R.rand((1, 2, 1032), 4)
+    inv = 10000.0 ** (-torch.arange(0, 512, dtype=torch.float64, device="cuda") / 512)
+    odd = torch.as_strided(k, (1, 2, 1032), (13, 1032, 1))
+    out = torch.empty_like(q)
+    assert pool.store(0, [c.handle], [1], odd, v, q=q, q_out=out, rope=B.Rope(1024, inv))[0] == 0
+    torch.cuda.synchronize()
+    pos = torch.tensor([8], device="cuda")
+    slot = pool.mem[0, pool.table(c.handle).tolist()[1], :, 0]
+    slack = (math.pi * 2.0 ** -24 + 2.0 ** -22 + 2.0 ** -23) * 2  # as in the test above
+    for got, x in ((out[0], q), (slot[0], k)):
+        ref = R.rotate_ref(x, pos, inv, 1024, False, 1.0)[0]
+        lim = 2.0 ** -8 * ref.abs() + slack * x.double().abs().amax() * (1 + 2.0 ** -8)
+        assert ((got.double() - ref).abs() <= lim).all()
+    assert torch.equal(slot[1], v[0])
+    d = B.aaf_kv_store_desc(C.sizeof(B.aaf_kv_store_desc), 0, 2 ** 28, 0, 0, 1.0, None, None, q.data_ptr(), q.data_ptr(), k.data_ptr(),
+                            v.data_ptr(), 2 ** 40, 2 ** 40, 2064, 2064)
+    h, one = (C.c_int32 * 1)(c.handle), (C.c_int32 * 1)(1)
+    assert B.aaf_kv_store(pool.h, 0, d, 1, h, one, None) == B.AAF_ERR_INVALID_ARG
+
+
 def test_store_many_sequences_and_long_prefill():
     pool = R.make_pool(1, 2, 64, 16, 700, max_ctx=80)
     n = 70
