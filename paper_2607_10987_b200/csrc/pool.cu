@@ -1673,7 +1673,10 @@ int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int3
     if (p->broken) return AAF_ERR_CUDA;
     if (layer < 0 || layer >= p->g.L || !dtype_ok(d->dtype)) return AAF_ERR_INVALID_ARG;
     if (p->g.E != 2 || p->g.D % 8 != 0) return AAF_ERR_INCOMPAT;
-    if ((long long)std::max(d->n_q_heads, p->g.H) * p->g.D > (1ll << 30)) return AAF_ERR_INVALID_ARG;  // 32-bit places within a token
+    // the kernel's 32-bit places within a token (H * D) and its division of them (H * (D / 8)^2)
+    if ((long long)std::max(d->n_q_heads, p->g.H) * p->g.D > 1ll << 30 ||
+        (double)std::max(d->n_q_heads, p->g.H) * (p->g.D / 8) * (p->g.D / 8) >= 4294967296.0)
+        return AAF_ERR_INVALID_ARG;
     if (!aligned16(d->k) || !aligned16(d->v) || d->n_q_heads < 0) return AAF_ERR_INVALID_ARG;
     if (d->n_q_heads > 0 && (!aligned16(d->q) || !aligned16(d->q_out))) return AAF_ERR_INVALID_ARG;
     const long long kv_min = (long long)p->g.H * p->g.D, q_min = (long long)d->n_q_heads * p->g.D;

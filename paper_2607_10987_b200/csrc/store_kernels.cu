@@ -75,11 +75,9 @@ __global__ void __launch_bounds__(STORE_THREADS)
     auto copy_heads = [&](const T *src, long long src_stride, int heads, int which) {
         const bool rotate = which < 2 && p.rot > 0;
         const int units = rotate ? (paired ? pieces - turned : pieces) : pieces;
-        // i / units = high word of i * per_unit, exact while i * units < 2^32
-        const unsigned per_unit = 0xffffffffu / (unsigned)units + 1;
-        const bool by_word = units > 1 && (long long)heads * units * units < 1ll << 32;
+        const unsigned per_unit = 0xffffffffu / (unsigned)units + 1;  // i / units = high word of i * per_unit while i * units < 2^32
         for (int i = threadIdx.x; i < heads * units; i += STORE_THREADS) {  // the same unit of all the CTA's tokens
-            const int h = by_word ? (int)__umulhi((unsigned)i, per_unit) : i / units, u = i - h * units;
+            const int h = units == 1 ? i : (int)__umulhi((unsigned)i, per_unit), u = i - h * units;
             const int d = (rotate && paired && u >= turned ? u + turned : u) * 8;
             const bool two = rotate && paired && u < turned;
             const T *s = src + t0 * src_stride + (long long)h * p.D;
