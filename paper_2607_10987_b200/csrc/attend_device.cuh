@@ -33,6 +33,12 @@ template <> struct Elt<__nv_bfloat16> {
     static __device__ __forceinline__ float from(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
     static __device__ __forceinline__ uint16_t to(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
     static constexpr uint32_t EXP = 0x7f807f80u, ONE = 0x3f80u;
+    // magnitudes of at most the type's largest finite value, signs kept
+    static __device__ __forceinline__ uint32_t bounded(uint32_t v) {
+        uint32_t r;
+        asm("min.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0x7f7f7f7fu));
+        return r;
+    }
     static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                                uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
@@ -52,6 +58,12 @@ template <> struct Elt<__half> {
     static __device__ __forceinline__ float from(uint16_t v) { return __half2float(__ushort_as_half(v)); }
     static __device__ __forceinline__ uint16_t to(float v) { return __half_as_ushort(__float2half_rn(v)); }
     static constexpr uint32_t EXP = 0x7c007c00u, ONE = 0x3c00u;
+    // magnitudes of at most the type's largest finite value, signs kept
+    static __device__ __forceinline__ uint32_t bounded(uint32_t v) {
+        uint32_t r;
+        asm("min.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0x7bff7bffu));
+        return r;
+    }
     static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                                uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "

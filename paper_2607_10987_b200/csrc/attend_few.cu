@@ -30,43 +30,6 @@ template <int DP> struct FewShape {
     static_assert(2 * (SMEM + 1024) <= 228 * 1024, "shared memory of a CTA");
 };
 
-// An infinite value times one part of its weight is infinite, times the other NaN (the low part may be zero or negative).
-// So a warp that ends with a NaN looks through its values once more: where the row's weights are numbers, what the row sees
-// decides between infinite and NaN.  Everything it needs is read again, the kernel keeps nothing for it.
-template <typename T>
-__device__ __noinline__ void mend_infinite(const AttnParams &p, const AttnSeq *record, int part, int head, int beg, int end, const float *sums) {
-    __syncwarp();  // the rows are written, and their sums
-    const AttnSeq sq = *record;
-    const int R = sq.nq * p.G;
-    const int *table = p.tables + (long long)sq.ctx * p.max_blk;
-    const char *vb = p.kbase + p.run + (long long)head * p.D * 2;
-    for (int d = threadIdx.x & 31; d < p.D; d += 32) {
-        uint32_t up = 0, down = 0;  // rows that see +inf or NaN, -inf or NaN
-        for (int t = beg; t < end; ++t) {
-            const int b = block_of(t, p.BS, p.bs_shift);
-            const float x = Elt<T>::from(*reinterpret_cast<const uint16_t *>(vb + (long long)table[b] * 2 * p.run + (long long)(t - b * p.BS) * p.row + d * 2));
-            if (fabsf(x) < CUDART_INF_F) continue;
-            for (int r = 0; r < R; ++r) {
-                const RowSpan sp = row_span(p, sq, r / p.G);
-                if (t < sp.lo || t >= sp.hi) continue;
-                if (!(x < 0.0f)) up |= 1u << r;
-                if (!(x > 0.0f)) down |= 1u << r;
-            }
-        }
-        for (int r = 0; r < R; ++r) {
-            const float x = nonfinite_of(up >> r & 1 ? 1.0f : 0.0f, down >> r & 1 ? 1.0f : 0.0f);
-            if (x == 0.0f || !(sums[r] > 0.0f)) continue;
-            if (sq.part0 >= 0) {
-                float *o = p.part_o + (sq.part0 + ((long long)part * p.H + head) * R + r) * p.D + d;
-                if (*o != *o) *o = x;
-            } else {
-                uint16_t *o = static_cast<uint16_t *>(p.out) + ((long long)(sq.row0 + r / p.G) * p.H * p.G + head * p.G + r % p.G) * p.D + d;
-                if (Elt<T>::from(*o) != Elt<T>::from(*o)) *o = Elt<T>::to(x);
-            }
-        }
-    }
-}
-
 // SIMPLE: one query token a sequence, no cap, bias or spans: every row sees every key of its part, a score is a multiple of the
 // product.  Two in five instructions of a tile go into the general case (486 at 128 dims).
 template <typename T, int DP, int NT, bool SIMPLE>
@@ -81,8 +44,7 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
     const int unit = (int)(task / p.H), head = (int)(task - (long long)unit * p.H);
     asm volatile("griddepcontrol.launch_dependents;");  // the join may be brought up beside this kernel
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
-    const AttnSeq *record = seqs + find_seq(seqs, p.n, unit);
-    const AttnSeq sq = *record;
+    const AttnSeq sq = seqs[find_seq(seqs, p.n, unit)];
     const int part = unit - sq.unit0;
     const int R = sq.nq * p.G;
 
@@ -287,10 +249,15 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
                         for (int i = 0; i < 4; ++i) a[i] = f[i];
                     }
                 }
+                // An infinite value times the high part of its weight is infinite; times the low part, which may be zero or
+                // negative, it would make a NaN of that: there it is the type's largest value.
+                uint32_t b[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[i] = Elt<T>::bounded(a[i]);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     Elt<T>::mma(o[nt][4 * c + j], a[0], a[1], a[2], a[3], ph[nt][0], ph[nt][1]);
-                    Elt<T>::mma(o[nt][4 * c + j], a[0], a[1], a[2], a[3], pl[nt][0], pl[nt][1]);
+                    Elt<T>::mma(o[nt][4 * c + j], b[0], b[1], b[2], b[3], pl[nt][0], pl[nt][1]);
                 }
             }
         }
@@ -300,14 +267,6 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
         id = nxt;
     }
     copy_wait<0>();
-    bool odd = false;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int i = 0; i < DP / 16; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) odd |= o[nt][i][k] != o[nt][i][k];
-    odd = __any_sync(0xffffffffu, odd);
 
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -318,7 +277,6 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
             for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
             const int r = nt * 8 + 2 * t4 + c;
             if (r >= R) continue;
-            if (odd && g == 0) reinterpret_cast<float *>(smem + warp * (S::STAGES * S::STAGE_BYTES))[r] = sum;
             if (sq.part0 >= 0) {  // a part of a longer range: (m, l, o) for the join
                 const float some = sum == 0.0f ? 0.0f : 1.0f;
                 const long long pr = sq.part0 + ((long long)part * p.H + head) * R + r;
@@ -358,7 +316,6 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
                     sum == 0.0f ? -CUDART_INF_F
                                 : (m[nt][c] + log2f(sum)) * LN2 - (SIMPLE ? 0.0f : slope[SIMPLE ? 0 : nt][c] * (float)span[SIMPLE ? 0 : nt][c].near);
         }
-    if (odd) mend_infinite<T>(p, record, part, head, beg, end, reinterpret_cast<float *>(smem + warp * (S::STAGES * S::STAGE_BYTES)));
     asm volatile("griddepcontrol.wait;" ::: "memory");  // what it ran beside is done before it is
 }
 
