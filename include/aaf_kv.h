@@ -331,9 +331,9 @@ int aaf_kv_reserve(aaf_kv_pool *pool, int32_t n, const aaf_ctx_t *ctxs, const in
  * pairs being (i, i + rot_dim / 2), or (2i, 2i + 1) with `interleaved`.  The angle is taken in 64 bits, the results are
  * rounded once.  The position of a token is its index in the context, or pos[token] if pos is given (a pruned context,
  * a context that starts elsewhere).  k, v, q, q_out: heads contiguous, *_stride elements from token to token (multiples
- * of 8; views into a fused projection are fine).  Only slots that no other context can share are written: a call that
- * reaches back before the tokens added since the context was last forked or merged by reference is AAF_ERR_INVALID_ARG,
- * and so is a context listed twice. */
+ * of 8; views into a fused projection are fine; heads * (head_dim / 8)^2 below 2^32).  Only slots that no other context
+ * can share are written: a call that reaches back before the tokens added since the context was last forked or merged by
+ * reference is AAF_ERR_INVALID_ARG, and so is a context listed twice. */
 typedef struct aaf_kv_store_desc {
     uint32_t struct_size;   /* sizeof(aaf_kv_store_desc)                                     */
     int32_t dtype;          /* AAF_DTYPE_*                                                   */
