@@ -10,8 +10,8 @@ namespace aafkv {
 // cosine are computed once per (token, frequency) into shared memory and used by all heads; results are rounded to the
 // payload's type once.  Bound: bytes (q read and written, k and v read and written).  A thread handles units of 16 bytes, or
 // two of them where the halves of pairs lie apart, the same unit of two tokens at a time: the loads are under way together and the
-// place of a unit is worked out once.  Rows are fetched to L2 while the angles are computed.  201 MB moved in 44.7 us (4.5 TB/s;
-// 53.3 without that and with eight tokens a CTA, four at a time).
+// place of a unit is worked out once.  Rows are fetched to L2 while the angles are computed.  201 MB moved in 41 us (4.9 TB/s;
+// 44.7 with a prefetch for each line instead of each row, 53.3 with none and eight tokens a CTA, four at a time).
 constexpr int STORE_THREADS = 256;
 constexpr int STORE_ANGLES = 2048;  // (token, frequency) pairs of a CTA
 constexpr int STORE_AHEAD = 2;
@@ -46,16 +46,14 @@ __global__ void __launch_bounds__(STORE_THREADS)
         return lo;
     };
     // the CTA's rows are on their way to L2 while the angles are computed
-    auto ahead = [&](const void *src, long long stride, int heads) {
-        const int lines = (heads * p.D * 2 + 127) / 128;
-        for (int i = threadIdx.x; i < cnt * lines; i += STORE_THREADS) {
-            const int tl = i / lines;
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char *>(src) + (t0 + tl) * stride * 2 + (long long)(i - tl * lines) * 128));
-        }
+    auto ahead = [&](const void *src, long long stride, int heads, int tl) {
+        if (tl >= 0 && tl < cnt)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const char *>(src) + (t0 + tl) * stride * 2),
+                         "r"((uint32_t)(heads * p.D * 2)) : "memory");
     };
-    if (p.q) ahead(p.q, p.q_stride, p.Hq);
-    ahead(p.k, p.k_stride, p.H);
-    ahead(p.v, p.v_stride, p.H);
+    if (p.q) ahead(p.q, p.q_stride, p.Hq, (int)threadIdx.x - 32);
+    ahead(p.k, p.k_stride, p.H, (int)threadIdx.x - 64);
+    ahead(p.v, p.v_stride, p.H, (int)threadIdx.x - 96);
     if (threadIdx.x < cnt) {
         const int tok = t0 + threadIdx.x;
         const StoreSeq s = seqs[seq_of(tok)];
@@ -158,7 +156,7 @@ __global__ void __launch_bounds__(STORE_THREADS)
 }
 
 cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16, cudaStream_t st) {
-    // tokens of a CTA: enough CTAs for every SM while there are few tokens, at most 4 (45 us at 4, 47 at 2, 49 at 8 and 16) and the angle table's room
+    // tokens of a CTA: enough CTAs for every SM while there are few tokens, at most 4 (41 us; 44 at 6 and 8) and the angle table's room
     int tokens = max(1, min(STORE_TOKENS, p.total / 1184));
     if (p.rot) tokens = max(1, min(tokens, STORE_ANGLES / (p.rot / 2)));
     const unsigned grid = (unsigned)((p.total + tokens - 1) / tokens);
