@@ -5,8 +5,10 @@
 // (row block by row block, head by head, eight rows at a time): no atomics, the same bits every time.  Bound: the bytes of
 // K while there are few rows, the exponentials' surroundings (masks, sums) from about a hundred rows on.  Keys come through
 // the block table into stages of the warp's own, two heads ahead; the queries of as many heads as fit (64 rows) are shared by the
-// CTA's four warps.  CTAs are small, four an SM: while one waits for its first keys or its next queries, the others work.  Products as in attend_few.cu: tokens
-// as the M side, eight query rows as the N side.
+// CTA's four warps.  CTAs are small, three or four an SM: while one waits for its first keys or its next queries, the others
+// work.  111 MB of keys, one token a context, four rows a head: 30 us (3.7 TB/s; 31.7 with two stages, 35.7 with four, when
+// fewer CTAs fit; 32 with the rows fetched to L2 ahead).  Products as in attend_few.cu: tokens as the M side, eight query
+// rows as the N side.
 #include <type_traits>
 
 #include "attend_device.cuh"
@@ -18,7 +20,7 @@ static_assert(MASS_WARPS * MASS_TOKENS == MASS_CHUNK, "tokens of a CTA");
 
 template <int DP> struct MassShape {
     static constexpr int ROW = DP * 2, PIECES = DP / 8, ROWS = DP <= 128 ? 64 : 32;  // rows of a batch of queries
-    static constexpr int TILE_BYTES = MASS_TOKENS * ROW, STAGES = 2;
+    static constexpr int TILE_BYTES = MASS_TOKENS * ROW, STAGES = 3;
     static constexpr int K_BYTES = MASS_WARPS * STAGES * TILE_BYTES;
 };
 struct MassRow {  // what a query row of any head sees
