@@ -1674,7 +1674,7 @@ int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int3
     if (layer < 0 || layer >= p->g.L || !dtype_ok(d->dtype)) return AAF_ERR_INVALID_ARG;
     if (p->g.E != 2 || p->g.D % 8 != 0) return AAF_ERR_INCOMPAT;
     // the kernel's 32-bit places within a token (H * D) and its division of them (H * (D / 8)^2)
-    if ((long long)std::max(d->n_q_heads, p->g.H) * p->g.D > 1ll << 30 ||
+    if ((long long)std::max(d->n_q_heads, p->g.H) * p->g.D >= 1ll << 30 ||
         (double)std::max(d->n_q_heads, p->g.H) * (p->g.D / 8) * (p->g.D / 8) >= 4294967296.0)
         return AAF_ERR_INVALID_ARG;
     if (!aligned16(d->k) || !aligned16(d->v) || d->n_q_heads < 0) return AAF_ERR_INVALID_ARG;
