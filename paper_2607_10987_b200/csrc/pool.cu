@@ -1632,8 +1632,9 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
     k.mass_stride = mass_stride;
     int max_rows = 1;
     for (int i = 0; i < n; ++i) max_rows = std::max(max_rows, (n_q ? n_q[i] : 1) * k.a.G);
-    // Many query rows go to the tensor cores (up to 16 rows the bytes of the keys decide either way, and the kernel that
-    // streams them has less to set up; 32763 tokens, 128 rows: 76 us there, 29 here).
+    // Many query rows go to the tensor cores; up to 16 rows the bytes of the keys decide either way, and the kernel that
+    // streams them has less to set up.  16 contexts of 3300 tokens, streamed and on the tensor cores: 4 rows 35 and 41 us, 16 rows
+    // 39 and 41, 20 rows 50 and 41, 64 rows 72 and 41; one context of 32763 tokens: 4 rows 29 and 27, 20 rows 45 and 25.
     const bool wide = p->map_ok && max_rows > 16;
     const int chunk = wide ? MASS_WIDE_CHUNK : MASS_CHUNK;
     k.a.status = &p->s.ctl->status;
