@@ -301,10 +301,14 @@ PlanSlot begin_plan(aaf_kv_pool *p) {
     cudaStreamWaitEvent(p->meta_stream, p->copy_done[ps.buf], 0);
     return ps;
 }
-// After the planner: the caller's stream (where the copy runs) waits for it.
+// After the planner: the caller's stream (where the copy runs) waits for it, and for the pool's payload work on other streams.
+// A call that turns out to copy nothing waits all the same: end_copy makes its stream the one that later calls are ordered by.
 bool end_plan(aaf_kv_pool *p, const PlanSlot &ps, cudaStream_t st) {
-    return cudaEventRecord(p->plan_done[ps.buf], p->meta_stream) == cudaSuccess &&
-           cudaStreamWaitEvent(st, p->plan_done[ps.buf], 0) == cudaSuccess;
+    if (cudaEventRecord(p->plan_done[ps.buf], p->meta_stream) != cudaSuccess ||
+        cudaStreamWaitEvent(st, p->plan_done[ps.buf], 0) != cudaSuccess)
+        return false;
+    if (!after_readers_on(p, st, stream_id(st))) return false;
+    return !p->last_copy_event || st == p->last_copy_stream || cudaStreamWaitEvent(st, p->last_copy_event, 0) == cudaSuccess;
 }
 // After the operator's last copy launch: mark the buffer's readers done and switch buffers.
 void end_copy(aaf_kv_pool *p, const PlanSlot &ps, cudaStream_t st) {
@@ -362,11 +366,6 @@ int run_copy(aaf_kv_pool *p, const PlanSlot &ps, int cls, int n_slots, long long
     view.pieces += piece0;  // a launch may cover a sub-range of the planned pieces (chunked transfers)
     const long long avg_piece = n_slots > 0 ? payload_tokens * p->g.row / n_slots : 0;
     if (n_slots <= 0) return AAF_OK;
-    if (!after_readers_on(p, st, stream_id(st))) return broke(p);
-    if (p->last_copy_event && st != p->last_copy_stream) {  // a different stream: serialise behind the last copy launch
-        if (cudaStreamWaitEvent(st, p->last_copy_event, 0) != cudaSuccess) return broke(p);
-        p->last_copy_stream = st;  // the wait is queued; later launches of this operator need not repeat it
-    }
     TimedLaunch t{};
     if (p->timing) {
         t.start = get_event(p);

@@ -1,0 +1,183 @@
+"""Order of a pool's work across streams, on the CPU: the library's host side (pool.cu) runs on a model of the CUDA runtime
+(order_model.cpp) that computes nothing and remembers for every launch what had to be over before it."""
+from __future__ import annotations
+
+import ctypes as C
+import os
+import subprocess
+
+import pytest
+
+from paper_2607_10987_b200 import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2607_10987_b200", "csrc")
+CUDA = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+L, H, D, BS, NB, CTX, BLK = 1, 2, 64, 16, 4096, 32, 2048
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    out = str(tmp_path_factory.mktemp("order") / "liborder.so")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-Wl,-Bsymbolic", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+                           "-I", os.path.join(CUDA, "include"), "-x", "c++", os.path.join(CSRC, "pool.cu"),
+                           os.path.join(ROOT, "tests", "order_model.cpp"), "-o", out])
+    lib = C.CDLL(out)
+    for name, (res, args) in B.SYMBOLS.items():
+        if hasattr(lib, name):
+            f = getattr(lib, name)
+            f.restype, f.argtypes = res, args
+    for name in ("order_stream", "order_replace_stream", "order_where"):
+        getattr(lib, name).restype = C.c_void_p
+    for name in ("order_name", "order_wrong"):
+        getattr(lib, name).restype = C.c_char_p
+    lib.order_replace_stream.argtypes = [C.c_void_p, C.c_int]
+    lib.order_capture.argtypes = [C.c_void_p, C.c_int]
+    lib.order_fail.argtypes = [C.c_char_p, C.c_int]
+    return lib
+
+
+class Pool:
+    """A pool on the model.  Calls take the stream first and return the names and numbers of what they launched."""
+
+    def __init__(self, lib):
+        self.lib = lib
+        lib.order_reset()
+        self.mem = (C.c_char * 4096)()
+        base = (C.addressof(self.mem) + 1023) // 1024 * 1024  # nothing is read or written through it
+        d = B.make_desc(L, H, D, BS, 2, NB, CTX, BLK, 0, 0, 0, 0)
+        size = lib.aaf_kv_pool_workspace_bytes(C.byref(d))
+        self.ws = (C.c_char * (size + 256))()
+        d.pool_base, d.layer_stride_bytes = base, NB * 2 * BS * H * D * 2
+        d.workspace, d.workspace_bytes = (C.addressof(self.ws) + 255) // 256 * 256, size
+        self.desc, self.base, self.h = d, base, C.c_void_p()
+        assert lib.aaf_kv_pool_create(C.byref(d), C.byref(self.h)) == 0
+        self.status = 0
+
+    def close(self):
+        self.lib.aaf_kv_pool_destroy(self.h)
+
+    def _ran(self, first, status, want):
+        self.status = status
+        if want is not None:
+            assert status == want, status
+        return {self.lib.order_name(i).decode(): i for i in range(first, self.lib.order_ops())}
+
+    def call(self, name, *args, want=0):
+        first = self.lib.order_ops()
+        return self._ran(first, getattr(self.lib, "aaf_kv_" + name)(self.h, *args), want)
+
+    def ints(self, v):
+        return (C.c_int32 * len(v))(*v)
+
+    def imp(self, st, tokens, want=0):
+        x = B.aaf_kv_xfer_desc()
+        x.n_layers, x.n_kv_heads, x.head_dim, x.elt_bytes, x.n_tokens = L, H, D, 2, tokens
+        out = C.c_int32(-1)
+        ran = self.call("import", self.base, C.byref(x), C.byref(out), st, want=want)
+        return ran, out.value
+
+    def reserve(self, st, ctxs, n_new, want=0):
+        return self.call("reserve", len(ctxs), self.ints(ctxs), self.ints(n_new), st, want=want)
+
+    def append(self, st, ctxs, n_new, want=0):
+        src = (C.c_void_p * len(ctxs))(*[self.base] * len(ctxs))
+        return self.call("append", len(ctxs), self.ints(ctxs), self.ints(n_new), src, st, want=want)
+
+    def fork(self, st, ctx, k=1, want=0):
+        out = (C.c_int32 * k)()
+        ran = self.call("fork", ctx, k, out, st, want=want)
+        return ran, list(out)
+
+    def compose(self, st, ctxs, want=0):
+        out = C.c_int32(-1)
+        ran = self.call("compose", len(ctxs), self.ints(ctxs), B.AAF_COMPOSE_SHARE, C.byref(out), st, want=want)
+        return ran, out.value
+
+    def evict(self, st, ctxs, want=0):
+        return self.call("evict", len(ctxs), self.ints(ctxs), st, want=want)
+
+    def materialize(self, st, ctx, tokens, want=0):
+        return self.call("materialize", ctx, 0, tokens, self.base, 1 << 40, None, st, want=want)
+
+    def store(self, st, ctxs, n_new, want=0):
+        d = B.aaf_kv_store_desc(C.sizeof(B.aaf_kv_store_desc), 0, 0, 0, 0, 1.0, None, None, None, None, self.base, self.base, 0, 0, H * D, H * D)
+        return self.call("store", 0, C.byref(d), len(ctxs), self.ints(ctxs), self.ints(n_new), st, want=want)
+
+    def _attn(self):
+        return B.aaf_kv_attn(C.sizeof(B.aaf_kv_attn), 0, H, 0, 0.1, 0.0, None, None, H * D)
+
+    def attend(self, st, ctxs, n_q=None, want=0):
+        return self.call("attend", 0, C.byref(self._attn()), len(ctxs), self.ints(ctxs), None if n_q is None else self.ints(n_q), self.base,
+                         self.base, None, self.base, 1 << 40, st, want=want)
+
+    def mass(self, st, ctxs, want=0):
+        return self.call("attn_mass", 0, C.byref(self._attn()), len(ctxs), self.ints(ctxs), None, self.base, self.base, None, self.base, 1 << 20, st,
+                         want=want)
+
+    def prune(self, st, ctx, budget, want=0):
+        out = C.c_int32(-1)
+        ran = self.call("prune", ctx, self.base, budget, 0, 0, self.base, None, C.byref(out), st, want=want)
+        return ran, out.value
+
+    def before(self, a, b):
+        return bool(self.lib.order_before(a, b))
+
+    def wrongs(self):
+        return [self.lib.order_wrong(i).decode() for i in range(self.lib.order_wrongs())]
+
+
+@pytest.fixture
+def pool(lib):
+    p = Pool(lib)
+    yield p
+    p.close()
+
+
+READERS = {"attend": lambda p, s, c: p.attend(s, [c])["attend"], "store": lambda p, s, c: p.store(s, [c], [1])["store"],
+           "mass": lambda p, s, c: p.mass(s, [c])["mass"], "prune": lambda p, s, c: p.prune(s, c, 5)[0]["gather"],
+           "materialize": lambda p, s, c: p.materialize(s, c, 5)["copy"]}
+
+
+@pytest.mark.parametrize("reader", READERS)
+def test_a_reserve_that_copies_nothing_keeps_the_order_behind_an_import(lib, pool, reader):
+    a, b = lib.order_stream(), lib.order_stream()
+    ran, c = pool.imp(a, 160)
+    assert "copy" not in pool.reserve(b, [c], [16])
+    assert pool.before(ran["copy"], READERS[reader](pool, b, c))
+
+
+@pytest.mark.parametrize("reader", READERS)
+def test_a_merge_of_whole_blocks_keeps_the_order_behind_an_import(lib, pool, reader):
+    a, b = lib.order_stream(), lib.order_stream()
+    ran, c = pool.imp(a, 160)
+    merged, m = pool.compose(b, [c, c])
+    assert "copy" not in merged
+    if reader == "store":  # a store takes slots of its own
+        pool.reserve(b, [m], [1])
+    assert pool.before(ran["copy"], READERS[reader](pool, b, m))
+
+
+@pytest.mark.parametrize("calls", [1, 2, 3])
+def test_calls_that_copy_nothing_keep_the_order_of_all_work_before_them(lib, pool, calls):
+    a, b, d = lib.order_stream(), lib.order_stream(), lib.order_stream()
+    ran, c = pool.imp(a, 160)
+    stored = pool.store(a, [c], [1])["store"]
+    for _ in range(calls):  # the two piece buffers take turns
+        pool.reserve(b, [c], [16])
+    read = pool.attend(d, [c])["attend"]
+    assert pool.before(ran["copy"], read) and pool.before(stored, read)
+    copied = pool.append(d, [c], [5])["copy"]
+    assert pool.before(read, copied) and pool.before(stored, copied)
+
+
+def test_the_copies_of_a_pool_run_one_after_the_other(lib, pool):
+    st = [lib.order_stream() for _ in range(3)]
+    ran, c = pool.imp(st[0], 160)
+    copies = [ran["copy"]]
+    for i in range(1, 9):
+        pool.reserve(st[(i + 1) % 3], [c], [16])
+        copies.append(pool.materialize(st[i % 3], c, 20)["copy"])
+    for x, y in zip(copies, copies[1:]):
+        assert pool.before(x, y)
+    assert not pool.wrongs()
