@@ -311,7 +311,8 @@ int aaf_kv_import_host_chunked(aaf_kv_pool *pool, const void *src_host, const aa
  * queries of context i are its LAST n_q[i] tokens, so token j of them is at position p = length - n_q[i] + j.
  * All run on `stream`, behind the pool's earlier calls, and wait for nothing on the host.  They read host arrays and
  * order streams, which a replayed graph would not do again: during stream capture they return AAF_ERR_INVALID_ARG.
- * A stream that a call named stays valid until a later call of the pool on another stream, or its destruction, has returned.
+ * A stream that a call named stays valid until a later call of the pool on another stream has returned AAF_OK, or the pool has
+ * been destroyed; it may be captured meanwhile.
  * Catalog counters (reuse, last access) are stamped by reserve and prune, not by store, attend and attn_mass.
  * Device buffers must not overlap each other unless said so.  A context longer than 2^30 tokens: AAF_ERR_TOO_LONG. */
 #define AAF_DTYPE_BF16 0

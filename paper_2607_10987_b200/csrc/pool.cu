@@ -145,14 +145,14 @@ struct aaf_kv_pool {
     cudaEvent_t last_copy_event = nullptr;
     // Kernels that compute with the pool (attention, stores, gathers of a prune) read block tables on the caller's
     // stream: they wait for the metadata launched so far, and the next kernel that changes metadata waits for them.  Streams
-    // are told apart by their ids, which are never reused.  read_ev is recorded when someone has to wait.
+    // are told apart by their ids, which are never reused.  read_ev is recorded by each such call itself, while its stream is
+    // there and not being captured: who has to wait later has no other use for that stream.
     cudaEvent_t meta_ev = nullptr, read_ev = nullptr;
     long long meta_mark = -1;  // meta_launches when meta_ev was recorded
     bool meta_drained = false; // meta_ev has been seen complete
-    bool read_pending = false; // work on read_stream that the metadata stream has not been ordered behind,
-    std::vector<char> row_read; // and the handles whose table rows it may read
-    cudaStream_t read_stream = nullptr;
-    unsigned long long read_id = 0, copy_id = 0;  // streams of the last reader and of the last copy launch
+    bool read_pending = false; // readers that the metadata stream has not been ordered behind,
+    std::vector<char> row_read; // and the handles whose table rows they may read
+    unsigned long long read_id = 0, copy_id = 0;  // streams that are ordered behind the last reader and the last copy launch
     PoolMap map;               // tensor map of the pool memory (wide attention kernel)
     bool map_ok = false;
     // pinned argument ring
@@ -273,8 +273,7 @@ void after_readers(aaf_kv_pool *p, const int *handles, int n) {
     bool read = false;
     for (int i = 0; i < n && !read; ++i) read = p->row_read[(size_t)handles[i]] != 0;
     if (!read) return;
-    if (cudaEventRecord(p->read_ev, p->read_stream) != cudaSuccess || cudaStreamWaitEvent(p->meta_stream, p->read_ev, 0) != cudaSuccess)
-        p->broken = true;
+    if (cudaStreamWaitEvent(p->meta_stream, p->read_ev, 0) != cudaSuccess) p->broken = true;
     p->read_pending = false;
     std::fill(p->row_read.begin(), p->row_read.end(), 0);
 }
@@ -289,7 +288,9 @@ unsigned long long stream_id(cudaStream_t st) {
 // Before payload work on `st`: readers on another stream come first.
 bool after_readers_on(aaf_kv_pool *p, cudaStream_t st, unsigned long long id) {
     if (!p->read_id || id == p->read_id) return true;
-    return cudaEventRecord(p->read_ev, p->read_stream) == cudaSuccess && cudaStreamWaitEvent(st, p->read_ev, 0) == cudaSuccess;
+    if (cudaStreamWaitEvent(st, p->read_ev, 0) != cudaSuccess) return false;
+    p->read_id = id;
+    return true;
 }
 // Before a planner: pick the next piece buffer and make the metadata stream wait until the copy launch
 // that last read that buffer has finished.
@@ -326,7 +327,6 @@ bool begin_read(aaf_kv_pool *p, const int *handles, int n, cudaStream_t st) {
     if (!after_readers_on(p, st, id)) return false;
     if (p->last_copy_event && id != p->copy_id && cudaStreamWaitEvent(st, p->last_copy_event, 0) != cudaSuccess) return false;
     p->read_id = id;
-    p->read_stream = st;
     p->read_pending = true;
     for (int i = 0; i < n; ++i) p->row_read[(size_t)handles[i]] = 1;
     if (p->meta_mark != p->meta_launches) {
@@ -349,6 +349,8 @@ bool begin_read(aaf_kv_pool *p, const int *handles, int n, cudaStream_t st) {
     }
     return true;
 }
+// Behind the last of its launches: what later calls wait for.
+bool end_read(aaf_kv_pool *p, cudaStream_t st) { return cudaEventRecord(p->read_ev, st) == cudaSuccess; }
 // A call reads host arrays and orders the pool's streams, neither of which a replayed graph would do again.
 bool capturing(cudaStream_t st) {
     cudaStreamCaptureStatus s = cudaStreamCaptureStatusNone;
@@ -1601,7 +1603,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
             ok = place_records(p, again, small, &km.seqs, 3, st) && launch_attend_tile(km, small, f16, st) == cudaSuccess;
         }
     }
-    return ok ? AAF_OK : broke(p);
+    return ok && end_read(p, st) ? AAF_OK : broke(p);
 } catch (const std::bad_alloc &) {
     return AAF_ERR_INVALID_ARG;  // the host has no memory for the records; nothing was launched
 }
@@ -1661,7 +1663,7 @@ int aaf_kv_attn_mass(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
     const bool ok = place_records(p, rec, small, &k.a.seqs, 0, st) &&
                     (wide ? launch_attn_mass_wide(k, small, a->dtype == AAF_DTYPE_F16, &p->map, layer, st)
                           : launch_attn_mass(k, small, a->dtype == AAF_DTYPE_F16, max_rows, st)) == cudaSuccess;
-    return ok ? AAF_OK : broke(p);
+    return ok && end_read(p, st) ? AAF_OK : broke(p);
 } catch (const std::bad_alloc &) {
     return AAF_ERR_INVALID_ARG;  // the host has no memory for the records; nothing was launched
 }
@@ -1728,7 +1730,7 @@ int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int3
     SmallStores small;
     const bool ok = place_records(p, rec, small, &k.seqs, 0, st) &&
                     launch_store(k, small, d->dtype == AAF_DTYPE_F16, st) == cudaSuccess;
-    return ok ? AAF_OK : broke(p);
+    return ok && end_read(p, st) ? AAF_OK : broke(p);
 } catch (const std::bad_alloc &) {
     return AAF_ERR_INVALID_ARG;  // the host has no memory for the records; nothing was launched
 }
@@ -1771,7 +1773,7 @@ int aaf_kv_prune(aaf_kv_pool *p, aaf_ctx_t ctx, const float *scores_dev, int64_t
     const int *tables = p->s.tables;
     ok = begin_read(p, &ctx, 1, st) && launch_gather_rows(p->g, tables + (long long)ctx * p->g.max_blk, ps.view.pieces, kept_dev, (int)budget, p->sm_count, st) == cudaSuccess;
     end_copy(p, ps, st);
-    if (!ok) return broke(p);
+    if (!ok || !end_read(p, st)) return broke(p);
     *out_ctx = c;
     return AAF_OK;
 }

@@ -181,3 +181,47 @@ def test_the_copies_of_a_pool_run_one_after_the_other(lib, pool):
     for x, y in zip(copies, copies[1:]):
         assert pool.before(x, y)
     assert not pool.wrongs()
+
+
+def every_call(pool, st, c):
+    """One of each kind on `st`; c: a context that nothing else names."""
+    pool.attend(st, [c])
+    pool.mass(st, [c])
+    pool.reserve(st, [c], [16])
+    pool.store(st, [c], [1])
+    pool.append(st, [c], [3])
+    pool.materialize(st, c, 5)
+    _, kids = pool.fork(st, c, 2)
+    _, merged = pool.compose(st, [c, kids[0]])
+    _, small = pool.prune(st, c, 5)
+    pool.evict(st, kids + [merged, small])
+    pool.imp(st, 40)
+
+
+@pytest.mark.parametrize("first", READERS)
+def test_a_stream_may_be_destroyed_once_a_call_on_another_has_returned(lib, pool, first):
+    a, b = lib.order_stream(), lib.order_stream()
+    _, c = pool.imp(b, 160)
+    _, other = pool.imp(b, 160)
+    read = READERS[first](pool, a, c)
+    pool.fork(b, other)  # orders nothing behind the reader
+    lib.order_replace_stream(a, 0)
+    second = pool.materialize(b, c, 5)
+    every_call(pool, b, c)
+    assert pool.before(read, second["copy"])
+    assert lib.aaf_kv_sync_status(pool.h) == 0
+    assert not pool.wrongs()
+
+
+@pytest.mark.parametrize("first", READERS)
+def test_the_last_reader_s_stream_may_be_captured_meanwhile(lib, pool, first):
+    a, b = lib.order_stream(), lib.order_stream()
+    _, c = pool.imp(b, 160)
+    read = READERS[first](pool, a, c)
+    lib.order_capture(a, 1)
+    at = lib.order_ops()
+    second = pool.attend(b, [c])["attend"]
+    every_call(pool, b, c)
+    assert pool.before(read, second)
+    assert not any(lib.order_captured(i) for i in range(at, lib.order_ops()))
+    assert not pool.wrongs()
