@@ -42,6 +42,7 @@ using namespace aafkv;
 namespace {
 
 constexpr int ARG_SLOTS = 16;
+constexpr unsigned long long NO_STREAM = ~0ull;  // the id of no stream, or of one whose id could not be had
 constexpr size_t ARG_RECORD_BYTES = 96;  // per-record room in a slot of the pinned argument ring
 static_assert(sizeof(ComposeSeg) <= ARG_RECORD_BYTES && sizeof(AppendEntry) <= ARG_RECORD_BYTES &&
                   sizeof(MatEntry) <= ARG_RECORD_BYTES && sizeof(ImpEntry) <= ARG_RECORD_BYTES,
@@ -141,7 +142,6 @@ struct aaf_kv_pool {
     // Copy launches of a pool share the ticket counter of its control block, so they must never overlap on the
     // device.  Calls on one stream are ordered anyway; when a call arrives on ANOTHER stream than the previous
     // copy launch, that stream is made to wait for the previous operator's last copy launch first.
-    cudaStream_t last_copy_stream = nullptr;
     cudaEvent_t last_copy_event = nullptr;
     // Kernels that compute with the pool (attention, stores, gathers of a prune) read block tables on the caller's
     // stream: they wait for the metadata launched so far, and the next kernel that changes metadata waits for them.  Streams
@@ -152,7 +152,7 @@ struct aaf_kv_pool {
     bool meta_drained = false; // meta_ev has been seen complete
     bool read_pending = false; // readers that the metadata stream has not been ordered behind,
     std::vector<char> row_read; // and the handles whose table rows they may read
-    unsigned long long read_id = 0, copy_id = 0;  // streams that are ordered behind the last reader and the last copy launch
+    unsigned long long read_id = NO_STREAM, copy_id = NO_STREAM;  // streams that are ordered behind the last reader, the last copy launch
     PoolMap map;               // tensor map of the pool memory (wide attention kernel)
     bool map_ok = false;
     // pinned argument ring
@@ -281,15 +281,22 @@ unsigned long long stream_id(cudaStream_t st) {
     unsigned long long id = 0;
     if (cudaStreamGetId(st, &id) != cudaSuccess) {
         cudaGetLastError();
-        return ~0ull;
+        return NO_STREAM;
     }
     return id;
 }
-// Before payload work on `st`: readers on another stream come first.
-bool after_readers_on(aaf_kv_pool *p, cudaStream_t st, unsigned long long id) {
-    if (!p->read_id || id == p->read_id) return true;
-    if (cudaStreamWaitEvent(st, p->read_ev, 0) != cudaSuccess) return false;
-    p->read_id = id;
+bool is_stream(unsigned long long known, unsigned long long id) { return known == id && id != NO_STREAM; }
+// Before payload work on `st`: the pool's earlier readers and copies on other streams come first.
+bool after_payload_work(aaf_kv_pool *p, cudaStream_t st) {
+    const unsigned long long id = stream_id(st);
+    if (!is_stream(p->read_id, id)) {
+        if (cudaStreamWaitEvent(st, p->read_ev, 0) != cudaSuccess) return false;
+        p->read_id = id;
+    }
+    if (p->last_copy_event && !is_stream(p->copy_id, id)) {
+        if (cudaStreamWaitEvent(st, p->last_copy_event, 0) != cudaSuccess) return false;
+        p->copy_id = id;
+    }
     return true;
 }
 // Before a planner: pick the next piece buffer and make the metadata stream wait until the copy launch
@@ -305,16 +312,12 @@ PlanSlot begin_plan(aaf_kv_pool *p) {
 // After the planner: the caller's stream (where the copy runs) waits for it, and for the pool's payload work on other streams.
 // A call that turns out to copy nothing waits all the same: end_copy makes its stream the one that later calls are ordered by.
 bool end_plan(aaf_kv_pool *p, const PlanSlot &ps, cudaStream_t st) {
-    if (cudaEventRecord(p->plan_done[ps.buf], p->meta_stream) != cudaSuccess ||
-        cudaStreamWaitEvent(st, p->plan_done[ps.buf], 0) != cudaSuccess)
-        return false;
-    if (!after_readers_on(p, st, stream_id(st))) return false;
-    return !p->last_copy_event || st == p->last_copy_stream || cudaStreamWaitEvent(st, p->last_copy_event, 0) == cudaSuccess;
+    return cudaEventRecord(p->plan_done[ps.buf], p->meta_stream) == cudaSuccess &&
+           cudaStreamWaitEvent(st, p->plan_done[ps.buf], 0) == cudaSuccess && after_payload_work(p, st);
 }
 // After the operator's last copy launch: mark the buffer's readers done and switch buffers.
 void end_copy(aaf_kv_pool *p, const PlanSlot &ps, cudaStream_t st) {
     cudaEventRecord(p->copy_done[ps.buf], st);
-    p->last_copy_stream = st;
     p->copy_id = stream_id(st);
     p->last_copy_event = p->copy_done[ps.buf];
     p->next_buf ^= 1;
@@ -323,10 +326,7 @@ void end_copy(aaf_kv_pool *p, const PlanSlot &ps, cudaStream_t st) {
 // Before a kernel on `st` that reads block tables or payload: it comes after the pool's earlier payload work, whatever
 // stream that was on, and after the metadata launched so far.
 bool begin_read(aaf_kv_pool *p, const int *handles, int n, cudaStream_t st) {
-    const unsigned long long id = stream_id(st);
-    if (!after_readers_on(p, st, id)) return false;
-    if (p->last_copy_event && id != p->copy_id && cudaStreamWaitEvent(st, p->last_copy_event, 0) != cudaSuccess) return false;
-    p->read_id = id;
+    if (!after_payload_work(p, st)) return false;
     p->read_pending = true;
     for (int i = 0; i < n; ++i) p->row_read[(size_t)handles[i]] = 1;
     if (p->meta_mark != p->meta_launches) {

@@ -37,14 +37,14 @@ std::map<cudaStream_t, Stream> streams;
 std::map<cudaEvent_t, Event> events;
 std::vector<Op> ops;
 std::vector<std::string> wrong;
-std::map<std::string, int> fail_at;  // calls of a function until the one that fails
+std::map<std::string, int> fail_at;  // calls of a function until the one that fails; -1: all fail
 Done host;                           // what the host has waited for
 unsigned long long ids = 0;
 uintptr_t handles = 0x1000;
 
 bool fails(const char *fn) {
     auto f = fail_at.find(fn);
-    return f != fail_at.end() && f->second > 0 && --f->second == 0;
+    return f != fail_at.end() && (f->second < 0 || (f->second > 0 && --f->second == 0));
 }
 Stream &of(cudaStream_t s) {
     auto it = streams.find(s);

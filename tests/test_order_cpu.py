@@ -225,3 +225,22 @@ def test_the_last_reader_s_stream_may_be_captured_meanwhile(lib, pool, first):
     assert pool.before(read, second)
     assert not any(lib.order_captured(i) for i in range(at, lib.order_ops()))
     assert not pool.wrongs()
+
+
+@pytest.mark.parametrize("second", READERS)
+def test_a_new_stream_under_an_old_handle_is_another_stream(lib, pool, second):
+    a = lib.order_stream()
+    ran, c = pool.imp(a, 160)
+    a = lib.order_replace_stream(a, 1)
+    assert pool.before(ran["copy"], READERS[second](pool, a, c))
+    a = lib.order_replace_stream(a, 1)
+    assert pool.before(ran["copy"], pool.append(a, [c], [5])["copy"])
+
+
+@pytest.mark.parametrize("second", READERS)
+def test_streams_whose_ids_cannot_be_had_are_taken_for_different_ones(lib, pool, second):
+    a, b = lib.order_stream(), lib.order_stream()
+    lib.order_fail(b"cudaStreamGetId", -1)
+    ran, c = pool.imp(a, 160)
+    pool.attend(a, [c])
+    assert pool.before(ran["copy"], READERS[second](pool, b, c))
