@@ -268,14 +268,15 @@ struct PlanSlot {
 
 // Before a kernel that writes the table rows of n handles: readers of those rows on the caller's stream come first.
 // (Reference counts and the ring are the metadata stream's own.)
-void after_readers(aaf_kv_pool *p, const int *handles, int n) {
-    if (!p->read_pending) return;
+bool after_readers(aaf_kv_pool *p, const int *handles, int n) {
+    if (!p->read_pending) return true;
     bool read = false;
     for (int i = 0; i < n && !read; ++i) read = p->row_read[(size_t)handles[i]] != 0;
-    if (!read) return;
-    if (cudaStreamWaitEvent(p->meta_stream, p->read_ev, 0) != cudaSuccess) p->broken = true;
+    if (!read) return true;
+    if (cudaStreamWaitEvent(p->meta_stream, p->read_ev, 0) != cudaSuccess) return false;
     p->read_pending = false;
     std::fill(p->row_read.begin(), p->row_read.end(), 0);
+    return true;
 }
 unsigned long long stream_id(cudaStream_t st) {
     unsigned long long id = 0;
@@ -438,7 +439,7 @@ int import_impl(aaf_kv_pool *p, const void *src_dev, const aaf_kv_xfer_desc *des
                             st) != cudaSuccess)
             return broke(p);
     }
-    after_readers(p, &c, 1);
+    if (!after_readers(p, &c, 1)) return broke(p);
     const PlanSlot ps = begin_plan(p);
     if (launch_plan_import(p->g, ps.view, c, n, static_cast<const char *>(src_dev), p->clock + 1, p->meta_stream) !=
             cudaSuccess ||
@@ -756,7 +757,8 @@ int aaf_kv_import_batch(aaf_kv_pool *p, int32_t n, const void *const *src_dev, c
         e.ctx = c; e.block_off = off; e.out_index = i; e.parent = -1;
         off += (int)nblk_of(p, e.n);
     }
-    for (int i = 0; i < n; ++i) after_readers(p, &ent[i].ctx, 1);
+    for (int i = 0; i < n; ++i)
+        if (!after_readers(p, &ent[i].ctx, 1)) return broke(p);
     const PlanSlot ps = begin_plan(p);
     const cudaError_t e = launch_plan_import_batch(p->g, ps.view, by_value ? nullptr : ent, small, n, (int)blocks,
                                                    p->clock + 1, p->meta_stream);
@@ -870,7 +872,7 @@ int aaf_kv_import_host_chunked(aaf_kv_pool *p, const void *src_host, const aaf_k
     // previous aaf_kv_import_host_chunked, so the upload waits for that and for nothing else on `stream`
     bool ok = !p->import_reader_pending ||
               cudaStreamWaitEvent(p->upload_stream, p->import_reader_done, 0) == cudaSuccess;
-    after_readers(p, &c, 1);
+    if (!after_readers(p, &c, 1)) return broke(p);
     const PlanSlot ps = begin_plan(p);
     ok = ok && launch_plan_import(p->g, ps.view, c, n, static_cast<const char *>(staging_dev), p->clock + 1,
                                   p->meta_stream) == cudaSuccess &&
@@ -923,7 +925,7 @@ int aaf_kv_fork(aaf_kv_pool *p, aaf_ctx_t parent, int32_t k, aaf_ctx_t *out_chil
         children[j] = c;
     }
     const long long T = p->len[parent];
-    after_readers(p, children, k);
+    if (!after_readers(p, children, k)) return broke(p);
     const cudaError_t e = launch_fork(p->g, p->s, parent, T, k, by_value ? nullptr : children, small, p->clock + 1,
                                       p->meta_stream);
     if (!by_value) release_args(p, p->meta_stream);
@@ -1027,7 +1029,7 @@ static int append_impl(aaf_kv_pool *p, int32_t n, const aaf_ctx_t *ctxs, const i
             return rc;
         }
     }
-    after_readers(p, ctxs, n);
+    if (!after_readers(p, ctxs, n)) return broke(p);
     const PlanSlot ps = begin_plan(p);
     const cudaError_t e = launch_plan_append(p->g, ps.view, ent_dev, small, n, (int)slots, p->lay.max_batch, 0,
                                              p->clock + 1, p->meta_stream);
@@ -1161,7 +1163,7 @@ static int compose_impl(aaf_kv_pool *p, int32_t n_out, const int32_t *seg_off, c
     const bool by_value = m <= SMALL_RECORDS;
     ComposeSeg *dev_rec = by_value ? nullptr : reinterpret_cast<ComposeSeg *>(acquire_args(p));
     memcpy(by_value ? small.s : dev_rec, rec.data(), sizeof(ComposeSeg) * (size_t)m);
-    after_readers(p, handles.data(), n_out);
+    if (!after_readers(p, handles.data(), n_out)) return broke(p);
     const PlanSlot ps = begin_plan(p);
     const cudaError_t e = launch_plan_compose(p->g, ps.view, dev_rec, small, m, (int)work, (int)fresh, (int)slots,
                                               p->clock + 1, p->meta_stream);
@@ -1756,7 +1758,7 @@ int aaf_kv_prune(aaf_kv_pool *p, aaf_ctx_t ctx, const float *scores_dev, int64_t
     const int rc0 = ensure_free(p, nb, st);
     if (rc0 != AAF_OK) return rc0;
     p->last_stream = st;
-    after_readers(p, &c, 1);
+    if (!after_readers(p, &c, 1)) return broke(p);
     const PlanSlot ps = begin_plan(p);
     // the new context's table, blocks and catalog entry; its piece list (no buffer behind it) is not run
     bool ok = launch_plan_import(p->g, ps.view, c, budget, nullptr, p->clock + 1, p->meta_stream, ctx) == cudaSuccess;

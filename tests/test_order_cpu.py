@@ -244,3 +244,48 @@ def test_streams_whose_ids_cannot_be_had_are_taken_for_different_ones(lib, pool,
     ran, c = pool.imp(a, 160)
     pool.attend(a, [c])
     assert pool.before(ran["copy"], READERS[second](pool, b, c))
+
+
+def imp_batch(pool, st, want):
+    x = B.aaf_kv_xfer_desc()
+    x.n_layers, x.n_kv_heads, x.head_dim, x.elt_bytes, x.n_tokens = L, H, D, 2, 40
+    descs, src, out = (B.aaf_kv_xfer_desc * 1)(x), (C.c_void_p * 1)(pool.base), (C.c_int32 * 1)()
+    return pool.call("import_batch", 1, src, descs, out, st, want=want)
+
+
+def imp_chunked(pool, st, want):
+    x = B.aaf_kv_xfer_desc()
+    x.n_layers, x.n_kv_heads, x.head_dim, x.elt_bytes, x.n_tokens = L, H, D, 2, 40
+    return pool.call("import_host_chunked", pool.base, C.byref(x), pool.base, 1 << 40, 32, C.byref(C.c_int32()), st, want=want)
+
+
+# calls that write the table row of `old` (a handle that was read and is free again) or of `read` (one that was read and lives)
+ROW_WRITERS = {"import": lambda p, s, read, want: p.imp(s, 40, want=want)[0], "import_batch": lambda p, s, read, want: imp_batch(p, s, want),
+               "import_host_chunked": lambda p, s, read, want: imp_chunked(p, s, want),
+               "fork": lambda p, s, read, want: p.fork(s, read, want=want)[0], "compose": lambda p, s, read, want: p.compose(s, [read], want=want)[0],
+               "prune": lambda p, s, read, want: p.prune(s, read, 5, want=want)[0],
+               "append": lambda p, s, read, want: p.append(s, [read], [3], want=want), "reserve": lambda p, s, read, want: p.reserve(s, [read], [3], want=want)}
+
+
+@pytest.mark.parametrize("writer", ROW_WRITERS)
+def test_a_table_row_is_not_rewritten_when_the_wait_for_its_readers_fails(lib, pool, writer):
+    a, b = lib.order_stream(), lib.order_stream()
+    _, old = pool.imp(b, 160)
+    _, read = pool.imp(b, 160)
+    seen = pool.attend(a, [old, read])["attend"]
+    pool.evict(b, [old])
+    lib.order_fail(b"cudaStreamWaitEvent", 1)
+    assert not ROW_WRITERS[writer](pool, b, read, B.AAF_ERR_CUDA), "a planner was launched all the same"
+    pool.attend(b, [read], want=B.AAF_ERR_CUDA)
+
+
+@pytest.mark.parametrize("writer", ROW_WRITERS)
+def test_a_table_row_is_rewritten_behind_its_readers(lib, pool, writer):
+    a, b = lib.order_stream(), lib.order_stream()
+    _, old = pool.imp(b, 160)
+    _, read = pool.imp(b, 160)
+    seen = pool.attend(a, [old, read])["attend"]
+    pool.evict(b, [old])
+    ran = ROW_WRITERS[writer](pool, b, read, 0)
+    plan = [i for name, i in ran.items() if name.startswith("plan_") or name == "fork"]
+    assert len(plan) == 1 and pool.before(seen, plan[0])
