@@ -154,6 +154,7 @@ size_t aaf_kv_pool_workspace_bytes(const aaf_kv_pool_desc *desc);
  * Errors: INVALID_ARG (bad geometry, row not a multiple of 16, misaligned pointers, workspace
  * too small, free_order not a permutation), CUDA. */
 int aaf_kv_pool_create(const aaf_kv_pool_desc *desc, aaf_kv_pool **out);
+/* Returns when the pool's work is over, on whatever streams it was issued: its memory may be freed then. */
 int aaf_kv_pool_destroy(aaf_kv_pool *pool);
 
 /* materialize -- Alg. "KV-Transfer" (select the blocks of a position range, hand raw buffers to

@@ -609,6 +609,9 @@ int aaf_kv_pool_destroy(aaf_kv_pool *p) {
     DeviceGuard guard(p->device);
     if (p->meta_stream) cudaStreamSynchronize(p->meta_stream);
     if (p->last_stream || !p->pending.empty()) cudaStreamSynchronize(p->last_stream);
+    // readers and copies on other streams use the pinned ring and memory that the caller frees next
+    if (p->read_ev) cudaEventSynchronize(p->read_ev);
+    if (p->last_copy_event) cudaEventSynchronize(p->last_copy_event);
     for (auto &t : p->pending) {
         cudaEventDestroy(t.start);
         cudaEventDestroy(t.stop);

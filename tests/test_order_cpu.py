@@ -289,3 +289,16 @@ def test_a_table_row_is_rewritten_behind_its_readers(lib, pool, writer):
     ran = ROW_WRITERS[writer](pool, b, read, 0)
     plan = [i for name, i in ran.items() if name.startswith("plan_") or name == "fork"]
     assert len(plan) == 1 and pool.before(seen, plan[0])
+
+
+@pytest.mark.parametrize("last", READERS)
+def test_destroying_a_pool_waits_for_its_work_on_every_stream(lib, pool, last):
+    a, b = lib.order_stream(), lib.order_stream()
+    _, c = pool.imp(b, 160)
+    _, other = pool.imp(b, 40)
+    ran = READERS[last](pool, a, c)
+    pool.fork(b, other)
+    pool.close()
+    pool.h = None
+    assert lib.order_host_knows(ran)
+    assert not pool.wrongs()
