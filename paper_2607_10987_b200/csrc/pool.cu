@@ -99,14 +99,19 @@ struct TimedLaunch {
     int cls;
 };
 
+// The pool's device is the current one meanwhile.  The thread may be capturing another stream, which waiting on the host for the
+// pool's own streams and events would end unless it is allowed to pass: they are none of that capture's.
 struct DeviceGuard {
     int prev = -1;
     bool switched = false;
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
     explicit DeviceGuard(int dev) {
+        cudaThreadExchangeStreamCaptureMode(&mode);
         if (cudaGetDevice(&prev) == cudaSuccess && prev != dev) switched = cudaSetDevice(dev) == cudaSuccess;
     }
     ~DeviceGuard() {
         if (switched) cudaSetDevice(prev);
+        cudaThreadExchangeStreamCaptureMode(&mode);
     }
 };
 
@@ -218,8 +223,9 @@ void release_args(aaf_kv_pool *p, cudaStream_t st) {
 int refresh_free(aaf_kv_pool *p, cudaStream_t st) {
     (void)st;
     unsigned long long ht[2];
-    if (cudaStreamSynchronize(p->meta_stream) != cudaSuccess) return AAF_ERR_CUDA;  // the counters are metadata
-    if (cudaMemcpy(ht, p->s.ctl, sizeof(ht), cudaMemcpyDeviceToHost) != cudaSuccess) return AAF_ERR_CUDA;
+    // the counters are metadata; the default stream, which a blocking stream's capture closes, is not needed for them
+    if (cudaMemcpyAsync(ht, p->s.ctl, sizeof(ht), cudaMemcpyDeviceToHost, p->meta_stream) != cudaSuccess) return AAF_ERR_CUDA;
+    if (cudaStreamSynchronize(p->meta_stream) != cudaSuccess) return AAF_ERR_CUDA;
     p->free_lb = (long long)(ht[1] - ht[0]);
     return AAF_OK;
 }
@@ -336,11 +342,7 @@ bool begin_read(aaf_kv_pool *p, const int *handles, int n, cudaStream_t st) {
         p->meta_drained = false;
     }
     if (!p->meta_drained) {
-        // another stream of this thread may be capturing, which a query would end unless it is allowed to pass
-        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
-        cudaThreadExchangeStreamCaptureMode(&mode);
         const cudaError_t e = cudaEventQuery(p->meta_ev);
-        cudaThreadExchangeStreamCaptureMode(&mode);
         if (e == cudaSuccess) {
             p->meta_drained = true;
         } else {

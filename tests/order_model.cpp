@@ -39,6 +39,7 @@ std::vector<Op> ops;
 std::vector<std::string> wrong;
 std::map<std::string, int> fail_at;  // calls of a function until the one that fails; -1: all fail
 Done host;                           // what the host has waited for
+cudaStreamCaptureMode mode = cudaStreamCaptureModeGlobal;  // the calling thread's
 unsigned long long ids = 0;
 uintptr_t handles = 0x1000;
 
@@ -53,6 +54,12 @@ Stream &of(cudaStream_t s) {
         it->second.id = ++ids;
     }
     return it->second;
+}
+// calls that end a capture of the same thread unless its mode lets them pass
+void may_end_a_capture(const char *what) {
+    if (mode == cudaStreamCaptureModeRelaxed) return;
+    for (const auto &s : streams)
+        if (s.second.alive && s.second.capturing) wrong.push_back(std::string(what) + " beside a capture");
 }
 cudaError_t launch(const char *name, cudaStream_t s) {
     if (fails(name)) return cudaErrorUnknown;
@@ -123,9 +130,13 @@ cudaError_t CUDARTAPI cudaStreamIsCapturing(cudaStream_t s, cudaStreamCaptureSta
     *c = of(s).capturing ? cudaStreamCaptureStatusActive : cudaStreamCaptureStatusNone;
     return cudaSuccess;
 }
-cudaError_t CUDARTAPI cudaThreadExchangeStreamCaptureMode(cudaStreamCaptureMode *) { return cudaSuccess; }
+cudaError_t CUDARTAPI cudaThreadExchangeStreamCaptureMode(cudaStreamCaptureMode *m) {
+    std::swap(*m, mode);
+    return cudaSuccess;
+}
 cudaError_t CUDARTAPI cudaStreamSynchronize(cudaStream_t s) {
     if (fails("cudaStreamSynchronize")) return cudaErrorUnknown;
+    may_end_a_capture("waiting for a stream");
     if (!of(s).alive) wrong.push_back("the host waits for a destroyed stream");
     if (of(s).capturing) wrong.push_back("the host waits for a stream that is being captured");
     host.insert(of(s).done.begin(), of(s).done.end());
@@ -166,9 +177,13 @@ cudaError_t CUDARTAPI cudaEventRecord(cudaEvent_t e, cudaStream_t s) {
     events[e].done.insert(host.begin(), host.end());
     return cudaSuccess;
 }
-cudaError_t CUDARTAPI cudaEventQuery(cudaEvent_t) { return cudaErrorNotReady; }  // the device is as slow as it may be
+cudaError_t CUDARTAPI cudaEventQuery(cudaEvent_t) {
+    may_end_a_capture("asking for an event");
+    return cudaErrorNotReady;  // the device is as slow as it may be
+}
 cudaError_t CUDARTAPI cudaEventSynchronize(cudaEvent_t e) {
     if (fails("cudaEventSynchronize")) return cudaErrorUnknown;
+    may_end_a_capture("waiting for an event");
     if (events[e].captured) wrong.push_back("the host waits for an event of a capture");
     host.insert(events[e].done.begin(), events[e].done.end());
     return cudaSuccess;
@@ -205,6 +220,7 @@ cudaError_t CUDARTAPI cudaMemset(void *p, int v, size_t n) {
     return cudaSuccess;
 }
 cudaError_t CUDARTAPI cudaMemcpy(void *d, const void *s, size_t n, cudaMemcpyKind) {
+    may_end_a_capture("a copy through the default stream");
     memcpy(d, s, n);
     return cudaSuccess;
 }

@@ -302,3 +302,20 @@ def test_destroying_a_pool_waits_for_its_work_on_every_stream(lib, pool, last):
     pool.h = None
     assert lib.order_host_knows(ran)
     assert not pool.wrongs()
+
+
+def test_calls_beside_a_capture_wait_on_the_host_without_ending_it(lib, pool):
+    a, b = lib.order_stream(), lib.order_stream()
+    _, c = pool.imp(b, 160)
+    lib.order_capture(a, 1)
+    for _ in range(20):  # more batches in the pinned ring than it has room for at once
+        pool.attend(b, [c] * 70)
+    for _ in range(6):   # as many blocks as the pool has, so that the device's count is asked for
+        _, big = pool.imp(b, 16000)
+        pool.reserve(b, [big], [1])
+        pool.prune(b, big, 2)
+        pool.evict(b, [big])
+    pool.close()
+    pool.h = None
+    assert not pool.wrongs()
+    assert not any(lib.order_captured(i) for i in range(lib.order_ops()))
