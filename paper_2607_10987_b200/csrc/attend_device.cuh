@@ -21,6 +21,10 @@ __device__ __forceinline__ float rcp(float x) {
     return y;
 }
 
+// RAISE: weights are computed as 2^(x - m + RAISE), m the row's maximum, so that the largest is near the top of the type's range.
+// f16 ends at 2^-24: with a largest weight of 1, weights below 2^-14 would lose bits and those below 2^-25 vanish from the
+// products while the sum, in 32 bits, still counts them (131072 keys at 2^-24.6 of one: an error of five half steps).
+// What is kept for the join and the log-sum is the base of the exponents, m - RAISE.
 template <typename T> struct Elt;
 template <> struct Elt<__nv_bfloat16> {
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -33,6 +37,7 @@ template <> struct Elt<__nv_bfloat16> {
     static __device__ __forceinline__ float from(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
     static __device__ __forceinline__ uint16_t to(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
     static constexpr uint32_t EXP = 0x7f807f80u, ONE = 0x3f80u;
+    static constexpr float RAISE = 0.0f;
     // magnitudes of at most the type's largest finite value, signs kept
     static __device__ __forceinline__ uint32_t bounded(uint32_t v) {
         uint32_t r;
@@ -58,6 +63,7 @@ template <> struct Elt<__half> {
     static __device__ __forceinline__ float from(uint16_t v) { return __half2float(__ushort_as_half(v)); }
     static __device__ __forceinline__ uint16_t to(float v) { return __half_as_ushort(__float2half_rn(v)); }
     static constexpr uint32_t EXP = 0x7c007c00u, ONE = 0x3c00u;
+    static constexpr float RAISE = 15.0f;
     // magnitudes of at most the type's largest finite value, signs kept
     static __device__ __forceinline__ uint32_t bounded(uint32_t v) {
         uint32_t r;

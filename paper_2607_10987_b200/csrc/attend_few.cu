@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
                 m[nt][0] = n0;
                 m[nt][1] = n1;
             }
-            const float b0 = n0 == -CUDART_INF_F ? 0.0f : n0, b1 = n1 == -CUDART_INF_F ? 0.0f : n1;
+            const float b0 = n0 == -CUDART_INF_F ? 0.0f : n0 - Elt<T>::RAISE, b1 = n1 == -CUDART_INF_F ? 0.0f : n1 - Elt<T>::RAISE;
             const float p0 = ex2(s[nt][0] - b0), p1 = ex2(s[nt][1] - b1);
             const float p2 = ex2(s[nt][2] - b0), p3 = ex2(s[nt][3] - b1);
             l[nt][0] += p0 + p2;
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
                                              scaled(o[nt][4 * cc + 2 * i + 1][c], some), scaled(o[nt][4 * cc + 2 * i + 1][2 + c], some));
                 }
                 if (g == 0) {
-                    p.part_ml[2 * pr] = m[nt][c];
+                    p.part_ml[2 * pr] = m[nt][c] - Elt<T>::RAISE;
                     p.part_ml[2 * pr + 1] = sum;
                 }
                 continue;
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(FewShape<DP>::WARPS * 32, 2)
             if (p.lse && g == 0)
                 p.lse[qt * p.H * p.G + hq] =
                     sum == 0.0f ? -CUDART_INF_F
-                                : (m[nt][c] + log2f(sum)) * LN2 - (SIMPLE ? 0.0f : slope[SIMPLE ? 0 : nt][c] * (float)span[SIMPLE ? 0 : nt][c].near);
+                                : (m[nt][c] - Elt<T>::RAISE + log2f(sum)) * LN2 - (SIMPLE ? 0.0f : slope[SIMPLE ? 0 : nt][c] * (float)span[SIMPLE ? 0 : nt][c].near);
         }
     asm volatile("griddepcontrol.wait;" ::: "memory");  // what it ran beside is done before it is
 }

@@ -41,7 +41,7 @@ struct AttnParams {
     void *out;
     float *lse;           // may be null
     float *part_o;        // [partial rows][D]
-    float *part_ml;       // [partial rows][2]: running maximum (log2 domain) and sum
+    float *part_ml;       // [partial rows][2]: base of the exponents (log2 domain) and sum
     const AttnSeq *seqs;  // device records, null: the kernel parameter holds them
     const int *tables;
     const char *kbase;    // layer's first byte

@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
                 o[i][2 * h + 1] *= a;
             }
             m[h] = n;
-            base[h] = n == -CUDART_INF_F ? 0.0f : n;
+            base[h] = n == -CUDART_INF_F ? 0.0f : n - Elt<T>::RAISE;
         }
         partial = !full && __any_sync(0xffffffffu, partial);
 #pragma unroll
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
                     *reinterpret_cast<float2 *>(p.part_o + pr * p.D + d) = make_float2(scaled(o[i][2 * h], some), scaled(o[i][2 * h + 1], some));
             }
             if (t4 == 0) {
-                p.part_ml[2 * pr] = m[h];
+                p.part_ml[2 * pr] = m[h] - Elt<T>::RAISE;
                 p.part_ml[2 * pr + 1] = sum;
             }
             continue;
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
         }
         if (p.lse && t4 == 0)
             p.lse[qt * p.H * p.G + hq] =
-                sum == 0.0f ? -CUDART_INF_F : (m[h] + log2f(sum)) * LN2 - slope[h] * (float)span[h].near;
+                sum == 0.0f ? -CUDART_INF_F : (m[h] - Elt<T>::RAISE + log2f(sum)) * LN2 - slope[h] * (float)span[h].near;
     }
     __syncthreads();  // the next unit loads over this one's tiles
     }

@@ -225,6 +225,8 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
         const uint32_t tS = tmem + lanes + w * 128, tP = tS + 64, tO = tmem + lanes + 256 + w * D;
         const float c = fabsf(p.scale) * LOG2E, k1 = fabsf(p.scale) * p.inv_cap, cap2 = p.softcap * LOG2E;
         const CapPoly capped(c, k1);
+        constexpr float GROWTH = 8.0f;  // how far (log2) a score may outgrow the maximum in use
+        constexpr float RAISE = Elt<T>::RAISE > 0.0f ? Elt<T>::RAISE - GROWTH : 0.0f;
         float m = -CUDART_INF_F, l = 0.0f;
         const bool active = w == 0 || two;
         bool ok = true;
@@ -296,7 +298,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                 // The maximum in use serves this tile too unless a score outgrows it by 2^8, so the first half of the weights is
                 // computed beside the tile's maximum, not behind it, and once more in the tiles where it was too small.
                 for (;;) {
-                    const float base = m == -CUDART_INF_F ? 0.0f : m;
+                    const float base = m == -CUDART_INF_F ? 0.0f : m - RAISE;
                     float mx[4] = {s[0], s[1], s[2], s[3]};
                     sums[0] = sums[1] = 0;
 #pragma unroll
@@ -311,7 +313,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                     const float most = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                     const float top = poly.value && most > -CUDART_INF_F ? cap2 * tanh_f32(most * k1) : most * times;
                     // the first maximum, or one that outgrew the one in use
-                    const bool grow = top > m + 8.0f || (m == -CUDART_INF_F && top > m);
+                    const bool grow = top > m + GROWTH || (m == -CUDART_INF_F && top > m);
                     if (!__any_sync(0xffffffffu, grow)) break;
                     const float f = grow && m != -CUDART_INF_F ? ex2(m - top) : 1.0f;
                     if (grow) m = top;
@@ -332,7 +334,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                     }
                 }
                 done_half(0, pk);
-                const float base = m == -CUDART_INF_F ? 0.0f : m;
+                const float base = m == -CUDART_INF_F ? 0.0f : m - RAISE;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     const f2 x = pair_of(s[64 + 2 * i], s[65 + 2 * i], times, base, poly);
@@ -388,10 +390,10 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                 }
             }
             if (live && part_out) {
-                p.part_ml[2 * pr] = m;
+                p.part_ml[2 * pr] = m - RAISE;
                 p.part_ml[2 * pr + 1] = l;
             } else if (live && p.lse) {
-                p.lse[qt * p.H * p.G + hq] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * LN2 - slope * (float)span.near;
+                p.lse[qt * p.H * p.G + hq] = l == 0.0f ? -CUDART_INF_F : (m - RAISE + log2f(l)) * LN2 - slope * (float)span.near;
             }
         }
     } else {
