@@ -282,8 +282,8 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             }
             if (MODE == 0 || small) {
                 times = c;
-            } else if (MODE == 2 && p.softcap == 0.0f) {
-                // distances are whole numbers, measured from the nearest visible key (see RowSpan)
+            } else if (MODE == 2 && p.softcap == 0.0f && abs(span.pos - tb) + WIDE_KEYS < 1 << 24) {
+                // distances are whole numbers, which 32 bits hold up to 2^24, measured from the nearest visible key (see RowSpan)
                 const float d0 = (float)(span.pos - tb), slope2 = slope * LOG2E, c2 = p.scale * LOG2E, near = (float)span.near;
 #pragma unroll
                 for (int i = 0; i < 128; ++i) s[i] = fmaf(-slope2, fabsf(d0 - (float)i) - near, s[i] * c2);

@@ -49,3 +49,40 @@ def test_many_small_weights_beside_a_large_one(dim, group, n_q, p_rounded, raise
     ref = R.attend_ref([c], [n_q], q, scale=scale)
     grid = 24 + raised if dtype == torch.float16 else 126  # bf16 has the exponents of 32 bits
     check_with_floor([x[0] for x in got], ref, dtype, dim, p_rounded, keys, grid, float(rows.max()))
+
+
+@pytest.mark.parametrize("n_q", [1, 8])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_bias_of_distances_that_32_bits_cannot_tell_apart(dim, n_q):
+    """Rows whose span lies more than 2^24 keys behind them: neighbouring keys differ by one in distance all the same."""
+    seen, far, group = 300, (1 << 24) + 1001, 8
+    blocks = (seen + far) // 128 + 2
+    pool = R.make_pool(1, 1, dim, 128, blocks, max_ctx=2)
+    c = R.add_ctx(pool, seen, 1)
+    assert pool.reserve([c.handle], [far])[0] == 0  # slots that nothing was stored in: no row sees them
+    q = R.rand((n_q, group, dim), 2, scale=2.0)
+    slopes = torch.linspace(0.05, 0.7, group, device="cuda")
+    spans = torch.tensor([[3 * j, seen - j] for j in range(n_q)], dtype=torch.int32, device="cuda")
+    st, (out, lse) = pool.attend(0, [c.handle], [n_q], q, slopes=slopes, spans=spans)
+    assert st == 0
+    torch.cuda.synchronize()
+    assert pool.sync_status() == 0
+    k, v = c.rows[0, :, :, 0].double()
+    key = torch.arange(seen, device="cuda")
+    refs, lses, slacks, big = [], [], [], 0.0
+    for j in range(n_q):
+        p = seen + far - n_q + j
+        lo, hi = spans[j].tolist()
+        x = q[j].double() @ k.T * dim ** -0.5
+        big = max(big, float((q[j].double().abs() @ k.abs().T).max()) * dim ** -0.5)
+        x = x - slopes.double()[:, None] * ((p - key) - (p - (hi - 1)))  # from the nearest key that is seen
+        x = x.masked_fill((key < lo) | (key >= hi), -math.inf)
+        w = torch.softmax(x, -1)
+        refs.append(w @ v)
+        slacks.append(w @ v.abs())
+        lses.append(torch.logsumexp(x, -1) - slopes.double() * (p - (hi - 1)))
+    # the bias of a visible key is at most 0.7 * 300 = 210 and rounded once more than a score is
+    big += 210.0
+    R.check_attend((out, None), (torch.stack(refs), None, torch.stack(slacks), big), torch.bfloat16, dim, True)
+    ref = torch.stack(lses)
+    assert ((lse.double() - ref).abs() <= 4 * 2.0 ** -24 * ref.abs() + 2.0 ** -10).all()
