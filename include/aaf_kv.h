@@ -328,7 +328,7 @@ int aaf_kv_reserve(aaf_kv_pool *pool, int32_t n, const aaf_ctx_t *ctxs, const in
 
 /* store -- rotary positions and the write of one layer's new keys and values.  For the last n_new[i] tokens of context
  * ctxs[i]: k is rotated and written with v into the token's slot of layer `layer`; with n_q_heads > 0, q is rotated
- * into q_out (which may be q itself).  A pair (a, b) of the first rot_dim dimensions of a head becomes
+ * into q_out (which may be q itself, with the same stride).  A pair (a, b) of the first rot_dim dimensions of a head becomes
  *   (a cos w - b sin w, a sin w + b cos w) * mscale,   w = position * inv_freq[pair],
  * pairs being (i, i + rot_dim / 2), or (2i, 2i + 1) with `interleaved`.  The angle is taken in 64 bits, the results are
  * rounded once.  The position of a token is its index in the context, or pos[token] if pos is given (a pruned context,

@@ -100,8 +100,9 @@ class Pool:
     def materialize(self, st, ctx, tokens, want=0):
         return self.call("materialize", ctx, 0, tokens, self.base, 1 << 40, None, st, want=want)
 
-    def store(self, st, ctxs, n_new, want=0):
-        d = B.aaf_kv_store_desc(C.sizeof(B.aaf_kv_store_desc), 0, 0, 0, 0, 1.0, None, None, None, None, self.base, self.base, 0, 0, H * D, H * D)
+    def store(self, st, ctxs, n_new, want=0, heads=0, q=None, q_out=None, q_stride=0, q_out_stride=0):
+        d = B.aaf_kv_store_desc(C.sizeof(B.aaf_kv_store_desc), 0, heads, 0, 0, 1.0, None, None, q, q_out, self.base, self.base, q_stride, q_out_stride,
+                                H * D, H * D)
         return self.call("store", 0, C.byref(d), len(ctxs), self.ints(ctxs), self.ints(n_new), st, want=want)
 
     def _attn(self):
@@ -319,3 +320,12 @@ def test_calls_beside_a_capture_wait_on_the_host_without_ending_it(lib, pool):
     pool.h = None
     assert not pool.wrongs()
     assert not any(lib.order_captured(i) for i in range(lib.order_ops()))
+
+
+def test_a_store_in_place_has_one_stride(lib, pool):
+    st = lib.order_stream()
+    _, c = pool.imp(st, 160)
+    q = dict(heads=2, q=pool.base, q_stride=2 * D)
+    pool.store(st, [c], [3], q_out=pool.base, q_out_stride=2 * D, **q)
+    pool.store(st, [c], [3], q_out=pool.base + 4096, q_out_stride=4 * D, **q)
+    assert not pool.store(st, [c], [3], q_out=pool.base, q_out_stride=4 * D, want=B.AAF_ERR_INVALID_ARG, **q)
