@@ -396,7 +396,7 @@ int aaf_kv_rope_freqs(int32_t rot_dim, double base, int32_t scaling, const aaf_k
 typedef struct aaf_kv_attn {
     uint32_t struct_size; /* sizeof(aaf_kv_attn)                                  */
     int32_t dtype;        /* AAF_DTYPE_*                                          */
-    int32_t n_q_heads;    /* a multiple of n_kv_heads                             */
+    int32_t n_q_heads;    /* a multiple of n_kv_heads; n_q_heads * head_dim below 2^31 */
     int32_t window;       /* 0: none                                              */
     float scale;
     float softcap;        /* 0: none; its reciprocal must be finite               */

@@ -1326,6 +1326,7 @@ int attn_check(const aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_
     if (layer < 0 || layer >= p->g.L || !dtype_ok(a->dtype)) return AAF_ERR_INVALID_ARG;
     if (p->g.E != 2 || p->g.D % 8 != 0 || p->g.D > AAF_ATTN_MAX_HEAD_DIM) return AAF_ERR_INCOMPAT;
     if (a->n_q_heads < 1 || a->n_q_heads % p->g.H != 0 || a->window < 0) return AAF_ERR_INVALID_ARG;
+    if ((long long)a->n_q_heads * p->g.D >= 1ll << 31) return AAF_ERR_INVALID_ARG;  // places within a token are ints in the kernels
     if (!is_finite(a->scale * 1.4427f) || !is_finite(a->softcap) || a->softcap < 0.0f) return AAF_ERR_INVALID_ARG;
     if (a->softcap > 0.0f && !is_finite(1.0f / a->softcap)) return AAF_ERR_INVALID_ARG;  // 0 / softcap would be NaN
     if (a->q_stride % 8 != 0 || a->q_stride < (long long)a->n_q_heads * p->g.D) return AAF_ERR_INVALID_ARG;

@@ -105,15 +105,15 @@ class Pool:
                                 H * D, H * D)
         return self.call("store", 0, C.byref(d), len(ctxs), self.ints(ctxs), self.ints(n_new), st, want=want)
 
-    def _attn(self):
-        return B.aaf_kv_attn(C.sizeof(B.aaf_kv_attn), 0, H, 0, 0.1, 0.0, None, None, H * D)
+    def _attn(self, heads=H):
+        return B.aaf_kv_attn(C.sizeof(B.aaf_kv_attn), 0, heads, 0, 0.1, 0.0, None, None, heads * D)
 
-    def attend(self, st, ctxs, n_q=None, want=0):
-        return self.call("attend", 0, C.byref(self._attn()), len(ctxs), self.ints(ctxs), None if n_q is None else self.ints(n_q), self.base,
+    def attend(self, st, ctxs, n_q=None, want=0, heads=H):
+        return self.call("attend", 0, C.byref(self._attn(heads)), len(ctxs), self.ints(ctxs), None if n_q is None else self.ints(n_q), self.base,
                          self.base, None, self.base, 1 << 40, st, want=want)
 
-    def mass(self, st, ctxs, want=0):
-        return self.call("attn_mass", 0, C.byref(self._attn()), len(ctxs), self.ints(ctxs), None, self.base, self.base, None, self.base, 1 << 20, st,
+    def mass(self, st, ctxs, want=0, heads=H):
+        return self.call("attn_mass", 0, C.byref(self._attn(heads)), len(ctxs), self.ints(ctxs), None, self.base, self.base, None, self.base, 1 << 20, st,
                          want=want)
 
     def prune(self, st, ctx, budget, want=0):
@@ -329,3 +329,12 @@ def test_a_store_in_place_has_one_stride(lib, pool):
     pool.store(st, [c], [3], q_out=pool.base, q_out_stride=2 * D, **q)
     pool.store(st, [c], [3], q_out=pool.base + 4096, q_out_stride=4 * D, **q)
     assert not pool.store(st, [c], [3], q_out=pool.base, q_out_stride=4 * D, want=B.AAF_ERR_INVALID_ARG, **q)
+
+
+def test_tokens_of_2_to_the_31_elements_are_refused(lib, pool):
+    st = lib.order_stream()
+    _, c = pool.imp(st, 160)
+    most = (1 << 31) // D - H
+    for call in (pool.attend, pool.mass):
+        assert call(st, [c], heads=most)
+        assert not call(st, [c], heads=most + H, want=B.AAF_ERR_INVALID_ARG)
