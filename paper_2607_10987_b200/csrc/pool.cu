@@ -1693,8 +1693,6 @@ int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int3
     if (d->k_stride < kv_min || d->v_stride < kv_min || d->k_stride % 8 || d->v_stride % 8) return AAF_ERR_INVALID_ARG;
     if (d->n_q_heads > 0 && (d->q_stride < q_min || d->q_out_stride < q_min || d->q_stride % 8 || d->q_out_stride % 8))
         return AAF_ERR_INVALID_ARG;
-    // in place, a token is written where it was read; with another stride it would be written where another one is still to be read
-    if (d->n_q_heads > 0 && d->q == d->q_out && d->q_stride != d->q_out_stride) return AAF_ERR_INVALID_ARG;
     if (d->rot_dim < 0 || d->rot_dim % 2 || d->rot_dim > p->g.D || d->rot_dim > AAF_ROPE_MAX_DIM || !is_finite(d->mscale))
         return AAF_ERR_INVALID_ARG;
     if (d->rot_dim > 0 && (!d->inv_freq || (reinterpret_cast<uintptr_t>(d->inv_freq) & 7u))) return AAF_ERR_INVALID_ARG;
@@ -1719,6 +1717,8 @@ int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int3
         total += n_new[i];
         if (total > (1ll << 30)) return AAF_ERR_TOO_MANY;
     }
+    // in place, a token is written where it was read; with another stride it would be written where another one is still to be read
+    if (d->n_q_heads > 0 && d->q == d->q_out && d->q_stride != d->q_out_stride && total > 1) return AAF_ERR_INVALID_ARG;
     if (std::adjacent_find(sorted.begin(), sorted.end()) != sorted.end()) return AAF_ERR_INVALID_ARG;
     DeviceGuard guard(p->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);

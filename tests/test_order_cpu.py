@@ -329,6 +329,7 @@ def test_a_store_in_place_has_one_stride(lib, pool):
     pool.store(st, [c], [3], q_out=pool.base, q_out_stride=2 * D, **q)
     pool.store(st, [c], [3], q_out=pool.base + 4096, q_out_stride=4 * D, **q)
     assert not pool.store(st, [c], [3], q_out=pool.base, q_out_stride=4 * D, want=B.AAF_ERR_INVALID_ARG, **q)
+    pool.store(st, [c], [1], q_out=pool.base, q_out_stride=4 * D, **q)  # no stride is used
 
 
 def test_tokens_of_2_to_the_31_elements_are_refused(lib, pool):
