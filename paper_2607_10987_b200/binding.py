@@ -495,6 +495,9 @@ class KVPool:
             self._flat(lse, torch.float32, tokens * heads, "lse")
         ws = self._attend_ws
         if ws is None:
+            with torch.cuda.device(self.device):
+                if torch.cuda.is_current_stream_capturing():  # refused anyway; kept scratch must not be a graph's memory
+                    return AAF_ERR_INVALID_ARG, None
             ws = self._attend_ws = torch.empty(aaf_kv_attend_workspace_bytes(self.h), dtype=torch.uint8, device=self.device)
         st = load().aaf_kv_attend(self.h, layer, a, n, (C.c_int32 * (n or 1))(*ctxs),
                                   None if n_q is None else (C.c_int32 * (n or 1))(*n_q), q.data_ptr(), out.data_ptr(),

@@ -4,6 +4,7 @@ from __future__ import annotations
 import pytest
 import torch
 
+from paper_2607_10987_b200 import binding as B
 from tests import serve_reference as R
 
 pytestmark = pytest.mark.gpu
@@ -99,3 +100,21 @@ def test_streams_come_and_go_between_calls():
         assert st == 0 and torch.equal(rows.view(torch.bfloat16).view(c.rows.shape), c.rows)
         R.check_attend(got, ref, torch.bfloat16, 64, False)
     assert pool.sync_status() == 0
+
+
+def test_a_first_call_in_a_capture_leaves_no_scratch_of_the_graph_s_memory():
+    pool = R.make_pool(1, 2, 64, 16, 64)
+    c = R.add_ctx(pool, 320, 1)
+    q = R.rand((1, 8, 64), 1)
+    x = torch.zeros(1, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.add_(1.0)
+        st, got = pool.attend(0, [c.handle], None, q)
+    assert st == B.AAF_ERR_INVALID_ARG and got is None and pool._attend_ws is None
+    graph.replay()
+    st, got = pool.attend(0, [c.handle], None, q)
+    assert st == 0
+    torch.cuda.synchronize()
+    assert float(x) == 1 and pool.sync_status() == 0
+    R.check_attend(got, R.attend_ref([c], [1], q), torch.bfloat16, 64, False)
