@@ -396,8 +396,8 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32)
         row = sq.part0 + (long long)head * R + r;
         step = (long long)p.H * R;
         const int gr = sq.grow + r;
-        grow = sq.gpart0 + ((long long)(gr / WIDE_ROWS) * sq.gsplit * p.H + head) * WIDE_ROWS + gr % WIDE_ROWS;
-        gstep = (long long)p.H * WIDE_ROWS;
+        grow = sq.gpart0 + ((long long)(gr / GROUP_ROWS) * sq.gsplit * p.H + head) * GROUP_ROWS + gr % GROUP_ROWS;
+        gstep = (long long)p.H * GROUP_ROWS;
     }
     const int parts = sq.nsplit + sq.gsplit, dims = p.D;
     auto at = [&](int s) { return s < sq.nsplit ? row + s * step : grow + (s - sq.nsplit) * gstep; };

@@ -18,10 +18,10 @@ struct AttnSeq {          // 56 bytes
     int row0;             // first query token of the sequence in the packed batch
     int unit0;            // first unit
     int nsplit;           // parts that the key range of a row tile is cut into
-    int chunk;            // few-row kernel: keys of a part; wide kernel: query tokens of each member of a group, 0: a sequence
+    int chunk;            // few-row kernel: keys of a part; a group: query tokens of each member
     int part0;            // first row of the sequence's partial results, -1: written straight to the output
     int key0;             // few-row kernel: first key
-    int gpart0;           // parts of the keys before key0, which a group of sequences shares (wide kernel's rows)
+    int gpart0;           // parts of the keys before key0, which a group of sequences shares (GROUP_ROWS rows a unit)
     int gsplit;           // how many, 0: none
     int grow;             // the sequence's first row within the group
     int tok0;             // query tokens of the records before this one
@@ -107,8 +107,10 @@ cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f
                               cudaStream_t st);
 cudaError_t launch_attend_tile(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
 constexpr int WIDE_ROWS = 256;                   // rows of a unit of the wide kernel
+constexpr int GROUP_ROWS = 128;                  // the same over the keys that a group of sequences shares
 bool wide_takes(int D, int BS);                  // pool geometries of the wide kernel
-cudaError_t launch_attend_wide(const AttnParams &p, const SmallSeqs &small, int f16, const void *map, int layer,
+// groups: the records are groups
+cudaError_t launch_attend_wide(const AttnParams &p, const SmallSeqs &small, int f16, bool groups, const void *map, int layer,
                                cudaStream_t st);
 struct alignas(64) PoolMap {                     // a tensor map, opaque to the host side
     unsigned char bytes[128];

@@ -18,6 +18,11 @@
 // others do not raises `flag`: the caller then runs the 64-row kernel over the batch, which keeps such rows apart.
 // The last tile of keys costs the same as a full one, at most 127 keys of it are masked.
 //
+// Weights are rounded to the values' type before O += P V, as the tensor pipe takes them: one more rounding of the output's kind,
+// half a step of each weight, while their sum stays in 32 bits.  A second product with what the rounding left would take the tensor
+// pipe as long again.  Error against 64 bits with 16 contexts of 8699 tokens, 512 of them new: 2.3e-3 of the output's norm, of
+// which the output's own rounding to bf16 is 1.7e-3.
+//
 // Every wait is bounded; one that gives up records AAF_ERR_TIMEOUT and ends the kernel.
 #include <cuda.h>
 
@@ -64,7 +69,14 @@ struct CapPoly {
 };
 
 // MODE: what a score is.  0: a multiple of the product; 1: capped; 2: anything (with a distance bias, or a scale of zero)
-template <typename T, int D, int MODE>
+// GROUP: the rows of contexts forked from one, over the keys that they share.  Each of these contexts would else be attend_few's,
+// which multiplies the weights in two 16-bit parts; so does this variant, for a row must not lose digits because of what else
+// is in the batch.  It has one row tile, and two threads a row: both look at all of a tile's scores, so that they agree on
+// the maximum, and each computes the weights of 64 keys.  Both parts go where the second row tile's scores would be, the low parts'
+// product into the columns of its outputs.  (The sum of the two is the output unless the high parts' product is not finite: an infinite
+// value is infinite there, and times a low part, which may be zero or negative, NaN.)  16 contexts forked at 8187 tokens: 34.6 us a
+// call; 32.5 with the weights rounded once, 40.3 with one thread a row.
+template <typename T, int D, int MODE, bool GROUP>
 __global__ void __launch_bounds__(WIDE_THREADS, 1)
     attend_wide_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small,
                        const __grid_constant__ CUtensorMap map, int layer) {
@@ -88,9 +100,10 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
     const int unit = blockIdx.x / p.H, head = blockIdx.x - unit * p.H;
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
     const AttnSeq sq = seqs[p.first + find_seq(seqs + p.first, p.n, unit)];
+    constexpr int ROWS = GROUP ? GROUP_ROWS : WIDE_ROWS;
     // query token j of the record, its place in the packed batch and the keys it sees
     auto token = [&](int j, int &packed) -> RowSpan {
-        if (sq.chunk == 0) {
+        if (!GROUP) {
             packed = sq.row0 + j;
             return row_span(p, sq, j);
         }
@@ -104,11 +117,11 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
         r.near = 0;
         return r;
     };
-    const int R = sq.nq * p.G, n_tiles = (R + WIDE_ROWS - 1) / WIDE_ROWS;
+    const int R = sq.nq * p.G, n_tiles = (R + ROWS - 1) / ROWS;
     const int u = unit - sq.unit0, part = u % sq.nsplit;
     const int tile = n_tiles - 1 - u / sq.nsplit;  // the latest rows see the most keys: they start first
-    const int r0 = tile * WIDE_ROWS;
-    const bool two = r0 + WIDE_TILE < R;           // the second row tile has rows
+    const int r0 = tile * ROWS;
+    const bool two = !GROUP && r0 + WIDE_TILE < R;  // the second row tile has rows
 
     if (warp == 8) {
         if (lane == 0) {
@@ -138,7 +151,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
     }
     // spans of the two row tiles, each looked at by one warp
     if (warp >= 10) {
-        const int w = warp - 10, a = min(r0 + w * WIDE_TILE, R - 1), b = min(r0 + w * WIDE_TILE + WIDE_TILE - 1, R - 1);
+        const int w = warp - 10, first = r0 + (GROUP ? 0 : w * WIDE_TILE), a = min(first, R - 1), b = min(first + WIDE_TILE - 1, R - 1);
         int lo = 0x7fffffff, hi = 0, lo_max = 0, hi_min = 0x7fffffff;
         for (int j = a / p.G + lane; j <= b / p.G; j += 32) {
             int packed;
@@ -186,11 +199,11 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
     if (warp < 8) {
         // ---------------------------------------------------------------- a thread per row: weights
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        const int w = warp >> 2, rl = (warp & 3) * 32 + lane, rr = r0 + w * WIDE_TILE + rl;
+        const int w = warp >> 2, rl = (warp & 3) * 32 + lane, rr = r0 + (GROUP ? 0 : w) * WIDE_TILE + rl;
         const int rc = min(rr, R - 1), rj = token_of(p, rc), hq = head * p.G + rc - rj * p.G;
         int packed;
         const RowSpan span = token(rj, packed);
-        {   // the warp's 32 rows of queries into the swizzled tile, D / 8 lanes a row (rows behind the last: zeros); a negative
+        if (!GROUP || w == 0) {   // the warp's 32 rows of queries into the swizzled tile, D / 8 lanes a row (rows behind the last: zeros); a negative
             // scale moves into their sign
             constexpr int PIECES = D / 8, AT_ONCE = 32 / PIECES;
             const uint32_t flip = MODE < 2 && p.scale < 0.0f ? 0x80008000u : 0u;
@@ -212,8 +225,8 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                              "r"(v[i].x ^ flip), "r"(v[i].y ^ flip), "r"(v[i].z ^ flip), "r"(v[i].w ^ flip) : "memory");
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            bar_arrive(q_ready);
         }
+        bar_arrive(q_ready);
         const float slope = MODE == 2 && p.slopes ? p.slopes[hq] : 0.0f;
         int w_lo_max = span.lo, w_hi_min = span.hi;
 #pragma unroll
@@ -222,13 +235,14 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             w_hi_min = min(w_hi_min, __shfl_xor_sync(0xffffffffu, w_hi_min, d));
         }
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tS = tmem + lanes + w * 128, tP = tS + 64, tO = tmem + lanes + 256 + w * D;
+        const int rt = GROUP ? 0 : w;  // row tile
+        const uint32_t tS = tmem + lanes + rt * 128, tP = GROUP ? tmem + lanes + 128 : tS + 64, tO = tmem + lanes + 256 + w * D;
         const float c = fabsf(p.scale) * LOG2E, k1 = fabsf(p.scale) * p.inv_cap, cap2 = p.softcap * LOG2E;
         const CapPoly capped(c, k1);
         constexpr float GROWTH = 8.0f;  // how far (log2) a score may outgrow the maximum in use
         constexpr float RAISE = Elt<T>::RAISE > 0.0f ? Elt<T>::RAISE - GROWTH : 0.0f;
         float m = -CUDART_INF_F, l = 0.0f;
-        const bool active = w == 0 || two;
+        const bool active = GROUP || w == 0 || two;
         bool ok = true;
         // weights of two keys: scores are multiples of the products, or, with a cap and all of them small, a polynomial
         auto pair_of = [&](float s0, float s1, float times, float base, auto poly) -> f2 {
@@ -246,10 +260,35 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             tmem_wait_st();
             tmem_before();
             __syncwarp();
-            if (lane == 0) bar_arrive((h ? p_rest : p_ready) + 8 * w);
+            if (lane == 0) bar_arrive((h ? p_rest : p_ready) + 8 * rt);
+        };
+        // a tile's largest score against the maximum in use: 0, it serves; 1, it is another one now; -1, a wait gave up
+        auto settle = [&](int j, float most, float times, auto poly) -> int {
+            const float top = poly.value && most > -CUDART_INF_F ? cap2 * tanh_f32(most * k1) : most * times;
+            // the first maximum, or one that outgrew the one in use
+            const bool grow = top > m + GROWTH || (m == -CUDART_INF_F && top > m);
+            if (!__any_sync(0xffffffffu, grow)) return 0;
+            const float f = grow && m != -CUDART_INF_F ? ex2(m - top) : 1.0f;
+            if (grow) m = top;
+            l *= f;
+            if (j > 0 && __any_sync(0xffffffffu, f != 1.0f)) {
+                if (!warp_wait(o_done + 8 * rt, (j - 1) & 1, &sh_abort, p.status)) return -1;
+                tmem_after();
+#pragma unroll 1
+                for (int d = 0; d < D; d += 16) {
+                    float o[16];
+                    tmem_ld16(tO + d, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] *= f;
+                    tmem_st16(tO + d, reinterpret_cast<const uint32_t *>(o));
+                }
+                tmem_wait_st();
+            }
+            return 1;
         };
         for (int j = 0; active && j < tiles; ++j) {
-            if (!(ok = warp_wait(s_full + 8 * w, j & 1, &sh_abort, p.status))) break;
+            if (!(ok = warp_wait(s_full + 8 * rt, j & 1, &sh_abort, p.status))) break;
             tmem_after();
             float s[128];
 #pragma unroll
@@ -295,6 +334,30 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             auto weights = [&](auto poly) -> bool {
                 uint32_t pk[32];
                 f2 sums[2];
+                if constexpr (GROUP) {
+                    float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+                    for (int i = 4; i < 128; ++i) mx[i & 3] = fmaxf(mx[i & 3], s[i]);
+                    if (settle(j, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), times, poly) < 0) return false;
+                    const float base = m == -CUDART_INF_F ? 0.0f : m - RAISE;
+                    uint32_t low[32];  // what the rounding leaves of the weights
+                    sums[0] = sums[1] = 0;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const f2 x = pair_of(w ? s[64 + 2 * i] : s[2 * i], w ? s[65 + 2 * i] : s[2 * i + 1], times, base, poly);
+                        sums[i & 1] = add2(sums[i & 1], x);
+                        float a, b;
+                        unpair(x, a, b);
+                        pk[i] = Elt<T>::pack(a, b);
+                        low[i] = Elt<T>::pack(a - Elt<T>::lo(pk[i]), b - Elt<T>::hi(pk[i]));
+                    }
+                    tmem_st32(tP + 64 + 32 * w, low);
+                    done_half(w, pk);
+                    float a, b;
+                    unpair(add2(sums[0], sums[1]), a, b);
+                    l += a + b;
+                    return true;
+                }
                 // The maximum in use serves this tile too unless a score outgrows it by 2^8, so the first half of the weights is
                 // computed beside the tile's maximum, not behind it, and once more in the tiles where it was too small.
                 for (;;) {
@@ -311,27 +374,9 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                         mx[i & 3] = fmaxf(fmaxf(fmaxf(mx[i & 3], s[4 * i]), fmaxf(s[4 * i + 1], s[4 * i + 2])), s[4 * i + 3]);
                     }
                     const float most = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                    const float top = poly.value && most > -CUDART_INF_F ? cap2 * tanh_f32(most * k1) : most * times;
-                    // the first maximum, or one that outgrew the one in use
-                    const bool grow = top > m + GROWTH || (m == -CUDART_INF_F && top > m);
-                    if (!__any_sync(0xffffffffu, grow)) break;
-                    const float f = grow && m != -CUDART_INF_F ? ex2(m - top) : 1.0f;
-                    if (grow) m = top;
-                    l *= f;
-                    if (j > 0 && __any_sync(0xffffffffu, f != 1.0f)) {
-                        if (!warp_wait(o_done + 8 * w, (j - 1) & 1, &sh_abort, p.status)) return false;
-                        tmem_after();
-#pragma unroll 1
-                        for (int d = 0; d < D; d += 16) {
-                            float o[16];
-                            tmem_ld16(tO + d, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] *= f;
-                            tmem_st16(tO + d, reinterpret_cast<const uint32_t *>(o));
-                        }
-                        tmem_wait_st();
-                    }
+                    const int changed = settle(j, most, times, poly);
+                    if (changed < 0) return false;
+                    if (!changed) break;
                 }
                 done_half(0, pk);
                 const float base = m == -CUDART_INF_F ? 0.0f : m - RAISE;
@@ -356,24 +401,40 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             if (!ok) break;
         }
         if (ok && active && tiles > 0) {
-            ok = warp_wait(o_done + 8 * w, (tiles - 1) & 1, &sh_abort, p.status);
+            ok = warp_wait(o_done + 8 * rt, (tiles - 1) & 1, &sh_abort, p.status);
             tmem_after();
+        }
+        if (GROUP) {  // the row's other sum; the place of the second row tile's queries is free
+            float *other = reinterpret_cast<float *>(smem_raw + S::TILE_BYTES);
+            if (!w) other[rl] = l;
+            asm volatile("bar.sync 1, 256;" ::: "memory");  // every weights' warp comes here, whatever it waited for in vain
+            const float first = other[rl];
+            if (w) other[128 + rl] = l;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            l = first + other[128 + rl];
         }
         if (ok && active) {
             const bool live = rr < R;
             const bool part_out = sq.part0 >= 0;
             const long long qt = packed;
-            const long long pr = sq.part0 + (((long long)tile * sq.nsplit + part) * p.H + head) * WIDE_ROWS + w * WIDE_TILE + rl;
+            const long long pr = sq.part0 + (((long long)tile * sq.nsplit + part) * p.H + head) * ROWS + rt * WIDE_TILE + rl;
             const float inv = l > 0.0f || l != l ? (part_out ? 1.0f : 1.0f / l) : 0.0f;  // a row that sees nothing is zero
             T *out = static_cast<T *>(p.out) + (qt * p.H * p.G + hq) * D;
             float *part_o = p.part_o + pr * D;
 #pragma unroll 1
-            for (int d = 0; d < D; d += 32) {
+            for (int d = GROUP ? w * (D / 2) : 0; d < (GROUP && !w ? D / 2 : D); d += 32) {
                 float o[32];
                 __syncwarp();
                 if (tiles > 0) {
-                    tmem_ld32(tO + d, o);
+                    tmem_ld32(tmem + lanes + 256 + rt * D + d, o);
                     tmem_wait_ld();
+                }
+                if (GROUP && tiles > 0) {
+                    float low[32];
+                    tmem_ld32(tmem + lanes + 256 + D + d, low);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] += fabsf(o[i]) < CUDART_INF_F ? low[i] : 0.0f;
                 }
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = tiles > 0 ? scaled(o[i], inv) : 0.0f;
@@ -389,7 +450,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                                        Elt<T>::pack(o[i + 4], o[i + 5]), Elt<T>::pack(o[i + 6], o[i + 7]));
                 }
             }
-            if (live && part_out) {
+            if (live && part_out) {  // (both threads of a group's row write the same)
                 p.part_ml[2 * pr] = m - RAISE;
                 p.part_ml[2 * pr + 1] = l;
             } else if (live && p.lse) {
@@ -467,7 +528,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
             constexpr uint32_t PV = 1u << 4 | F << 7 | F << 10 | 1u << 16 | (D / 8) << 17 | (WIDE_TILE / 16) << 24;
             const int n_tile = __shfl_sync(0xffffffffu, tiles, 0), w = __shfl_sync(0xffffffffu, warp == 9 ? 0 : 1, 0);
             const uint64_t dQ = smem_desc(sQ, 16, 1024) + w * (S::TILE_BYTES >> 4), dK = smem_desc(sKV, 16, 1024), dV = smem_desc(sKV, 16384, 1024);
-            const uint32_t tS = w * 128, tO = 256 + w * D;
+            const uint32_t tS = w * 128, tP = GROUP ? 128 : tS + 64, tO = 256 + w * D;
             auto scores = [&](int stage, bool release) {
                 if (elected()) {
                     uint64_t a = dQ, b = dK + stage * (S::TILE_BYTES >> 4);
@@ -501,16 +562,19 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
                 if (two && (w || j) && !(ok = warp_wait(turn + 8 * w, w ? j & 1 : (j - 1) & 1, &sh_abort, p.status))) break;
                 if (!(ok = warp_wait(p_ready + 8 * w, j & 1, &sh_abort, p.status))) break;
                 tmem_after();
-                if (elected()) {
+                if (!GROUP && elected()) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_ts(tO, tS + 64 + 8 * k, b + k * (2048 >> 4), PV, j > 0 || k > 0);
+                    for (int k = 0; k < 4; ++k) mma_ts(tO, tP + 8 * k, b + k * (2048 >> 4), PV, j > 0 || k > 0);
                 }
                 __syncwarp();
                 if (!(ok = warp_wait(p_rest + 8 * w, j & 1, &sh_abort, p.status))) break;
                 tmem_after();
                 if (elected()) {
 #pragma unroll
-                    for (int k = 4; k < 8; ++k) mma_ts(tO, tS + 64 + 8 * k, b + k * (2048 >> 4), PV, 1);
+                    for (int k = GROUP ? 0 : 4; k < 8; ++k) {  // a group's first half too: the second half's warps may still rescale outputs
+                        mma_ts(tO, tP + 8 * k, b + k * (2048 >> 4), PV, j > 0 || k > 0);
+                        if (GROUP) mma_ts(tO + D, tP + 64 + 8 * k, b + k * (2048 >> 4), PV, j > 0 || k > 0);
+                    }
                     mma_commit(o_done + 8 * w);
                     if (2 * j + 1 + S::STAGES < loads) mma_commit(empty + 8 * sv);
                 }
@@ -537,26 +601,27 @@ __global__ void __launch_bounds__(WIDE_THREADS, 1)
 
 bool wide_takes(int D, int BS) { return (D == 64 || D == 128) && BS >= 8 && BS <= WIDE_KEYS && (BS & (BS - 1)) == 0; }
 
-template <typename T, int D, int MODE>
+template <typename T, int D, int MODE, bool GROUP>
 static cudaError_t wide_go(const AttnParams &p, const SmallSeqs &small, const void *map, int layer, cudaStream_t st) {
     static unsigned long long seen = 0;
-    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_wide_kernel<T, D, MODE>), WideShape<D>::SMEM, &seen);
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_wide_kernel<T, D, MODE, GROUP>), WideShape<D>::SMEM, &seen);
     if (e != cudaSuccess) return e;
-    attend_wide_kernel<T, D, MODE><<<(unsigned)((long long)p.total_units * p.H), WIDE_THREADS, WideShape<D>::SMEM, st>>>(
+    attend_wide_kernel<T, D, MODE, GROUP><<<(unsigned)((long long)p.total_units * p.H), WIDE_THREADS, WideShape<D>::SMEM, st>>>(
         p, small, *static_cast<const CUtensorMap *>(map), layer);
     return cudaGetLastError();
 }
-template <typename T> static cudaError_t wide_pick(const AttnParams &p, const SmallSeqs &small, const void *map, int layer, cudaStream_t st) {
+template <typename T, int D, bool GROUP>
+static cudaError_t wide_mode(const AttnParams &p, const SmallSeqs &small, const void *map, int layer, cudaStream_t st) {
     // a scale of zero would undo a mask (0 * -inf) where scores are multiples of the product
-    const int mode = p.slopes || p.scale == 0.0f ? 2 : (p.softcap != 0.0f ? 1 : 0);
-    if (p.D == 64)
-        return mode == 0 ? wide_go<T, 64, 0>(p, small, map, layer, st)
-                         : (mode == 1 ? wide_go<T, 64, 1>(p, small, map, layer, st) : wide_go<T, 64, 2>(p, small, map, layer, st));
-    return mode == 0 ? wide_go<T, 128, 0>(p, small, map, layer, st)
-                     : (mode == 1 ? wide_go<T, 128, 1>(p, small, map, layer, st) : wide_go<T, 128, 2>(p, small, map, layer, st));
+    if (p.slopes || p.scale == 0.0f) return wide_go<T, D, 2, GROUP>(p, small, map, layer, st);
+    return p.softcap != 0.0f ? wide_go<T, D, 1, GROUP>(p, small, map, layer, st) : wide_go<T, D, 0, GROUP>(p, small, map, layer, st);
 }
-cudaError_t launch_attend_wide(const AttnParams &p, const SmallSeqs &small, int f16, const void *map, int layer, cudaStream_t st) {
-    return f16 ? wide_pick<__half>(p, small, map, layer, st) : wide_pick<__nv_bfloat16>(p, small, map, layer, st);
+template <typename T> static cudaError_t wide_pick(const AttnParams &p, const SmallSeqs &small, bool groups, const void *map, int layer, cudaStream_t st) {
+    if (p.D == 64) return groups ? wide_mode<T, 64, true>(p, small, map, layer, st) : wide_mode<T, 64, false>(p, small, map, layer, st);
+    return groups ? wide_mode<T, 128, true>(p, small, map, layer, st) : wide_mode<T, 128, false>(p, small, map, layer, st);
+}
+cudaError_t launch_attend_wide(const AttnParams &p, const SmallSeqs &small, int f16, bool groups, const void *map, int layer, cudaStream_t st) {
+    return f16 ? wide_pick<__half>(p, small, groups, map, layer, st) : wide_pick<__nv_bfloat16>(p, small, groups, map, layer, st);
 }
 
 // Tensor map of a whole pool: [layer][slot of a block's keys or values][kv head and dim], boxes of a block's slots, 64 dims.

@@ -1460,17 +1460,17 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
             g.chunk = few[i].nq;
             g.nq = (int)(members * g.chunk);
             g.row0 = (int)i;
-            const long long tiles = ((long long)g.nq * G + WIDE_ROWS - 1) / WIDE_ROWS;
+            const long long tiles = ((long long)g.nq * G + GROUP_ROWS - 1) / GROUP_ROWS;
             long long parts = std::max<long long>(1, std::min(p->sm_count / (tiles * H), (shared + 255) / 256));
             // its partial results, and one part of each member's own keys, have to fit into half of the workspace
             const long long room = PART_ROWS / 2 - part_rows - own_rows - members * H * g.chunk * G;
-            while (parts > 1 && tiles * parts * H * WIDE_ROWS > room) --parts;
-            if (tiles * parts * H * WIDE_ROWS > room) continue;
+            while (parts > 1 && tiles * parts * H * GROUP_ROWS > room) --parts;
+            if (tiles * parts * H * GROUP_ROWS > room) continue;
             own_rows += members * H * g.chunk * G;
             g.nsplit = (int)parts;
             g.unit0 = group_units;
             g.part0 = (int)part_rows;
-            part_rows += tiles * parts * H * WIDE_ROWS;
+            part_rows += tiles * parts * H * GROUP_ROWS;
             group_units += (int)(tiles * parts);
             for (size_t m = i; m < e; ++m) {
                 few[m].key0 = (int)shared;
@@ -1582,7 +1582,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
             kg.first = (int)n_few;
             kg.n = (int)(few.size() - n_few);
             kg.total_units = group_units;
-            ok = launch_attend_wide(kg, small, f16, &p->map, layer, st) == cudaSuccess;
+            ok = launch_attend_wide(kg, small, f16, true, &p->map, layer, st) == cudaSuccess;
         }
         if (ok && few_units) ok = launch_attend_few(kf, small, f16, few_rows, few_tokens == (int)n_few, group_units > 0, st) == cudaSuccess;
         if (ok && few_joined) ok = launch_attend_join(kf, small, f16, 0, few_tokens, few_parts, p->sm_count, st) == cudaSuccess;
@@ -1597,7 +1597,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
         if (wide) {
             km.flag = reinterpret_cast<int *>(k.part_ml + 2 * PART_ROWS);
             km.epoch = next_epoch();
-            ok = ok && launch_attend_wide(km, small, f16, &p->map, layer, st) == cudaSuccess;
+            ok = ok && launch_attend_wide(km, small, f16, false, &p->map, layer, st) == cudaSuccess;
         } else {
             ok = ok && launch_attend_tile(km, small, f16, st) == cudaSuccess;
         }

@@ -280,7 +280,7 @@ bool wide_takes(int, int) { return true; }
 bool encode_pool_map(const Geom &, PoolMap *) { return true; }
 cudaError_t launch_attend_few(const AttnParams &, const SmallSeqs &, int, int, bool, bool, cudaStream_t st) { return launch("attend", st); }
 cudaError_t launch_attend_tile(const AttnParams &, const SmallSeqs &, int, cudaStream_t st) { return launch("attend", st); }
-cudaError_t launch_attend_wide(const AttnParams &, const SmallSeqs &, int, const void *, int, cudaStream_t st) { return launch("attend", st); }
+cudaError_t launch_attend_wide(const AttnParams &, const SmallSeqs &, int, bool, const void *, int, cudaStream_t st) { return launch("attend", st); }
 cudaError_t launch_attend_join(const AttnParams &, const SmallSeqs &, int, int, int, int, int, cudaStream_t st) { return launch("join", st); }
 cudaError_t launch_attn_mass(const MassParams &, const SmallSeqs &, int, int, cudaStream_t st) { return launch("mass", st); }
 cudaError_t launch_attn_mass_wide(const MassParams &, const SmallSeqs &, int, const void *, int, cudaStream_t st) { return launch("mass", st); }

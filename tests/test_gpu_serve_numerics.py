@@ -86,3 +86,32 @@ def test_bias_of_distances_that_32_bits_cannot_tell_apart(dim, n_q):
     R.check_attend((out, None), (torch.stack(refs), None, torch.stack(slacks), big), torch.bfloat16, dim, True)
     ref = torch.stack(lses)
     assert ((lse.double() - ref).abs() <= 4 * 2.0 ** -24 * ref.abs() + 2.0 ** -10).all()
+
+
+@pytest.mark.parametrize("opts", [{}, dict(softcap=20.0), dict(slopes=True)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim,heads,group,members,shared,n_q", [(128, 8, 4, 16, 1000, 1), (128, 8, 4, 9, 2100, 3), (64, 2, 8, 40, 1000, 1),
+                                                                (64, 2, 8, 70, 1500, 2), (128, 1, 16, 33, 2049, 1)])
+def test_forked_contexts_lose_no_digits_to_the_shared_reading(dim, heads, group, members, shared, n_q, dtype, opts):
+    """Rows of contexts forked from one come out as exact as a single context's: weights in two 16-bit parts."""
+    pool = R.make_pool(1, heads, dim, 16, shared // 16 + members * 8 + 4, max_ctx=members + 2, dtype=dtype)
+    parent = R.add_ctx(pool, shared, 1)
+    st, kids = pool.fork(parent.handle, members)
+    assert st == 0
+    own = [1 + n_q + 7 * i % 50 for i in range(members)]
+    tails = [R.rand((1, 2, t, heads, dim), 100 + i, dtype) for i, t in enumerate(own)]
+    assert pool.append(kids, own, tails)[0] == 0
+    ctxs = [R.Ctx(h, torch.cat((parent.rows, t), 2)) for h, t in zip(kids, tails)]
+    q = R.rand((members * n_q, heads * group, dim), 2, dtype, 2.0)
+    if opts.get("slopes"):
+        opts = dict(slopes=torch.linspace(0.001, 0.02, heads * group, device="cuda"))
+    st, got = pool.attend(0, kids, [n_q] * members, q, **opts)
+    assert st == 0
+    torch.cuda.synchronize()
+    assert pool.sync_status() == 0
+    st, again = pool.attend(0, kids, [n_q] * members, q, **opts)
+    assert st == 0 and all(torch.equal(x, y) for x, y in zip(got, again))
+    out, lse, slack, big = R.attend_ref(ctxs, [n_q] * members, q, **opts)
+    if "slopes" in opts:
+        big += 0.02 * (shared + 64)  # the bias is a part of the score, rounded as it is
+    R.check_attend(got, (out, lse, slack, big), dtype, dim, False)
