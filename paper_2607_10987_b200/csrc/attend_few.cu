@@ -323,7 +323,7 @@ int few_rows_limit(int D) { return D <= 64 ? 32 : (D <= 128 ? 16 : 8); }
 
 template <typename T, int DP, int NT, bool SIMPLE>
 static cudaError_t few_go(const AttnParams &p, const SmallSeqs &small, bool beside, cudaStream_t st) {
-    static unsigned long long seen = 0;
+    static SmemSeen seen{0};
     cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_few_kernel<T, DP, NT, SIMPLE>), FewShape<DP>::SMEM, &seen);
     if (e != cudaSuccess) return e;
     constexpr int W = FewShape<DP>::WARPS;

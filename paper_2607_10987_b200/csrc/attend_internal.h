@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "aafkv_internal.h"
 
 namespace aafkv {
@@ -87,13 +89,15 @@ struct StoreParams {
     float mscale;
 };
 
-// Shared memory beyond 48 KB is allowed once per kernel and device; `seen` is the kernel's own.
-inline cudaError_t allow_smem(const void *kernel, int bytes, unsigned long long *seen) {
+// Shared memory beyond 48 KB is allowed once per kernel and device; `seen` is the kernel's own.  Pools of several threads share it:
+// two that come first together both ask, which does no harm.
+typedef std::atomic<unsigned long long> SmemSeen;
+inline cudaError_t allow_smem(const void *kernel, int bytes, SmemSeen *seen) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess || (dev < 64 && (*seen >> dev & 1))) return e;
+    if (e != cudaSuccess || (dev < 64 && (seen->load(std::memory_order_acquire) >> dev & 1))) return e;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess && dev < 64) *seen |= 1ull << dev;
+    if (e == cudaSuccess && dev < 64) seen->fetch_or(1ull << dev, std::memory_order_release);
     return e;
 }
 

@@ -216,7 +216,7 @@ template <typename T, int DP> static cudaError_t mass_go(const MassParams &p, co
     using S = MassShape<DP>;
     const int block = min((max_rows + 7) / 8 * 8, S::ROWS), rows = (int)min((long long)S::ROWS, (long long)block * p.a.H);
     const int smem = S::K_BYTES + rows * S::ROW;
-    static unsigned long long seen = 0;
+    static SmemSeen seen{0};
     const cudaError_t e = allow_smem(reinterpret_cast<const void *>(attn_mass_kernel<T, DP>), S::K_BYTES + S::ROWS * S::ROW, &seen);
     if (e != cudaSuccess) return e;
     attn_mass_kernel<T, DP><<<(unsigned)p.a.total_units, MASS_WARPS * 32, smem, st>>>(p, small);

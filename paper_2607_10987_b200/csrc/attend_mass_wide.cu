@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(MW_THREADS, 1)
 }
 
 template <typename T, int D> static cudaError_t mass_wide_go(const MassParams &p, const SmallSeqs &small, const void *map, int layer, cudaStream_t st) {
-    static unsigned long long seen = 0;
+    static SmemSeen seen{0};
     const cudaError_t e = allow_smem(reinterpret_cast<const void *>(attn_mass_wide_kernel<T, D>), MassWideShape<D>::SMEM, &seen);
     if (e != cudaSuccess) return e;
     attn_mass_wide_kernel<T, D><<<(unsigned)p.a.total_units, MW_THREADS, MassWideShape<D>::SMEM, st>>>(

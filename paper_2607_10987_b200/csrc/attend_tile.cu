@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
 }
 
 template <typename T, int DP> static cudaError_t tile_go(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
-    static unsigned long long seen = 0;
+    static SmemSeen seen{0};
     const cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_tile_kernel<T, DP>), TileShape<DP>::SMEM, &seen);
     if (e != cudaSuccess) return e;
     long long ctas = (long long)p.total_units * p.H;

@@ -603,7 +603,7 @@ bool wide_takes(int D, int BS) { return (D == 64 || D == 128) && BS >= 8 && BS <
 
 template <typename T, int D, int MODE, bool GROUP>
 static cudaError_t wide_go(const AttnParams &p, const SmallSeqs &small, const void *map, int layer, cudaStream_t st) {
-    static unsigned long long seen = 0;
+    static SmemSeen seen{0};
     const cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_wide_kernel<T, D, MODE, GROUP>), WideShape<D>::SMEM, &seen);
     if (e != cudaSuccess) return e;
     attend_wide_kernel<T, D, MODE, GROUP><<<(unsigned)((long long)p.total_units * p.H), WIDE_THREADS, WideShape<D>::SMEM, st>>>(

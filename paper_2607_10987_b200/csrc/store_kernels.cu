@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(SELECT_THREADS)
 cudaError_t launch_select(const float *scores, int len, int budget, int sink, int recent, int *kept, float *kept_scores,
                           cudaStream_t st) {
     const int n = len - sink - recent, cached = n <= SELECT_CACHED;
-    static unsigned long long seen = 0;
+    static SmemSeen seen{0};
     const cudaError_t e = allow_smem(reinterpret_cast<const void *>(select_kernel), SELECT_CACHED * 4, &seen);
     if (e != cudaSuccess) return e;
     select_kernel<<<1, SELECT_THREADS, cached ? 4 * (size_t)n : 0, st>>>(scores, len, budget, sink, recent, kept, kept_scores, cached);

@@ -339,3 +339,16 @@ def test_tokens_of_2_to_the_31_elements_are_refused(lib, pool):
     for call in (pool.attend, pool.mass):
         assert call(st, [c], heads=most)
         assert not call(st, [c], heads=most + H, want=B.AAF_ERR_INVALID_ARG)
+
+
+def test_threads_with_a_pool_each_launch_a_kernel_for_the_first_time(tmp_path):
+    out = str(tmp_path / "threads")
+    gcc = ["g++", "-std=c++17", "-O1", "-g", "-pthread", "-fsanitize=thread"]
+    if subprocess.run(gcc + ["-x", "c++", "-", "-o", out], input="int main() {}", text=True, capture_output=True).returncode or \
+            subprocess.run([out], capture_output=True).returncode:
+        pytest.skip("no thread sanitizer here")
+    subprocess.check_call(gcc + ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", os.path.join(CUDA, "include"),
+                                 os.path.join(ROOT, "tests", "smem_threads.cpp"), "-o", out])
+    run = subprocess.run([out], capture_output=True, text=True)
+    assert "WARNING: ThreadSanitizer" not in run.stderr, run.stderr
+    assert run.returncode == 0, run.stderr
