@@ -109,7 +109,7 @@ constexpr int MASS_CHUNK = 64;                   // keys of a CTA of the mass ke
 // single: one query token each; beside: brought up beside the kernel launched before it, which it does not depend on
 cudaError_t launch_attend_few(const AttnParams &p, const SmallSeqs &small, int f16, int max_rows, bool single, bool beside,
                               cudaStream_t st);
-cudaError_t launch_attend_tile(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
+cudaError_t launch_attend_tile(const AttnParams &p, const SmallSeqs &small, int f16, int sm_count, cudaStream_t st);
 constexpr int WIDE_ROWS = 256;                   // rows of a unit of the wide kernel
 constexpr int GROUP_ROWS = 128;                  // the same over the keys that a group of sequences shares
 bool wide_takes(int D, int BS);                  // pool geometries of the wide kernel
@@ -126,7 +126,7 @@ cudaError_t launch_attn_mass(const MassParams &p, const SmallSeqs &small, int f1
 constexpr int MASS_WIDE_CHUNK = 256;             // keys of a CTA of the mass kernel for many rows
 cudaError_t launch_attn_mass_wide(const MassParams &p, const SmallSeqs &small, int f16, const void *map, int layer,
                                   cudaStream_t st);
-cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16, cudaStream_t st);
+cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16, int sm_count, cudaStream_t st);
 // keep list of a pruned context: kept[budget] ascending, kept_scores (may be null); then the row gather
 cudaError_t launch_select(const float *scores, int len, int budget, int sink, int recent, int *kept, float *kept_scores,
                           cudaStream_t st);

@@ -270,22 +270,22 @@ __global__ void __launch_bounds__(TILE_WARPS * 32)
     }
 }
 
-template <typename T, int DP> static cudaError_t tile_go(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
+template <typename T, int DP> static cudaError_t tile_go(const AttnParams &p, const SmallSeqs &small, int sm_count, cudaStream_t st) {
     static SmemSeen seen{0};
     const cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_tile_kernel<T, DP>), TileShape<DP>::SMEM, &seen);
     if (e != cudaSuccess) return e;
     long long ctas = (long long)p.total_units * p.H;
-    if (p.flag && ctas > 296) ctas = 296;
+    if (p.flag) ctas = min(ctas, 2ll * sm_count);  // what the GPU holds at once: most often they return at once
     attend_tile_kernel<T, DP><<<(unsigned)ctas, TILE_WARPS * 32, TileShape<DP>::SMEM, st>>>(p, small);
     return cudaGetLastError();
 }
-template <typename T> static cudaError_t tile_pick(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
-    if (p.D <= 64) return tile_go<T, 64>(p, small, st);
-    if (p.D <= 128) return tile_go<T, 128>(p, small, st);
-    return tile_go<T, 256>(p, small, st);
+template <typename T> static cudaError_t tile_pick(const AttnParams &p, const SmallSeqs &small, int sm_count, cudaStream_t st) {
+    if (p.D <= 64) return tile_go<T, 64>(p, small, sm_count, st);
+    if (p.D <= 128) return tile_go<T, 128>(p, small, sm_count, st);
+    return tile_go<T, 256>(p, small, sm_count, st);
 }
-cudaError_t launch_attend_tile(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st) {
-    return f16 ? tile_pick<__half>(p, small, st) : tile_pick<__nv_bfloat16>(p, small, st);
+cudaError_t launch_attend_tile(const AttnParams &p, const SmallSeqs &small, int f16, int sm_count, cudaStream_t st) {
+    return f16 ? tile_pick<__half>(p, small, sm_count, st) : tile_pick<__nv_bfloat16>(p, small, sm_count, st);
 }
 
 }  // namespace aafkv

@@ -1599,7 +1599,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
             km.epoch = next_epoch();
             ok = ok && launch_attend_wide(km, small, f16, false, &p->map, layer, st) == cudaSuccess;
         } else {
-            ok = ok && launch_attend_tile(km, small, f16, st) == cudaSuccess;
+            ok = ok && launch_attend_tile(km, small, f16, p->sm_count, st) == cudaSuccess;
         }
         if (ok && many_joined) {
             AttnParams kj = km;
@@ -1608,7 +1608,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
         }
         if (ok && wide) {
             km.total_units = again_units;
-            ok = place_records(p, again, small, &km.seqs, 3, st) && launch_attend_tile(km, small, f16, st) == cudaSuccess;
+            ok = place_records(p, again, small, &km.seqs, 3, st) && launch_attend_tile(km, small, f16, p->sm_count, st) == cudaSuccess;
         }
     }
     return ok && end_read(p, st) ? AAF_OK : broke(p);
@@ -1739,7 +1739,7 @@ int aaf_kv_store(aaf_kv_pool *p, int32_t layer, const aaf_kv_store_desc *d, int3
     if (!begin_read(p, ctxs, n, st)) return broke(p);
     SmallStores small;
     const bool ok = place_records(p, rec, small, &k.seqs, 0, st) &&
-                    launch_store(k, small, d->dtype == AAF_DTYPE_F16, st) == cudaSuccess;
+                    launch_store(k, small, d->dtype == AAF_DTYPE_F16, p->sm_count, st) == cudaSuccess;
     return ok && end_read(p, st) ? AAF_OK : broke(p);
 } catch (const std::bad_alloc &) {
     return AAF_ERR_INVALID_ARG;  // the host has no memory for the records; nothing was launched

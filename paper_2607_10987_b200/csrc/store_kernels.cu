@@ -155,9 +155,9 @@ __global__ void __launch_bounds__(STORE_THREADS)
     copy_heads(static_cast<const T *>(p.v), p.v_stride, p.H, 2);
 }
 
-cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16, cudaStream_t st) {
-    // tokens of a CTA: enough CTAs for every SM while there are few tokens, at most 4 (41 us; 44 at 6 and 8) and the angle table's room
-    int tokens = max(1, min(STORE_TOKENS, p.total / 1184));
+cudaError_t launch_store(const StoreParams &p, const SmallStores &small, int f16, int sm_count, cudaStream_t st) {
+    // tokens of a CTA: eight CTAs an SM while there are few tokens, at most 4 (41 us; 44 at 6 and 8) and the angle table's room
+    int tokens = max(1, min(STORE_TOKENS, p.total / (8 * sm_count)));
     if (p.rot) tokens = max(1, min(tokens, STORE_ANGLES / (p.rot / 2)));
     const unsigned grid = (unsigned)((p.total + tokens - 1) / tokens);
     if (f16)

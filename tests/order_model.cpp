@@ -279,12 +279,12 @@ int few_rows_limit(int D) { return D <= 64 ? 32 : (D <= 128 ? 16 : 8); }
 bool wide_takes(int, int) { return true; }
 bool encode_pool_map(const Geom &, PoolMap *) { return true; }
 cudaError_t launch_attend_few(const AttnParams &, const SmallSeqs &, int, int, bool, bool, cudaStream_t st) { return launch("attend", st); }
-cudaError_t launch_attend_tile(const AttnParams &, const SmallSeqs &, int, cudaStream_t st) { return launch("attend", st); }
+cudaError_t launch_attend_tile(const AttnParams &, const SmallSeqs &, int, int, cudaStream_t st) { return launch("attend", st); }
 cudaError_t launch_attend_wide(const AttnParams &, const SmallSeqs &, int, bool, const void *, int, cudaStream_t st) { return launch("attend", st); }
 cudaError_t launch_attend_join(const AttnParams &, const SmallSeqs &, int, int, int, int, int, cudaStream_t st) { return launch("join", st); }
 cudaError_t launch_attn_mass(const MassParams &, const SmallSeqs &, int, int, cudaStream_t st) { return launch("mass", st); }
 cudaError_t launch_attn_mass_wide(const MassParams &, const SmallSeqs &, int, const void *, int, cudaStream_t st) { return launch("mass", st); }
-cudaError_t launch_store(const StoreParams &, const SmallStores &, int, cudaStream_t st) { return launch("store", st); }
+cudaError_t launch_store(const StoreParams &, const SmallStores &, int, int, cudaStream_t st) { return launch("store", st); }
 cudaError_t launch_select(const float *, int, int, int, int, int *, float *, cudaStream_t st) { return launch("select", st); }
 cudaError_t launch_gather_rows(const Geom &, const int *, const Piece *, const int *, int, int, cudaStream_t st) {
     return launch("gather", st);
