@@ -1301,7 +1301,12 @@ int aaf_kv_evict_to_budget(aaf_kv_pool *p, double alpha, double beta, double gam
 namespace {
 
 constexpr long long PART_ROWS = 65536;  // rows of partial results that a workspace holds
-constexpr long long SHARED_MIN = 16ll << 20;
+// Bytes of shared keys and values that a group of forked contexts does not read again, from which on it is formed: a launch more and a
+// longer join against what is then read from L2, which keeps it within a call.  Microseconds of a decode step with and without
+// groups (2 KB of keys a token), 16 contexts with 512 tokens of their own: 120 MiB 26.9 and 25.2, 240 MiB 29.8 and 37.5,
+// 480 MiB 35.5 and 61.8; 64 contexts with 64: 126 MiB 38.1 and 32.7, 252 MiB 38.3 and 38.4, 504 MiB 38.2 and 70.6; 4 contexts
+// with 512: 24 MiB 20.1 and 17.5, 96 MiB 27.1 and 23.1.
+constexpr long long SHARED_MIN = 192ll << 20;
 
 size_t attend_ws_bytes(const aaf_kv_pool *p) { return (size_t)PART_ROWS * ((size_t)p->g.D + 2) * sizeof(float) + 16; }
 
@@ -1439,9 +1444,7 @@ int aaf_kv_attend(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, int32_t n
     const size_t n_few = few.size();
     if (forked && p->map_ok && !k.window && !k.spans) {
         // Forked contexts: the blocks they share are read once for all of them (the wide kernel takes the members' rows together),
-        // each reads what is its own.  Worth a launch more and a longer join from about SHARED_MIN bytes that are not
-        // read again.
-        // Only queries behind the shared keys: every row of a group then sees all of them.
+        // each reads what is its own.  Only queries behind the shared keys: every row of a group then sees all of them.
         auto group_of = [&](const AttnSeq &x) {
             return (long long)x.len - x.nq + 1 >= p->fork_len[x.ctx] ? p->fork_id[x.ctx] : 0;
         };

@@ -90,8 +90,8 @@ def test_bias_of_distances_that_32_bits_cannot_tell_apart(dim, n_q):
 
 @pytest.mark.parametrize("opts", [{}, dict(softcap=20.0), dict(slopes=True)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("dim,heads,group,members,shared,n_q", [(128, 8, 4, 16, 1000, 1), (128, 8, 4, 9, 2100, 3), (64, 2, 8, 40, 1000, 1),
-                                                                (64, 2, 8, 70, 1500, 2), (128, 1, 16, 33, 2049, 1)])
+@pytest.mark.parametrize("dim,heads,group,members,shared,n_q", [(128, 8, 4, 30, 2100, 1), (128, 8, 4, 26, 2100, 3), (64, 2, 8, 100, 4100, 1),
+                                                                (64, 2, 8, 100, 4200, 2), (128, 1, 16, 64, 6300, 1)])
 def test_forked_contexts_lose_no_digits_to_the_shared_reading(dim, heads, group, members, shared, n_q, dtype, opts):
     """Rows of contexts forked from one come out as exact as a single context's: weights in two 16-bit parts."""
     pool = R.make_pool(1, heads, dim, 16, shared // 16 + members * 8 + 4, max_ctx=members + 2, dtype=dtype)
@@ -115,3 +115,61 @@ def test_forked_contexts_lose_no_digits_to_the_shared_reading(dim, heads, group,
     if "slopes" in opts:
         big += 0.02 * (shared + 64)  # the bias is a part of the score, rounded as it is
     R.check_attend(got, (out, lse, slack, big), dtype, dim, False)
+
+
+@pytest.mark.parametrize("opts", [{}, dict(softcap=20.0), dict(slopes=True)])
+@pytest.mark.parametrize("dim,heads,group", [(128, 8, 4), (64, 8, 2)])
+def test_generations_of_forks_in_one_large_batch(dim, heads, group, opts):
+    """As many listed contexts as make reading their shared blocks together worth it, of two generations, some several times."""
+    if opts.get("slopes"):
+        opts = dict(slopes=torch.linspace(0.001, 0.02, heads * group, device="cuda"))
+    pool = R.make_pool(1, heads, dim, 16, 1200, max_ctx=64)
+    root = R.add_ctx(pool, 2100, 1)
+    alone = R.add_ctx(pool, 777, 2)
+    st, kids = pool.fork(root.handle, 9)
+    assert st == 0
+    own = [1, 2, 5, 16, 17, 300, 33, 64, 4]
+    tails = [R.rand((1, 2, t, heads, dim), 60 + i) for i, t in enumerate(own)]
+    assert pool.append(kids, own, tails)[0] == 0
+    ctxs = [R.Ctx(h, torch.cat((root.rows, t), 2)) for h, t in zip(kids, tails)]
+    st, more = pool.fork(ctxs[5].handle, 7)
+    assert st == 0
+    ctxs += [R.Ctx(h, ctxs[5].rows) for h in more] + [alone, root]
+    batch = [ctxs[i] for i in [3, 17, 0, 9, 10, 16, 11, 1, 2, 4, 12, 5, 13, 6, 7, 14, 8, 15, 3] * 6]
+    for n_q in ([1] * len(batch), [1 + i % 2 for i in range(len(batch))], [1] * 50 + [40] + [1] * (len(batch) - 51)):
+        q = R.rand((sum(n_q), heads * group, dim), sum(n_q), scale=2.0)
+        st, got = pool.attend(0, [c.handle for c in batch], n_q, q, **opts)
+        assert st == 0
+        st, again = pool.attend(0, [c.handle for c in batch], n_q, q, **opts)
+        assert st == 0 and all(torch.equal(x, y) for x, y in zip(got, again))
+        torch.cuda.synchronize()
+        assert pool.sync_status() == 0
+        out, lse, slack, big = R.attend_ref(batch, n_q, q, **opts)
+        if "slopes" in opts:
+            big += 0.02 * 2500
+        R.check_attend(got, (out, lse, slack, big), torch.bfloat16, dim, max(n_q) > 2)
+
+
+@pytest.mark.parametrize("times", [1, 7])
+def test_nonfinite_values_of_blocks_that_a_large_batch_of_forks_shares(times):
+    pool = R.make_pool(1, 8, 128, 16, 400)
+    rows = R.rand((1, 2, 1600, 8, 128), 5)
+    rows[0, 1, 1599, 0, 3] = math.inf
+    rows[0, 1, 1598, 2, 5] = -math.inf
+    rows[0, 1, 700, 1, 4] = math.nan
+    root = R.add_ctx(pool, 1600, 0, rows)
+    st, kids = pool.fork(root.handle, 6)
+    assert st == 0 and pool.reserve(kids[:3], [1, 1, 1])[0] == 0
+    kv = torch.zeros(3, 8, 128, dtype=torch.bfloat16, device="cuda")
+    assert pool.store(0, kids[:3], [1, 1, 1], kv, kv)[0] == 0
+    q = R.rand((6 * times, 32, 128), 6, scale=2.0)
+    st, (out, lse) = pool.attend(0, kids * times, None, q)
+    assert st == 0
+    torch.cuda.synchronize()
+    assert pool.sync_status() == 0 and torch.isfinite(lse).all()
+    assert (out[:, :4, 3] == math.inf).all() and (out[:, 8:12, 5] == -math.inf).all() and torch.isnan(out[:, 4:8, 4]).all()
+    rest = out.clone()
+    rest[:, :4, 3], rest[:, 8:12, 5], rest[:, 4:8, 4] = 0, 0, 0
+    assert torch.isfinite(rest).all()
+    st, (out, lse) = pool.attend(0, kids[3:] * times, [2] * (3 * times), q)  # the first of two queries before the last shared token
+    assert st == 0 and torch.isfinite(out[0::2, :4, 3]).all() and (out[1::2, :4, 3] == math.inf).all()
