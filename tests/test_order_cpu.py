@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import random
 import subprocess
 
 import pytest
@@ -352,3 +353,83 @@ def test_threads_with_a_pool_each_launch_a_kernel_for_the_first_time(tmp_path):
     run = subprocess.run([out], capture_output=True, text=True)
     assert "WARNING: ThreadSanitizer" not in run.stderr, run.stderr
     assert run.returncode == 0, run.stderr
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_calls_on_random_streams_keep_every_order_that_they_need(lib, pool, seed):
+    """Payload kernels (copies, readers) all run one after the other; they come behind the metadata before them; and a table row is
+    written behind the readers that were given it."""
+    r = random.Random(seed)
+    streams = [lib.order_stream() for _ in range(4)]
+    live, payload, meta, readers = {}, [], [], {}
+
+    def did(ran, rows=()):
+        for name, i in ran.items():
+            if name in ("select", "memcpy"):
+                continue
+            if name.startswith("plan_") or name in ("fork", "evict"):
+                for h in rows:
+                    for j in readers.pop(h, ()):
+                        assert pool.before(j, i), (name, h)
+                meta.append(i)
+            else:
+                for j in payload[-6:] + meta[-6:]:
+                    assert pool.before(j, i), (pool.lib.order_name(j), name)
+                payload.append(i)
+
+    for _ in range(150):
+        st = r.choice(streams)
+        kind = r.choice(["imp", "reserve", "append", "fork", "compose", "evict", "materialize", "attend", "store", "mass", "prune", "attend", "swap"])
+        if kind == "swap":  # a stream that was used goes, another one comes, under its handle or not
+            i = r.randrange(4)
+            st = streams[(i + 1) % 4]
+            if live:
+                did(pool.materialize(st, r.choice(list(live)), 1))
+                streams[i] = lib.order_replace_stream(streams[i], r.randrange(2))
+            continue
+        if kind == "imp" or not live:
+            if len(live) < 24:
+                n = r.choice([16, 160, 37])
+                ran, c = pool.imp(st, n)
+                live[c] = n
+                did(ran, [c])
+            continue
+        c = r.choice(list(live))
+        if kind in ("reserve", "append"):
+            n = r.choice([1, 16, 5])
+            did(getattr(pool, kind)(st, [c], [n]), [c])
+            live[c] += n
+        elif kind in ("fork", "compose", "prune"):
+            if len(live) < 24:
+                if kind == "fork":
+                    ran, (new,) = pool.fork(st, c)
+                    n = live[c]
+                elif kind == "compose":
+                    other = r.choice(list(live))
+                    ran, new = pool.compose(st, [c, other])
+                    n = live[c] + live[other]
+                else:
+                    ran, new = pool.prune(st, c, 1)
+                    n = 1
+                live[new] = n
+                did(ran, [new])
+                if kind == "prune":
+                    readers.setdefault(c, []).append(ran["gather"])
+        elif kind == "evict":
+            did(pool.evict(st, [c]))
+            del live[c]
+        elif kind == "materialize":
+            did(pool.materialize(st, c, live[c]))
+        else:
+            if kind == "store":
+                status = pool.lib.order_ops()
+                ran = pool.store(st, [c], [1], want=None)
+                if pool.status:
+                    assert not ran and status == pool.lib.order_ops()
+                    continue
+            else:
+                ran = getattr(pool, kind)(st, [c])
+            did(ran)
+            readers.setdefault(c, []).extend(ran.values())
+    assert lib.aaf_kv_sync_status(pool.h) == 0
+    assert not pool.wrongs()
