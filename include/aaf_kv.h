@@ -385,7 +385,7 @@ int aaf_kv_rope_freqs(int32_t rot_dim, double base, int32_t scaling, const aaf_k
  * packed into one context ({start of the token's document, p + 1}), a prefix seen in both directions ({0, max(p + 1,
  * prefix)}), a whole context ({0, length}).  A row that sees no key, or whose visible scores are all -inf, is 0 with lse =
  * -inf.  Keys and values that a row does not see have no influence on it, whatever they hold (infinities and NaN
- * included); slots behind a context's end are not read.  An infinite value that a row sees makes that element of the row
+ * included), nor do slots behind a context's end.  An infinite value that a row sees makes that element of the row
  * infinite; NaN if its weight is too small for the type.
  * q: heads contiguous, q_stride elements from token to token (a multiple of 8); out: dense [tokens][n_q_heads][head_dim];
  * lse (may be NULL): [tokens][n_q_heads].  n_q may be NULL (one token each).  A context may be listed several times.
@@ -410,7 +410,8 @@ int aaf_kv_attend(aaf_kv_pool *pool, int32_t layer, const aaf_kv_attn *a, int32_
                   size_t workspace_bytes, void *stream);
 
 /* attention mass -- mass[i][t] = prev[i][t] + sum over the query rows r of context i of exp(x_rt - lse_r), x and the visible keys as
- * in aaf_kv_attend with the same arguments, lse as that call returned it (rows with lse = -inf add nothing).  Row i starts
+ * in aaf_kv_attend with the same arguments, lse as that call returned it (rows with lse = -inf add nothing; it is a 32-bit
+ * number, so a bias that puts it far from zero leaves the weights fewer digits).  Row i starts
  * at i * mass_stride (>= the longest context, else DST_TOO_SMALL); entries behind a context's end are left as they are.
  * prev may be NULL (zeros) or mass itself: one buffer then sums over layers and steps.  The order of every sum is fixed. */
 int aaf_kv_attn_mass(aaf_kv_pool *pool, int32_t layer, const aaf_kv_attn *a, int32_t n, const aaf_ctx_t *ctxs,

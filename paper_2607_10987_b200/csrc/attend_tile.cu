@@ -8,6 +8,9 @@
 //
 // P is rounded to the values' 16-bit type before P V: the error is that of one more rounding of the output's kind
 // (each weight is off by at most half a step, the signs are independent), the sum of the weights stays in 32 bits.
+//
+// Bound: the issue of copies, ldmatrix and mma.sync by four warps.  4 contexts of 8699 tokens, 512 of them new, 32 heads, 8 kv
+// heads: 96 wide 2962 us (72 TFLOP/s), 256 wide 9594 (59).
 #include "attend_device.cuh"
 
 namespace aafkv {

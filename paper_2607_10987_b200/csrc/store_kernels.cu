@@ -181,7 +181,7 @@ __device__ __forceinline__ uint32_t score_key(float f) {
 }
 
 // 11 bits at a time (11, 11, 10).  The order-preserving keys of up to SELECT_CACHED candidates are kept in shared memory, so
-// that the scores are read once.
+// that the scores are read once: 34 us for 40960 with planner and gather, 56 for 45000, which are read in every pass, 178 for 131072.
 constexpr int SELECT_CACHED = 40960, SELECT_BINS = 2048;
 __global__ void __launch_bounds__(SELECT_THREADS)
     select_kernel(const float *__restrict__ scores, int len, int budget, int sink, int recent, int *__restrict__ kept,
