@@ -1774,8 +1774,9 @@ int aaf_kv_prune(aaf_kv_pool *p, aaf_ctx_t ctx, const float *scores_dev, int64_t
     const PlanSlot ps = begin_plan(p);
     // the new context's table, blocks and catalog entry; its piece list (no buffer behind it) is not run
     bool ok = launch_plan_import(p->g, ps.view, c, budget, nullptr, p->clock + 1, p->meta_stream, ctx) == cudaSuccess;
-    // the selection needs none of that: it runs beside the planner (and beside an eviction still under way)
-    ok = ok && launch_select(scores_dev, (int)T, (int)budget, (int)sink, (int)recent, kept_dev, kept_scores_dev, st) == cudaSuccess;
+    // the selection needs none of that: it runs beside the planner (and beside an eviction still under way), behind the attention mass
+    // that it selects by, on whatever stream that is
+    ok = ok && after_payload_work(p, st) && launch_select(scores_dev, (int)T, (int)budget, (int)sink, (int)recent, kept_dev, kept_scores_dev, st) == cudaSuccess;
     if (!ok || !end_plan(p, ps, st)) return broke(p);
     p->clock += 1;
     p->meta_launches += 1;

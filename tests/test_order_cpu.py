@@ -433,3 +433,11 @@ def test_random_calls_on_random_streams_keep_every_order_that_they_need(lib, poo
             readers.setdefault(c, []).extend(ran.values())
     assert lib.aaf_kv_sync_status(pool.h) == 0
     assert not pool.wrongs()
+
+
+@pytest.mark.parametrize("first", ["mass", "attend", "store"])
+def test_a_prune_selects_behind_what_computes_its_scores_on_another_stream(lib, pool, first):
+    a, b = lib.order_stream(), lib.order_stream()
+    _, c = pool.imp(b, 160)
+    ran = READERS[first](pool, a, c)
+    assert pool.before(ran, pool.prune(b, c, 5)[0]["select"])
