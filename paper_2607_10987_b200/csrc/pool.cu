@@ -364,6 +364,14 @@ bool capturing(cudaStream_t st) {
     return s != cudaStreamCaptureStatusNone;
 }
 
+// Host side of the introspection calls: the metadata and the most recent call's stream.  A stream that is being captured cannot be
+// waited for; the pool's work there was queued before, and its events are waited for instead.
+bool wait_for_calls(aaf_kv_pool *p) {
+    if (cudaStreamSynchronize(p->meta_stream) != cudaSuccess) return false;
+    if (!capturing(p->last_stream)) return cudaStreamSynchronize(p->last_stream) == cudaSuccess;
+    return cudaEventSynchronize(p->read_ev) == cudaSuccess && (!p->last_copy_event || cudaEventSynchronize(p->last_copy_event) == cudaSuccess);
+}
+
 int run_copy(aaf_kv_pool *p, const PlanSlot &ps, int cls, int n_slots, long long payload_tokens, cudaStream_t st,
              int piece0 = 0) {
     const int plane0 = 0, n_planes = 2 * p->g.L;
@@ -610,7 +618,7 @@ int aaf_kv_pool_destroy(aaf_kv_pool *p) {
     if (!p) return AAF_ERR_INVALID_ARG;
     DeviceGuard guard(p->device);
     if (p->meta_stream) cudaStreamSynchronize(p->meta_stream);
-    if (p->last_stream || !p->pending.empty()) cudaStreamSynchronize(p->last_stream);
+    if ((p->last_stream || !p->pending.empty()) && !capturing(p->last_stream)) cudaStreamSynchronize(p->last_stream);
     // readers and copies on other streams use the pinned ring and memory that the caller frees next
     if (p->read_ev) cudaEventSynchronize(p->read_ev);
     if (p->last_copy_event) cudaEventSynchronize(p->last_copy_event);
@@ -1831,8 +1839,7 @@ int aaf_kv_export_catalog(aaf_kv_pool *p, const aaf_kv_catalog_cols *cols, void 
 int aaf_kv_get_catalog(aaf_kv_pool *p, int64_t *clock, int64_t *reuse_out, int64_t *last_access_out) {
     if (!p || !clock || !reuse_out || !last_access_out) return AAF_ERR_INVALID_ARG;
     DeviceGuard guard(p->device);
-    if (cudaStreamSynchronize(p->meta_stream) != cudaSuccess || cudaStreamSynchronize(p->last_stream) != cudaSuccess)
-        return AAF_ERR_CUDA;
+    if (!wait_for_calls(p)) return AAF_ERR_CUDA;
     const size_t nbytes = sizeof(long long) * (size_t)p->g.max_ctx;
     if (cudaMemcpy(reuse_out, p->s.cat_reuse, nbytes, cudaMemcpyDeviceToHost) != cudaSuccess ||
         cudaMemcpy(last_access_out, p->s.cat_last, nbytes, cudaMemcpyDeviceToHost) != cudaSuccess)
@@ -1856,8 +1863,7 @@ int aaf_kv_get_table(aaf_kv_pool *p, aaf_ctx_t ctx, int32_t *host_out, int32_t c
     const long long nb = nblk_of(p, p->len[ctx]);
     if (cap < nb) return AAF_ERR_DST_TOO_SMALL;
     DeviceGuard guard(p->device);
-    if (cudaStreamSynchronize(p->meta_stream) != cudaSuccess || cudaStreamSynchronize(p->last_stream) != cudaSuccess)
-        return AAF_ERR_CUDA;
+    if (!wait_for_calls(p)) return AAF_ERR_CUDA;
     if (cudaMemcpy(host_out, p->s.tables + (long long)ctx * p->g.max_blk, sizeof(int) * (size_t)nb,
                    cudaMemcpyDeviceToHost) != cudaSuccess)
         return AAF_ERR_CUDA;
@@ -1868,8 +1874,7 @@ int aaf_kv_get_table(aaf_kv_pool *p, aaf_ctx_t ctx, int32_t *host_out, int32_t c
 int aaf_kv_get_refcounts(aaf_kv_pool *p, int32_t *host_out) {
     if (!p || !host_out) return AAF_ERR_INVALID_ARG;
     DeviceGuard guard(p->device);
-    if (cudaStreamSynchronize(p->meta_stream) != cudaSuccess || cudaStreamSynchronize(p->last_stream) != cudaSuccess)
-        return AAF_ERR_CUDA;
+    if (!wait_for_calls(p)) return AAF_ERR_CUDA;
     return cudaMemcpy(host_out, p->s.refcount, sizeof(int) * (size_t)p->g.NB, cudaMemcpyDeviceToHost) == cudaSuccess
                ? AAF_OK
                : AAF_ERR_CUDA;
@@ -1878,8 +1883,7 @@ int aaf_kv_get_refcounts(aaf_kv_pool *p, int32_t *host_out) {
 int aaf_kv_get_free_list(aaf_kv_pool *p, int32_t *host_out, int32_t *n_free) {
     if (!p || !host_out || !n_free) return AAF_ERR_INVALID_ARG;
     DeviceGuard guard(p->device);
-    if (cudaStreamSynchronize(p->meta_stream) != cudaSuccess || cudaStreamSynchronize(p->last_stream) != cudaSuccess)
-        return AAF_ERR_CUDA;
+    if (!wait_for_calls(p)) return AAF_ERR_CUDA;
     unsigned long long ht[2];
     std::vector<int> ring((size_t)p->g.NB);
     if (cudaMemcpy(ht, p->s.ctl, sizeof(ht), cudaMemcpyDeviceToHost) != cudaSuccess ||
@@ -1896,8 +1900,7 @@ int aaf_kv_get_free_list(aaf_kv_pool *p, int32_t *host_out, int32_t *n_free) {
 int aaf_kv_pool_stats(aaf_kv_pool *p, aaf_kv_stats *out) {
     if (!p || !out) return AAF_ERR_INVALID_ARG;
     DeviceGuard guard(p->device);
-    if (cudaStreamSynchronize(p->meta_stream) != cudaSuccess || cudaStreamSynchronize(p->last_stream) != cudaSuccess)
-        return AAF_ERR_CUDA;
+    if (!wait_for_calls(p)) return AAF_ERR_CUDA;
     drain_timing(p);
     DevCtl ctl;
     if (cudaMemcpy(&ctl, p->s.ctl, sizeof(ctl), cudaMemcpyDeviceToHost) != cudaSuccess) return AAF_ERR_CUDA;
@@ -1921,8 +1924,7 @@ int aaf_kv_pool_stats(aaf_kv_pool *p, aaf_kv_stats *out) {
 int aaf_kv_sync_status(aaf_kv_pool *p) {
     if (!p) return AAF_ERR_INVALID_ARG;
     DeviceGuard guard(p->device);
-    if (cudaStreamSynchronize(p->meta_stream) != cudaSuccess || cudaStreamSynchronize(p->last_stream) != cudaSuccess)
-        return AAF_ERR_CUDA;
+    if (!wait_for_calls(p)) return AAF_ERR_CUDA;
     int st[2] = {0, 0};
     if (cudaMemcpy(st, &p->s.ctl->status, sizeof(st), cudaMemcpyDeviceToHost) != cudaSuccess) return AAF_ERR_CUDA;
     if (st[0] != 0) {

@@ -118,3 +118,25 @@ def test_a_first_call_in_a_capture_leaves_no_scratch_of_the_graph_s_memory():
     torch.cuda.synchronize()
     assert float(x) == 1 and pool.sync_status() == 0
     R.check_attend(got, R.attend_ref([c], [1], q), torch.bfloat16, 64, False)
+
+
+def test_introspection_and_the_end_of_a_pool_beside_a_capture_of_its_stream():
+    pool = R.make_pool(1, 2, 64, 16, 64)
+    c = R.add_ctx(pool, 320, 1)
+    q = R.rand((1, 8, 64), 1)
+    x = torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    a, b = two_streams()
+    with torch.cuda.stream(a):
+        st, got = pool.attend(0, [c.handle], None, q)
+    assert st == 0
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=a):
+        x.add_(1.0)
+        status, stats, table = pool.sync_status(), pool.stats(), pool.table(c.handle)
+        pool.close()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert float(x) == 1 and status == 0 and stats["live_ctx"] == 1 and len(table) == 20
+    R.check_attend(got, R.attend_ref([c], [1], q), torch.bfloat16, 64, False)

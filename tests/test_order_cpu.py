@@ -441,3 +441,18 @@ def test_a_prune_selects_behind_what_computes_its_scores_on_another_stream(lib, 
     _, c = pool.imp(b, 160)
     ran = READERS[first](pool, a, c)
     assert pool.before(ran, pool.prune(b, c, 5)[0]["select"])
+
+
+@pytest.mark.parametrize("last", READERS)
+def test_introspection_while_the_last_call_s_stream_is_captured(lib, pool, last):
+    a, b = lib.order_stream(), lib.order_stream()
+    _, c = pool.imp(b, 160)
+    ran = READERS[last](pool, a, c)
+    lib.order_capture(a, 1)
+    assert lib.aaf_kv_sync_status(pool.h) == 0
+    assert lib.order_host_knows(ran)
+    stats = B.aaf_kv_stats()
+    assert lib.aaf_kv_pool_stats(pool.h, C.byref(stats)) == 0
+    pool.close()
+    pool.h = None
+    assert not pool.wrongs()
