@@ -429,6 +429,90 @@ int aaf_kv_attn_mass(aaf_kv_pool *pool, int32_t layer, const aaf_kv_attn *a, int
 int aaf_kv_prune(aaf_kv_pool *pool, aaf_ctx_t ctx, const float *scores_dev, int64_t budget, int64_t sink, int64_t recent,
                  int32_t *kept_dev, float *kept_scores_dev, aaf_ctx_t *out_ctx, void *stream);
 
+/* ---- sparse attention: the blocks that matter to a query, chosen by a cheap score, and attention over them alone --------
+ *   aaf_kv_summarize      bounds of every block's keys, in 8 bits: 1/32 of a 16-token block's keys and values
+ *   aaf_kv_select         for every query token and kv head, the blocks with the largest bound on a score
+ *   aaf_kv_attend_blocks  aaf_kv_attend over those blocks
+ * A serving loop calls them behind aaf_kv_store, layer by layer: the blocks of the new tokens are summed up anew, the choice is
+ * made from all summaries, the attention reads what was chosen.  They obey the rules of the calls above (packed batches, the
+ * contexts' last n_q[i] tokens as queries, 16-bit floats, head_dim a multiple of 8 and at most AAF_ATTN_MAX_HEAD_DIM, order
+ * across streams, refused during capture), and their results do not depend on timing.
+ *
+ * Summaries are the caller's: one device buffer of aaf_kv_summary_bytes(pool) bytes (0 for a pool that has none), 16-byte aligned,
+ * [n_layers][n_blocks] records of n_kv_heads * 2 * head_dim codes (per head the upper, then the lower bounds) and n_kv_heads
+ * exponents (int8 all), filled up to a multiple of 16 bytes (the filling is neither read nor written).  With F(x) = x clamped to
+ * +-127 * 2^113, and a NaN counting as the largest and as the smallest value,
+ *   hi_d = max F(k_td), lo_d = min F(k_td) over the block's tokens t;   e = the smallest exponent >= -60 with all |hi_d|, |lo_d| <= 127 * 2^e
+ *   codes ceil(hi_d / 2^e), floor(lo_d / 2^e)
+ * so code * 2^e bounds the keys.  A block's summary goes with the block: contexts that share it (fork, merge) share its summary.  It is
+ * as old as the last aaf_kv_summarize of a context that holds the block: call it for what import, append, store, compose, prune or a copied
+ * tail have put into blocks, before aaf_kv_select is to know of it. */
+#define AAF_ALL_LAYERS (-1)
+#define AAF_SELECT_MAX_BLOCKS 49152 /* of a context that aaf_kv_select chooses from */
+#define AAF_LIST_MAX_BLOCKS 1048576 /* of a list                                   */
+
+size_t aaf_kv_summary_bytes(const aaf_kv_pool *pool);
+
+/* summarize -- writes the summaries of the blocks that hold the last n_new[i] tokens of ctxs[i] (n_new NULL: of all its blocks), from all
+ * tokens that the context has in them, in one layer or (AAF_ALL_LAYERS) in all.  A context may be listed several times.
+ * Errors: BAD_CTX, INVALID_ARG (n_new < 1 or longer than the context, pointers, layer, dtype), INCOMPAT, DST_TOO_SMALL, TOO_MANY, TOO_LONG. */
+int aaf_kv_summarize(aaf_kv_pool *pool, int32_t layer, int32_t dtype, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_new,
+                     void *summary_dev, size_t summary_bytes, void *stream);
+
+/* select -- for every query token (position p; its blocks are 0 .. B = p / block_size) and kv head the blocks that it is to attend to.  With
+ *   f = the smallest exponent >= -60 with all |F(q_d)| <= 127 * 2^f;   c_d = F(q_d) / 2^f rounded to a whole number, half to even; 0 for a NaN
+ *   dot_b = sum_d max(c_d * hi_bd, c_d * lo_bd)   over the codes of the block
+ *   score_b = the largest of dot_b * 2^(e_b + f) over the query heads of the kv head's group, a 32-bit float
+ * (up to the rounding of q the largest product that any key of the block could have with it; a positive attention scale is assumed) it
+ * takes blocks 0 .. sink - 1, blocks B - recent + 1 .. B, and of the others those with the largest scores (equal scores: the lower
+ * block), at most keep in all.  All of it is exact: no rounding decides.  A block's summary covers tokens behind p too, where
+ * the context has them: those of block B, which is always taken.
+ * blocks_dev: [tokens][n_kv_heads][keep] block numbers within the context, ascending, -1 behind the last; scores_dev (may be NULL): the same
+ * shape, their scores, -inf behind the last.  q: heads contiguous, q_stride elements from token to token (a multiple of 8).  n_q may be NULL
+ * (one token each).  A context may be listed several times.
+ * Errors: BAD_CTX, INVALID_ARG (n_q, keep outside [1, AAF_LIST_MAX_BLOCKS], recent < 1, sink < 0, sink + recent > keep, pointers, strides),
+ * INCOMPAT, DST_TOO_SMALL (summary_bytes), TOO_MANY, TOO_LONG (more than AAF_SELECT_MAX_BLOCKS blocks). */
+typedef struct aaf_kv_select_desc {
+    uint32_t struct_size; /* sizeof(aaf_kv_select_desc)      */
+    int32_t dtype;        /* AAF_DTYPE_*                     */
+    int32_t n_q_heads;    /* a multiple of n_kv_heads        */
+    int32_t keep;         /* blocks of a list                */
+    int32_t sink, recent; /* first and last blocks, always taken; recent >= 1 */
+    int64_t q_stride;     /* elements                        */
+} aaf_kv_select_desc;
+int aaf_kv_select(aaf_kv_pool *pool, int32_t layer, const aaf_kv_select_desc *d, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_q,
+                  const void *q_dev, const void *summary_dev, size_t summary_bytes, int32_t *blocks_dev, float *scores_dev,
+                  void *stream);
+
+/* attend_blocks -- aaf_kv_attend with the same arguments, over the listed blocks alone: a row of kv head h sees the keys that it would see
+ * there (its span, its window) and that lie in a block of its token's list, blocks_dev[token][h][0 .. keep) (block numbers within the context,
+ * in any order; entries outside the context, -1 among them, name nothing; a block that is listed twice counts twice).  A row that sees
+ * nothing is 0 with lse = -inf.  keep * block_size at most 2^30.  workspace_dev as for aaf_kv_attend, the same buffer. */
+int aaf_kv_attend_blocks(aaf_kv_pool *pool, int32_t layer, const aaf_kv_attn *a, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_q,
+                         const void *q_dev, const int32_t *blocks_dev, int32_t keep, void *out_dev, float *lse_dev,
+                         void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* batch_tables -- the tables of a batch as device arrays, for kernels of the caller's own that read and write the pool, built on the device
+ * from the pool's block tables (no copy to the host, no wait).  n_new[i] (NULL: one each) are the new tokens of ctxs[i], its last ones.
+ * `rows` and `tokens` may be larger than the batch, so that shapes stay the same from step to step.  Any of the arrays may be NULL:
+ *   tables    [rows][cols]  block ids of each context, -1 behind its last block and in rows behind the batch
+ *   lens      [rows]        tokens of each context, 0 behind the batch
+ *   offsets   [rows + 1]    first new token of each context among the batch's, their number behind the batch
+ *   token_row [tokens]      for each new token its row, -1 behind the last
+ *   positions [tokens]      its index in its context, 0 behind the last
+ *   slots     [tokens]      block id * block_size + place in the block, -1 behind the last: layer l's key row is at pool_base + l *
+ *                           layer_stride_bytes + (slot / BS * 2 * BS + slot % BS) * row, the value row run bytes further
+ * Errors: BAD_CTX, INVALID_ARG (n_new, pointers, nothing asked for), DST_TOO_SMALL (rows, tokens, or cols below a context's blocks), TOO_MANY,
+ * TOO_LONG. */
+typedef struct aaf_kv_batch_desc {
+    uint32_t struct_size; /* sizeof(aaf_kv_batch_desc) */
+    int32_t rows, tokens, cols;
+    int32_t *tables, *lens, *offsets, *token_row; /* (device) */
+    int64_t *positions, *slots;                   /* (device) */
+} aaf_kv_batch_desc;
+int aaf_kv_batch_tables(aaf_kv_pool *pool, const aaf_kv_batch_desc *d, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_new,
+                        void *stream);
+
 /* Introspection (metadata catalog of App. A.2).  These synchronise the library's metadata stream and
  * the stream of the most recent call. */
 int aaf_kv_ctx_len(aaf_kv_pool *pool, aaf_ctx_t ctx, int64_t *n_tokens);

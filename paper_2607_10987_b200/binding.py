@@ -26,6 +26,7 @@ AAF_ENGINE_AUTO, AAF_ENGINE_VEC, AAF_ENGINE_BULK, AAF_ENGINE_WARP = 0, 1, 2, 3
 AAF_OP_MATERIALIZE, AAF_OP_IMPORT, AAF_OP_APPEND, AAF_OP_COMPOSE, AAF_OP_CLASSES = 0, 1, 2, 3, 4
 AAF_DTYPE_BF16, AAF_DTYPE_F16 = 0, 1
 AAF_ROPE_NONE, AAF_ROPE_LINEAR, AAF_ROPE_BASE, AAF_ROPE_WAVELENGTH, AAF_ROPE_RAMP = 0, 1, 2, 3, 4
+AAF_ALL_LAYERS, AAF_SELECT_MAX_BLOCKS, AAF_LIST_MAX_BLOCKS = -1, 49152, 1048576
 OP_NAMES = ("materialize", "import", "append", "compose")
 
 
@@ -84,6 +85,17 @@ class aaf_kv_attn(C.Structure):
                 ("q_stride", C.c_int64)]
 
 
+class aaf_kv_select_desc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("keep", C.c_int32),
+                ("sink", C.c_int32), ("recent", C.c_int32), ("q_stride", C.c_int64)]
+
+
+class aaf_kv_batch_desc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("rows", C.c_int32), ("tokens", C.c_int32), ("cols", C.c_int32),
+                ("tables", C.c_void_p), ("lens", C.c_void_p), ("offsets", C.c_void_p), ("token_row", C.c_void_p),
+                ("positions", C.c_void_p), ("slots", C.c_void_p)]
+
+
 # every symbol include/aaf_kv.h declares: name -> (restype, argtypes)
 _vp, _i32, _i64, _u32, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint32, C.c_size_t
 _p32 = C.POINTER(C.c_int32)
@@ -116,6 +128,11 @@ SYMBOLS = {
     "aaf_kv_attend": (C.c_int, [_vp, _i32, C.POINTER(aaf_kv_attn), _i32, _p32, _p32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "aaf_kv_attn_mass": (C.c_int, [_vp, _i32, C.POINTER(aaf_kv_attn), _i32, _p32, _p32, _vp, _vp, _vp, _vp, _i64, _vp]),
     "aaf_kv_prune": (C.c_int, [_vp, _i32, _vp, _i64, _i64, _i64, _vp, _vp, _p32, _vp]),
+    "aaf_kv_summary_bytes": (_sz, [_vp]),
+    "aaf_kv_summarize": (C.c_int, [_vp, _i32, _i32, _i32, _p32, _p32, _vp, _sz, _vp]),
+    "aaf_kv_select": (C.c_int, [_vp, _i32, C.POINTER(aaf_kv_select_desc), _i32, _p32, _p32, _vp, _vp, _sz, _vp, _vp, _vp]),
+    "aaf_kv_attend_blocks": (C.c_int, [_vp, _i32, C.POINTER(aaf_kv_attn), _i32, _p32, _p32, _vp, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "aaf_kv_batch_tables": (C.c_int, [_vp, C.POINTER(aaf_kv_batch_desc), _i32, _p32, _p32, _vp]),
     "aaf_kv_catalog_rows": (C.c_int, [_vp, _p32, C.POINTER(_i64)]),
     "aaf_kv_export_catalog": (C.c_int, [_vp, C.POINTER(aaf_kv_catalog_cols), _vp]),
     "aaf_kv_get_catalog": (C.c_int, [_vp, C.POINTER(_i64), C.POINTER(_i64), C.POINTER(_i64)]),
@@ -205,6 +222,15 @@ def aaf_kv_attn_mass(pool, layer, attn, n, ctxs, n_q, q, lse, prev, mass, mass_s
     return _fn("aaf_kv_attn_mass")(pool, layer, attn, n, ctxs, n_q, q, lse, prev, mass, mass_stride, stream)
 def aaf_kv_prune(pool, ctx, scores, budget, sink, recent, kept, kept_scores, out_ctx, stream):
     return _fn("aaf_kv_prune")(pool, ctx, scores, budget, sink, recent, kept, kept_scores, out_ctx, stream)
+def aaf_kv_summary_bytes(pool): return _fn("aaf_kv_summary_bytes")(pool)
+def aaf_kv_summarize(pool, layer, dtype, n, ctxs, n_new, summary, summary_bytes, stream):
+    return _fn("aaf_kv_summarize")(pool, layer, dtype, n, ctxs, n_new, summary, summary_bytes, stream)
+def aaf_kv_select(pool, layer, desc, n, ctxs, n_q, q, summary, summary_bytes, blocks, scores, stream):
+    return _fn("aaf_kv_select")(pool, layer, desc, n, ctxs, n_q, q, summary, summary_bytes, blocks, scores, stream)
+def aaf_kv_attend_blocks(pool, layer, attn, n, ctxs, n_q, q, blocks, keep, out, lse, workspace, workspace_bytes, stream):
+    return _fn("aaf_kv_attend_blocks")(pool, layer, attn, n, ctxs, n_q, q, blocks, keep, out, lse, workspace, workspace_bytes, stream)
+def aaf_kv_batch_tables(pool, desc, n, ctxs, n_new, stream):
+    return _fn("aaf_kv_batch_tables")(pool, desc, n, ctxs, n_new, stream)
 def aaf_kv_catalog_rows(pool, n_states, n_rows): return _fn("aaf_kv_catalog_rows")(pool, n_states, n_rows)
 def aaf_kv_export_catalog(pool, cols, stream): return _fn("aaf_kv_export_catalog")(pool, cols, stream)
 def aaf_kv_get_catalog(pool, clock, reuse, last): return _fn("aaf_kv_get_catalog")(pool, clock, reuse, last)
@@ -478,13 +504,9 @@ class KVPool:
                            None if slopes is None else self._flat(slopes, self.torch.float32, heads, "slopes"),
                            None if spans is None else self._flat(spans, self.torch.int32, 2 * tokens, "spans"), stride)
 
-    def attend(self, layer, ctxs, n_q, q, out=None, lse=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):
-        """Attention of the contexts' last n_q tokens (None: one each); returns (status, (out, lse))."""
+    def _attn_out(self, q, tokens, heads, out, lse):
+        """Outputs of an attention call and its scratch, None for the latter if it is not there and must not be made."""
         torch = self.torch
-        n = len(ctxs)
-        tokens = n if n_q is None else sum(n_q)
-        a = self._attn(q, tokens, scale, softcap, window, slopes, spans)
-        heads = a.n_q_heads
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif self._rows(out, tokens, heads, "out", q.dtype) != heads * self.D:
@@ -497,8 +519,18 @@ class KVPool:
         if ws is None:
             with torch.cuda.device(self.device):
                 if torch.cuda.is_current_stream_capturing():  # refused anyway; kept scratch must not be a graph's memory
-                    return AAF_ERR_INVALID_ARG, None
+                    return out, lse, None
             ws = self._attend_ws = torch.empty(aaf_kv_attend_workspace_bytes(self.h), dtype=torch.uint8, device=self.device)
+        return out, lse, ws
+
+    def attend(self, layer, ctxs, n_q, q, out=None, lse=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):
+        """Attention of the contexts' last n_q tokens (None: one each); returns (status, (out, lse))."""
+        n = len(ctxs)
+        tokens = n if n_q is None else sum(n_q)
+        a = self._attn(q, tokens, scale, softcap, window, slopes, spans)
+        out, lse, ws = self._attn_out(q, tokens, a.n_q_heads, out, lse)
+        if ws is None:
+            return AAF_ERR_INVALID_ARG, None
         st = load().aaf_kv_attend(self.h, layer, a, n, (C.c_int32 * (n or 1))(*ctxs),
                                   None if n_q is None else (C.c_int32 * (n or 1))(*n_q), q.data_ptr(), out.data_ptr(),
                                   lse.data_ptr(), ws.data_ptr(), ws.numel(), self._stream())
@@ -536,6 +568,92 @@ class KVPool:
                                  None if kept_scores is None else self._flat(kept_scores, torch.float32, max(budget, 1), "kept_scores"),
                                  C.byref(out), self._stream())
         return st, (out.value if st == AAF_OK else None)
+
+    # Sparse attention: summaries (int8, a tensor of aaf_kv_summary_bytes entries of any shape, see new_summary), the choice of
+    # blocks for every query token and kv head (int32 [tokens, kv heads, keep]), attention over them.
+    def summary_bytes(self):
+        return aaf_kv_summary_bytes(self.h)
+
+    def new_summary(self):
+        """Room for the summaries of all blocks: int8 [layers, blocks, bytes of a record]; not initialised."""
+        size = self.summary_bytes()
+        if not size:
+            raise ValueError("a pool of 16-bit elements with a head_dim that is a multiple of 8 and at most 256 has summaries")
+        return self.torch.empty((self.L, self.NB, size // (self.L * self.NB)), dtype=self.torch.int8, device=self.device)
+
+    def summarize(self, layer, ctxs, n_new, summary, dtype):
+        """Sums up the blocks of the contexts' last n_new tokens (None: all blocks) in one layer (None: in all).  dtype: torch type of the
+        pool's elements."""
+        n = len(ctxs)
+        code = self._codes.get(dtype)
+        if code is None:
+            raise ValueError(f"bfloat16 or float16 expected, got {dtype}")
+        return load().aaf_kv_summarize(self.h, AAF_ALL_LAYERS if layer is None else layer, code, n, (C.c_int32 * (n or 1))(*ctxs),
+                                       None if n_new is None else (C.c_int32 * (n or 1))(*n_new),
+                                       self._flat(summary, self.torch.int8, self.summary_bytes(), "summary"), summary.numel(),
+                                       self._stream()), None
+
+    def select(self, layer, ctxs, n_q, q, summary, keep, sink=1, recent=1, blocks=None, scores=None):
+        """For every query token and kv head the `keep` blocks with the largest bound on a score, the first `sink` and the last `recent`
+        among them: (status, blocks), int32 [tokens, kv heads, keep], -1 behind the last.  scores: float32 tensor of the same shape."""
+        n = len(ctxs)
+        tokens = n if n_q is None else sum(n_q)
+        heads = q.shape[1] if q.dim() == 3 else 0
+        d = aaf_kv_select_desc(C.sizeof(aaf_kv_select_desc), self._code(q), heads, keep, sink, recent, self._rows(q, tokens, heads, "q", q.dtype))
+        if blocks is None:
+            blocks = q.new_empty((tokens, self.H, max(keep, 0)), dtype=self.torch.int32)
+        size = tokens * self.H * max(keep, 0)
+        st = load().aaf_kv_select(self.h, layer, d, n, (C.c_int32 * (n or 1))(*ctxs), None if n_q is None else (C.c_int32 * (n or 1))(*n_q),
+                                  q.data_ptr(), self._flat(summary, self.torch.int8, self.summary_bytes(), "summary"), summary.numel(),
+                                  self._flat(blocks, self.torch.int32, size, "blocks"),
+                                  None if scores is None else self._flat(scores, self.torch.float32, size, "scores"), self._stream())
+        return st, (blocks if st == AAF_OK else None)
+
+    def attend_blocks(self, layer, ctxs, n_q, q, blocks, out=None, lse=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):
+        """attend over the listed blocks alone: blocks is int32 [tokens, kv heads, keep]; returns (status, (out, lse))."""
+        n = len(ctxs)
+        tokens = n if n_q is None else sum(n_q)
+        a = self._attn(q, tokens, scale, softcap, window, slopes, spans)
+        if blocks.dim() != 3 or blocks.shape[:2] != (tokens, self.H):
+            raise ValueError(f"blocks: expected [{tokens}, {self.H}, keep], got {tuple(blocks.shape)}")
+        keep = blocks.shape[2]
+        out, lse, ws = self._attn_out(q, tokens, a.n_q_heads, out, lse)
+        if ws is None:
+            return AAF_ERR_INVALID_ARG, None
+        st = load().aaf_kv_attend_blocks(self.h, layer, a, n, (C.c_int32 * (n or 1))(*ctxs),
+                                         None if n_q is None else (C.c_int32 * (n or 1))(*n_q), q.data_ptr(),
+                                         self._flat(blocks, self.torch.int32, blocks.numel(), "blocks"), keep, out.data_ptr(), lse.data_ptr(),
+                                         ws.data_ptr(), ws.numel(), self._stream())
+        return st, ((out, lse) if st == AAF_OK else None)
+
+    _BATCH_ARRAYS = ("tables", "lens", "offsets", "token_row", "positions", "slots")
+
+    def batch_tables(self, ctxs, n_new=None, rows=None, tokens=None, cols=None, out=None):
+        """Device arrays of a batch for kernels of one's own (see aaf_kv_batch_tables): (status, dict of tables, lens, offsets,
+        token_row (int32), positions, slots (int64)).  rows, tokens, cols: the arrays' sizes, by default the batch's own.  out: a dict of
+        some or all of them to be filled instead."""
+        torch = self.torch
+        n = len(ctxs)
+        total = n if n_new is None else sum(n_new)
+        rows, tokens = n if rows is None else rows, total if tokens is None else tokens
+        if cols is None:
+            if out is not None and "tables" in out:
+                cols = out["tables"].shape[-1]
+            else:
+                cols = max([-(-(self.ctx_len(c) or 0) // self.BS) for c in ctxs], default=0)
+        shapes = dict(tables=(rows, cols), lens=(rows,), offsets=(rows + 1,), token_row=(tokens,), positions=(tokens,), slots=(tokens,))
+        types = {k: torch.int64 if k in ("positions", "slots") else torch.int32 for k in shapes}
+        if out is None:
+            if min(rows, tokens, cols) < 0:
+                return AAF_ERR_DST_TOO_SMALL, None
+            out = {k: torch.empty(shapes[k], dtype=types[k], device=self.device) for k in self._BATCH_ARRAYS}
+        elif set(out) - set(shapes) or any(t.shape != shapes[k] for k, t in out.items()):
+            raise ValueError(f"out: expected some of {shapes}")
+        ptrs = [self._flat(out[k], types[k], out[k].numel(), k) if k in out else None for k in self._BATCH_ARRAYS]
+        d = aaf_kv_batch_desc(C.sizeof(aaf_kv_batch_desc), rows, tokens, cols, *ptrs)
+        st = load().aaf_kv_batch_tables(self.h, d, n, (C.c_int32 * (n or 1))(*ctxs), None if n_new is None else (C.c_int32 * (n or 1))(*n_new),
+                                        self._stream())
+        return st, (out if st == AAF_OK else None)
 
     def materialize_host(self, ctx, t0, t1, dst_host, staging):
         return aaf_kv_materialize_host(self.h, ctx, t0, t1, dst_host.data_ptr(),

@@ -1,0 +1,340 @@
+// Attention of query tokens over listed blocks of their contexts: every query token and kv head has a list of its own.
+//
+//   s_rt = score(q_r . k_t) for the tokens t of the listed blocks that the row sees,  o_r = sum_t exp(s_rt) v_t / sum_t exp(s_rt)
+//
+// Bound: a listed block's keys and values are used by one kv head's group of query heads only, so their bytes decide.  The shape
+// is that of the kernel for few rows: a warp owns a query token, a kv head and a part of the list, shares nothing with
+// other warps, and takes 16 tokens at a time as the M side of the products with its rows as the N side; weights in two 16-bit parts.
+// What differs: tokens come through the list and then the table, two loads that are asked for ahead of the copies; and all
+// rows of a warp belong to one query token, so they see the same keys.  A key that is not seen is not read: its key and value are
+// zeros, its score is -inf.
+#include "sparse_device.cuh"
+
+namespace aafkv {
+
+template <int DP> struct ListShape {
+    static constexpr int PIECES = DP / 8;           // 16-byte pieces of a row
+    static constexpr int ROW = DP * 2, HALF = 16 * ROW;  // bytes of a row, of a tile of 16 keys (or values)
+    static constexpr int STAGE_BYTES = 2 * HALF;
+    static constexpr int WARPS = DP <= 128 ? 4 : 3;
+    static constexpr int STAGES = DP == 64 ? 6 : (DP == 128 ? 3 : 2);
+    static constexpr int SMEM = WARPS * STAGES * STAGE_BYTES;
+    static_assert(2 * (SMEM + 1024) <= 228 * 1024, "shared memory of a CTA");
+};
+
+// SIMPLE: neither cap nor bias, a score is a multiple of the product
+template <typename T, int DP, int NT, bool SIMPLE>
+__global__ void __launch_bounds__(ListShape<DP>::WARPS * 32, 2)
+    attend_blocks_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small, int row_groups) {
+    using S = ListShape<DP>;
+    extern __shared__ __align__(16) char smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int g = lane >> 2, t4 = lane & 3;
+    const long long task = (long long)blockIdx.x * S::WARPS + warp;
+    if (task >= (long long)p.total_units * p.H * row_groups) return;
+    const long long unit_h = task / row_groups;
+    const int first_row = (int)(task - unit_h * row_groups) * NT * 8;  // of the group's heads
+    const int unit = (int)(unit_h / p.H), head = (int)(unit_h - (long long)unit * p.H);
+    asm volatile("griddepcontrol.launch_dependents;");  // the join may be brought up beside this kernel
+    const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
+    const AttnSeq sq = seqs[find_seq(seqs, p.n, unit)];
+    const int j = (unit - sq.unit0) / sq.nsplit, part = unit - sq.unit0 - j * sq.nsplit;
+    const int R = min(NT * 8, p.G - first_row);
+    const long long tok = sq.row0 + j;
+    RowSpan span = row_span(p, sq, j);
+    const int *list = p.lists + (tok * p.H + head) * p.keep;
+    if (!SIMPLE && p.slopes) span.near = listed_near(p, sq, list, span);
+    float slope[SIMPLE ? 1 : NT][2];
+    if (!SIMPLE) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                slope[nt][c] = p.slopes ? p.slopes[head * p.G + first_row + min(nt * 8 + 2 * t4 + c, R - 1)] : 0.0f;
+    }
+    // listed tokens, numbered through the list: those of this part
+    const int blocks = (sq.len + p.BS - 1) / p.BS;
+    int used = p.keep;
+    if (p.keep > blocks) {  // such a list is filled up: its last entry that names a block
+        used = 0;
+        for (int i = lane; i < p.keep; i += 32) {
+            const int b = __ldg(list + i);
+            if (b >= 0 && b < blocks) used = i + 1;
+        }
+        used = (int)__reduce_max_sync(0xffffffffu, (unsigned)used);
+    }
+    const int beg = part * sq.chunk, end = part + 1 < sq.nsplit ? min(beg + sq.chunk, used * p.BS) : used * p.BS;
+    const int tiles = max(0, end - beg + 15) / 16;
+
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S::STAGES * S::STAGE_BYTES);
+    // where piece c of row r lies: lanes that read together have two rows and four pieces of K, four even (odd) rows and two
+    // pieces of V
+    auto k_at = [](int r, int c) { return (uint32_t)(r * S::ROW + ((c ^ ((r & 1) << 2)) << 4)); };
+    auto v_at = [](int r, int c) { return (uint32_t)(S::HALF + r * S::ROW + ((c ^ (r & 6)) << 4)); };
+    const int *table = p.tables + (long long)sq.ctx * p.max_blk;
+    const char *kb = p.kbase + (long long)head * p.D * 2;
+
+    // lane l looks after the tile's token l % 16: its block's table position, then its position in the context (-1: not seen)
+    // and its block
+    auto listed = [&](int tile) -> int {
+        const int u = beg + tile * 16 + (lane & 15);
+        return u < end ? __ldg(list + block_of(u, p.BS, p.bs_shift)) : -1;
+    };
+    struct Key {
+        int t, id;
+    };
+    auto key_of = [&](int tile, int entry) -> Key {
+        Key k{-1, 0};
+        if (entry >= 0 && entry < blocks) {
+            const int u = beg + tile * 16 + (lane & 15);
+            const int t = entry * p.BS + (u - block_of(u, p.BS, p.bs_shift) * p.BS);
+            if (t >= span.lo && t < span.hi) {
+                k.t = t;
+                k.id = __ldg(table + entry);
+            }
+        }
+        return k;
+    };
+    auto issue = [&](int tile, const Key &k) {
+        if (tile < tiles) {
+            const int b = block_of(max(k.t, 0), p.BS, p.bs_shift);
+            const long long off = k.t < 0 ? -1 : (long long)k.id * 2 * p.run + (long long)(k.t - b * p.BS) * p.row;
+            const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
+            constexpr int AT_ONCE = 32 / S::PIECES;  // rows of one copy instruction
+            const int c = lane % S::PIECES;
+#pragma unroll
+            for (int i = 0; i < 16 / AT_ONCE; ++i) {
+                const int r = i * AT_ONCE + lane / S::PIECES;
+                const long long at = __shfl_sync(0xffffffffu, off, r);
+                const bool in = at >= 0 && c * 8 < p.D;
+                const char *src = kb + at + c * 16;
+                copy16(st + k_at(r, c), in ? src : kb, in ? 16 : 0);
+                copy16(st + v_at(r, c), in ? src + p.run : kb, in ? 16 : 0);
+            }
+        }
+        copy_commit();
+    };
+
+    int pos[S::STAGES];  // of the tokens whose copies are under way
+    int entry = listed(0), after = listed(1);
+    Key key = key_of(0, entry);
+    entry = after;
+#pragma unroll
+    for (int s = 0; s < S::STAGES; ++s) {
+        after = listed(s + 2);
+        const Key nxt = key_of(s + 1, entry);
+        issue(s, key);
+        pos[s] = key.t;
+        key = nxt;
+        entry = after;
+    }
+
+    // query fragments: row nt * 8 + g, 8 dimensions at kk * 32 + t4 * 8
+    uint4 qf[NT][DP / 32];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int r = nt * 8 + g;
+        const T *q = static_cast<const T *>(p.q) + tok * p.q_stride + (long long)(head * p.G + first_row + min(r, R - 1)) * p.D;
+#pragma unroll
+        for (int kk = 0; kk < DP / 32; ++kk) {
+            const int d = kk * 32 + t4 * 8;
+            qf[nt][kk] = r < R && d < p.D ? __ldg(reinterpret_cast<const uint4 *>(q + d)) : make_uint4(0, 0, 0, 0);
+        }
+    }
+
+    const float c2 = p.scale * LOG2E;
+    float o[NT][DP / 16][4];
+    float m[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        m[nt][0] = m[nt][1] = -CUDART_INF_F;
+        l[nt][0] = l[nt][1] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.0f;
+    }
+
+    for (int tile = 0; tile < tiles; ++tile) {
+        copy_wait<S::STAGES - 1>();
+        __syncwarp();  // every lane's pieces have landed
+        const unsigned seen = __ballot_sync(0xffffffffu, pos[0] >= 0);
+        if (seen) {
+            const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
+            float s[NT][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
+#pragma unroll
+            for (int kk = 0; kk < DP / 32; ++kk) {
+                const uint4 w = lds16(st + k_at(g, kk * 4 + t4)), x = lds16(st + k_at(g + 8, kk * 4 + t4));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    Elt<T>::mma(s[nt], w.x, x.x, w.y, x.y, qf[nt][kk].x, qf[nt][kk].y);
+                    Elt<T>::mma(s[nt], w.z, x.z, w.w, x.w, qf[nt][kk].z, qf[nt][kk].w);
+                }
+            }
+            const int t_of[2] = {SIMPLE ? 0 : __shfl_sync(0xffffffffu, pos[0], g), SIMPLE ? 0 : __shfl_sync(0xffffffffu, pos[0], g + 8)};
+            uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float mx[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float &x = s[nt][2 * h + c];
+                        x = seen >> (g + 8 * h) & 1 ? (SIMPLE ? x * c2 : score2(p, x, slope[SIMPLE ? 0 : nt][c], span, t_of[h])) : -CUDART_INF_F;
+                    }
+                    mx[c] = fmaxf(s[nt][c], s[nt][2 + c]);
+                }
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                    mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], d));
+                    mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], d));
+                }
+                const float n0 = fmaxf(m[nt][0], mx[0]), n1 = fmaxf(m[nt][1], mx[1]);
+                if (__any_sync(0xffffffffu, n0 > m[nt][0] || n1 > m[nt][1])) {  // a new maximum: rescale what is summed
+                    const float a0 = n0 == -CUDART_INF_F ? 1.0f : ex2(m[nt][0] - n0);
+                    const float a1 = n1 == -CUDART_INF_F ? 1.0f : ex2(m[nt][1] - n1);
+                    l[nt][0] *= a0;
+                    l[nt][1] *= a1;
+#pragma unroll
+                    for (int i = 0; i < DP / 16; ++i) {
+                        o[nt][i][0] *= a0;
+                        o[nt][i][1] *= a1;
+                        o[nt][i][2] *= a0;
+                        o[nt][i][3] *= a1;
+                    }
+                    m[nt][0] = n0;
+                    m[nt][1] = n1;
+                }
+                const float b0 = n0 == -CUDART_INF_F ? 0.0f : n0 - Elt<T>::RAISE, b1 = n1 == -CUDART_INF_F ? 0.0f : n1 - Elt<T>::RAISE;
+                const float p0 = ex2(s[nt][0] - b0), p1 = ex2(s[nt][1] - b1);
+                const float p2 = ex2(s[nt][2] - b0), p3 = ex2(s[nt][3] - b1);
+                l[nt][0] += p0 + p2;
+                l[nt][1] += p1 + p3;
+                const uint32_t h01 = Elt<T>::pack(p0, p1), h23 = Elt<T>::pack(p2, p3);
+                const uint32_t l01 = Elt<T>::pack(p0 - Elt<T>::lo(h01), p1 - Elt<T>::hi(h01));
+                const uint32_t l23 = Elt<T>::pack(p2 - Elt<T>::lo(h23), p3 - Elt<T>::hi(h23));
+                ph[nt][0] = transpose8x8(h01);
+                ph[nt][1] = transpose8x8(h23);
+                pl[nt][0] = transpose8x8(l01);
+                pl[nt][1] = transpose8x8(l23);
+            }
+#pragma unroll
+            for (int c = 0; c < DP / 64; ++c) {
+                uint4 v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = lds16(st + v_at(2 * t4 + (i & 1) + (i >> 1) * 8, c * 8 + g));
+                const uint32_t w0[4] = {v[0].x, v[0].y, v[0].z, v[0].w}, w1[4] = {v[1].x, v[1].y, v[1].z, v[1].w};
+                const uint32_t w2[4] = {v[2].x, v[2].y, v[2].z, v[2].w}, w3[4] = {v[3].x, v[3].y, v[3].z, v[3].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t a[4] = {prmt(w0[i], w1[i], 0x5410), prmt(w0[i], w1[i], 0x7632), prmt(w2[i], w3[i], 0x5410),
+                                           prmt(w2[i], w3[i], 0x7632)};
+                    // An infinite value times the high part of its weight is infinite; times the low part, which may be zero
+                    // or negative, it would make a NaN of that: there it is the type's largest value.
+                    uint32_t b[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) b[e] = Elt<T>::bounded(a[e]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        Elt<T>::mma(o[nt][4 * c + i], a[0], a[1], a[2], a[3], ph[nt][0], ph[nt][1]);
+                        Elt<T>::mma(o[nt][4 * c + i], b[0], b[1], b[2], b[3], pl[nt][0], pl[nt][1]);
+                    }
+                }
+            }
+        }
+        after = listed(tile + S::STAGES + 2);
+        const Key nxt = key_of(tile + S::STAGES + 1, entry);
+        __syncwarp();  // every lane has read this stage
+        issue(tile + S::STAGES, key);
+#pragma unroll
+        for (int s = 0; s + 1 < S::STAGES; ++s) pos[s] = pos[s + 1];
+        pos[S::STAGES - 1] = key.t;
+        key = nxt;
+        entry = after;
+    }
+    copy_wait<0>();
+
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float sum = l[nt][c];
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            const int r = nt * 8 + 2 * t4 + c;
+            if (r >= R) continue;
+            const int hg = first_row + r;  // head of the group
+            if (sq.part0 >= 0) {  // a part of the list: (m, l, o) for the join, laid out as the kernel for few rows does
+                const float some = sum == 0.0f ? 0.0f : 1.0f;
+                const long long pr = sq.part0 + ((long long)part * p.H + head) * sq.nq * p.G + (long long)j * p.G + hg;
+#pragma unroll
+                for (int cc = 0; cc < DP / 64; ++cc) {
+                    const int d = cc * 64 + g * 8;
+                    if (d >= p.D) continue;
+                    float4 *dst = reinterpret_cast<float4 *>(p.part_o + pr * p.D + d);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        dst[i] = make_float4(scaled(o[nt][4 * cc + 2 * i][c], some), scaled(o[nt][4 * cc + 2 * i][2 + c], some),
+                                             scaled(o[nt][4 * cc + 2 * i + 1][c], some), scaled(o[nt][4 * cc + 2 * i + 1][2 + c], some));
+                }
+                if (g == 0) {
+                    p.part_ml[2 * pr] = m[nt][c] - Elt<T>::RAISE;
+                    p.part_ml[2 * pr + 1] = sum;
+                }
+                continue;
+            }
+            const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;  // a row that sees nothing is zero
+            const int hq = head * p.G + hg;
+            T *out = static_cast<T *>(p.out) + (tok * p.H * p.G + hq) * p.D;
+#pragma unroll
+            for (int cc = 0; cc < DP / 64; ++cc) {
+                const int d = cc * 64 + g * 8;
+                if (d >= p.D) continue;
+                uint4 w;
+                w.x = Elt<T>::pack(scaled(o[nt][4 * cc][c], inv), scaled(o[nt][4 * cc][2 + c], inv));
+                w.y = Elt<T>::pack(scaled(o[nt][4 * cc + 1][c], inv), scaled(o[nt][4 * cc + 1][2 + c], inv));
+                w.z = Elt<T>::pack(scaled(o[nt][4 * cc + 2][c], inv), scaled(o[nt][4 * cc + 2][2 + c], inv));
+                w.w = Elt<T>::pack(scaled(o[nt][4 * cc + 3][c], inv), scaled(o[nt][4 * cc + 3][2 + c], inv));
+                *reinterpret_cast<uint4 *>(out + d) = w;
+            }
+            if (p.lse && g == 0)
+                p.lse[tok * p.H * p.G + hq] =
+                    sum == 0.0f ? -CUDART_INF_F
+                                : (m[nt][c] - Elt<T>::RAISE + log2f(sum)) * LN2 - (SIMPLE ? 0.0f : slope[SIMPLE ? 0 : nt][c] * (float)span.near);
+        }
+}
+
+// rows that a lane's registers hold accumulators for, as in the kernel for few rows; larger groups go to several warps
+static int list_tiles(int D, int G) { return std::min((G + 7) / 8, few_rows_limit(D) / 8); }
+int attend_blocks_rows(int D, int G) {
+    const int nt = list_tiles(D, G);
+    return 8 * (nt == 3 ? 4 : nt);
+}
+
+template <typename T, int DP, int NT, bool SIMPLE>
+static cudaError_t list_go(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
+    static SmemSeen seen{0};
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_blocks_kernel<T, DP, NT, SIMPLE>), ListShape<DP>::SMEM, &seen);
+    if (e != cudaSuccess) return e;
+    constexpr int W = ListShape<DP>::WARPS;
+    const int groups = (p.G + NT * 8 - 1) / (NT * 8);
+    const long long tasks = (long long)p.total_units * p.H * groups;
+    attend_blocks_kernel<T, DP, NT, SIMPLE><<<(unsigned)((tasks + W - 1) / W), W * 32, ListShape<DP>::SMEM, st>>>(p, small, groups);
+    return cudaGetLastError();
+}
+template <typename T, int DP, int NT> static cudaError_t list_kind(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
+    return p.softcap == 0.0f && !p.slopes ? list_go<T, DP, NT, true>(p, small, st) : list_go<T, DP, NT, false>(p, small, st);
+}
+template <typename T> static cudaError_t list_pick(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
+    const int nt = list_tiles(p.D, p.G);
+    if (p.D <= 64)
+        return nt == 1 ? list_kind<T, 64, 1>(p, small, st) : (nt == 2 ? list_kind<T, 64, 2>(p, small, st) : list_kind<T, 64, 4>(p, small, st));
+    if (p.D <= 128) return nt == 1 ? list_kind<T, 128, 1>(p, small, st) : list_kind<T, 128, 2>(p, small, st);
+    return list_kind<T, 256, 1>(p, small, st);
+}
+cudaError_t launch_attend_blocks(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st) {
+    return f16 ? list_pick<__half>(p, small, st) : list_pick<__nv_bfloat16>(p, small, st);
+}
+
+}  // namespace aafkv

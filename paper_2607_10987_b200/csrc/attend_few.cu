@@ -18,7 +18,7 @@
 // then carries the output's own rounding only.
 //
 // 64 ragged contexts, 780 MB of keys and values: 145 us with the join (5.4 TB/s); one of 33787 tokens, 138 MB: 33.7.
-#include "attend_device.cuh"
+#include "sparse_device.cuh"
 
 namespace aafkv {
 
@@ -490,9 +490,11 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32)
             *reinterpret_cast<uint2 *>(out + d) = make_uint2(Elt<T>::pack(scaled(acc[half].x, inv), scaled(acc[half].y, inv)),
                                                              Elt<T>::pack(scaled(acc[half].z, inv), scaled(acc[half].w, inv)));
     }
-    if (lane == 0 && p.lse) {
-        const RowSpan sp = row_span(p, sq, j);
-        const float slope = p.slopes ? p.slopes[hq] : 0.0f;
+    if (!p.lse) return;
+    RowSpan sp = row_span(p, sq, j);
+    const float slope = p.slopes ? p.slopes[hq] : 0.0f;
+    if (p.lists && p.slopes) sp.near = listed_near(p, sq, p.lists + (qt * p.H + head) * p.keep, sp);
+    if (lane == 0) {
         p.lse[qt * Hq + hq] = sum == 0.0f ? -CUDART_INF_F : (m + log2f(sum)) * LN2 - slope * (float)sp.near;
     }
 }

@@ -58,6 +58,8 @@ struct AttnParams {
     int *flag;            // wide kernel: written; tile kernel: run only if it holds `epoch` (null: always)
     int *status;          // sticky device status of the pool
     float scale, softcap, inv_cap;  // softcap 0: none
+    const int *lists;     // attention over listed blocks: table positions [query tokens][H][keep]; else null
+    int keep;
 };
 
 struct MassParams {

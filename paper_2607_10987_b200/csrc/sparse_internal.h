@@ -1,0 +1,50 @@
+// Declarations shared by the kernels of sparse attention (block summaries, selection, attention over listed blocks) and of a
+// batch's tables, and their host side in sparse.cu.
+#pragma once
+#include "attend_internal.h"
+
+namespace aafkv {
+
+// A block's summary of one layer: [H][2][D] codes (upper, lower bound of every channel's keys), H exponents, filled up to 16
+// bytes.  Bounds are code * 2^exponent.
+constexpr int SUMMARY_LEAST_EXP = -60;
+inline long long summary_record(int H, int D) { return (long long)H * 2 * D + (H + 15) / 16 * 16; }
+
+struct SummaryParams {
+    const AttnSeq *seqs;  // device records, null: the kernel parameter holds them.  nq: tokens whose blocks are summed up, unit0: first block
+    const int *tables;
+    const char *pool;     // first layer's first byte
+    signed char *summary; // that layer's first record
+    long long layer_stride, run, row, record, summary_stride;  // bytes
+    int max_blk, BS, H, D, n, blocks, layers;
+};
+
+struct SelectParams {
+    const void *q;
+    const AttnSeq *seqs;  // unit0: first unit (a query token and kv head)
+    const int *tables;
+    const signed char *summary;  // the layer's first record
+    int *blocks;          // [query tokens][H][keep]
+    float *scores;        // the same shape, may be null
+    long long q_stride;   // elements
+    long long record;     // bytes
+    int max_blk, BS, H, G, D, n, keep, sink, recent, widest;  // widest: blocks of the longest context
+};
+constexpr int SELECT_MAX_BLOCKS = 49152;  // of a context: their scores stay on the chip
+
+struct TablesParams {
+    const AttnSeq *seqs;
+    const int *src;       // the pool's tables
+    int *tables, *lens, *offsets, *token_row;
+    long long *positions, *slots;
+    int max_blk, BS, n, cols, rows, tokens, total;
+};
+
+cudaError_t launch_summarize(const SummaryParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
+cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, int f16, long long tokens, cudaStream_t st);
+// p.first is not read; a record's nsplit parts of `chunk` listed keys (lists of `keep` blocks); units are (query token, part)
+cudaError_t launch_attend_blocks(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
+int attend_blocks_rows(int D, int G);  // query rows of a unit's warp
+cudaError_t launch_batch_tables(const TablesParams &p, const SmallSeqs &small, cudaStream_t st);
+
+}  // namespace aafkv
