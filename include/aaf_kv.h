@@ -448,8 +448,8 @@ int aaf_kv_prune(aaf_kv_pool *pool, aaf_ctx_t ctx, const float *scores_dev, int6
  * as old as the last aaf_kv_summarize of a context that holds the block: call it for what import, append, store, compose, prune or a copied
  * tail have put into blocks, before aaf_kv_select is to know of it. */
 #define AAF_ALL_LAYERS (-1)
-#define AAF_SELECT_MAX_BLOCKS 49152 /* of a context that aaf_kv_select chooses from */
-#define AAF_LIST_MAX_BLOCKS 1048576 /* of a list                                   */
+#define AAF_SELECT_MAX_BLOCKS 262144 /* of a context that aaf_kv_select chooses from */
+#define AAF_LIST_MAX_BLOCKS 1048576  /* of a list                                     */
 
 size_t aaf_kv_summary_bytes(const aaf_kv_pool *pool);
 

@@ -26,7 +26,7 @@ AAF_ENGINE_AUTO, AAF_ENGINE_VEC, AAF_ENGINE_BULK, AAF_ENGINE_WARP = 0, 1, 2, 3
 AAF_OP_MATERIALIZE, AAF_OP_IMPORT, AAF_OP_APPEND, AAF_OP_COMPOSE, AAF_OP_CLASSES = 0, 1, 2, 3, 4
 AAF_DTYPE_BF16, AAF_DTYPE_F16 = 0, 1
 AAF_ROPE_NONE, AAF_ROPE_LINEAR, AAF_ROPE_BASE, AAF_ROPE_WAVELENGTH, AAF_ROPE_RAMP = 0, 1, 2, 3, 4
-AAF_ALL_LAYERS, AAF_SELECT_MAX_BLOCKS, AAF_LIST_MAX_BLOCKS = -1, 49152, 1048576
+AAF_ALL_LAYERS, AAF_SELECT_MAX_BLOCKS, AAF_LIST_MAX_BLOCKS = -1, 262144, 1048576
 OP_NAMES = ("materialize", "import", "append", "compose")
 
 

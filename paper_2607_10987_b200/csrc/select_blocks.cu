@@ -5,127 +5,382 @@
 //
 // max(c hi, c lo) = max(c, 0) hi + min(c, 0) lo: a product of [c+, c-] with the block's [hi, lo], in whole numbers, exact in any
 // order, and so is the scaling by a power of two; equal scores go to the lower block.
+//
+// A unit is a tile of query tokens of a context and a kv head; a cluster of CTAs takes it, each CTA a stretch of the context's
+// blocks.  Scores: 16 blocks as the M side of 8-bit products, the tile's query rows as the N side, codes straight from memory into
+// the lanes that need them (the order of the channels is free as long as both sides agree: a lane takes 16 consecutive
+// bytes).  They stay in shared memory, as whole numbers of the same order.  Selection: the smallest score that is taken is
+// found eight bits at a time by histograms, which the CTAs of a cluster read from one another; then every CTA knows how many blocks come
+// before its own and writes its part of the list.
+//
+// Bound: the bytes of the summaries where there is a token each; the selection's passes where there are many.
 #include "sparse_device.cuh"
 
 namespace aafkv {
 
-constexpr int SELECT_THREADS = 256;
+constexpr int SELECT_WARPS = 8, SELECT_ROWS = 64;  // query rows of a pass over the summaries
+constexpr int SELECT_TOKENS = 16;                  // of a tile, at most
 
-template <typename T>
-__global__ void __launch_bounds__(SELECT_THREADS)
-    select_blocks_kernel(const __grid_constant__ SelectParams p, const __grid_constant__ SmallSeqs small) {
-    extern __shared__ __align__(16) unsigned char smem_s[];
-    uint32_t *keys = reinterpret_cast<uint32_t *>(smem_s);                               // [widest]
-    int *codes = reinterpret_cast<int *>(smem_s + ((size_t)p.widest * 4 + 15) / 16 * 16);  // [G][2 D / 4]
-    __shared__ int count_s[SELECT_THREADS / 32 + 1], exps[128];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int unit = blockIdx.x / p.H, head = blockIdx.x - unit * p.H;
+__device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// a word of another CTA's shared memory: the one that lies there where `addr` lies here
+__device__ __forceinline__ uint32_t peer_word(uint32_t addr, int cta) {
+    uint32_t at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(cta));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+
+// SPANS: 64-byte stretches of a head's codes (2 head_dim bytes); NT: n-tiles of 8 query rows that are accumulated at a time
+template <int SPANS, int NT>
+__global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
+    select_blocks_kernel(const __grid_constant__ SelectParams p, const __grid_constant__ SmallSeqs small, const __grid_constant__ SelectShape z) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    uint32_t *keys = reinterpret_cast<uint32_t *>(smem);                    // [tile][room]
+    uint32_t *hist = keys + z.tile * z.room;                                // [2][tile][256]
+    unsigned char *codes = reinterpret_cast<unsigned char *>(hist + 2 * z.tile * 256);  // [rows][stride]
+    __shared__ int exps[SELECT_ROWS];
+    __shared__ uint32_t prefix_s[SELECT_TOKENS];                            // of a list: the threshold's leading bits
+    __shared__ int want_s[SELECT_TOKENS];                                   // how many of those with these bits are taken; -1: all
+    __shared__ uint32_t counts_s[SELECT_WARPS][2];                          // of a warp's pieces: certainly taken, equal to the threshold
+    __shared__ uint32_t list_counts_s[SELECT_TOKENS][2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t4 = lane & 3;
+    const int cta = z.ctas > 1 ? (int)cluster_rank() : 0;
+    const int unit = blockIdx.x / z.ctas / p.H, head = blockIdx.x / z.ctas - unit * p.H;
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
     const AttnSeq s = seqs[find_seq(seqs, p.n, unit)];
-    const int j = unit - s.unit0;
-    const long long row = s.row0 + j;
-    const int last = (s.len - s.nq + j) / p.BS, total = last + 1, words = p.D / 2;
-    int *out = p.blocks + (row * p.H + head) * p.keep;
-    float *out_s = p.scores ? p.scores + (row * p.H + head) * p.keep : nullptr;
-    for (int b = threadIdx.x; b < total; b += SELECT_THREADS) keys[b] = 0;
-    for (int g0 = 0; g0 < p.G; g0 += 16) {
-        const int rows = min(16, p.G - g0);
-        __syncthreads();
-        for (int r = warp; r < rows; r += SELECT_THREADS / 32) {
-            const T *q = static_cast<const T *>(p.q) + row * p.q_stride + (long long)(head * p.G + g0 + r) * p.D;
-            float top = 0.0f;
-            for (int d = lane; d < p.D; d += 32) {
-                const float x = Elt<T>::from(reinterpret_cast<const uint16_t *>(q)[d]);
-                if (x == x) top = fmaxf(top, fminf(fabsf(x), 127.0f * 0x1p113f));
+    const int j0 = (unit - s.unit0) * z.tile, tokens = min(z.tile, s.nq - j0);
+    const int pos0 = s.len - s.nq + j0;  // position of the tile's first token
+    const int total = (pos0 + tokens - 1) / p.BS + 1;  // blocks that some token of the tile may take
+    const int stretch = ((total + z.ctas - 1) / z.ctas + 15) / 16 * 16;
+    const int b0 = min(cta * stretch, total), count = min(stretch, total - b0);
+    auto sync_all = [&]() {
+        if (z.ctas > 1) cluster_sync();
+        else __syncthreads();
+    };
+    auto key_at = [&](int list, int i) -> uint32_t & { return keys[list * z.room + i]; };
+
+    for (int i = threadIdx.x; i < z.tile * 256; i += SELECT_WARPS * 32) hist[i] = 0;
+    if (threadIdx.x < z.tile) {
+        const int last = (pos0 + min((int)threadIdx.x, tokens - 1)) / p.BS;
+        const int want = p.keep - p.sink - p.recent;
+        prefix_s[threadIdx.x] = 0;
+        want_s[threadIdx.x] = last + 1 <= p.keep ? -1 : want;
+    }
+
+    // ---- scores
+    const int *table = p.tables + (long long)s.ctx * p.max_blk + b0;
+    const int rows_all = z.tile * z.heads_p;
+    for (int row0 = 0; row0 < rows_all; row0 += z.rows) {
+        if (row0) __syncthreads();
+        const int rows = min(z.rows, (rows_all - row0 + 7) / 8 * 8);
+        for (int r = warp; r < rows; r += SELECT_WARPS) {  // a row's codes: [c+, c-], zeros behind them
+            const int tok = min((row0 + r) / z.heads_p, tokens - 1), gh = min((row0 + r) % z.heads_p, p.G - 1);
+            const uint16_t *q = static_cast<const uint16_t *>(p.q) + (long long)(s.row0 + j0 + tok) * p.q_stride + (long long)(head * p.G + gh) * p.D;
+            const uint4 v = lane * 8 < p.D ? __ldg(reinterpret_cast<const uint4 *>(q) + lane) : make_uint4(0, 0, 0, 0);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            float x[8], top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint16_t b = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+                x[i] = z.f16 ? Elt<__half>::from(b) : Elt<__nv_bfloat16>::from(b);
+                x[i] = x[i] != x[i] ? 0.0f : fminf(fmaxf(x[i], -127.0f * 0x1p113f), 127.0f * 0x1p113f);
+                top = fmaxf(top, fabsf(x[i]));
             }
             const int f = code_exponent(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top))));
-            signed char *c = reinterpret_cast<signed char *>(codes + r * words);
-            for (int d = lane; d < p.D; d += 32) {
-                const float x = Elt<T>::from(reinterpret_cast<const uint16_t *>(q)[d]);
-                const int v = x != x ? 0 : __float2int_rn(fminf(fmaxf(x, -127.0f * 0x1p113f), 127.0f * 0x1p113f) * power_of_two(-f));
-                c[d] = (signed char)max(v, 0);
-                c[p.D + d] = (signed char)min(v, 0);
+            const float unit_inv = power_of_two(-f);
+            uint32_t up[2] = {0, 0}, down[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = __float2int_rn(x[i] * unit_inv);
+                up[i / 4] |= (uint32_t)max(c, 0) << (8 * (i & 3));
+                down[i / 4] |= ((uint32_t)min(c, 0) & 255u) << (8 * (i & 3));
             }
+            unsigned char *dst = codes + r * z.stride;
+            if (lane * 8 < p.D) {
+                *reinterpret_cast<uint2 *>(dst + lane * 8) = make_uint2(up[0], up[1]);
+                *reinterpret_cast<uint2 *>(dst + p.D + lane * 8) = make_uint2(down[0], down[1]);
+            }
+            for (int i = 2 * p.D + lane * 8; i < SPANS * 64; i += 256) *reinterpret_cast<uint2 *>(dst + i) = make_uint2(0, 0);
             if (lane == 0) exps[r] = f;
         }
         __syncthreads();
-        for (int b = threadIdx.x; b < total; b += SELECT_THREADS) {
-            const signed char *rec = p.summary + (long long)__ldg(p.tables + (long long)s.ctx * p.max_blk + b) * p.record;
-            const int e = rec[(long long)p.H * 2 * p.D + head];
-            const int *code = reinterpret_cast<const int *>(rec + (long long)head * 2 * p.D);
-            uint32_t best = keys[b];
-            for (int r = 0; r < rows; ++r) {
-                int dot = 0;
-                for (int w = 0; w < words; ++w) dot = __dp4a(code[w], codes[r * words + w], dot);
-                const int x = e + exps[r];  // -120 ... 226
-                best = max(best, ordered((float)dot * power_of_two(min(x, 100)) * power_of_two(max(x, 100) - 100)));
+        auto id_of = [&](int m) {
+            const int i = m * 16 + (lane & 15);
+            return i < count ? __ldg(table + i) : -1;
+        };
+        int id = id_of(warp);
+        for (int m = warp; m * 16 < count; m += SELECT_WARPS) {
+            const int ids[2] = {__shfl_sync(0xffffffffu, id, g), __shfl_sync(0xffffffffu, id, g + 8)};
+            id = id_of(m + SELECT_WARPS);
+            uint4 a[SPANS][2];
+            int e[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const signed char *rec = p.summary + (long long)max(ids[h], 0) * p.record;
+                e[h] = ids[h] < 0 ? 0 : __ldg(rec + (long long)p.H * 2 * p.D + head);
+#pragma unroll
+                for (int sp = 0; sp < SPANS; ++sp) {
+                    const int at = sp * 64 + t4 * 16;
+                    a[sp][h] = ids[h] >= 0 && at < 2 * p.D ? __ldg(reinterpret_cast<const uint4 *>(rec + (long long)head * 2 * p.D + at)) : make_uint4(0, 0, 0, 0);
+                }
             }
-            keys[b] = best;
+            for (int n0 = 0; n0 < rows; n0 += NT * 8) {
+                int c[NT][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0;
+                    if (n0 + nt * 8 < rows) {
+                        const unsigned char *src = codes + (n0 + nt * 8 + g) * z.stride + t4 * 16;
+#pragma unroll
+                        for (int sp = 0; sp < SPANS; ++sp) {
+                            const uint4 b = *reinterpret_cast<const uint4 *>(src + sp * 64);
+                            mma_s8(c[nt], a[sp][0].x, a[sp][1].x, a[sp][0].y, a[sp][1].y, b.x, b.y);
+                            mma_s8(c[nt], a[sp][0].z, a[sp][1].z, a[sp][0].w, a[sp][1].w, b.z, b.w);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int r = n0 + nt * 8 + 2 * t4;  // this lane's rows: r, r + 1
+                    if (n0 + nt * 8 >= rows) break;
+                    const int f[2] = {exps[r], exps[r + 1]};
+                    uint32_t k[2][2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int x = e[h] + f[i];  // -120 ... 226
+                            k[h][i] = ordered((float)c[nt][2 * h + i] * power_of_two(min(x, 100)) * power_of_two(max(x, 100) - 100));
+                        }
+                    auto put = [&](int list, int h, uint32_t v) {
+                        const int i = m * 16 + g + 8 * h;
+                        if (list < z.tile && i < count) {
+                            uint32_t &at = key_at(list, i);
+                            at = z.heads_p > 8 && (row0 + n0 + nt * 8) % z.heads_p ? max(at, v) : v;  // a token's later rows
+                        }
+                    };
+                    if (z.heads_p == 1) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            put(row0 + r, h, k[h][0]);
+                            put(row0 + r + 1, h, k[h][1]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t v = max(k[h][0], k[h][1]);
+                            if (z.heads_p >= 4) v = max(v, __shfl_xor_sync(0xffffffffu, v, 1));
+                            if (z.heads_p >= 8) v = max(v, __shfl_xor_sync(0xffffffffu, v, 2));
+                            if (((2 * t4) & (min(z.heads_p, 8) - 1)) == 0) put((row0 + r) / z.heads_p, h, v);
+                        }
+                    }
+                }
+            }
         }
     }
     __syncthreads();
-    // the middle [sink, total - recent): the smallest key of those taken, bit by bit
-    const int m0 = min(p.sink, total), m1 = max(m0, total - p.recent), want = p.keep - p.sink - p.recent;
-    auto count = [&](uint32_t from) {
-        int c = 0;
-        for (int b = m0 + threadIdx.x; b < m1; b += SELECT_THREADS) c += keys[b] >= from;
-        c = __reduce_add_sync(0xffffffffu, c);
+
+    // ---- selection: a list is looked after by `team` warps, each with a piece of the CTA's stretch
+    const int team = max(1, SELECT_WARPS / z.tile), wl = warp % team, lists_at_once = SELECT_WARPS / team;
+    const int piece = ((count + team - 1) / team + 31) / 32 * 32, i0 = min(wl * piece, count), i1 = min(i0 + piece, count);
+    auto last_of = [&](int list) { return (pos0 + list) / p.BS; };
+    for (int pass = 0; pass < 4; ++pass) {
+        const int shift = 24 - 8 * pass;
+        uint32_t *now = hist + (pass & 1) * z.tile * 256, *next = hist + (~pass & 1) * z.tile * 256;
+        bool any = false;
+        for (int list = 0; list < tokens; ++list) any |= want_s[list] > 0;
+        if (!any) break;  // the same in all CTAs of the cluster
+        for (int list = warp / team; list < tokens; list += lists_at_once) {
+            if (want_s[list] <= 0) continue;
+            const uint32_t prefix = prefix_s[list];
+            const int lo = max(i0, p.sink - b0), hi = min(i1, last_of(list) + 1 - p.recent - b0);
+            for (int i = lo + lane; i < hi; i += 32) {
+                const uint32_t k = key_at(list, i);
+                if (pass == 0 || k >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(now + list * 256 + (k >> shift & 255), 1u);
+            }
+        }
+        sync_all();
+        for (int i = threadIdx.x; i < z.tile * 256; i += SELECT_WARPS * 32) next[i] = 0;
+        for (int list = warp / team; list < tokens; list += lists_at_once) {
+            const int want = want_s[list];
+            if (want <= 0 || wl) continue;
+            uint32_t n[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n[i] = 0;
+            const uint32_t at = (uint32_t)__cvta_generic_to_shared(now + list * 256 + lane * 8);
+            for (int c = 0; c < z.ctas; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) n[i] += z.ctas > 1 ? peer_word(at + 4 * i, c) : now[list * 256 + lane * 8 + i];
+            uint32_t mine = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mine += n[i];
+            uint32_t above = mine;  // of this lane's digits and larger ones
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const uint32_t v = __shfl_down_sync(0xffffffffu, above, d);
+                if (lane + d < 32) above += v;
+            }
+            above -= mine;
+            if ((int)above < want && want <= (int)(above + mine)) {  // one lane
+                uint32_t left = (uint32_t)want - above, here = 0;
+                int digit = 7;
+#pragma unroll
+                for (int i = 7; i >= 0; --i) {
+                    if (digit == i && left > n[i]) {
+                        left -= n[i];
+                        digit = i - 1;
+                    }
+                    if (digit == i) here = n[i];
+                }
+                prefix_s[list] |= (uint32_t)(lane * 8 + digit) << shift;
+                // all with these bits are taken: the threshold is the smallest number with them
+                want_s[list] = here == left ? -2 : (int)left;
+            }
+        }
         __syncthreads();
-        if (lane == 0) count_s[warp] = c;
-        __syncthreads();
-        int t = 0;
-        for (int w = 0; w < SELECT_THREADS / 32; ++w) t += count_s[w];
-        return t;
+    }
+    // want_s: -1 every block is taken; -2 those from prefix_s on; else (0 too) those above prefix_s, and so many of those equal to it
+    auto kind_of = [&](int list, int i, bool &tie) -> bool {  // certainly taken
+        const int b = b0 + i, last = last_of(list);
+        tie = false;
+        if (b > last) return false;
+        if (b < p.sink || b > last - p.recent) return true;
+        const int want = want_s[list];
+        const uint32_t k = key_at(list, i), least = prefix_s[list];
+        if (want == -1) return true;
+        if (want == -2) return k >= least;
+        if (p.keep == p.sink + p.recent) return false;
+        tie = k == least;
+        return k > least;
     };
-    uint32_t least = 0;
-    int ties = 0x7fffffff;
-    if (m1 - m0 > want) {
-        if (want <= 0) {
-            least = 0xffffffffu;
-            ties = 0;
-        } else {
-            for (int bit = 31; bit >= 0; --bit)
-                if (count(least | 1u << bit) >= want) least |= 1u << bit;
-            ties = want - (least == 0xffffffffu ? 0 : count(least + 1));
+    for (int list = warp / team; list < tokens; list += lists_at_once) {
+        uint32_t sure = 0, ties = 0;
+        for (int i = i0 + lane; i < i1; i += 32) {
+            bool tie;
+            sure += kind_of(list, i, tie);
+            ties += tie;
+        }
+        sure = __reduce_add_sync(0xffffffffu, sure);
+        ties = __reduce_add_sync(0xffffffffu, ties);
+        if (lane == 0) {
+            if (team > 1) {
+                counts_s[warp][0] = sure;
+                counts_s[warp][1] = ties;
+            } else {
+                list_counts_s[list][0] = sure;
+                list_counts_s[list][1] = ties;
+            }
         }
     }
-    __syncthreads();
-    if (warp == 0) {
-        int at = 0, tied = 0;
-        for (int b0 = 0; b0 < total; b0 += 32) {
-            const int b = b0 + lane;
-            const bool in = b < total, middle = in && b >= m0 && b < m1;
-            const uint32_t k = in ? keys[b] : 0;
-            const bool tie = middle && k == least;
-            const unsigned tm = __ballot_sync(0xffffffffu, tie);
-            const int before = tied + __popc(tm & ((1u << lane) - 1));
-            const bool take = in && (!middle || k > least || (tie && before < ties));
-            const unsigned mask = __ballot_sync(0xffffffffu, take);
-            const int to = at + __popc(mask & ((1u << lane) - 1));
-            if (take) {
-                out[to] = b;
-                if (out_s) out_s[to] = from_ordered(k);
+    if (team > 1) {
+        __syncthreads();
+        if (threadIdx.x < tokens) {
+            uint32_t a = 0, b = 0;
+            for (int w = 0; w < team; ++w) {
+                a += counts_s[threadIdx.x * team + w][0];
+                b += counts_s[threadIdx.x * team + w][1];
             }
-            at += __popc(mask);
-            tied += __popc(tm);
+            list_counts_s[threadIdx.x][0] = a;
+            list_counts_s[threadIdx.x][1] = b;
         }
-        for (int i = at + lane; i < p.keep; i += 32) {
-            out[i] = -1;
-            if (out_s) out_s[i] = -CUDART_INF_F;
+    }
+    sync_all();
+    for (int list = warp / team; list < tokens; list += lists_at_once) {
+        const int ties_taken = max(want_s[list], 0);
+        uint32_t sure = 0, ties = 0;  // before this warp's piece
+        for (int c = 0; c < cta; ++c) {
+            const uint32_t at = (uint32_t)__cvta_generic_to_shared(&list_counts_s[list][0]);
+            sure += peer_word(at, c);
+            ties += peer_word(at + 4, c);
         }
+        for (int w = 0; w < wl; ++w) {
+            sure += counts_s[warp - wl + w][0];
+            ties += counts_s[warp - wl + w][1];
+        }
+        const long long at0 = ((long long)(s.row0 + j0 + list) * p.H + head) * p.keep;
+        for (int base = i0; base < i1; base += 32) {
+            const int i = base + lane;
+            bool tie = false;
+            const bool certain = i < i1 && kind_of(list, i, tie);
+            const unsigned cm = __ballot_sync(0xffffffffu, certain), tm = __ballot_sync(0xffffffffu, tie), under = (1u << lane) - 1;
+            const int ties_before = (int)ties + __popc(tm & under);
+            if (certain || (tie && ties_before < ties_taken)) {
+                const int to = (int)sure + __popc(cm & under) + min(ties_before, ties_taken);
+                p.blocks[at0 + to] = b0 + i;
+                if (p.scores) p.scores[at0 + to] = from_ordered(key_at(list, i));
+            }
+            sure += __popc(cm);
+            ties += __popc(tm);
+        }
+        if (cta == 0)
+            for (int i = min(p.keep, last_of(list) + 1) + wl * 32 + lane; i < p.keep; i += team * 32) {
+                p.blocks[at0 + i] = -1;
+                if (p.scores) p.scores[at0 + i] = -CUDART_INF_F;
+            }
+    }
+    if (z.ctas > 1) cluster_sync();  // the others have read this CTA's counts
+}
+
+static size_t select_smem(const SelectShape &z) { return (size_t)z.tile * z.room * 4 + (size_t)2 * z.tile * 256 * 4 + (size_t)z.rows * z.stride; }
+constexpr size_t SELECT_SMEM = 220 * 1024;
+
+// How a batch is cut: tokens of a tile, CTAs of a cluster.
+SelectShape select_shape(const SelectParams &p, int max_nq, long long tokens, int sm_count, int f16) {
+    SelectShape z{};
+    z.f16 = f16;
+    z.heads_p = p.G > 8 ? (p.G + 7) / 8 * 8 : (p.G > 4 ? 8 : (p.G > 2 ? 4 : p.G));
+    const int spans = p.D <= 64 ? 2 : (p.D <= 128 ? 4 : 8);
+    z.stride = spans * 64 + 64;
+    for (z.tile = 1; z.tile < SELECT_TOKENS && z.tile < max_nq && 2 * z.tile * z.heads_p <= SELECT_ROWS; z.tile *= 2) {}
+    for (;;) {
+        z.rows = std::min((z.tile * z.heads_p + 7) / 8 * 8, SELECT_ROWS);
+        const long long units = (tokens + z.tile - 1) / z.tile * p.H;
+        for (z.ctas = 1;; z.ctas *= 2) {
+            z.room = ((p.widest + z.ctas - 1) / z.ctas + 15) / 16 * 16;
+            if (z.ctas == 8) break;
+            const bool fits = select_smem(z) <= SELECT_SMEM / 2;  // two CTAs an SM
+            if (fits && (units * z.ctas >= 2ll * sm_count || z.room <= 128)) break;
+        }
+        if (z.tile == 1 || select_smem(z) <= SELECT_SMEM) return z;
+        z.tile /= 2;
     }
 }
 
-template <typename T> static cudaError_t select_go(const SelectParams &p, const SmallSeqs &small, long long tokens, cudaStream_t st) {
+template <int SPANS, int NT> static cudaError_t select_go(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, cudaStream_t st) {
     static SmemSeen seen{0};
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(select_blocks_kernel<T>), 220 * 1024, &seen);
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(select_blocks_kernel<SPANS, NT>), (int)SELECT_SMEM, &seen);
     if (e != cudaSuccess) return e;
-    const size_t smem = ((size_t)p.widest * 4 + 15) / 16 * 16 + (size_t)std::min(p.G, 16) * 2 * p.D;
-    select_blocks_kernel<T><<<(unsigned)(tokens * p.H), SELECT_THREADS, smem, st>>>(p, small);
-    return cudaGetLastError();
+    cudaLaunchAttribute cluster;
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = (unsigned)z.ctas;
+    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(units * p.H * z.ctas));
+    cfg.blockDim = dim3(SELECT_WARPS * 32);
+    cfg.dynamicSmemBytes = select_smem(z);
+    cfg.stream = st;
+    cfg.attrs = &cluster;
+    cfg.numAttrs = z.ctas > 1 ? 1 : 0;
+    e = cudaLaunchKernelEx(&cfg, select_blocks_kernel<SPANS, NT>, p, small, z);
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
-cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, int f16, long long tokens, cudaStream_t st) {
-    return f16 ? select_go<__half>(p, small, tokens, st) : select_go<__nv_bfloat16>(p, small, tokens, st);
+template <int SPANS> static cudaError_t select_rows(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, cudaStream_t st) {
+    return z.rows <= 8 ? select_go<SPANS, 1>(p, small, z, units, st) : (z.rows <= 16 ? select_go<SPANS, 2>(p, small, z, units, st) : select_go<SPANS, 4>(p, small, z, units, st));
+}
+cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, cudaStream_t st) {
+    return p.D <= 64 ? select_rows<2>(p, small, z, units, st) : (p.D <= 128 ? select_rows<4>(p, small, z, units, st) : select_rows<8>(p, small, z, units, st));
 }
 
 }  // namespace aafkv

@@ -102,13 +102,13 @@ int aaf_kv_select(aaf_kv_pool *p, int32_t layer, const aaf_kv_select_desc *d, in
     long long total = 0;
     const int rc = batch_records(p, n, ctxs, n_q, false, rec, &total);
     if (rc != AAF_OK) return rc;
-    if (total * p->g.H > (1ll << 31) - 1) return AAF_ERR_TOO_MANY;
     SelectParams k{};
-    for (AttnSeq &s : rec) {
-        s.unit0 = s.row0;
+    int max_nq = 1;
+    for (const AttnSeq &s : rec) {
         k.widest = std::max(k.widest, (s.len + p->g.BS - 1) / p->g.BS);
+        max_nq = std::max(max_nq, s.nq);
     }
-    if (k.widest > SELECT_MAX_BLOCKS) return AAF_ERR_TOO_LONG;
+    if (k.widest > AAF_SELECT_MAX_BLOCKS) return AAF_ERR_TOO_LONG;
     DeviceGuard guard(p->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (capturing(st)) return AAF_ERR_INVALID_ARG;
@@ -121,11 +121,19 @@ int aaf_kv_select(aaf_kv_pool *p, int32_t layer, const aaf_kv_select_desc *d, in
     k.q_stride = d->q_stride;
     k.max_blk = p->g.max_blk; k.BS = p->g.BS; k.H = p->g.H; k.G = d->n_q_heads / p->g.H; k.D = p->g.D;
     k.n = n; k.keep = d->keep; k.sink = d->sink; k.recent = d->recent;
+    const SelectShape z = select_shape(k, max_nq, total, p->sm_count, d->dtype == AAF_DTYPE_F16);
+    std::stable_sort(rec.begin(), rec.end(), [](const AttnSeq &x, const AttnSeq &y) { return x.len > y.len; });  // the longest first
+    long long units = 0;
+    for (AttnSeq &s : rec) {
+        s.unit0 = (int)units;
+        units += (s.nq + z.tile - 1) / z.tile;
+    }
+    if (units * p->g.H * z.ctas > (1ll << 31) - 1) return AAF_ERR_TOO_MANY;
     p->last_stream = st;
     if (!begin_read(p, ctxs, n, st)) return broke(p);
     SmallSeqs small;
     const bool ok = place_records(p, rec, small, &k.seqs, 0, st) &&
-                    launch_select_blocks(k, small, d->dtype == AAF_DTYPE_F16, total, st) == cudaSuccess;
+                    launch_select_blocks(k, small, z, units, st) == cudaSuccess;
     return ok && end_read(p, st) ? AAF_OK : broke(p);
 } catch (const std::bad_alloc &) {
     return AAF_ERR_INVALID_ARG;  // the host has no memory for the records; nothing was launched

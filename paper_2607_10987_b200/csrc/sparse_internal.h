@@ -21,7 +21,7 @@ struct SummaryParams {
 
 struct SelectParams {
     const void *q;
-    const AttnSeq *seqs;  // unit0: first unit (a query token and kv head)
+    const AttnSeq *seqs;  // unit0: first unit (a tile of query tokens)
     const int *tables;
     const signed char *summary;  // the layer's first record
     int *blocks;          // [query tokens][H][keep]
@@ -30,7 +30,16 @@ struct SelectParams {
     long long record;     // bytes
     int max_blk, BS, H, G, D, n, keep, sink, recent, widest;  // widest: blocks of the longest context
 };
-constexpr int SELECT_MAX_BLOCKS = 49152;  // of a context: their scores stay on the chip
+// How a batch is cut (see select_shape)
+struct SelectShape {
+    int tile;      // query tokens of a unit
+    int heads_p;   // rows of a token: the group's heads, repeated up to a power of two or a multiple of 8
+    int ctas;      // of a cluster
+    int room;      // blocks of a CTA's stretch at most
+    int stride;    // bytes from one row's codes to the next in shared memory
+    int rows;      // rows that are held at a time
+    int f16;
+};
 
 struct TablesParams {
     const AttnSeq *seqs;
@@ -41,7 +50,8 @@ struct TablesParams {
 };
 
 cudaError_t launch_summarize(const SummaryParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
-cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, int f16, long long tokens, cudaStream_t st);
+SelectShape select_shape(const SelectParams &p, int max_nq, long long tokens, int sm_count, int f16);
+cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, cudaStream_t st);
 // p.first is not read; a record's nsplit parts of `chunk` listed keys (lists of `keep` blocks); units are (query token, part)
 cudaError_t launch_attend_blocks(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
 int attend_blocks_rows(int D, int G);  // query rows of a unit's warp
