@@ -34,11 +34,20 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// a word of another CTA's shared memory: the one that lies there where `addr` lies here
-__device__ __forceinline__ uint32_t peer_word(uint32_t addr, int cta) {
-    uint32_t at, v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(cta));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+// words of another CTA's shared memory: those that lie there where `addr` lies here
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, int cta) {
+    uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(cta));
+    return at;
+}
+__device__ __forceinline__ uint4 peer_words(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint2 peer_pair(uint32_t at) {
+    uint2 v;
+    asm volatile("ld.shared::cluster.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
     return v;
 }
 
@@ -54,7 +63,8 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
     __shared__ uint32_t prefix_s[SELECT_TOKENS];                            // of a list: the threshold's leading bits
     __shared__ int want_s[SELECT_TOKENS];                                   // how many of those with these bits are taken; -1: all
     __shared__ uint32_t counts_s[SELECT_WARPS][2];                          // of a warp's pieces: certainly taken, equal to the threshold
-    __shared__ uint32_t list_counts_s[SELECT_TOKENS][2];
+    __shared__ __align__(8) uint32_t list_counts_s[SELECT_TOKENS][2];
+    __shared__ int last_s[SELECT_TOKENS];                                   // a token's own block
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t4 = lane & 3;
     const int cta = z.ctas > 1 ? (int)cluster_rank() : 0;
     const int unit = blockIdx.x / z.ctas / p.H, head = blockIdx.x / z.ctas - unit * p.H;
@@ -75,6 +85,7 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
     if (threadIdx.x < z.tile) {
         const int last = (pos0 + min((int)threadIdx.x, tokens - 1)) / p.BS;
         const int want = p.keep - p.sink - p.recent;
+        last_s[threadIdx.x] = last;
         prefix_s[threadIdx.x] = 0;
         want_s[threadIdx.x] = last + 1 <= p.keep ? -1 : want;
     }
@@ -195,7 +206,6 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
     // ---- selection: a list is looked after by `team` warps, each with a piece of the CTA's stretch
     const int team = max(1, SELECT_WARPS / z.tile), wl = warp % team, lists_at_once = SELECT_WARPS / team;
     const int piece = ((count + team - 1) / team + 31) / 32 * 32, i0 = min(wl * piece, count), i1 = min(i0 + piece, count);
-    auto last_of = [&](int list) { return (pos0 + list) / p.BS; };
     for (int pass = 0; pass < 4; ++pass) {
         const int shift = 24 - 8 * pass;
         uint32_t *now = hist + (pass & 1) * z.tile * 256, *next = hist + (~pass & 1) * z.tile * 256;
@@ -205,7 +215,7 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
         for (int list = warp / team; list < tokens; list += lists_at_once) {
             if (want_s[list] <= 0) continue;
             const uint32_t prefix = prefix_s[list];
-            const int lo = max(i0, p.sink - b0), hi = min(i1, last_of(list) + 1 - p.recent - b0);
+            const int lo = max(i0, p.sink - b0), hi = min(i1, last_s[list] + 1 - p.recent - b0);
             for (int i = lo + lane; i < hi; i += 32) {
                 const uint32_t k = key_at(list, i);
                 if (pass == 0 || k >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(now + list * 256 + (k >> shift & 255), 1u);
@@ -217,12 +227,29 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
             const int want = want_s[list];
             if (want <= 0 || wl) continue;
             uint32_t n[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) n[i] = 0;
             const uint32_t at = (uint32_t)__cvta_generic_to_shared(now + list * 256 + lane * 8);
-            for (int c = 0; c < z.ctas; ++c)
+            if (z.ctas > 1) {
+                uint4 v[8][2];  // all under way at once
 #pragma unroll
-                for (int i = 0; i < 8; ++i) n[i] += z.ctas > 1 ? peer_word(at + 4 * i, c) : now[list * 256 + lane * 8 + i];
+                for (int c = 0; c < 8; ++c)
+                    if (c < z.ctas) {
+                        const uint32_t there = peer_addr(at, c);
+                        v[c][0] = peer_words(there);
+                        v[c][1] = peer_words(there + 16);
+                    }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) n[i] = 0;
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (c < z.ctas) {
+                        n[0] += v[c][0].x; n[1] += v[c][0].y; n[2] += v[c][0].z; n[3] += v[c][0].w;
+                        n[4] += v[c][1].x; n[5] += v[c][1].y; n[6] += v[c][1].z; n[7] += v[c][1].w;
+                    }
+            } else {
+                const uint4 a = lds16(at), b = lds16(at + 16);
+                n[0] = a.x; n[1] = a.y; n[2] = a.z; n[3] = a.w;
+                n[4] = b.x; n[5] = b.y; n[6] = b.z; n[7] = b.w;
+            }
             uint32_t mine = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) mine += n[i];
@@ -251,25 +278,33 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
         }
         __syncthreads();
     }
-    // want_s: -1 every block is taken; -2 those from prefix_s on; else (0 too) those above prefix_s, and so many of those equal to it
-    auto kind_of = [&](int list, int i, bool &tie) -> bool {  // certainly taken
-        const int b = b0 + i, last = last_of(list);
+    // want_s: -1 every block is taken; -2 those from prefix_s on; 0 none of the middle; else those above prefix_s and so many of those
+    // equal to it
+    struct Rule {
+        int first, end, want, last;  // of the middle, within the stretch
+        uint32_t least;
+    };
+    auto rule_of = [&](int list) {
+        const int last = last_s[list], want = want_s[list];
+        Rule r{p.sink - b0, last + 1 - p.recent - b0, want, last - b0, prefix_s[list]};
+        if (want == -1) r.end = -0x7fffffff;  // everything counts as first or last
+        return r;
+    };
+    auto kind_of = [&](const Rule &r, int list, int i, bool &tie) -> bool {  // certainly taken
         tie = false;
-        if (b > last) return false;
-        if (b < p.sink || b > last - p.recent) return true;
-        const int want = want_s[list];
-        const uint32_t k = key_at(list, i), least = prefix_s[list];
-        if (want == -1) return true;
-        if (want == -2) return k >= least;
-        if (p.keep == p.sink + p.recent) return false;
-        tie = k == least;
-        return k > least;
+        if (i > r.last) return false;
+        if (i < r.first || i >= r.end) return true;
+        const uint32_t k = key_at(list, i);
+        if (r.want == -2) return k >= r.least;
+        tie = r.want > 0 && k == r.least;
+        return r.want > 0 && k > r.least;
     };
     for (int list = warp / team; list < tokens; list += lists_at_once) {
         uint32_t sure = 0, ties = 0;
+        const Rule rule = rule_of(list);
         for (int i = i0 + lane; i < i1; i += 32) {
             bool tie;
-            sure += kind_of(list, i, tie);
+            sure += kind_of(rule, list, i, tie);
             ties += tie;
         }
         sure = __reduce_add_sync(0xffffffffu, sure);
@@ -298,13 +333,16 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
     }
     sync_all();
     for (int list = warp / team; list < tokens; list += lists_at_once) {
-        const int ties_taken = max(want_s[list], 0);
+        const Rule rule = rule_of(list);
+        const int ties_taken = max(rule.want, 0);
         uint32_t sure = 0, ties = 0;  // before this warp's piece
-        for (int c = 0; c < cta; ++c) {
-            const uint32_t at = (uint32_t)__cvta_generic_to_shared(&list_counts_s[list][0]);
-            sure += peer_word(at, c);
-            ties += peer_word(at + 4, c);
+        if (lane < cta) {  // a lane asks one CTA
+            const uint2 v = peer_pair(peer_addr((uint32_t)__cvta_generic_to_shared(&list_counts_s[list][0]), lane));
+            sure = v.x;
+            ties = v.y;
         }
+        sure = __reduce_add_sync(0xffffffffu, sure);
+        ties = __reduce_add_sync(0xffffffffu, ties);
         for (int w = 0; w < wl; ++w) {
             sure += counts_s[warp - wl + w][0];
             ties += counts_s[warp - wl + w][1];
@@ -313,7 +351,7 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
         for (int base = i0; base < i1; base += 32) {
             const int i = base + lane;
             bool tie = false;
-            const bool certain = i < i1 && kind_of(list, i, tie);
+            const bool certain = i < i1 && kind_of(rule, list, i, tie);
             const unsigned cm = __ballot_sync(0xffffffffu, certain), tm = __ballot_sync(0xffffffffu, tie), under = (1u << lane) - 1;
             const int ties_before = (int)ties + __popc(tm & under);
             if (certain || (tie && ties_before < ties_taken)) {
@@ -325,7 +363,7 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
             ties += __popc(tm);
         }
         if (cta == 0)
-            for (int i = min(p.keep, last_of(list) + 1) + wl * 32 + lane; i < p.keep; i += team * 32) {
+            for (int i = min(p.keep, last_s[list] + 1) + wl * 32 + lane; i < p.keep; i += team * 32) {
                 p.blocks[at0 + i] = -1;
                 if (p.scores) p.scores[at0 + i] = -CUDART_INF_F;
             }
