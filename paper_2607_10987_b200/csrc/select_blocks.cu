@@ -60,11 +60,12 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
     uint32_t *hist = keys + z.tile * z.room;                                // [2][tile][256]
     unsigned char *codes = reinterpret_cast<unsigned char *>(hist + 2 * z.tile * 256);  // [rows][stride]
     __shared__ int exps[SELECT_ROWS];
-    __shared__ uint32_t prefix_s[SELECT_TOKENS];                            // of a list: the threshold's leading bits
-    __shared__ int want_s[SELECT_TOKENS];                                   // how many of those with these bits are taken; -1: all
-    __shared__ uint32_t counts_s[SELECT_WARPS][2];                          // of a warp's pieces: certainly taken, equal to the threshold
-    __shared__ __align__(8) uint32_t list_counts_s[SELECT_TOKENS][2];
+    __shared__ __align__(8) uint32_t range_s[2];                            // smallest and largest score of the stretch, of any token
     __shared__ int last_s[SELECT_TOKENS];                                   // a token's own block
+    __shared__ uint32_t prefix_s[SELECT_TOKENS];                            // of a list: the threshold's leading bits
+    __shared__ int want_s[SELECT_TOKENS];                                   // how many of those with these bits are taken; see below
+    __shared__ uint32_t before_s[SELECT_TOKENS][2];                         // in other CTAs' earlier stretches: above the threshold, equal to it
+    __shared__ uint32_t counts_s[SELECT_WARPS][2];                          // of a warp's piece: certainly taken, equal to the threshold
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t4 = lane & 3;
     const int cta = z.ctas > 1 ? (int)cluster_rank() : 0;
     const int unit = blockIdx.x / z.ctas / p.H, head = blockIdx.x / z.ctas - unit * p.H;
@@ -86,11 +87,17 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
         const int last = (pos0 + min((int)threadIdx.x, tokens - 1)) / p.BS;
         const int want = p.keep - p.sink - p.recent;
         last_s[threadIdx.x] = last;
-        prefix_s[threadIdx.x] = 0;
+        prefix_s[threadIdx.x] = before_s[threadIdx.x][0] = before_s[threadIdx.x][1] = 0;
         want_s[threadIdx.x] = last + 1 <= p.keep ? -1 : want;
     }
 
+    if (threadIdx.x == 0) {
+        range_s[0] = 0xffffffffu;
+        range_s[1] = 0;
+    }
+
     // ---- scores
+    uint32_t least_k = 0xffffffffu, most_k = 0;
     const int *table = p.tables + (long long)s.ctx * p.max_blk + b0;
     const int rows_all = z.tile * z.heads_p;
     for (int row0 = 0; row0 < rows_all; row0 += z.rows) {
@@ -178,6 +185,8 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
                     auto put = [&](int list, int h, uint32_t v) {
                         const int i = m * 16 + g + 8 * h;
                         if (list < z.tile && i < count) {
+                            least_k = min(least_k, v);
+                            most_k = max(most_k, v);
                             uint32_t &at = key_at(list, i);
                             at = z.heads_p > 8 && (row0 + n0 + nt * 8) % z.heads_p ? max(at, v) : v;  // a token's later rows
                         }
@@ -201,24 +210,48 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
             }
         }
     }
-    __syncthreads();
+    least_k = __reduce_min_sync(0xffffffffu, least_k);
+    most_k = __reduce_max_sync(0xffffffffu, most_k);
+    if (lane == 0) {
+        atomicMin(&range_s[0], least_k);
+        atomicMax(&range_s[1], most_k);
+    }
+    sync_all();
 
-    // ---- selection: a list is looked after by `team` warps, each with a piece of the CTA's stretch
+    // ---- selection: a list is looked after by `team` warps, each with a piece of the CTA's stretch.  The leading bits that all scores
+    // have in common are skipped; then eight bits a pass.  want_s: -1 every block is taken; -2 those from prefix_s on; 0 none of the
+    // middle; else those above prefix_s and so many of those equal to it.
     const int team = max(1, SELECT_WARPS / z.tile), wl = warp % team, lists_at_once = SELECT_WARPS / team;
     const int piece = ((count + team - 1) / team + 31) / 32 * 32, i0 = min(wl * piece, count), i1 = min(i0 + piece, count);
-    for (int pass = 0; pass < 4; ++pass) {
-        const int shift = 24 - 8 * pass;
+    if (z.ctas > 1) {
+        uint2 r = make_uint2(0xffffffffu, 0);
+        if (lane < z.ctas) r = peer_pair(peer_addr((uint32_t)__cvta_generic_to_shared(range_s), lane));
+        least_k = __reduce_min_sync(0xffffffffu, r.x);
+        most_k = __reduce_max_sync(0xffffffffu, r.y);
+    } else {
+        least_k = range_s[0];
+        most_k = range_s[1];
+    }
+    int shift = 32 - __clz(least_k ^ most_k);  // bits that are not decided
+    const uint32_t common = shift == 32 ? 0 : least_k >> shift << shift;
+    for (int pass = 0; shift > 0; ++pass) {
+        const int width = min(shift, 8);
+        shift -= width;
         uint32_t *now = hist + (pass & 1) * z.tile * 256, *next = hist + (~pass & 1) * z.tile * 256;
         bool any = false;
         for (int list = 0; list < tokens; ++list) any |= want_s[list] > 0;
         if (!any) break;  // the same in all CTAs of the cluster
         for (int list = warp / team; list < tokens; list += lists_at_once) {
             if (want_s[list] <= 0) continue;
-            const uint32_t prefix = prefix_s[list];
+            const uint32_t prefix = (common | prefix_s[list]) >> shift >> width, mask = (1u << width) - 1;
             const int lo = max(i0, p.sink - b0), hi = min(i1, last_s[list] + 1 - p.recent - b0);
-            for (int i = lo + lane; i < hi; i += 32) {
-                const uint32_t k = key_at(list, i);
-                if (pass == 0 || k >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(now + list * 256 + (k >> shift & 255), 1u);
+            for (int i = lo + lane; i < hi; i += 128) {
+                uint32_t k[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) k[e] = i + 32 * e < hi ? key_at(list, i + 32 * e) : 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + 32 * e < hi && k[e] >> shift >> width == prefix) atomicAdd(now + list * 256 + (k[e] >> shift & mask), 1u);
             }
         }
         sync_all();
@@ -226,8 +259,10 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
         for (int list = warp / team; list < tokens; list += lists_at_once) {
             const int want = want_s[list];
             if (want <= 0 || wl) continue;
-            uint32_t n[8];
+            uint32_t n[8], before[8];  // in all CTAs, in those with earlier stretches
             const uint32_t at = (uint32_t)__cvta_generic_to_shared(now + list * 256 + lane * 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n[i] = before[i] = 0;
             if (z.ctas > 1) {
                 uint4 v[8][2];  // all under way at once
 #pragma unroll
@@ -238,55 +273,70 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
                         v[c][1] = peer_words(there + 16);
                     }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) n[i] = 0;
+                for (int c = 0; c < 8; ++c) {
+                    if (c >= z.ctas) break;
+                    const uint32_t w[8] = {v[c][0].x, v[c][0].y, v[c][0].z, v[c][0].w, v[c][1].x, v[c][1].y, v[c][1].z, v[c][1].w};
 #pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    if (c < z.ctas) {
-                        n[0] += v[c][0].x; n[1] += v[c][0].y; n[2] += v[c][0].z; n[3] += v[c][0].w;
-                        n[4] += v[c][1].x; n[5] += v[c][1].y; n[6] += v[c][1].z; n[7] += v[c][1].w;
+                    for (int i = 0; i < 8; ++i) {
+                        n[i] += w[i];
+                        if (c < cta) before[i] += w[i];
                     }
+                }
             } else {
                 const uint4 a = lds16(at), b = lds16(at + 16);
                 n[0] = a.x; n[1] = a.y; n[2] = a.z; n[3] = a.w;
                 n[4] = b.x; n[5] = b.y; n[6] = b.z; n[7] = b.w;
             }
-            uint32_t mine = 0;
+            uint32_t mine = 0, mine_before = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) mine += n[i];
-            uint32_t above = mine;  // of this lane's digits and larger ones
+            for (int i = 0; i < 8; ++i) {
+                mine += n[i];
+                mine_before += before[i];
+            }
+            uint32_t above = mine, above_before = mine_before;  // of this lane's digits and larger ones
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
-                const uint32_t v = __shfl_down_sync(0xffffffffu, above, d);
-                if (lane + d < 32) above += v;
+                const uint32_t v = __shfl_down_sync(0xffffffffu, above, d), w = __shfl_down_sync(0xffffffffu, above_before, d);
+                if (lane + d < 32) {
+                    above += v;
+                    above_before += w;
+                }
             }
             above -= mine;
+            above_before -= mine_before;
             if ((int)above < want && want <= (int)(above + mine)) {  // one lane
-                uint32_t left = (uint32_t)want - above, here = 0;
+                uint32_t left = (uint32_t)want - above, here = 0, here_before = 0;
                 int digit = 7;
 #pragma unroll
                 for (int i = 7; i >= 0; --i) {
                     if (digit == i && left > n[i]) {
                         left -= n[i];
+                        above_before += before[i];
                         digit = i - 1;
                     }
-                    if (digit == i) here = n[i];
+                    if (digit == i) {
+                        here = n[i];
+                        here_before = before[i];
+                    }
                 }
-                prefix_s[list] |= (uint32_t)(lane * 8 + digit) << shift;
+                prefix_s[list] |= common | (uint32_t)(lane * 8 + digit) << shift;
                 // all with these bits are taken: the threshold is the smallest number with them
                 want_s[list] = here == left ? -2 : (int)left;
+                before_s[list][0] += above_before + (here == left ? here_before : 0);
+                before_s[list][1] = here_before;
             }
         }
         __syncthreads();
     }
-    // want_s: -1 every block is taken; -2 those from prefix_s on; 0 none of the middle; else those above prefix_s and so many of those
-    // equal to it
+    // nobody reads this CTA's memory any more once all have come here; they need not wait for its lists
+    if (z.ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     struct Rule {
         int first, end, want, last;  // of the middle, within the stretch
         uint32_t least;
     };
     auto rule_of = [&](int list) {
         const int last = last_s[list], want = want_s[list];
-        Rule r{p.sink - b0, last + 1 - p.recent - b0, want, last - b0, prefix_s[list]};
+        Rule r{p.sink - b0, last + 1 - p.recent - b0, want, last - b0, common | prefix_s[list]};
         if (want == -1) r.end = -0x7fffffff;  // everything counts as first or last
         return r;
     };
@@ -299,50 +349,34 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
         tie = r.want > 0 && k == r.least;
         return r.want > 0 && k > r.least;
     };
-    for (int list = warp / team; list < tokens; list += lists_at_once) {
+    if (team > 1) {  // a warp's piece comes behind those of the warps before it
+        const int list = warp / team;
         uint32_t sure = 0, ties = 0;
-        const Rule rule = rule_of(list);
-        for (int i = i0 + lane; i < i1; i += 32) {
-            bool tie;
-            sure += kind_of(rule, list, i, tie);
-            ties += tie;
+        if (list < tokens) {
+            const Rule rule = rule_of(list);
+            for (int i = i0 + lane; i < i1; i += 32) {
+                bool tie;
+                sure += kind_of(rule, list, i, tie);
+                ties += tie;
+            }
         }
         sure = __reduce_add_sync(0xffffffffu, sure);
         ties = __reduce_add_sync(0xffffffffu, ties);
         if (lane == 0) {
-            if (team > 1) {
-                counts_s[warp][0] = sure;
-                counts_s[warp][1] = ties;
-            } else {
-                list_counts_s[list][0] = sure;
-                list_counts_s[list][1] = ties;
-            }
+            counts_s[warp][0] = sure;
+            counts_s[warp][1] = ties;
         }
-    }
-    if (team > 1) {
         __syncthreads();
-        if (threadIdx.x < tokens) {
-            uint32_t a = 0, b = 0;
-            for (int w = 0; w < team; ++w) {
-                a += counts_s[threadIdx.x * team + w][0];
-                b += counts_s[threadIdx.x * team + w][1];
-            }
-            list_counts_s[threadIdx.x][0] = a;
-            list_counts_s[threadIdx.x][1] = b;
-        }
     }
-    sync_all();
     for (int list = warp / team; list < tokens; list += lists_at_once) {
         const Rule rule = rule_of(list);
-        const int ties_taken = max(rule.want, 0);
-        uint32_t sure = 0, ties = 0;  // before this warp's piece
-        if (lane < cta) {  // a lane asks one CTA
-            const uint2 v = peer_pair(peer_addr((uint32_t)__cvta_generic_to_shared(&list_counts_s[list][0]), lane));
-            sure = v.x;
-            ties = v.y;
-        }
-        sure = __reduce_add_sync(0xffffffffu, sure);
-        ties = __reduce_add_sync(0xffffffffu, ties);
+        const int ties_taken = max(rule.want, 0), own = last_s[list];
+        // taken in earlier stretches: all of them, or the first, the last and those above the threshold
+        uint32_t sure = rule.want == -1 ? (uint32_t)min(b0, own + 1)
+                                        : (uint32_t)(min(b0, p.sink) + max(0, min(b0, own + 1) - (own + 1 - p.recent))) + before_s[list][0];
+        uint32_t ties = before_s[list][1];
+        if (least_k == most_k) ties = max(0, min(b0, own + 1 - p.recent) - p.sink);  // no pass: the middle is all equal
+        if (rule.want <= 0) ties = 0;
         for (int w = 0; w < wl; ++w) {
             sure += counts_s[warp - wl + w][0];
             ties += counts_s[warp - wl + w][1];
@@ -363,12 +397,12 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
             ties += __popc(tm);
         }
         if (cta == 0)
-            for (int i = min(p.keep, last_s[list] + 1) + wl * 32 + lane; i < p.keep; i += team * 32) {
+            for (int i = min(p.keep, own + 1) + wl * 32 + lane; i < p.keep; i += team * 32) {
                 p.blocks[at0 + i] = -1;
                 if (p.scores) p.scores[at0 + i] = -CUDART_INF_F;
             }
     }
-    if (z.ctas > 1) cluster_sync();  // the others have read this CTA's counts
+    if (z.ctas > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 static size_t select_smem(const SelectShape &z) { return (size_t)z.tile * z.room * 4 + (size_t)2 * z.tile * 256 * 4 + (size_t)z.rows * z.stride; }
@@ -389,7 +423,7 @@ SelectShape select_shape(const SelectParams &p, int max_nq, long long tokens, in
             z.room = ((p.widest + z.ctas - 1) / z.ctas + 15) / 16 * 16;
             if (z.ctas == 8) break;
             const bool fits = select_smem(z) <= SELECT_SMEM / 2;  // two CTAs an SM
-            if (fits && (units * z.ctas >= 2ll * sm_count || z.room <= 128)) break;
+            if (fits && (units * z.ctas * 2 > 2ll * sm_count || z.room <= 256)) break;
         }
         if (z.tile == 1 || select_smem(z) <= SELECT_SMEM) return z;
         z.tile /= 2;

@@ -173,6 +173,21 @@ def test_select_equal_scores_go_to_the_lower_block():
     check_select(pool, [c], [1], torch.zeros_like(q), 20, 0, 1, summary)
 
 
+@pytest.mark.parametrize("n_q", [1, 20])
+def test_select_equal_scores_of_a_long_context(n_q):
+    # nothing but equal scores, and a few that differ, over more blocks than a CTA looks after
+    pool = R.make_pool(1, 2, 16, 4, 8000)
+    rows = torch.ones(1, 2, 4 * 7000 + 1, 2, 16, dtype=torch.bfloat16, device="cuda")
+    c = R.add_ctx(pool, rows.shape[2], 0, rows)
+    q = torch.ones(n_q, 4, 16, dtype=torch.bfloat16, device="cuda")
+    check_select(pool, [c], [n_q], q, 3000, 7, 5)
+    rows[0, 0, 4 * 6000:4 * 6003, 0] = 2.0
+    rows[0, 0, 4 * 100:4 * 3100, 1] = 0.5
+    pool = R.make_pool(1, 2, 16, 4, 8000)
+    c = R.add_ctx(pool, rows.shape[2], 0, rows)
+    check_select(pool, [c], [n_q], q, 5000, 7, 5)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_select_odd_values(dtype):
     big, tiny = torch.finfo(dtype).max, torch.finfo(dtype).smallest_normal
