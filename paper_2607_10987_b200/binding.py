@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libaafkv.so")
@@ -259,6 +260,11 @@ def aaf_kv_policy(local_and_compatible, t_transfer, t_prefill):
 def aaf_kv_debug_expire_wait(pool, limit_cycles, stream): return _fn("aaf_kv_debug_expire_wait")(pool, limit_cycles, stream)
 def aaf_kv_debug_mark_unusable(pool): return _fn("aaf_kv_debug_mark_unusable")(pool)
 def aaf_kv_strerror(status): return _fn("aaf_kv_strerror")(status).decode()
+
+
+def _ints(v):
+    """A list as a C array of int32 (through the buffer protocol: a ctypes array takes its entries one by one)."""
+    return C.byref(C.c_int32.from_buffer(array("i", v or (0,))))
 
 
 def make_desc(n_layers, n_kv_heads, head_dim, block_size, elt_bytes, n_blocks, max_ctx, max_blocks_per_ctx,
@@ -588,8 +594,8 @@ class KVPool:
         code = self._codes.get(dtype)
         if code is None:
             raise ValueError(f"bfloat16 or float16 expected, got {dtype}")
-        return load().aaf_kv_summarize(self.h, AAF_ALL_LAYERS if layer is None else layer, code, n, (C.c_int32 * (n or 1))(*ctxs),
-                                       None if n_new is None else (C.c_int32 * (n or 1))(*n_new),
+        return load().aaf_kv_summarize(self.h, AAF_ALL_LAYERS if layer is None else layer, code, n, _ints(ctxs),
+                                       None if n_new is None else _ints(n_new),
                                        self._flat(summary, self.torch.int8, self.summary_bytes(), "summary"), summary.numel(),
                                        self._stream()), None
 
@@ -603,7 +609,7 @@ class KVPool:
         if blocks is None:
             blocks = q.new_empty((tokens, self.H, max(keep, 0)), dtype=self.torch.int32)
         size = tokens * self.H * max(keep, 0)
-        st = load().aaf_kv_select(self.h, layer, d, n, (C.c_int32 * (n or 1))(*ctxs), None if n_q is None else (C.c_int32 * (n or 1))(*n_q),
+        st = load().aaf_kv_select(self.h, layer, d, n, _ints(ctxs), None if n_q is None else _ints(n_q),
                                   q.data_ptr(), self._flat(summary, self.torch.int8, self.summary_bytes(), "summary"), summary.numel(),
                                   self._flat(blocks, self.torch.int32, size, "blocks"),
                                   None if scores is None else self._flat(scores, self.torch.float32, size, "scores"), self._stream())
@@ -620,13 +626,11 @@ class KVPool:
         out, lse, ws = self._attn_out(q, tokens, a.n_q_heads, out, lse)
         if ws is None:
             return AAF_ERR_INVALID_ARG, None
-        st = load().aaf_kv_attend_blocks(self.h, layer, a, n, (C.c_int32 * (n or 1))(*ctxs),
-                                         None if n_q is None else (C.c_int32 * (n or 1))(*n_q), q.data_ptr(),
+        st = load().aaf_kv_attend_blocks(self.h, layer, a, n, _ints(ctxs),
+                                         None if n_q is None else _ints(n_q), q.data_ptr(),
                                          self._flat(blocks, self.torch.int32, blocks.numel(), "blocks"), keep, out.data_ptr(), lse.data_ptr(),
                                          ws.data_ptr(), ws.numel(), self._stream())
         return st, ((out, lse) if st == AAF_OK else None)
-
-    _BATCH_ARRAYS = ("tables", "lens", "offsets", "token_row", "positions", "slots")
 
     def batch_tables(self, ctxs, n_new=None, rows=None, tokens=None, cols=None, out=None):
         """Device arrays of a batch for kernels of one's own (see aaf_kv_batch_tables): (status, dict of tables, lens, offsets,
@@ -641,18 +645,22 @@ class KVPool:
                 cols = out["tables"].shape[-1]
             else:
                 cols = max([-(-(self.ctx_len(c) or 0) // self.BS) for c in ctxs], default=0)
-        shapes = dict(tables=(rows, cols), lens=(rows,), offsets=(rows + 1,), token_row=(tokens,), positions=(tokens,), slots=(tokens,))
-        types = {k: torch.int64 if k in ("positions", "slots") else torch.int32 for k in shapes}
+        i32, i64, dev = torch.int32, torch.int64, self.device
         if out is None:
-            if min(rows, tokens, cols) < 0:
+            if rows < 0 or tokens < 0 or cols < 0:
                 return AAF_ERR_DST_TOO_SMALL, None
-            out = {k: torch.empty(shapes[k], dtype=types[k], device=self.device) for k in self._BATCH_ARRAYS}
-        elif set(out) - set(shapes) or any(t.shape != shapes[k] for k, t in out.items()):
-            raise ValueError(f"out: expected some of {shapes}")
-        ptrs = [self._flat(out[k], types[k], out[k].numel(), k) if k in out else None for k in self._BATCH_ARRAYS]
+            out = {"tables": torch.empty((rows, cols), dtype=i32, device=dev), "lens": torch.empty(rows, dtype=i32, device=dev),
+                   "offsets": torch.empty(rows + 1, dtype=i32, device=dev), "token_row": torch.empty(tokens, dtype=i32, device=dev),
+                   "positions": torch.empty(tokens, dtype=i64, device=dev), "slots": torch.empty(tokens, dtype=i64, device=dev)}
+            ptrs = [x.data_ptr() for x in out.values()]
+        else:
+            shapes = {"tables": (rows, cols), "lens": (rows,), "offsets": (rows + 1,), "token_row": (tokens,), "positions": (tokens,),
+                      "slots": (tokens,)}
+            if set(out) - set(shapes) or any(x.shape != shapes[k] for k, x in out.items()):
+                raise ValueError(f"out: expected some of {shapes}")
+            ptrs = [self._flat(out[k], i64 if k in ("positions", "slots") else i32, out[k].numel(), k) if k in out else None for k in shapes]
         d = aaf_kv_batch_desc(C.sizeof(aaf_kv_batch_desc), rows, tokens, cols, *ptrs)
-        st = load().aaf_kv_batch_tables(self.h, d, n, (C.c_int32 * (n or 1))(*ctxs), None if n_new is None else (C.c_int32 * (n or 1))(*n_new),
-                                        self._stream())
+        st = load().aaf_kv_batch_tables(self.h, d, n, _ints(ctxs), None if n_new is None else _ints(n_new), self._stream())
         return st, (out if st == AAF_OK else None)
 
     def materialize_host(self, ctx, t0, t1, dst_host, staging):

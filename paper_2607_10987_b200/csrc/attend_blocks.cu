@@ -2,12 +2,12 @@
 //
 //   s_rt = score(q_r . k_t) for the tokens t of the listed blocks that the row sees,  o_r = sum_t exp(s_rt) v_t / sum_t exp(s_rt)
 //
-// Bound: a listed block's keys and values are used by one kv head's group of query heads only, so their bytes decide.  The shape
-// is that of the kernel for few rows: a warp owns a query token, a kv head and a part of the list, shares nothing with
-// other warps, and takes 16 tokens at a time as the M side of the products with its rows as the N side; weights in two 16-bit parts.
-// What differs: tokens come through the list and then the table, two loads that are asked for ahead of the copies; and all
-// rows of a warp belong to one query token, so they see the same keys.  A key that is not seen is not read: its key and value are
-// zeros, its score is -inf.
+// Bound: a listed block's keys and values are used by one kv head's group of query heads only, so their bytes decide.  The products
+// are those of the kernel for few rows: a warp takes 16 tokens at a time as the M side and its rows as the N side, waits for its
+// own copies only, weights in two 16-bit parts.  What differs: a CTA takes a query token, a kv head and a part of the list, its warps
+// every WARPS-th tile of 16 tokens, and puts their results together in shared memory, so that short lists need no join; tokens
+// come through the list and then the table, two loads that are asked for ahead of the copies; and all rows of a CTA belong to one
+// query token, so they see the same keys.  A key that is not seen is not read: its key and value are zeros, its score is -inf.
 #include "sparse_device.cuh"
 
 namespace aafkv {
@@ -16,25 +16,25 @@ template <int DP> struct ListShape {
     static constexpr int PIECES = DP / 8;           // 16-byte pieces of a row
     static constexpr int ROW = DP * 2, HALF = 16 * ROW;  // bytes of a row, of a tile of 16 keys (or values)
     static constexpr int STAGE_BYTES = 2 * HALF;
-    static constexpr int WARPS = DP <= 128 ? 4 : 3;
+    static constexpr int WARPS = DP <= 128 ? 4 : 3;  // of a CTA that shares the SM with another; twice as many of one that does not
     static constexpr int STAGES = DP == 64 ? 6 : (DP == 128 ? 3 : 2);
-    static constexpr int SMEM = WARPS * STAGES * STAGE_BYTES;
-    static_assert(2 * (SMEM + 1024) <= 228 * 1024, "shared memory of a CTA");
+    static constexpr int WARP_BYTES = STAGES * STAGE_BYTES;
+    static_assert(2 * (WARPS * WARP_BYTES + 2048) <= 228 * 1024, "shared memory of a CTA");
 };
 
 // SIMPLE: neither cap nor bias, a score is a multiple of the product
-template <typename T, int DP, int NT, bool SIMPLE>
-__global__ void __launch_bounds__(ListShape<DP>::WARPS * 32, 2)
+template <typename T, int DP, int NT, bool SIMPLE, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, WARPS == ListShape<DP>::WARPS ? 2 : 1)
     attend_blocks_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small, int row_groups) {
     using S = ListShape<DP>;
     extern __shared__ __align__(16) char smem[];
+    __shared__ float2 ml_s[WARPS][NT * 8];  // of a warp's rows: base of the exponents, sum
+    static_assert(NT * 8 * DP * 4 <= S::WARP_BYTES, "a warp's results fit where its copies were");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int g = lane >> 2, t4 = lane & 3;
-    const long long task = (long long)blockIdx.x * S::WARPS + warp;
-    if (task >= (long long)p.total_units * p.H * row_groups) return;
-    const long long unit_h = task / row_groups;
-    const int first_row = (int)(task - unit_h * row_groups) * NT * 8;  // of the group's heads
-    const int unit = (int)(unit_h / p.H), head = (int)(unit_h - (long long)unit * p.H);
+    // One kv head after the other, so that query tokens of one context that list the same blocks find them in L2
+    const int per_head = p.total_units * row_groups, head = blockIdx.x / per_head, rest = blockIdx.x - head * per_head;
+    const int unit = rest / row_groups, first_row = (rest - unit * row_groups) * NT * 8;  // of the group's heads
     asm volatile("griddepcontrol.launch_dependents;");  // the join may be brought up beside this kernel
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
     const AttnSeq sq = seqs[find_seq(seqs, p.n, unit)];
@@ -64,9 +64,10 @@ __global__ void __launch_bounds__(ListShape<DP>::WARPS * 32, 2)
         used = (int)__reduce_max_sync(0xffffffffu, (unsigned)used);
     }
     const int beg = part * sq.chunk, end = part + 1 < sq.nsplit ? min(beg + sq.chunk, used * p.BS) : used * p.BS;
-    const int tiles = max(0, end - beg + 15) / 16;
+    const int tiles_all = max(0, end - beg + 15) / 16, tiles = (tiles_all - warp + WARPS - 1) / WARPS;  // of the part, of this warp
+    auto first_of = [&](int tile) { return beg + (tile * WARPS + warp) * 16; };
 
-    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S::STAGES * S::STAGE_BYTES);
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem) + warp * S::WARP_BYTES;
     // where piece c of row r lies: lanes that read together have two rows and four pieces of K, four even (odd) rows and two
     // pieces of V
     auto k_at = [](int r, int c) { return (uint32_t)(r * S::ROW + ((c ^ ((r & 1) << 2)) << 4)); };
@@ -77,7 +78,7 @@ __global__ void __launch_bounds__(ListShape<DP>::WARPS * 32, 2)
     // lane l looks after the tile's token l % 16: its block's table position, then its position in the context (-1: not seen)
     // and its block
     auto listed = [&](int tile) -> int {
-        const int u = beg + tile * 16 + (lane & 15);
+        const int u = first_of(tile) + (lane & 15);
         return u < end ? __ldg(list + block_of(u, p.BS, p.bs_shift)) : -1;
     };
     struct Key {
@@ -86,7 +87,7 @@ __global__ void __launch_bounds__(ListShape<DP>::WARPS * 32, 2)
     auto key_of = [&](int tile, int entry) -> Key {
         Key k{-1, 0};
         if (entry >= 0 && entry < blocks) {
-            const int u = beg + tile * 16 + (lane & 15);
+            const int u = first_of(tile) + (lane & 15);
             const int t = entry * p.BS + (u - block_of(u, p.BS, p.bs_shift) * p.BS);
             if (t >= span.lo && t < span.hi) {
                 k.t = t;
@@ -254,7 +255,10 @@ __global__ void __launch_bounds__(ListShape<DP>::WARPS * 32, 2)
         entry = after;
     }
     copy_wait<0>();
+    __syncwarp();
 
+    // every warp's results to shared memory, then (m, l, o) of the part from all of them, in warp order
+    float *o_s = reinterpret_cast<float *>(smem + warp * S::WARP_BYTES);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -262,79 +266,89 @@ __global__ void __launch_bounds__(ListShape<DP>::WARPS * 32, 2)
             float sum = l[nt][c];
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            const float some = sum == 0.0f ? 0.0f : 1.0f;
             const int r = nt * 8 + 2 * t4 + c;
-            if (r >= R) continue;
-            const int hg = first_row + r;  // head of the group
-            if (sq.part0 >= 0) {  // a part of the list: (m, l, o) for the join, laid out as the kernel for few rows does
-                const float some = sum == 0.0f ? 0.0f : 1.0f;
-                const long long pr = sq.part0 + ((long long)part * p.H + head) * sq.nq * p.G + (long long)j * p.G + hg;
-#pragma unroll
-                for (int cc = 0; cc < DP / 64; ++cc) {
-                    const int d = cc * 64 + g * 8;
-                    if (d >= p.D) continue;
-                    float4 *dst = reinterpret_cast<float4 *>(p.part_o + pr * p.D + d);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        dst[i] = make_float4(scaled(o[nt][4 * cc + 2 * i][c], some), scaled(o[nt][4 * cc + 2 * i][2 + c], some),
-                                             scaled(o[nt][4 * cc + 2 * i + 1][c], some), scaled(o[nt][4 * cc + 2 * i + 1][2 + c], some));
-                }
-                if (g == 0) {
-                    p.part_ml[2 * pr] = m[nt][c] - Elt<T>::RAISE;
-                    p.part_ml[2 * pr + 1] = sum;
-                }
-                continue;
-            }
-            const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;  // a row that sees nothing is zero
-            const int hq = head * p.G + hg;
-            T *out = static_cast<T *>(p.out) + (tok * p.H * p.G + hq) * p.D;
+            if (g == 0) ml_s[warp][r] = make_float2(m[nt][c] - Elt<T>::RAISE, sum);
 #pragma unroll
             for (int cc = 0; cc < DP / 64; ++cc) {
-                const int d = cc * 64 + g * 8;
-                if (d >= p.D) continue;
-                uint4 w;
-                w.x = Elt<T>::pack(scaled(o[nt][4 * cc][c], inv), scaled(o[nt][4 * cc][2 + c], inv));
-                w.y = Elt<T>::pack(scaled(o[nt][4 * cc + 1][c], inv), scaled(o[nt][4 * cc + 1][2 + c], inv));
-                w.z = Elt<T>::pack(scaled(o[nt][4 * cc + 2][c], inv), scaled(o[nt][4 * cc + 2][2 + c], inv));
-                w.w = Elt<T>::pack(scaled(o[nt][4 * cc + 3][c], inv), scaled(o[nt][4 * cc + 3][2 + c], inv));
-                *reinterpret_cast<uint4 *>(out + d) = w;
+                float4 *dst = reinterpret_cast<float4 *>(o_s + r * DP + cc * 64 + g * 8);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    dst[i] = make_float4(scaled(o[nt][4 * cc + 2 * i][c], some), scaled(o[nt][4 * cc + 2 * i][2 + c], some),
+                                         scaled(o[nt][4 * cc + 2 * i + 1][c], some), scaled(o[nt][4 * cc + 2 * i + 1][2 + c], some));
             }
-            if (p.lse && g == 0)
-                p.lse[tok * p.H * p.G + hq] =
-                    sum == 0.0f ? -CUDART_INF_F
-                                : (m[nt][c] - Elt<T>::RAISE + log2f(sum)) * LN2 - (SIMPLE ? 0.0f : slope[SIMPLE ? 0 : nt][c] * (float)span.near);
         }
+    __syncthreads();
+    const int quads = p.D / 4;
+    for (int i = threadIdx.x; i < R * quads; i += WARPS * 32) {
+        const int r = i / quads, d = (i - r * quads) * 4;
+        float top = -CUDART_INF_F;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) top = fmaxf(top, ml_s[w][r].x);
+        const float from = top == -CUDART_INF_F ? 0.0f : top;
+        float sum = 0.0f;
+        float4 acc = make_float4(0, 0, 0, 0);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float2 ml = ml_s[w][r];
+            const float f = ex2(ml.x - from);  // a warp that saw nothing: 0
+            const float4 v = *reinterpret_cast<const float4 *>(smem + w * S::WARP_BYTES + (r * DP + d) * 4);
+            sum += f * ml.y;
+            acc.x += f * v.x;
+            acc.y += f * v.y;
+            acc.z += f * v.z;
+            acc.w += f * v.w;
+        }
+        const int hg = first_row + r;  // head of the group
+        if (sq.part0 >= 0) {  // a part of the list, for the join; laid out as the kernel for few rows does
+            const long long pr = sq.part0 + ((long long)part * p.H + head) * sq.nq * p.G + (long long)j * p.G + hg;
+            *reinterpret_cast<float4 *>(p.part_o + pr * p.D + d) = acc;
+            if (d == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * pr) = make_float2(top, sum);
+            continue;
+        }
+        const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;  // a row that sees nothing is zero
+        const long long hq = tok * p.H * p.G + head * p.G + hg;
+        *reinterpret_cast<uint2 *>(static_cast<T *>(p.out) + hq * p.D + d) =
+            make_uint2(Elt<T>::pack(scaled(acc.x, inv), scaled(acc.y, inv)), Elt<T>::pack(scaled(acc.z, inv), scaled(acc.w, inv)));
+        if (p.lse && d == 0)
+            p.lse[hq] = sum == 0.0f ? -CUDART_INF_F : (top + log2f(sum)) * LN2 - (!SIMPLE && p.slopes ? p.slopes[head * p.G + hg] * (float)span.near : 0.0f);
+    }
 }
 
-// rows that a lane's registers hold accumulators for, as in the kernel for few rows; larger groups go to several warps
+// rows that a lane's registers hold accumulators for, as in the kernel for few rows; larger groups go to several CTAs
 static int list_tiles(int D, int G) { return std::min((G + 7) / 8, few_rows_limit(D) / 8); }
 int attend_blocks_rows(int D, int G) {
     const int nt = list_tiles(D, G);
     return 8 * (nt == 3 ? 4 : nt);
 }
 
-template <typename T, int DP, int NT, bool SIMPLE>
+int attend_blocks_warps(int D) { return D <= 64 ? ListShape<64>::WARPS : (D <= 128 ? ListShape<128>::WARPS : ListShape<256>::WARPS); }
+
+template <typename T, int DP, int NT, bool SIMPLE, int WARPS>
 static cudaError_t list_go(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
     static SmemSeen seen{0};
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_blocks_kernel<T, DP, NT, SIMPLE>), ListShape<DP>::SMEM, &seen);
+    constexpr int bytes = WARPS * ListShape<DP>::WARP_BYTES;
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_blocks_kernel<T, DP, NT, SIMPLE, WARPS>), bytes, &seen);
     if (e != cudaSuccess) return e;
-    constexpr int W = ListShape<DP>::WARPS;
     const int groups = (p.G + NT * 8 - 1) / (NT * 8);
-    const long long tasks = (long long)p.total_units * p.H * groups;
-    attend_blocks_kernel<T, DP, NT, SIMPLE><<<(unsigned)((tasks + W - 1) / W), W * 32, ListShape<DP>::SMEM, st>>>(p, small, groups);
+    attend_blocks_kernel<T, DP, NT, SIMPLE, WARPS><<<(unsigned)(p.total_units * p.H * groups), WARPS * 32, bytes, st>>>(p, small, groups);
     return cudaGetLastError();
 }
-template <typename T, int DP, int NT> static cudaError_t list_kind(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
-    return p.softcap == 0.0f && !p.slopes ? list_go<T, DP, NT, true>(p, small, st) : list_go<T, DP, NT, false>(p, small, st);
+template <typename T, int DP, int NT> static cudaError_t list_kind(const AttnParams &p, const SmallSeqs &small, bool alone, cudaStream_t st) {
+    constexpr int W = ListShape<DP>::WARPS;
+    if (p.softcap == 0.0f && !p.slopes)
+        return alone ? list_go<T, DP, NT, true, 2 * W>(p, small, st) : list_go<T, DP, NT, true, W>(p, small, st);
+    return alone ? list_go<T, DP, NT, false, 2 * W>(p, small, st) : list_go<T, DP, NT, false, W>(p, small, st);
 }
-template <typename T> static cudaError_t list_pick(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
+template <typename T> static cudaError_t list_pick(const AttnParams &p, const SmallSeqs &small, bool alone, cudaStream_t st) {
     const int nt = list_tiles(p.D, p.G);
     if (p.D <= 64)
-        return nt == 1 ? list_kind<T, 64, 1>(p, small, st) : (nt == 2 ? list_kind<T, 64, 2>(p, small, st) : list_kind<T, 64, 4>(p, small, st));
-    if (p.D <= 128) return nt == 1 ? list_kind<T, 128, 1>(p, small, st) : list_kind<T, 128, 2>(p, small, st);
-    return list_kind<T, 256, 1>(p, small, st);
+        return nt == 1 ? list_kind<T, 64, 1>(p, small, alone, st) : (nt == 2 ? list_kind<T, 64, 2>(p, small, alone, st) : list_kind<T, 64, 4>(p, small, alone, st));
+    if (p.D <= 128) return nt == 1 ? list_kind<T, 128, 1>(p, small, alone, st) : list_kind<T, 128, 2>(p, small, alone, st);
+    return list_kind<T, 256, 1>(p, small, alone, st);
 }
-cudaError_t launch_attend_blocks(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st) {
-    return f16 ? list_pick<__half>(p, small, st) : list_pick<__nv_bfloat16>(p, small, st);
+cudaError_t launch_attend_blocks(const AttnParams &p, const SmallSeqs &small, int f16, bool alone, cudaStream_t st) {
+    return f16 ? list_pick<__half>(p, small, alone, st) : list_pick<__nv_bfloat16>(p, small, alone, st);
 }
 
 }  // namespace aafkv

@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
     uint32_t *keys = reinterpret_cast<uint32_t *>(smem);                    // [tile][room]
     uint32_t *hist = keys + z.tile * z.room;                                // [2][tile][256]
     unsigned char *codes = reinterpret_cast<unsigned char *>(hist + 2 * z.tile * 256);  // [rows][stride]
-    __shared__ int exps[SELECT_ROWS];
+    __shared__ __align__(8) float units_s[SELECT_ROWS];                     // of a row's codes: 2^f
     __shared__ __align__(8) uint32_t range_s[2];                            // smallest and largest score of the stretch, of any token
     __shared__ int last_s[SELECT_TOKENS];                                   // a token's own block
     __shared__ uint32_t prefix_s[SELECT_TOKENS];                            // of a list: the threshold's leading bits
@@ -99,9 +99,30 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
     // ---- scores
     uint32_t least_k = 0xffffffffu, most_k = 0;
     const int *table = p.tables + (long long)s.ctx * p.max_blk + b0;
-    const int rows_all = z.tile * z.heads_p;
+    auto id_of = [&](int m) {  // block of lane l's row l % 16 of an m-tile; behind the stretch its last one again
+        return count ? __ldg(table + min(m * 16 + (lane & 15), count - 1)) : 0;
+    };
+    struct Codes {
+        uint4 a[SPANS][2];
+        int e[2];
+    };
+    const signed char *first = p.summary + (long long)head * 2 * p.D + t4 * 16;
+    const int e_at = (p.H - head) * 2 * p.D + head - t4 * 16;  // the head's exponent, from there
+    auto fetch = [&](int id, Codes &x) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const signed char *rec = first + (long long)__shfl_sync(0xffffffffu, id, g + 8 * h) * p.record;
+            x.e[h] = __ldg(rec + e_at);
+#pragma unroll
+            for (int sp = 0; sp < SPANS; ++sp)
+                x.a[sp][h] = sp * 64 + t4 * 16 < 2 * p.D ? __ldg(reinterpret_cast<const uint4 *>(rec + sp * 64)) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    constexpr bool AHEAD = SPANS <= 4;  // the next m-tile's codes are under way while one is multiplied, where registers allow it
+    const int rows_all = z.tile * z.heads_p, hp_shift = z.heads_p >= 8 ? 3 : z.heads_p >> 1;  // rows of a token in an n-tile: 2^hp_shift
     for (int row0 = 0; row0 < rows_all; row0 += z.rows) {
         if (row0) __syncthreads();
+        int id = id_of(warp);
         const int rows = min(z.rows, (rows_all - row0 + 7) / 8 * 8);
         for (int r = warp; r < rows; r += SELECT_WARPS) {  // a row's codes: [c+, c-], zeros behind them
             const int tok = min((row0 + r) / z.heads_p, tokens - 1), gh = min((row0 + r) % z.heads_p, p.G - 1);
@@ -131,29 +152,18 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
                 *reinterpret_cast<uint2 *>(dst + p.D + lane * 8) = make_uint2(down[0], down[1]);
             }
             for (int i = 2 * p.D + lane * 8; i < SPANS * 64; i += 256) *reinterpret_cast<uint2 *>(dst + i) = make_uint2(0, 0);
-            if (lane == 0) exps[r] = f;
+            if (lane == 0) units_s[r] = power_of_two(f);
+        }
+        Codes even, odd;
+        if (AHEAD) {
+            fetch(id, even);
+            id = id_of(warp + SELECT_WARPS);
         }
         __syncthreads();
-        auto id_of = [&](int m) {
-            const int i = m * 16 + (lane & 15);
-            return i < count ? __ldg(table + i) : -1;
-        };
-        int id = id_of(warp);
-        for (int m = warp; m * 16 < count; m += SELECT_WARPS) {
-            const int ids[2] = {__shfl_sync(0xffffffffu, id, g), __shfl_sync(0xffffffffu, id, g + 8)};
-            id = id_of(m + SELECT_WARPS);
-            uint4 a[SPANS][2];
-            int e[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const signed char *rec = p.summary + (long long)max(ids[h], 0) * p.record;
-                e[h] = ids[h] < 0 ? 0 : __ldg(rec + (long long)p.H * 2 * p.D + head);
-#pragma unroll
-                for (int sp = 0; sp < SPANS; ++sp) {
-                    const int at = sp * 64 + t4 * 16;
-                    a[sp][h] = ids[h] >= 0 && at < 2 * p.D ? __ldg(reinterpret_cast<const uint4 *>(rec + (long long)head * 2 * p.D + at)) : make_uint4(0, 0, 0, 0);
-                }
-            }
+        auto multiply = [&](int m, const Codes &x) {
+            const float e[2] = {power_of_two(x.e[0]), power_of_two(x.e[1])};
+            const int i0 = m * 16 + g;
+            const bool in[2] = {i0 < count, i0 + 8 < count};
             for (int n0 = 0; n0 < rows; n0 += NT * 8) {
                 int c[NT][4];
 #pragma unroll
@@ -164,8 +174,8 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
 #pragma unroll
                         for (int sp = 0; sp < SPANS; ++sp) {
                             const uint4 b = *reinterpret_cast<const uint4 *>(src + sp * 64);
-                            mma_s8(c[nt], a[sp][0].x, a[sp][1].x, a[sp][0].y, a[sp][1].y, b.x, b.y);
-                            mma_s8(c[nt], a[sp][0].z, a[sp][1].z, a[sp][0].w, a[sp][1].w, b.z, b.w);
+                            mma_s8(c[nt], x.a[sp][0].x, x.a[sp][1].x, x.a[sp][0].y, x.a[sp][1].y, b.x, b.y);
+                            mma_s8(c[nt], x.a[sp][0].z, x.a[sp][1].z, x.a[sp][0].w, x.a[sp][1].w, b.z, b.w);
                         }
                     }
                 }
@@ -173,40 +183,54 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
                 for (int nt = 0; nt < NT; ++nt) {
                     const int r = n0 + nt * 8 + 2 * t4;  // this lane's rows: r, r + 1
                     if (n0 + nt * 8 >= rows) break;
-                    const int f[2] = {exps[r], exps[r + 1]};
-                    uint32_t k[2][2];
+                    // dot * 2^e * 2^f, the smaller power first: exact, and beyond the type's range only where the score is
+                    const float2 f = *reinterpret_cast<const float2 *>(units_s + r);
+                    float v[2][2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int x = e[h] + f[i];  // -120 ... 226
-                            k[h][i] = ordered((float)c[nt][2 * h + i] * power_of_two(min(x, 100)) * power_of_two(max(x, 100) - 100));
-                        }
-                    auto put = [&](int list, int h, uint32_t v) {
-                        const int i = m * 16 + g + 8 * h;
-                        if (list < z.tile && i < count) {
-                            least_k = min(least_k, v);
-                            most_k = max(most_k, v);
-                            uint32_t &at = key_at(list, i);
-                            at = z.heads_p > 8 && (row0 + n0 + nt * 8) % z.heads_p ? max(at, v) : v;  // a token's later rows
+                    for (int h = 0; h < 2; ++h) {
+                        v[h][0] = (float)c[nt][2 * h] * fminf(e[h], f.x) * fmaxf(e[h], f.x);
+                        v[h][1] = (float)c[nt][2 * h + 1] * fminf(e[h], f.y) * fmaxf(e[h], f.y);
+                    }
+                    auto put = [&](int list, int h, float score) {
+                        if (list < z.tile && in[h]) {
+                            uint32_t k = ordered(score);
+                            uint32_t &at = key_at(list, i0 + 8 * h);
+                            if (z.heads_p > 8 && (row0 + n0 + nt * 8) % z.heads_p) k = max(k, at);  // a token's later rows
+                            at = k;
+                            least_k = min(least_k, k);
+                            most_k = max(most_k, k);
                         }
                     };
-                    if (z.heads_p == 1) {
+                    const int list = z.heads_p > 8 ? (row0 + n0 + nt * 8) / z.heads_p : (row0 + r) >> hp_shift;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            put(row0 + r, h, k[h][0]);
-                            put(row0 + r + 1, h, k[h][1]);
+                    for (int h = 0; h < 2; ++h) {
+                        if (hp_shift == 0) {
+                            put(list, h, v[h][0]);
+                            put(list + 1, h, v[h][1]);
+                            continue;
                         }
-                    } else {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t v = max(k[h][0], k[h][1]);
-                            if (z.heads_p >= 4) v = max(v, __shfl_xor_sync(0xffffffffu, v, 1));
-                            if (z.heads_p >= 8) v = max(v, __shfl_xor_sync(0xffffffffu, v, 2));
-                            if (((2 * t4) & (min(z.heads_p, 8) - 1)) == 0) put((row0 + r) / z.heads_p, h, v);
-                        }
+                        float best = fmaxf(v[h][0], v[h][1]);
+                        if (hp_shift >= 2) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
+                        if (hp_shift >= 3) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2));
+                        if ((2 * t4 & ((1 << hp_shift) - 1)) == 0) put(list, h, best);
                     }
                 }
+            }
+        };
+        for (int m = warp; m * 16 < count; m += SELECT_WARPS) {
+            if (AHEAD) {  // two m-tiles a round, so that no codes have to be moved from where they were loaded to
+                fetch(id, odd);
+                id = id_of(m + 2 * SELECT_WARPS);
+                multiply(m, even);
+                m += SELECT_WARPS;
+                if (m * 16 >= count) break;
+                fetch(id, even);
+                id = id_of(m + 2 * SELECT_WARPS);
+                multiply(m, odd);
+            } else {
+                fetch(id, even);
+                id = id_of(m + SELECT_WARPS);
+                multiply(m, even);
             }
         }
     }

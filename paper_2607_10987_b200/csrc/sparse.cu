@@ -164,32 +164,40 @@ int aaf_kv_attend_blocks(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, in
     k.lists = blocks_dev;
     k.keep = keep;
     const int Hq = k.H * k.G, groups = (k.G + attend_blocks_rows(k.D, k.G) - 1) / attend_blocks_rows(k.D, k.G);
-    // Lists are cut into parts so that the warps that the GPU holds are filled a whole number of times: a round costs its part's keys and
-    // a start (about 24 keys' time), the join another start.
-    long long longest = 0;
-    for (const AttnSeq &s : rec) longest = std::max(longest, std::min<long long>(keep, nblk_of(p, s.len)) * BS);
-    auto tasks = [&](long long chunk) {
+    // Lists are cut into parts so that the GPU is filled a whole number of times, by CTAs that share an SM or, where there is one for
+    // each of them, by CTAs that have it to themselves and twice the warps: a round costs its part's keys per warp and a start (about 24
+    // keys' time), a join twice that.
+    int longest = 0;
+    for (AttnSeq &s : rec) {
+        s.chunk = (int)(std::min<long long>(keep, nblk_of(p, s.len)) * BS);  // keys of a full list, for now
+        longest = std::max(longest, s.chunk);
+    }
+    const int warps = attend_blocks_warps(k.D);
+    int chunk = 16;
+    long long best = 1ll << 62;
+    bool alone = false;
+    for (int parts = 1; parts <= 64 && (parts == 1 || longest / 64 >= parts); parts += parts < 4 ? 1 : parts / 2) {
+        const int c = ((longest + parts - 1) / parts + 15) / 16 * 16;
         long long t = 0;
-        for (const AttnSeq &s : rec) t += (std::min<long long>(keep, nblk_of(p, s.len)) * BS + chunk - 1) / chunk * s.nq;
-        return t;
-    };
-    const long long warps = 8ll * p->sm_count;
-    long long chunk = (longest + 15) / 16 * 16, best = 1ll << 62;
-    for (long long parts = 1; parts <= 64 && (parts == 1 || longest >= 32 * parts); ++parts) {
-        const long long c = ((longest + parts - 1) / parts + 15) / 16 * 16, t = tasks(c);
+        for (const AttnSeq &s : rec) t += (long long)((s.chunk + c - 1) / c) * s.nq;
         if (parts > 1 && t * Hq > PART_ROWS) break;  // partial results have to fit
-        const long long cost = (t * k.H * groups + warps - 1) / warps * (c + 24) + (parts > 1 ? 24 : 0);
-        if (cost < best) {
-            best = cost;
-            chunk = c;
+        for (int per_sm = 2; per_sm >= 1; --per_sm) {
+            const long long rounds = (t * k.H * groups + per_sm * p->sm_count - 1) / (per_sm * p->sm_count);
+            const long long cost = rounds * (c * per_sm / (2 * warps) + 24) + (parts > 1 ? 48 : 0);
+            if (cost < best && (per_sm == 2 || rounds == 1)) {
+                best = cost;
+                chunk = c;
+                alone = per_sm == 1;
+            }
         }
+        if (t * k.H * groups > 16ll * p->sm_count) break;  // enough for even rounds
     }
     long long units = 0, rows = 0;
     int max_parts = 1;
     bool joined = false;
     for (AttnSeq &s : rec) {
-        s.chunk = (int)chunk;
-        s.nsplit = (int)((std::min<long long>(keep, nblk_of(p, s.len)) * BS + chunk - 1) / chunk);
+        s.nsplit = (s.chunk + chunk - 1) / chunk;
+        s.chunk = chunk;
         s.unit0 = (int)units;
         s.tok0 = s.row0;
         units += (long long)s.nsplit * s.nq;
@@ -211,7 +219,7 @@ int aaf_kv_attend_blocks(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, in
     if (!begin_read(p, ctxs, n, st)) return broke(p);
     const int f16 = a->dtype == AAF_DTYPE_F16;
     SmallSeqs small;
-    bool ok = place_records(p, rec, small, &k.seqs, 0, st) && launch_attend_blocks(k, small, f16, st) == cudaSuccess;
+    bool ok = place_records(p, rec, small, &k.seqs, 0, st) && launch_attend_blocks(k, small, f16, alone, st) == cudaSuccess;
     if (ok && joined) ok = launch_attend_join(k, small, f16, 0, (int)total, max_parts, p->sm_count, st) == cudaSuccess;
     return ok && end_read(p, st) ? AAF_OK : broke(p);
 } catch (const std::bad_alloc &) {

@@ -52,9 +52,11 @@ struct TablesParams {
 cudaError_t launch_summarize(const SummaryParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
 SelectShape select_shape(const SelectParams &p, int max_nq, long long tokens, int sm_count, int f16);
 cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, cudaStream_t st);
-// p.first is not read; a record's nsplit parts of `chunk` listed keys (lists of `keep` blocks); units are (query token, part)
-cudaError_t launch_attend_blocks(const AttnParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
-int attend_blocks_rows(int D, int G);  // query rows of a unit's warp
+// p.first is not read; a record's nsplit parts of `chunk` listed keys (lists of `keep` blocks); units are (query token, part).
+// alone: CTAs of twice as many warps that have an SM to themselves
+cudaError_t launch_attend_blocks(const AttnParams &p, const SmallSeqs &small, int f16, bool alone, cudaStream_t st);
+int attend_blocks_rows(int D, int G);  // query rows of a CTA
+int attend_blocks_warps(int D);        // of a CTA that is not alone
 cudaError_t launch_batch_tables(const TablesParams &p, const SmallSeqs &small, cudaStream_t st);
 
 }  // namespace aafkv
