@@ -242,6 +242,8 @@ int aaf_kv_batch_tables(aaf_kv_pool *p, const aaf_kv_batch_desc *d, int32_t n, c
     const int rc = batch_records(p, n, ctxs, n_new, false, rec, &total);
     if (rc != AAF_OK) return rc;
     if (d->rows < n || d->tokens < total) return AAF_ERR_DST_TOO_SMALL;
+    std::vector<TableRow> row(rec.size());
+    std::transform(rec.begin(), rec.end(), row.begin(), [](const AttnSeq &s) { return TableRow{s.ctx, s.len, s.nq, s.row0}; });
     if (d->tables)
         for (const AttnSeq &s : rec)
             if (d->cols < nblk_of(p, s.len)) return AAF_ERR_DST_TOO_SMALL;
@@ -258,8 +260,8 @@ int aaf_kv_batch_tables(aaf_kv_pool *p, const aaf_kv_batch_desc *d, int32_t n, c
     k.n = n; k.cols = d->cols; k.rows = d->rows; k.tokens = d->tokens; k.total = (int)total;
     p->last_stream = st;
     if (!begin_read(p, ctxs, n, st)) return broke(p);
-    SmallSeqs small;
-    const bool ok = place_records(p, rec, small, &k.seqs, 0, st) && launch_batch_tables(k, small, st) == cudaSuccess;
+    SmallRows<SMALL_SEQS> none;
+    const bool ok = (n <= SMALL_ROWS || place_records(p, row, none, &k.seqs, 0, st)) && launch_batch_tables(k, row.data(), st) == cudaSuccess;
     return ok && end_read(p, st) ? AAF_OK : broke(p);
 } catch (const std::bad_alloc &) {
     return AAF_ERR_INVALID_ARG;  // the host has no memory for the records; nothing was launched

@@ -41,8 +41,17 @@ struct SelectShape {
     int f16;
 };
 
+struct TableRow {
+    int ctx, len, nq, row0;
+};
+// Rows that travel as kernel parameters: a batch of up to 64 in 1 KB, up to 512 in 8 KB (256 rows: 7 us of the host's time less than
+// through pinned memory and a copy)
+template <int N> struct SmallRows {
+    TableRow e[N];
+};
+constexpr int SMALL_ROWS = 512;
 struct TablesParams {
-    const AttnSeq *seqs;
+    const TableRow *seqs;  // device records, null: the kernel parameter holds them
     const int *src;       // the pool's tables
     int *tables, *lens, *offsets, *token_row;
     long long *positions, *slots;
@@ -57,6 +66,6 @@ cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, 
 cudaError_t launch_attend_blocks(const AttnParams &p, const SmallSeqs &small, int f16, bool alone, cudaStream_t st);
 int attend_blocks_rows(int D, int G);  // query rows of a CTA
 int attend_blocks_warps(int D);        // of a CTA that is not alone
-cudaError_t launch_batch_tables(const TablesParams &p, const SmallSeqs &small, cudaStream_t st);
+cudaError_t launch_batch_tables(const TablesParams &p, const TableRow *rows, cudaStream_t st);  // rows: the batch, on the host
 
 }  // namespace aafkv

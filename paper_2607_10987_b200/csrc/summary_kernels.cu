@@ -115,9 +115,10 @@ cudaError_t launch_summarize(const SummaryParams &p, const SmallSeqs &small, int
 // 10 MB the bytes.
 constexpr int TABLES_THREADS = 256, TABLES_STRETCH = 1024;
 
+template <int N>
 __global__ void __launch_bounds__(TABLES_THREADS)
-    batch_tables_kernel(const __grid_constant__ TablesParams p, const __grid_constant__ SmallSeqs small, int table_ctas) {
-    const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
+    batch_tables_kernel(const __grid_constant__ TablesParams p, const __grid_constant__ SmallRows<N> small, int table_ctas) {
+    const TableRow *seqs = p.seqs ? p.seqs : small.e;
     const int cta = blockIdx.x;
     if (cta < table_ctas) {
         const int per_row = table_ctas / p.rows, row = cta / per_row, c0 = (cta - row * per_row) * TABLES_STRETCH;
@@ -149,12 +150,17 @@ __global__ void __launch_bounds__(TABLES_THREADS)
     if (p.slots) p.slots[i] = slot;
 }
 
-cudaError_t launch_batch_tables(const TablesParams &p, const SmallSeqs &small, cudaStream_t st) {
+template <int N> static cudaError_t tables_go(const TablesParams &p, const TableRow *rows, cudaStream_t st) {
+    SmallRows<N> small;
+    if (!p.seqs) std::copy(rows, rows + p.n, small.e);
     const int table_ctas = p.tables && p.rows ? (p.cols + TABLES_STRETCH - 1) / TABLES_STRETCH * p.rows : 0;
     const long long items = std::max<long long>(p.tokens, (long long)p.rows + 1);
     const unsigned grid = (unsigned)(table_ctas + (items + TABLES_THREADS - 1) / TABLES_THREADS);
-    batch_tables_kernel<<<grid, TABLES_THREADS, 0, st>>>(p, small, table_ctas);
+    batch_tables_kernel<N><<<grid, TABLES_THREADS, 0, st>>>(p, small, table_ctas);
     return cudaGetLastError();
+}
+cudaError_t launch_batch_tables(const TablesParams &p, const TableRow *rows, cudaStream_t st) {
+    return p.seqs || p.n <= 64 ? tables_go<64>(p, rows, st) : tables_go<SMALL_ROWS>(p, rows, st);
 }
 
 }  // namespace aafkv

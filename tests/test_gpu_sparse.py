@@ -440,6 +440,18 @@ def test_batch_tables_of_one_token_each_some_arrays_and_more_contexts_than_kerne
     assert some["slots"].tolist() == want["slots"] and some["lens"].tolist() == want["lens"]
 
 
+@pytest.mark.parametrize("n", [64, 65, 512, 513])
+def test_batch_tables_of_many_rows(n):
+    lens, new = [1 + 7 * i % 40 for i in range(n)], [1 + i % (1 + 7 * i % 40) for i in range(n)]
+    pool, ctxs = pool_of(1, 8, 8, lens)
+    handles = [c.handle for c in ctxs]
+    st, got = pool.batch_tables(handles, new, rows=n + 2)
+    assert st == 0
+    settle(pool)
+    want = S.batch_tables_ref([pool.table(h).tolist() for h in handles], lens, new, 8, n + 2, sum(new), 5)
+    assert {k: v.tolist() for k, v in got.items()} == want
+
+
 def test_slots_name_the_rows_that_store_writes():
     pool, ctxs = pool_of(2, 64, 16, [40, 16], layers=2)
     handles, new = [c.handle for c in ctxs], [5, 20]
