@@ -448,8 +448,7 @@ int aaf_kv_prune(aaf_kv_pool *pool, aaf_ctx_t ctx, const float *scores_dev, int6
  * as old as the last aaf_kv_summarize of a context that holds the block: call it for what import, append, store, compose, prune or a copied
  * tail have put into blocks, before aaf_kv_select is to know of it. */
 #define AAF_ALL_LAYERS (-1)
-#define AAF_SELECT_MAX_BLOCKS 262144 /* of a context that aaf_kv_select chooses from */
-#define AAF_LIST_MAX_BLOCKS 1048576  /* of a list                                     */
+#define AAF_LIST_MAX_BLOCKS 1048576 /* of a list */
 
 size_t aaf_kv_summary_bytes(const aaf_kv_pool *pool);
 
@@ -469,9 +468,10 @@ int aaf_kv_summarize(aaf_kv_pool *pool, int32_t layer, int32_t dtype, int32_t n,
  * the context has them: those of block B, which is always taken.
  * blocks_dev: [tokens][n_kv_heads][keep] block numbers within the context, ascending, -1 behind the last; scores_dev (may be NULL): the same
  * shape, their scores, -inf behind the last.  q: heads contiguous, q_stride elements from token to token (a multiple of 8).  n_q may be NULL
- * (one token each).  A context may be listed several times.
+ * (one token each).  A context may be listed several times.  workspace_dev as for aaf_kv_attend, the same buffer: it holds scores.
  * Errors: BAD_CTX, INVALID_ARG (n_q, keep outside [1, AAF_LIST_MAX_BLOCKS], recent < 1, sink < 0, sink + recent > keep, pointers, strides),
- * INCOMPAT, DST_TOO_SMALL (summary_bytes), TOO_MANY, TOO_LONG (more than AAF_SELECT_MAX_BLOCKS blocks). */
+ * INCOMPAT, DST_TOO_SMALL (summary, workspace), TOO_MANY, TOO_LONG (more blocks in the longest context, times n_kv_heads, than 65536 *
+ * (head_dim + 2)). */
 typedef struct aaf_kv_select_desc {
     uint32_t struct_size; /* sizeof(aaf_kv_select_desc)      */
     int32_t dtype;        /* AAF_DTYPE_*                     */
@@ -482,7 +482,7 @@ typedef struct aaf_kv_select_desc {
 } aaf_kv_select_desc;
 int aaf_kv_select(aaf_kv_pool *pool, int32_t layer, const aaf_kv_select_desc *d, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_q,
                   const void *q_dev, const void *summary_dev, size_t summary_bytes, int32_t *blocks_dev, float *scores_dev,
-                  void *stream);
+                  void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /* attend_blocks -- aaf_kv_attend with the same arguments, over the listed blocks alone: a row of kv head h sees the keys that it would see
  * there (its span, its window) and that lie in a block of its token's list, blocks_dev[token][h][0 .. keep) (block numbers within the context,

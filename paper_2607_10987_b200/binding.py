@@ -27,7 +27,7 @@ AAF_ENGINE_AUTO, AAF_ENGINE_VEC, AAF_ENGINE_BULK, AAF_ENGINE_WARP = 0, 1, 2, 3
 AAF_OP_MATERIALIZE, AAF_OP_IMPORT, AAF_OP_APPEND, AAF_OP_COMPOSE, AAF_OP_CLASSES = 0, 1, 2, 3, 4
 AAF_DTYPE_BF16, AAF_DTYPE_F16 = 0, 1
 AAF_ROPE_NONE, AAF_ROPE_LINEAR, AAF_ROPE_BASE, AAF_ROPE_WAVELENGTH, AAF_ROPE_RAMP = 0, 1, 2, 3, 4
-AAF_ALL_LAYERS, AAF_SELECT_MAX_BLOCKS, AAF_LIST_MAX_BLOCKS = -1, 262144, 1048576
+AAF_ALL_LAYERS, AAF_LIST_MAX_BLOCKS = -1, 1048576
 OP_NAMES = ("materialize", "import", "append", "compose")
 
 
@@ -131,7 +131,7 @@ SYMBOLS = {
     "aaf_kv_prune": (C.c_int, [_vp, _i32, _vp, _i64, _i64, _i64, _vp, _vp, _p32, _vp]),
     "aaf_kv_summary_bytes": (_sz, [_vp]),
     "aaf_kv_summarize": (C.c_int, [_vp, _i32, _i32, _i32, _p32, _p32, _vp, _sz, _vp]),
-    "aaf_kv_select": (C.c_int, [_vp, _i32, C.POINTER(aaf_kv_select_desc), _i32, _p32, _p32, _vp, _vp, _sz, _vp, _vp, _vp]),
+    "aaf_kv_select": (C.c_int, [_vp, _i32, C.POINTER(aaf_kv_select_desc), _i32, _p32, _p32, _vp, _vp, _sz, _vp, _vp, _vp, _sz, _vp]),
     "aaf_kv_attend_blocks": (C.c_int, [_vp, _i32, C.POINTER(aaf_kv_attn), _i32, _p32, _p32, _vp, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
     "aaf_kv_batch_tables": (C.c_int, [_vp, C.POINTER(aaf_kv_batch_desc), _i32, _p32, _p32, _vp]),
     "aaf_kv_catalog_rows": (C.c_int, [_vp, _p32, C.POINTER(_i64)]),
@@ -226,8 +226,8 @@ def aaf_kv_prune(pool, ctx, scores, budget, sink, recent, kept, kept_scores, out
 def aaf_kv_summary_bytes(pool): return _fn("aaf_kv_summary_bytes")(pool)
 def aaf_kv_summarize(pool, layer, dtype, n, ctxs, n_new, summary, summary_bytes, stream):
     return _fn("aaf_kv_summarize")(pool, layer, dtype, n, ctxs, n_new, summary, summary_bytes, stream)
-def aaf_kv_select(pool, layer, desc, n, ctxs, n_q, q, summary, summary_bytes, blocks, scores, stream):
-    return _fn("aaf_kv_select")(pool, layer, desc, n, ctxs, n_q, q, summary, summary_bytes, blocks, scores, stream)
+def aaf_kv_select(pool, layer, desc, n, ctxs, n_q, q, summary, summary_bytes, blocks, scores, workspace, workspace_bytes, stream):
+    return _fn("aaf_kv_select")(pool, layer, desc, n, ctxs, n_q, q, summary, summary_bytes, blocks, scores, workspace, workspace_bytes, stream)
 def aaf_kv_attend_blocks(pool, layer, attn, n, ctxs, n_q, q, blocks, keep, out, lse, workspace, workspace_bytes, stream):
     return _fn("aaf_kv_attend_blocks")(pool, layer, attn, n, ctxs, n_q, q, blocks, keep, out, lse, workspace, workspace_bytes, stream)
 def aaf_kv_batch_tables(pool, desc, n, ctxs, n_new, stream):
@@ -521,13 +521,16 @@ class KVPool:
             lse = q.new_empty((tokens, heads), dtype=torch.float32)
         else:
             self._flat(lse, torch.float32, tokens * heads, "lse")
-        ws = self._attend_ws
-        if ws is None:
-            with torch.cuda.device(self.device):
-                if torch.cuda.is_current_stream_capturing():  # refused anyway; kept scratch must not be a graph's memory
-                    return out, lse, None
-            ws = self._attend_ws = torch.empty(aaf_kv_attend_workspace_bytes(self.h), dtype=torch.uint8, device=self.device)
-        return out, lse, ws
+        return out, lse, self._attend_ws if self._attend_ws is not None else self._scratch()
+
+    def _scratch(self):
+        """Workspace of the attention calls, made by the first of them; None if it must not be made now."""
+        torch = self.torch
+        with torch.cuda.device(self.device):
+            if torch.cuda.is_current_stream_capturing():  # refused anyway; kept scratch must not be a graph's memory
+                return None
+        self._attend_ws = torch.empty(aaf_kv_attend_workspace_bytes(self.h), dtype=torch.uint8, device=self.device)
+        return self._attend_ws
 
     def attend(self, layer, ctxs, n_q, q, out=None, lse=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):
         """Attention of the contexts' last n_q tokens (None: one each); returns (status, (out, lse))."""
@@ -609,10 +612,14 @@ class KVPool:
         if blocks is None:
             blocks = q.new_empty((tokens, self.H, max(keep, 0)), dtype=self.torch.int32)
         size = tokens * self.H * max(keep, 0)
+        ws = self._attend_ws if self._attend_ws is not None else self._scratch()
+        if ws is None:
+            return AAF_ERR_INVALID_ARG, None
         st = load().aaf_kv_select(self.h, layer, d, n, _ints(ctxs), None if n_q is None else _ints(n_q),
                                   q.data_ptr(), self._flat(summary, self.torch.int8, self.summary_bytes(), "summary"), summary.numel(),
                                   self._flat(blocks, self.torch.int32, size, "blocks"),
-                                  None if scores is None else self._flat(scores, self.torch.float32, size, "scores"), self._stream())
+                                  None if scores is None else self._flat(scores, self.torch.float32, size, "scores"), ws.data_ptr(), ws.numel(),
+                                  self._stream())
         return st, (blocks if st == AAF_OK else None)
 
     def attend_blocks(self, layer, ctxs, n_q, q, blocks, out=None, lse=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):

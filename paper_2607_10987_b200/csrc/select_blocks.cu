@@ -6,126 +6,95 @@
 // max(c hi, c lo) = max(c, 0) hi + min(c, 0) lo: a product of [c+, c-] with the block's [hi, lo], in whole numbers, exact in any
 // order, and so is the scaling by a power of two; equal scores go to the lower block.
 //
-// A unit is a tile of query tokens of a context and a kv head; a cluster of CTAs takes it, each CTA a stretch of the context's
-// blocks.  Scores: 16 blocks as the M side of 8-bit products, the tile's query rows as the N side, codes straight from memory into
-// the lanes that need them (the order of the channels is free as long as both sides agree: a lane takes 16 consecutive
-// bytes).  They stay in shared memory, as whole numbers of the same order.  Selection: the smallest score that is taken is
-// found eight bits at a time by histograms, which the CTAs of a cluster read from one another; then every CTA knows how many blocks come
-// before its own and writes its part of the list.
+// Two kernels.  Scores: 128 blocks as the M side of 8-bit products on the fifth-generation tensor cores, the rows of a tile of query
+// tokens as the N side, sums in tensor memory, where a thread finds all of a block's and takes the largest of every token's heads.  A CTA
+// takes a kv head; those of one tile follow one another in the grid, so that the pieces of a block's record are asked for together.
+// Selection: a CTA a list; the smallest score that is taken is found by histograms of eight bits, starting behind the bits that all
+// scores share; a list's scores come from L2 and stay in shared memory where they fit.
 //
-// Bound: the bytes of the summaries where there is a token each; the selection's passes where there are many.
+// Bound: the bytes of the summaries where there is a token each (and the start of the two kernels); latency of the passes of the
+// selection where there are many tokens.
 #include "sparse_device.cuh"
+#include "tensor_device.cuh"
 
 namespace aafkv {
 
-constexpr int SELECT_WARPS = 8, SELECT_ROWS = 64;  // query rows of a pass over the summaries
-constexpr int SELECT_TOKENS = 16;                  // of a tile, at most
+constexpr int SCORE_BLOCKS = 128;  // of an m-tile
+constexpr int SCORE_THREADS = 128, PICK_WARPS = 8, PICK_KEYS = 12288;  // scores of a list that are kept in shared memory
 
-__device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// words of another CTA's shared memory: those that lie there where `addr` lies here
-__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, int cta) {
-    uint32_t at;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(cta));
-    return at;
-}
-__device__ __forceinline__ uint4 peer_words(uint32_t at) {
-    uint4 v;
-    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-    return v;
-}
-__device__ __forceinline__ uint2 peer_pair(uint32_t at) {
-    uint2 v;
-    asm volatile("ld.shared::cluster.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
-    return v;
+// 8-bit products, 32-bit sums
+__device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// SPANS: 64-byte stretches of a head's codes (2 head_dim bytes); NT: n-tiles of 8 query rows that are accumulated at a time
-template <int SPANS, int NT>
-__global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
-    select_blocks_kernel(const __grid_constant__ SelectParams p, const __grid_constant__ SmallSeqs small, const __grid_constant__ SelectShape z) {
-    extern __shared__ __align__(16) unsigned char smem[];
-    uint32_t *keys = reinterpret_cast<uint32_t *>(smem);                    // [tile][room]
-    uint32_t *hist = keys + z.tile * z.room;                                // [2][tile][256]
-    unsigned char *codes = reinterpret_cast<unsigned char *>(hist + 2 * z.tile * 256);  // [rows][stride]
-    __shared__ __align__(8) float units_s[SELECT_ROWS];                     // of a row's codes: 2^f
-    __shared__ __align__(8) uint32_t range_s[2];                            // smallest and largest score of the stretch, of any token
-    __shared__ int last_s[SELECT_TOKENS];                                   // a token's own block
-    __shared__ uint32_t prefix_s[SELECT_TOKENS];                            // of a list: the threshold's leading bits
-    __shared__ int want_s[SELECT_TOKENS];                                   // how many of those with these bits are taken; see below
-    __shared__ uint32_t before_s[SELECT_TOKENS][2];                         // in other CTAs' earlier stretches: above the threshold, equal to it
-    __shared__ uint32_t counts_s[SELECT_WARPS][2];                          // of a warp's piece: certainly taken, equal to the threshold
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t4 = lane & 3;
-    const int cta = z.ctas > 1 ? (int)cluster_rank() : 0;
-    const int unit = blockIdx.x / z.ctas / p.H, head = blockIdx.x / z.ctas - unit * p.H;
+// HP: log2 of the rows that a token has in a stretch of 32 columns (its group's heads, repeated up to a power of two)
+template <int HP>
+__global__ void __launch_bounds__(SCORE_THREADS)
+    score_blocks_kernel(const __grid_constant__ SelectParams p, const __grid_constant__ SmallSeqs small, const __grid_constant__ SelectShape z) {
+    extern __shared__ unsigned char smem[];  // codes of the blocks (z.buffers of z.slabs * 16 KB), of the rows (z.slabs * z.n * 128)
+    __shared__ __align__(8) uint64_t bar;
+    __shared__ uint32_t tmem_s;
+    __shared__ int abort_s;
+    __shared__ __align__(16) float units_s[SELECT_ROWS];  // of a row's codes: 2^(f - 64)
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int unit = blockIdx.x / p.H, head = blockIdx.x - unit * p.H;
     const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
     const AttnSeq s = seqs[find_seq(seqs, p.n, unit)];
-    const int j0 = (unit - s.unit0) * z.tile, tokens = min(z.tile, s.nq - j0);
-    const int pos0 = s.len - s.nq + j0;  // position of the tile's first token
-    const int total = (pos0 + tokens - 1) / p.BS + 1;  // blocks that some token of the tile may take
-    const int stretch = ((total + z.ctas - 1) / z.ctas + 15) / 16 * 16;
-    const int b0 = min(cta * stretch, total), count = min(stretch, total - b0);
-    auto sync_all = [&]() {
-        if (z.ctas > 1) cluster_sync();
-        else __syncthreads();
-    };
-    auto key_at = [&](int list, int i) -> uint32_t & { return keys[list * z.room + i]; };
-
-    for (int i = threadIdx.x; i < z.tile * 256; i += SELECT_WARPS * 32) hist[i] = 0;
-    if (threadIdx.x < z.tile) {
-        const int last = (pos0 + min((int)threadIdx.x, tokens - 1)) / p.BS;
-        const int want = p.keep - p.sink - p.recent;
-        last_s[threadIdx.x] = last;
-        prefix_s[threadIdx.x] = before_s[threadIdx.x][0] = before_s[threadIdx.x][1] = 0;
-        want_s[threadIdx.x] = last + 1 <= p.keep ? -1 : want;
-    }
-
-    if (threadIdx.x == 0) {
-        range_s[0] = 0xffffffffu;
-        range_s[1] = 0;
-    }
-
-    // ---- scores
-    uint32_t least_k = 0xffffffffu, most_k = 0;
-    const int *table = p.tables + (long long)s.ctx * p.max_blk + b0;
-    auto id_of = [&](int m) {  // block of lane l's row l % 16 of an m-tile; behind the stretch its last one again
-        return count ? __ldg(table + min(m * 16 + (lane & 15), count - 1)) : 0;
-    };
-    struct Codes {
-        uint4 a[SPANS][2];
-        int e[2];
-    };
-    const signed char *first = p.summary + (long long)head * 2 * p.D + t4 * 16;
-    const int e_at = (p.H - head) * 2 * p.D + head - t4 * 16;  // the head's exponent, from there
-    auto fetch = [&](int id, Codes &x) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const signed char *rec = first + (long long)__shfl_sync(0xffffffffu, id, g + 8 * h) * p.record;
-            x.e[h] = __ldg(rec + e_at);
-#pragma unroll
-            for (int sp = 0; sp < SPANS; ++sp)
-                x.a[sp][h] = sp * 64 + t4 * 16 < 2 * p.D ? __ldg(reinterpret_cast<const uint4 *>(rec + sp * 64)) : make_uint4(0, 0, 0, 0);
+    const int tile = (unit - s.unit0) / s.nsplit, group = unit - s.unit0 - tile * s.nsplit;
+    const int j0 = tile * z.tile, tokens = min(z.tile, s.nq - j0);
+    const int total = (s.key0 + j0 + tokens - 1) / p.BS + 1;  // blocks that some token of the tile may take
+    const int first = group * z.reps * SCORE_BLOCKS, m_tiles = min(z.reps, (total - first + SCORE_BLOCKS - 1) / SCORE_BLOCKS);
+    if (m_tiles <= 0) return;
+    const uint32_t s_0 = (uint32_t)__cvta_generic_to_shared(smem), s_a = (s_0 + 1023) & ~1023u, a_bytes = z.slabs * SCORE_BLOCKS * 128;
+    const uint32_t s_b = s_a + z.buffers * a_bytes, s_bar = (uint32_t)__cvta_generic_to_shared(&bar);
+    if (warp == 0) {
+        if (lane == 0) {
+            bar_init(s_bar, 1);
+            abort_s = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
+        __syncwarp();
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                         (uint32_t)__cvta_generic_to_shared(&tmem_s)), "r"(z.n) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+
+    // a thread looks after one block of an m-tile; a warp copies the codes of its 32 blocks, 16 bytes a lane
+    const int *table = p.tables + (long long)s.ctx * p.max_blk;
+    const int pieces = p.D / 8;  // of a block's codes, 16 bytes each
+    auto record_of = [&](int m) {
+        return p.summary + (long long)__ldg(table + min(first + m * SCORE_BLOCKS + (int)threadIdx.x, total - 1)) * p.record;
     };
-    constexpr bool AHEAD = SPANS <= 4;  // the next m-tile's codes are under way while one is multiplied, where registers allow it
-    const int rows_all = z.tile * z.heads_p, hp_shift = z.heads_p >= 8 ? 3 : z.heads_p >> 1;  // rows of a token in an n-tile: 2^hp_shift
-    for (int row0 = 0; row0 < rows_all; row0 += z.rows) {
-        if (row0) __syncthreads();
-        int id = id_of(warp);
-        const int rows = min(z.rows, (rows_all - row0 + 7) / 8 * 8);
-        for (int r = warp; r < rows; r += SELECT_WARPS) {  // a row's codes: [c+, c-], zeros behind them
-            const int tok = min((row0 + r) / z.heads_p, tokens - 1), gh = min((row0 + r) % z.heads_p, p.G - 1);
+    auto issue = [&](int m, const signed char *rec) {
+        const uint32_t dst = s_a + (m % z.buffers) * a_bytes;
+        for (int i = lane; i < 32 * pieces; i += 32) {  // 32 * pieces is a multiple of 32: all lanes take part
+            const int r = i / pieces, c = i - r * pieces, row = warp * 32 + r;
+            const signed char *src = reinterpret_cast<const signed char *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(rec), r));
+            copy16(dst + (c >> 3) * (SCORE_BLOCKS * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4), src + (long long)head * 2 * p.D + c * 16, 16);
+        }
+        copy_commit();
+    };
+    const signed char *rec = record_of(0);
+    issue(0, rec);
+
+    const int rows_token = z.heads_p, rows_all = tokens * rows_token;
+    const int list_of_tile = s.tok0 + j0;
+    bool ok = true;
+    int parity = 0;
+    const uint32_t idesc = 2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(z.n / 8) << 17 | (SCORE_BLOCKS / 16) << 24;
+    // a pass takes z.n rows: one, but for groups of more heads than that
+    for (int row0 = 0; row0 < rows_all; row0 += z.n) {
+        const int rows = min(z.n, rows_all - row0);
+        if (row0) {
+            __syncthreads();
+            rec = record_of(0);
+            issue(0, rec);
+        }
+        for (int r = warp; r < rows; r += SCORE_THREADS / 32) {  // a row's codes: [c+, c-], zeros up to a multiple of 32
+            const int tok = (row0 + r) / rows_token, gh = min((row0 + r) - tok * rows_token, p.G - 1);
             const uint16_t *q = static_cast<const uint16_t *>(p.q) + (long long)(s.row0 + j0 + tok) * p.q_stride + (long long)(head * p.G + gh) * p.D;
             const uint4 v = lane * 8 < p.D ? __ldg(reinterpret_cast<const uint4 *>(q) + lane) : make_uint4(0, 0, 0, 0);
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -146,243 +115,200 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
                 up[i / 4] |= (uint32_t)max(c, 0) << (8 * (i & 3));
                 down[i / 4] |= ((uint32_t)min(c, 0) & 255u) << (8 * (i & 3));
             }
-            unsigned char *dst = codes + r * z.stride;
+            unsigned char *dst = smem + (s_b - s_0) + r * 128;
+            auto place = [&](int at) { return (at >> 7) * z.n * 128 + (((at >> 4 & 7) ^ (r & 7)) << 4) + (at & 15); };
             if (lane * 8 < p.D) {
-                *reinterpret_cast<uint2 *>(dst + lane * 8) = make_uint2(up[0], up[1]);
-                *reinterpret_cast<uint2 *>(dst + p.D + lane * 8) = make_uint2(down[0], down[1]);
+                *reinterpret_cast<uint2 *>(dst + place(lane * 8)) = make_uint2(up[0], up[1]);
+                *reinterpret_cast<uint2 *>(dst + place(p.D + lane * 8)) = make_uint2(down[0], down[1]);
             }
-            for (int i = 2 * p.D + lane * 8; i < SPANS * 64; i += 256) *reinterpret_cast<uint2 *>(dst + i) = make_uint2(0, 0);
-            if (lane == 0) units_s[r] = power_of_two(f);
+            if (2 * p.D % 32 && lane < 2) *reinterpret_cast<uint2 *>(dst + place(2 * p.D + lane * 8)) = make_uint2(0, 0);
+            if (lane == 0) units_s[r] = power_of_two(f - 64);
         }
-        Codes even, odd;
-        if (AHEAD) {
-            fetch(id, even);
-            id = id_of(warp + SELECT_WARPS);
+        for (int m = 0; m < m_tiles; ++m) {
+            const int e = __ldg(rec + (long long)p.H * 2 * p.D + head);
+            if (m + 1 < m_tiles && z.buffers > 1) {
+                rec = record_of(m + 1);
+                issue(m + 1, rec);
+                copy_wait<1>();
+            } else {
+                copy_wait<0>();
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            tmem_before();
+            __syncthreads();
+            tmem_after();
+            const uint32_t tmem = tmem_s;
+            if (warp == 0 && elected()) {
+                const uint64_t da = smem_desc(s_a + (m % z.buffers) * a_bytes, 16, 1024), db = smem_desc(s_b, 16, 1024);
+                const int steps = (2 * p.D + 31) / 32;
+                for (int k = 0; k < steps; ++k)
+                    mma_i8(tmem, da + (k >> 2) * (SCORE_BLOCKS * 128 >> 4) + 2 * (k & 3), db + (k >> 2) * (z.n * 128 >> 4) + 2 * (k & 3), idesc, k > 0);
+                mma_commit(s_bar);
+            }
+            __syncwarp();
+            ok = warp_wait(s_bar, parity, &abort_s, p.status) && ok;
+            parity ^= 1;
+            tmem_after();
+            // dot * 2^(f - 64), the largest of a token's heads, * 2^(e + 64): exact, beyond the type's range only where the score is
+            const float m1 = power_of_two(e < 0 ? e + 64 : 64), m2 = power_of_two(e < 0 ? 0 : e);
+            const int block = first + m * SCORE_BLOCKS + threadIdx.x;
+            uint32_t *dst = p.keys + ((long long)list_of_tile * p.H + head) * p.pitch + block;
+            for (int c0 = 0; c0 < rows; c0 += 32) {
+                float x[32];
+                tmem_ld32(tmem + ((uint32_t)(warp * 32) << 16) + c0, x);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    const float4 u = *reinterpret_cast<const float4 *>(units_s + c0 + i);
+                    x[i] = (float)__float_as_int(x[i]) * u.x;
+                    x[i + 1] = (float)__float_as_int(x[i + 1]) * u.y;
+                    x[i + 2] = (float)__float_as_int(x[i + 2]) * u.z;
+                    x[i + 3] = (float)__float_as_int(x[i + 3]) * u.w;
+                }
+#pragma unroll
+                for (int t = 0; t < 32 >> HP; ++t) {
+                    float best = x[t << HP];
+#pragma unroll
+                    for (int i = 1; i < 1 << HP; ++i) best = fmaxf(best, x[(t << HP) + i]);
+                    const int row = row0 + c0 + (t << HP), tok = HP == 5 ? row / rows_token : row >> HP;
+                    if (row < rows_all && block < total) {
+                        uint32_t &at = dst[(long long)tok * p.H * p.pitch];
+                        const uint32_t k = ordered(best * m1 * m2);
+                        at = HP == 5 && row % rows_token ? max(at, k) : k;  // a token of more than 32 heads: this thread has written `at`
+                    }
+                }
+            }
+            tmem_before();
+            __syncthreads();  // sums and codes have been read
+            tmem_after();
+            if (m + 1 < m_tiles && z.buffers == 1) {
+                rec = record_of(m + 1);
+                issue(m + 1, rec);
+            }
+        }
+    }
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_s), "r"(z.n));
+}
+
+// A list from its scores: the first `sink`, the last `recent`, the best others.
+template <int WARPS>
+__global__ void __launch_bounds__(WARPS * 32)
+    pick_blocks_kernel(const __grid_constant__ SelectParams p, const __grid_constant__ SmallSeqs small, int room) {
+    extern __shared__ __align__(16) uint32_t keys_s[];
+    __shared__ __align__(16) uint32_t hist[4][256];
+    __shared__ uint32_t range_s[2], counts_s[WARPS][2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int token = blockIdx.x / p.H, head = blockIdx.x - token * p.H;  // tokens of this launch
+    const AttnSeq *seqs = p.seqs ? p.seqs : small.e;
+    int lo = 0, hi = p.n - 1;  // record of the token
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (seqs[mid].tok0 <= token) lo = mid; else hi = mid - 1;
+    }
+    const AttnSeq s = seqs[lo];
+    const int j = token - s.tok0, total = (s.key0 + j) / p.BS + 1;
+    for (int i = threadIdx.x; i < 4 * 256; i += WARPS * 32) hist[0][i] = 0;
+    if (threadIdx.x == 0) {
+        range_s[0] = 0xffffffffu;
+        range_s[1] = 0;
+    }
+    const uint32_t *keys = p.keys + (long long)blockIdx.x * p.pitch;
+    int *out = p.blocks + ((long long)(s.row0 + j) * p.H + head) * p.keep;
+    float *out_s = p.scores ? p.scores + ((long long)(s.row0 + j) * p.H + head) * p.keep : nullptr;
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the scores are written
+    const bool all = total <= p.keep;
+    const int m0 = min(p.sink, total), m1 = max(m0, total - p.recent);  // the middle
+    int want = p.keep - p.sink - p.recent;
+    uint32_t least = 0;
+    bool from = true;  // the threshold's equals are taken whole
+    __syncthreads();
+    if (!all && want > 0) {
+        uint32_t a = 0xffffffffu, b = 0;
+        const bool stay = total <= room;
+        for (int i = threadIdx.x * 4; i < total; i += WARPS * 128) {
+            const uint4 v = __ldcg(reinterpret_cast<const uint4 *>(keys + i));
+            if (stay) *reinterpret_cast<uint4 *>(keys_s + i) = v;
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e >= m0 && i + e < m1) {
+                    a = min(a, w[e]);
+                    b = max(b, w[e]);
+                }
+        }
+        a = __reduce_min_sync(0xffffffffu, a);
+        b = __reduce_max_sync(0xffffffffu, b);
+        if (lane == 0) {
+            atomicMin(&range_s[0], a);
+            atomicMax(&range_s[1], b);
         }
         __syncthreads();
-        auto multiply = [&](int m, const Codes &x) {
-            const float e[2] = {power_of_two(x.e[0]), power_of_two(x.e[1])};
-            const int i0 = m * 16 + g;
-            const bool in[2] = {i0 < count, i0 + 8 < count};
-            for (int n0 = 0; n0 < rows; n0 += NT * 8) {
-                int c[NT][4];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0;
-                    if (n0 + nt * 8 < rows) {
-                        const unsigned char *src = codes + (n0 + nt * 8 + g) * z.stride + t4 * 16;
-#pragma unroll
-                        for (int sp = 0; sp < SPANS; ++sp) {
-                            const uint4 b = *reinterpret_cast<const uint4 *>(src + sp * 64);
-                            mma_s8(c[nt], x.a[sp][0].x, x.a[sp][1].x, x.a[sp][0].y, x.a[sp][1].y, b.x, b.y);
-                            mma_s8(c[nt], x.a[sp][0].z, x.a[sp][1].z, x.a[sp][0].w, x.a[sp][1].w, b.z, b.w);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int r = n0 + nt * 8 + 2 * t4;  // this lane's rows: r, r + 1
-                    if (n0 + nt * 8 >= rows) break;
-                    // dot * 2^e * 2^f, the smaller power first: exact, and beyond the type's range only where the score is
-                    const float2 f = *reinterpret_cast<const float2 *>(units_s + r);
-                    float v[2][2];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        v[h][0] = (float)c[nt][2 * h] * fminf(e[h], f.x) * fmaxf(e[h], f.x);
-                        v[h][1] = (float)c[nt][2 * h + 1] * fminf(e[h], f.y) * fmaxf(e[h], f.y);
-                    }
-                    auto put = [&](int list, int h, float score) {
-                        if (list < z.tile && in[h]) {
-                            uint32_t k = ordered(score);
-                            uint32_t &at = key_at(list, i0 + 8 * h);
-                            if (z.heads_p > 8 && (row0 + n0 + nt * 8) % z.heads_p) k = max(k, at);  // a token's later rows
-                            at = k;
-                            least_k = min(least_k, k);
-                            most_k = max(most_k, k);
-                        }
-                    };
-                    const int list = z.heads_p > 8 ? (row0 + n0 + nt * 8) / z.heads_p : (row0 + r) >> hp_shift;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (hp_shift == 0) {
-                            put(list, h, v[h][0]);
-                            put(list + 1, h, v[h][1]);
-                            continue;
-                        }
-                        float best = fmaxf(v[h][0], v[h][1]);
-                        if (hp_shift >= 2) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
-                        if (hp_shift >= 3) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2));
-                        if ((2 * t4 & ((1 << hp_shift) - 1)) == 0) put(list, h, best);
-                    }
-                }
-            }
-        };
-        for (int m = warp; m * 16 < count; m += SELECT_WARPS) {
-            if (AHEAD) {  // two m-tiles a round, so that no codes have to be moved from where they were loaded to
-                fetch(id, odd);
-                id = id_of(m + 2 * SELECT_WARPS);
-                multiply(m, even);
-                m += SELECT_WARPS;
-                if (m * 16 >= count) break;
-                fetch(id, even);
-                id = id_of(m + 2 * SELECT_WARPS);
-                multiply(m, odd);
-            } else {
-                fetch(id, even);
-                id = id_of(m + SELECT_WARPS);
-                multiply(m, even);
-            }
-        }
-    }
-    least_k = __reduce_min_sync(0xffffffffu, least_k);
-    most_k = __reduce_max_sync(0xffffffffu, most_k);
-    if (lane == 0) {
-        atomicMin(&range_s[0], least_k);
-        atomicMax(&range_s[1], most_k);
-    }
-    sync_all();
-
-    // ---- selection: a list is looked after by `team` warps, each with a piece of the CTA's stretch.  The leading bits that all scores
-    // have in common are skipped; then eight bits a pass.  want_s: -1 every block is taken; -2 those from prefix_s on; 0 none of the
-    // middle; else those above prefix_s and so many of those equal to it.
-    const int team = max(1, SELECT_WARPS / z.tile), wl = warp % team, lists_at_once = SELECT_WARPS / team;
-    const int piece = ((count + team - 1) / team + 31) / 32 * 32, i0 = min(wl * piece, count), i1 = min(i0 + piece, count);
-    if (z.ctas > 1) {
-        uint2 r = make_uint2(0xffffffffu, 0);
-        if (lane < z.ctas) r = peer_pair(peer_addr((uint32_t)__cvta_generic_to_shared(range_s), lane));
-        least_k = __reduce_min_sync(0xffffffffu, r.x);
-        most_k = __reduce_max_sync(0xffffffffu, r.y);
-    } else {
-        least_k = range_s[0];
-        most_k = range_s[1];
-    }
-    int shift = 32 - __clz(least_k ^ most_k);  // bits that are not decided
-    const uint32_t common = shift == 32 ? 0 : least_k >> shift << shift;
-    for (int pass = 0; shift > 0; ++pass) {
-        const int width = min(shift, 8);
-        shift -= width;
-        uint32_t *now = hist + (pass & 1) * z.tile * 256, *next = hist + (~pass & 1) * z.tile * 256;
-        bool any = false;
-        for (int list = 0; list < tokens; ++list) any |= want_s[list] > 0;
-        if (!any) break;  // the same in all CTAs of the cluster
-        for (int list = warp / team; list < tokens; list += lists_at_once) {
-            if (want_s[list] <= 0) continue;
-            const uint32_t prefix = (common | prefix_s[list]) >> shift >> width, mask = (1u << width) - 1;
-            const int lo = max(i0, p.sink - b0), hi = min(i1, last_s[list] + 1 - p.recent - b0);
-            for (int i = lo + lane; i < hi; i += 128) {
+        if (stay) keys = keys_s;
+        a = range_s[0];
+        b = range_s[1];
+        int shift = 32 - __clz(a ^ b);  // bits that are not decided
+        least = shift == 32 ? 0 : a >> shift << shift;
+        from = false;
+        for (int pass = 0; shift > 0 && !from; ++pass) {
+            const int width = min(shift, 8);
+            shift -= width;
+            const uint32_t prefix = least >> shift >> width, mask = (1u << width) - 1;
+            for (int i = m0 + (int)threadIdx.x; i < m1; i += WARPS * 128) {
                 uint32_t k[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) k[e] = i + 32 * e < hi ? key_at(list, i + 32 * e) : 0;
+                for (int e = 0; e < 4; ++e) k[e] = i + e * WARPS * 32 < m1 ? keys[i + e * WARPS * 32] : 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (i + 32 * e < hi && k[e] >> shift >> width == prefix) atomicAdd(now + list * 256 + (k[e] >> shift & mask), 1u);
+                    if (i + e * WARPS * 32 < m1 && k[e] >> shift >> width == prefix) atomicAdd(&hist[pass][k[e] >> shift & mask], 1u);
             }
-        }
-        sync_all();
-        for (int i = threadIdx.x; i < z.tile * 256; i += SELECT_WARPS * 32) next[i] = 0;
-        for (int list = warp / team; list < tokens; list += lists_at_once) {
-            const int want = want_s[list];
-            if (want <= 0 || wl) continue;
-            uint32_t n[8], before[8];  // in all CTAs, in those with earlier stretches
-            const uint32_t at = (uint32_t)__cvta_generic_to_shared(now + list * 256 + lane * 8);
+            __syncthreads();
+            // every warp looks for the digit: a lane sees eight of them
+            const uint4 h0 = *reinterpret_cast<const uint4 *>(&hist[pass][lane * 8]), h1 = *reinterpret_cast<const uint4 *>(&hist[pass][lane * 8 + 4]);
+            const uint32_t n[8] = {h0.x, h0.y, h0.z, h0.w, h1.x, h1.y, h1.z, h1.w};
+            uint32_t mine = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) n[i] = before[i] = 0;
-            if (z.ctas > 1) {
-                uint4 v[8][2];  // all under way at once
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    if (c < z.ctas) {
-                        const uint32_t there = peer_addr(at, c);
-                        v[c][0] = peer_words(there);
-                        v[c][1] = peer_words(there + 16);
-                    }
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    if (c >= z.ctas) break;
-                    const uint32_t w[8] = {v[c][0].x, v[c][0].y, v[c][0].z, v[c][0].w, v[c][1].x, v[c][1].y, v[c][1].z, v[c][1].w};
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        n[i] += w[i];
-                        if (c < cta) before[i] += w[i];
-                    }
-                }
-            } else {
-                const uint4 a = lds16(at), b = lds16(at + 16);
-                n[0] = a.x; n[1] = a.y; n[2] = a.z; n[3] = a.w;
-                n[4] = b.x; n[5] = b.y; n[6] = b.z; n[7] = b.w;
-            }
-            uint32_t mine = 0, mine_before = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                mine += n[i];
-                mine_before += before[i];
-            }
-            uint32_t above = mine, above_before = mine_before;  // of this lane's digits and larger ones
+            for (int i = 0; i < 8; ++i) mine += n[i];
+            uint32_t above = mine;  // of this lane's digits and larger ones
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
-                const uint32_t v = __shfl_down_sync(0xffffffffu, above, d), w = __shfl_down_sync(0xffffffffu, above_before, d);
-                if (lane + d < 32) {
-                    above += v;
-                    above_before += w;
-                }
+                const uint32_t v = __shfl_down_sync(0xffffffffu, above, d);
+                if (lane + d < 32) above += v;
             }
             above -= mine;
-            above_before -= mine_before;
-            if ((int)above < want && want <= (int)(above + mine)) {  // one lane
-                uint32_t left = (uint32_t)want - above, here = 0, here_before = 0;
-                int digit = 7;
+            const bool here = (int)above < want && want <= (int)(above + mine);  // one lane
+            int left = want - (int)above, digit = 7, equal = 0;
 #pragma unroll
-                for (int i = 7; i >= 0; --i) {
-                    if (digit == i && left > n[i]) {
-                        left -= n[i];
-                        above_before += before[i];
-                        digit = i - 1;
-                    }
-                    if (digit == i) {
-                        here = n[i];
-                        here_before = before[i];
-                    }
+            for (int i = 7; i >= 0; --i) {
+                if (digit == i && left > (int)n[i]) {
+                    left -= (int)n[i];
+                    digit = i - 1;
                 }
-                prefix_s[list] |= common | (uint32_t)(lane * 8 + digit) << shift;
-                // all with these bits are taken: the threshold is the smallest number with them
-                want_s[list] = here == left ? -2 : (int)left;
-                before_s[list][0] += above_before + (here == left ? here_before : 0);
-                before_s[list][1] = here_before;
+                if (digit == i) equal = (int)n[i];
             }
+            const int who = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+            want = __shfl_sync(0xffffffffu, left, who);
+            least |= (uint32_t)__shfl_sync(0xffffffffu, lane * 8 + digit, who) << shift;
+            from = __shfl_sync(0xffffffffu, equal, who) == want;  // all with these bits are taken
         }
-        __syncthreads();
     }
-    // nobody reads this CTA's memory any more once all have come here; they need not wait for its lists
-    if (z.ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    struct Rule {
-        int first, end, want, last;  // of the middle, within the stretch
-        uint32_t least;
-    };
-    auto rule_of = [&](int list) {
-        const int last = last_s[list], want = want_s[list];
-        Rule r{p.sink - b0, last + 1 - p.recent - b0, want, last - b0, common | prefix_s[list]};
-        if (want == -1) r.end = -0x7fffffff;  // everything counts as first or last
-        return r;
-    };
-    auto kind_of = [&](const Rule &r, int list, int i, bool &tie) -> bool {  // certainly taken
+    // a warp's piece of the context: how many it takes, then which.  `from`: scores from `least` on, else those above it and the first `want`
+    // of its equals
+    const int piece = ((total + WARPS - 1) / WARPS + 31) / 32 * 32, i0 = min(warp * piece, total), i1 = min(i0 + piece, total);
+    const bool none = !all && p.keep == p.sink + p.recent;
+    auto kind_of = [&](int i, bool &tie) -> bool {  // certainly taken
         tie = false;
-        if (i > r.last) return false;
-        if (i < r.first || i >= r.end) return true;
-        const uint32_t k = key_at(list, i);
-        if (r.want == -2) return k >= r.least;
-        tie = r.want > 0 && k == r.least;
-        return r.want > 0 && k > r.least;
+        if (all || i < m0 || i >= m1) return true;
+        if (none) return false;
+        const uint32_t k = keys[i];
+        tie = !from && k == least;
+        return from ? k >= least : k > least;
     };
-    if (team > 1) {  // a warp's piece comes behind those of the warps before it
-        const int list = warp / team;
-        uint32_t sure = 0, ties = 0;
-        if (list < tokens) {
-            const Rule rule = rule_of(list);
-            for (int i = i0 + lane; i < i1; i += 32) {
-                bool tie;
-                sure += kind_of(rule, list, i, tie);
-                ties += tie;
-            }
+    uint32_t sure = 0, ties = 0;
+    if (!all) {
+        for (int i = i0 + lane; i < i1; i += 32) {
+            bool tie;
+            sure += kind_of(i, tie);
+            ties += tie;
         }
         sure = __reduce_add_sync(0xffffffffu, sure);
         ties = __reduce_add_sync(0xffffffffu, ties);
@@ -391,92 +317,92 @@ __global__ void __launch_bounds__(SELECT_WARPS * 32, 2)
             counts_s[warp][1] = ties;
         }
         __syncthreads();
-    }
-    for (int list = warp / team; list < tokens; list += lists_at_once) {
-        const Rule rule = rule_of(list);
-        const int ties_taken = max(rule.want, 0), own = last_s[list];
-        // taken in earlier stretches: all of them, or the first, the last and those above the threshold
-        uint32_t sure = rule.want == -1 ? (uint32_t)min(b0, own + 1)
-                                        : (uint32_t)(min(b0, p.sink) + max(0, min(b0, own + 1) - (own + 1 - p.recent))) + before_s[list][0];
-        uint32_t ties = before_s[list][1];
-        if (least_k == most_k) ties = max(0, min(b0, own + 1 - p.recent) - p.sink);  // no pass: the middle is all equal
-        if (rule.want <= 0) ties = 0;
-        for (int w = 0; w < wl; ++w) {
-            sure += counts_s[warp - wl + w][0];
-            ties += counts_s[warp - wl + w][1];
+        sure = ties = 0;
+        for (int w = 0; w < warp; ++w) {
+            sure += counts_s[w][0];
+            ties += counts_s[w][1];
         }
-        const long long at0 = ((long long)(s.row0 + j0 + list) * p.H + head) * p.keep;
-        for (int base = i0; base < i1; base += 32) {
-            const int i = base + lane;
-            bool tie = false;
-            const bool certain = i < i1 && kind_of(rule, list, i, tie);
-            const unsigned cm = __ballot_sync(0xffffffffu, certain), tm = __ballot_sync(0xffffffffu, tie), under = (1u << lane) - 1;
-            const int ties_before = (int)ties + __popc(tm & under);
-            if (certain || (tie && ties_before < ties_taken)) {
-                const int to = (int)sure + __popc(cm & under) + min(ties_before, ties_taken);
-                p.blocks[at0 + to] = b0 + i;
-                if (p.scores) p.scores[at0 + to] = from_ordered(key_at(list, i));
-            }
-            sure += __popc(cm);
-            ties += __popc(tm);
-        }
-        if (cta == 0)
-            for (int i = min(p.keep, own + 1) + wl * 32 + lane; i < p.keep; i += team * 32) {
-                p.blocks[at0 + i] = -1;
-                if (p.scores) p.scores[at0 + i] = -CUDART_INF_F;
-            }
+    } else {
+        sure = i0;
     }
-    if (z.ctas > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    for (int base = i0; base < i1; base += 32) {
+        const int i = base + lane;
+        bool tie = false;
+        const bool certain = i < i1 && kind_of(i, tie);
+        const unsigned cm = __ballot_sync(0xffffffffu, certain), tm = __ballot_sync(0xffffffffu, tie), under = (1u << lane) - 1;
+        const int ties_before = (int)ties + __popc(tm & under);
+        if (certain || (tie && ties_before < want)) {
+            const int to = (int)sure + __popc(cm & under) + min(ties_before, from ? 0 : want);
+            out[to] = i;
+            if (out_s) out_s[to] = from_ordered(keys[i]);
+        }
+        sure += __popc(cm);
+        ties += __popc(tm);
+    }
+    for (int i = min(p.keep, total) + (int)threadIdx.x; i < p.keep; i += WARPS * 32) {
+        out[i] = -1;
+        if (out_s) out_s[i] = -CUDART_INF_F;
+    }
 }
 
-static size_t select_smem(const SelectShape &z) { return (size_t)z.tile * z.room * 4 + (size_t)2 * z.tile * 256 * 4 + (size_t)z.rows * z.stride; }
-constexpr size_t SELECT_SMEM = 220 * 1024;
+static size_t score_smem(const SelectShape &z) { return (size_t)z.slabs * 128 * (z.buffers * SCORE_BLOCKS + z.n) + 1024; }
+constexpr int SCORE_SMEM = (4 * 128 * (2 * SCORE_BLOCKS + SELECT_ROWS)) + 1024;
 
-// How a batch is cut: tokens of a tile, CTAs of a cluster.
-SelectShape select_shape(const SelectParams &p, int max_nq, long long tokens, int sm_count, int f16) {
+// How a batch is cut.  Rows of a tile: 32 where there is a token each (the sums' columns that a thread reads at once), else as many as
+// the tokens fill, up to SELECT_ROWS.  A CTA takes several m-tiles in turn, so that its rows' codes are made once, where that leaves four
+// CTAs an SM.
+SelectShape select_shape(const SelectParams &p, int max_nq, long long m_tiles, int sm_count, int f16) {
     SelectShape z{};
     z.f16 = f16;
-    z.heads_p = p.G > 8 ? (p.G + 7) / 8 * 8 : (p.G > 4 ? 8 : (p.G > 2 ? 4 : p.G));
-    const int spans = p.D <= 64 ? 2 : (p.D <= 128 ? 4 : 8);
-    z.stride = spans * 64 + 64;
-    for (z.tile = 1; z.tile < SELECT_TOKENS && z.tile < max_nq && 2 * z.tile * z.heads_p <= SELECT_ROWS; z.tile *= 2) {}
-    for (;;) {
-        z.rows = std::min((z.tile * z.heads_p + 7) / 8 * 8, SELECT_ROWS);
-        const long long units = (tokens + z.tile - 1) / z.tile * p.H;
-        for (z.ctas = 1;; z.ctas *= 2) {
-            z.room = ((p.widest + z.ctas - 1) / z.ctas + 15) / 16 * 16;
-            if (z.ctas == 8) break;
-            const bool fits = select_smem(z) <= SELECT_SMEM / 2;  // two CTAs an SM
-            if (fits && (units * z.ctas * 2 > 2ll * sm_count || z.room <= 256)) break;
-        }
-        if (z.tile == 1 || select_smem(z) <= SELECT_SMEM) return z;
-        z.tile /= 2;
-    }
+    z.heads_p = p.G > 32 ? (p.G + 31) / 32 * 32 : 1;
+    while (z.heads_p < p.G) z.heads_p *= 2;
+    for (z.n = 32; z.n < SELECT_ROWS && z.n < max_nq * z.heads_p; z.n *= 2) {}
+    z.tile = std::max(1, z.n / z.heads_p);
+    z.slabs = (2 * p.D + 127) / 128;
+    z.reps = (int)std::max<long long>(1, std::min<long long>(8, m_tiles * p.H / z.tile / (4ll * sm_count)));
+    if (max_nq == 1) z.reps = 1;
+    z.buffers = z.reps > 1 ? 2 : 1;
+    return z;
 }
 
-template <int SPANS, int NT> static cudaError_t select_go(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, cudaStream_t st) {
+template <int HP> static cudaError_t score_go(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, cudaStream_t st) {
     static SmemSeen seen{0};
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(select_blocks_kernel<SPANS, NT>), (int)SELECT_SMEM, &seen);
+    const cudaError_t e = allow_smem(reinterpret_cast<const void *>(score_blocks_kernel<HP>), SCORE_SMEM, &seen);
     if (e != cudaSuccess) return e;
-    cudaLaunchAttribute cluster;
-    cluster.id = cudaLaunchAttributeClusterDimension;
-    cluster.val.clusterDim.x = (unsigned)z.ctas;
-    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    score_blocks_kernel<HP><<<(unsigned)(units * p.H), SCORE_THREADS, score_smem(z), st>>>(p, small, z);
+    return cudaGetLastError();
+}
+template <int WARPS> static cudaError_t pick_go(const SelectParams &p, const SmallSeqs &small, long long tokens, cudaStream_t st) {
+    // launched so that its CTAs come up while the scores are still being computed; it waits for them itself
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(units * p.H * z.ctas));
-    cfg.blockDim = dim3(SELECT_WARPS * 32);
-    cfg.dynamicSmemBytes = select_smem(z);
+    cfg.gridDim = dim3((unsigned)(tokens * p.H));
+    cfg.blockDim = dim3(WARPS * 32);
+    const int room = p.widest <= PICK_KEYS ? (p.widest + 3) / 4 * 4 : 0;
+    cfg.dynamicSmemBytes = (size_t)room * 4;
     cfg.stream = st;
-    cfg.attrs = &cluster;
-    cfg.numAttrs = z.ctas > 1 ? 1 : 0;
-    e = cudaLaunchKernelEx(&cfg, select_blocks_kernel<SPANS, NT>, p, small, z);
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    static SmemSeen seen{0};
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(pick_blocks_kernel<WARPS>), PICK_KEYS * 4, &seen);
+    if (e != cudaSuccess) return e;
+    e = cudaLaunchKernelEx(&cfg, pick_blocks_kernel<WARPS>, p, small, room);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
-template <int SPANS> static cudaError_t select_rows(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, cudaStream_t st) {
-    return z.rows <= 8 ? select_go<SPANS, 1>(p, small, z, units, st) : (z.rows <= 16 ? select_go<SPANS, 2>(p, small, z, units, st) : select_go<SPANS, 4>(p, small, z, units, st));
-}
-cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, cudaStream_t st) {
-    return p.D <= 64 ? select_rows<2>(p, small, z, units, st) : (p.D <= 128 ? select_rows<4>(p, small, z, units, st) : select_rows<8>(p, small, z, units, st));
+cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, long long tokens, cudaStream_t st) {
+    cudaError_t e;
+    switch (log2_up(std::min(z.heads_p, 32))) {
+        case 0: e = score_go<0>(p, small, z, units, st); break;
+        case 1: e = score_go<1>(p, small, z, units, st); break;
+        case 2: e = score_go<2>(p, small, z, units, st); break;
+        case 3: e = score_go<3>(p, small, z, units, st); break;
+        case 4: e = score_go<4>(p, small, z, units, st); break;
+        default: e = score_go<5>(p, small, z, units, st); break;
+    }
+    if (e != cudaSuccess) return e;
+    return p.widest <= 1024 ? pick_go<4>(p, small, tokens, st) : pick_go<PICK_WARPS>(p, small, tokens, st);
 }
 
 }  // namespace aafkv

@@ -86,9 +86,10 @@ int aaf_kv_summarize(aaf_kv_pool *p, int32_t layer, int32_t dtype, int32_t n, co
 
 int aaf_kv_select(aaf_kv_pool *p, int32_t layer, const aaf_kv_select_desc *d, int32_t n, const aaf_ctx_t *ctxs, const int32_t *n_q,
                   const void *q_dev, const void *summary_dev, size_t summary_bytes, int32_t *blocks_dev, float *scores_dev,
-                  void *stream) try {
+                  void *workspace_dev, size_t workspace_bytes, void *stream) try {
     AAF_RANGE("aaf_kv_select");
-    if (!p || !d || d->struct_size != sizeof(aaf_kv_select_desc) || n < 1 || !ctxs || !aligned16(q_dev) || !aligned16(summary_dev))
+    if (!p || !d || d->struct_size != sizeof(aaf_kv_select_desc) || n < 1 || !ctxs || !aligned16(q_dev) || !aligned16(summary_dev) ||
+        !aligned16(workspace_dev))
         return AAF_ERR_INVALID_ARG;
     if (!blocks_dev || ((reinterpret_cast<uintptr_t>(blocks_dev) | reinterpret_cast<uintptr_t>(scores_dev)) & 3u)) return AAF_ERR_INVALID_ARG;
     if (p->broken) return AAF_ERR_CUDA;
@@ -97,43 +98,75 @@ int aaf_kv_select(aaf_kv_pool *p, int32_t layer, const aaf_kv_select_desc *d, in
     if (d->n_q_heads < 1 || d->n_q_heads % p->g.H != 0 || (long long)d->n_q_heads * p->g.D >= 1ll << 31) return AAF_ERR_INVALID_ARG;
     if (d->q_stride % 8 != 0 || d->q_stride < (long long)d->n_q_heads * p->g.D) return AAF_ERR_INVALID_ARG;
     if (d->keep < 1 || d->keep > AAF_LIST_MAX_BLOCKS || d->sink < 0 || d->recent < 1 || d->sink > d->keep - d->recent) return AAF_ERR_INVALID_ARG;
-    if (summary_bytes < summary_size(p)) return AAF_ERR_DST_TOO_SMALL;
+    if (summary_bytes < summary_size(p) || workspace_bytes < attend_ws_bytes(p)) return AAF_ERR_DST_TOO_SMALL;
     std::vector<AttnSeq> rec;
-    long long total = 0;
+    long long total = 0, m_tiles = 0;
     const int rc = batch_records(p, n, ctxs, n_q, false, rec, &total);
     if (rc != AAF_OK) return rc;
     SelectParams k{};
     int max_nq = 1;
     for (const AttnSeq &s : rec) {
-        k.widest = std::max(k.widest, (s.len + p->g.BS - 1) / p->g.BS);
+        const int blocks = (s.len + p->g.BS - 1) / p->g.BS;
+        k.widest = std::max(k.widest, blocks);
         max_nq = std::max(max_nq, s.nq);
+        m_tiles += (blocks + 127ll) / 128 * s.nq;
     }
-    if (k.widest > AAF_SELECT_MAX_BLOCKS) return AAF_ERR_TOO_LONG;
-    DeviceGuard guard(p->device);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (capturing(st)) return AAF_ERR_INVALID_ARG;
+    // the scores of so many tokens fit into the workspace at a time
+    k.pitch = (k.widest + 3) / 4 * 4;
+    const long long at_once = (long long)(attend_ws_bytes(p) / 4) / (k.pitch * p->g.H);
+    if (at_once < 1) return AAF_ERR_TOO_LONG;
     k.q = q_dev;
     k.tables = p->s.tables;
     k.record = record_of(p);
     k.summary = static_cast<const signed char *>(summary_dev) + (long long)layer * p->g.NB * k.record;
+    k.keys = static_cast<uint32_t *>(workspace_dev);
     k.blocks = blocks_dev;
     k.scores = scores_dev;
+    k.status = &p->s.ctl->status;
     k.q_stride = d->q_stride;
     k.max_blk = p->g.max_blk; k.BS = p->g.BS; k.H = p->g.H; k.G = d->n_q_heads / p->g.H; k.D = p->g.D;
-    k.n = n; k.keep = d->keep; k.sink = d->sink; k.recent = d->recent;
-    const SelectShape z = select_shape(k, max_nq, total, p->sm_count, d->dtype == AAF_DTYPE_F16);
-    std::stable_sort(rec.begin(), rec.end(), [](const AttnSeq &x, const AttnSeq &y) { return x.len > y.len; });  // the longest first
-    long long units = 0;
-    for (AttnSeq &s : rec) {
-        s.unit0 = (int)units;
-        units += (s.nq + z.tile - 1) / z.tile;
-    }
-    if (units * p->g.H * z.ctas > (1ll << 31) - 1) return AAF_ERR_TOO_MANY;
+    k.keep = d->keep; k.sink = d->sink; k.recent = d->recent;
+    const SelectShape z = select_shape(k, max_nq, m_tiles, p->sm_count, d->dtype == AAF_DTYPE_F16);
+    if (std::min(at_once, total) * p->g.H > (1ll << 31) - 1) return AAF_ERR_TOO_MANY;
+    // what one launch takes: `units` CTAs a head, `tokens` lists a head
+    struct Launch {
+        size_t first, end;
+        long long units, tokens;
+    };
+    std::vector<AttnSeq> parts;
+    std::vector<Launch> launches;
+    for (const AttnSeq &s : rec)
+        for (int j = 0; j < s.nq;) {
+            if (launches.empty() || launches.back().tokens == at_once || (long long)(launches.back().end - launches.back().first) == p->lay.max_batch)
+                launches.push_back(Launch{parts.size(), parts.size(), 0, 0});
+            Launch &l = launches.back();
+            AttnSeq x = s;
+            x.nq = (int)std::min<long long>(s.nq - j, at_once - l.tokens);
+            x.row0 = s.row0 + j;
+            x.key0 = s.len - s.nq + j;
+            x.tok0 = (int)l.tokens;
+            x.unit0 = (int)l.units;
+            x.nsplit = ((x.key0 + x.nq - 1) / p->g.BS + 128 * z.reps) / (128 * z.reps);
+            l.units += (long long)((x.nq + z.tile - 1) / z.tile) * x.nsplit;
+            l.tokens += x.nq;
+            l.end += 1;
+            if (l.units * p->g.H > (1ll << 31) - 1) return AAF_ERR_TOO_MANY;
+            parts.push_back(x);
+            j += x.nq;
+        }
+    DeviceGuard guard(p->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (capturing(st)) return AAF_ERR_INVALID_ARG;
     p->last_stream = st;
     if (!begin_read(p, ctxs, n, st)) return broke(p);
-    SmallSeqs small;
-    const bool ok = place_records(p, rec, small, &k.seqs, 0, st) &&
-                    launch_select_blocks(k, small, z, units, st) == cudaSuccess;
+    bool ok = true;
+    for (size_t i = 0; i < launches.size() && ok; ++i) {
+        const Launch &l = launches[i];
+        const std::vector<AttnSeq> part(parts.begin() + (ptrdiff_t)l.first, parts.begin() + (ptrdiff_t)l.end);
+        SmallSeqs small;
+        k.n = (int)part.size();
+        ok = place_records(p, part, small, &k.seqs, 0, st) && launch_select_blocks(k, small, z, l.units, l.tokens, st) == cudaSuccess;
+    }
     return ok && end_read(p, st) ? AAF_OK : broke(p);
 } catch (const std::bad_alloc &) {
     return AAF_ERR_INVALID_ARG;  // the host has no memory for the records; nothing was launched

@@ -21,23 +21,28 @@ struct SummaryParams {
 
 struct SelectParams {
     const void *q;
-    const AttnSeq *seqs;  // unit0: first unit (a tile of query tokens)
+    // Records: the tokens of a context that one launch takes.  nq: how many, row0: the first in the batch, key0: its position, tok0: its
+    // place in this launch; unit0: first unit (a tile of tokens and z.reps * 128 blocks), nsplit: units of a tile
+    const AttnSeq *seqs;
     const int *tables;
     const signed char *summary;  // the layer's first record
+    uint32_t *keys;       // scores, as numbers of the same order: [tokens of the launch][H][pitch]
     int *blocks;          // [query tokens][H][keep]
     float *scores;        // the same shape, may be null
+    int *status;
     long long q_stride;   // elements
     long long record;     // bytes
+    long long pitch;      // a multiple of 4
     int max_blk, BS, H, G, D, n, keep, sink, recent, widest;  // widest: blocks of the longest context
 };
-// How a batch is cut (see select_shape)
+constexpr int SELECT_ROWS = 128;  // of a pass over the summaries
 struct SelectShape {
     int tile;      // query tokens of a unit
-    int heads_p;   // rows of a token: the group's heads, repeated up to a power of two or a multiple of 8
-    int ctas;      // of a cluster
-    int room;      // blocks of a CTA's stretch at most
-    int stride;    // bytes from one row's codes to the next in shared memory
-    int rows;      // rows that are held at a time
+    int heads_p;   // rows of a token: the group's heads, repeated up to a power of two or a multiple of 32
+    int n;         // rows that are multiplied at a time
+    int slabs;     // 128-byte stretches of a head's codes
+    int reps;      // m-tiles of a CTA
+    int buffers;   // for their codes
     int f16;
 };
 
@@ -58,9 +63,15 @@ struct TablesParams {
     int max_blk, BS, n, cols, rows, tokens, total;
 };
 
+inline int log2_up(int v) {  // of a power of two
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return s;
+}
+
 cudaError_t launch_summarize(const SummaryParams &p, const SmallSeqs &small, int f16, cudaStream_t st);
-SelectShape select_shape(const SelectParams &p, int max_nq, long long tokens, int sm_count, int f16);
-cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, cudaStream_t st);
+SelectShape select_shape(const SelectParams &p, int max_nq, long long m_tiles, int sm_count, int f16);
+cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, long long tokens, cudaStream_t st);
 // p.first is not read; a record's nsplit parts of `chunk` listed keys (lists of `keep` blocks); units are (query token, part).
 // alone: CTAs of twice as many warps that have an SM to themselves
 cudaError_t launch_attend_blocks(const AttnParams &p, const SmallSeqs &small, int f16, bool alone, cudaStream_t st);

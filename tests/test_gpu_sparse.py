@@ -215,14 +215,27 @@ def test_select_long_contexts():
     check_select(pool, ctxs, [3, 2, 9], R.rand((14, 8, 64), 5), 100, 1, 4)
 
 
-def test_select_a_context_of_as_many_blocks_as_there_may_be():
-    most = B.AAF_SELECT_MAX_BLOCKS
-    pool = R.make_pool(1, 1, 8, 1, most + 3, max_ctx=4, max_blk=most + 2)
-    c = R.add_ctx(pool, most, 1)
-    q = R.rand((1, 1, 8), 2)
-    check_select(pool, [c], [1], q, 50, 1, 4)
+def test_select_more_blocks_than_shared_memory_holds_scores_of():
+    pool = R.make_pool(1, 2, 8, 1, 60000, max_ctx=4)
+    c = R.add_ctx(pool, 50001, 1)
+    check_select(pool, [c], [3], R.rand((3, 4, 8), 2), 700, 1, 4)
+
+
+def test_select_more_blocks_than_the_workspace_holds_scores_of():
+    most = 65536 * 10 // 4
+    pool = R.make_pool(1, 4, 8, 1, most + 600, max_ctx=4, max_blk=most + 10)
+    c, d = R.add_ctx(pool, most, 1), R.add_ctx(pool, 500, 2)
+    q = R.rand((5, 4, 8), 2)
+    check_select(pool, [c, d], [2, 3], q, 50, 1, 4)  # a token at a time
     assert pool.reserve([c.handle], [1])[0] == 0
-    assert pool.select(0, [c.handle], None, q, pool.new_summary(), 50)[0] == B.AAF_ERR_TOO_LONG
+    assert pool.select(0, [c.handle], None, q[:1], pool.new_summary(), 50)[0] == B.AAF_ERR_TOO_LONG
+
+
+def test_select_in_several_launches():
+    # so many tokens that their scores do not fit into the workspace at once; a context's tokens go to two of the launches
+    lens, n_q = [16 * 700 + 3, 16 * 600], [130, 90]
+    pool, ctxs = pool_of(8, 8, 16, lens)
+    check_select(pool, ctxs, n_q, R.rand((220, 8, 8), 5), 6, 1, 2)
 
 
 def test_select_many_sequences_strided_queries_and_no_scores():
@@ -521,7 +534,8 @@ def test_pools_without_summaries():
         one, room = (B.C.c_int32 * 1)(h), torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
         assert B.aaf_kv_summarize(pool.h, 0, 0, 1, one, None, room.data_ptr(), room.numel(), None) == B.AAF_ERR_INCOMPAT
         d = B.aaf_kv_select_desc(B.C.sizeof(B.aaf_kv_select_desc), 0, heads, 4, 1, 1, heads * dim)
-        assert B.aaf_kv_select(pool.h, 0, d, 1, one, None, room.data_ptr(), room.data_ptr(), room.numel(), room.data_ptr(), None, None) == B.AAF_ERR_INCOMPAT
+        assert B.aaf_kv_select(pool.h, 0, d, 1, one, None, room.data_ptr(), room.data_ptr(), room.numel(), room.data_ptr(), None, room.data_ptr(),
+                               room.numel(), None) == B.AAF_ERR_INCOMPAT
         st, got = pool.batch_tables([h])  # tables know nothing of elements
         assert st == 0 and got["tables"].tolist() == [pool.table(h).tolist()]
 
