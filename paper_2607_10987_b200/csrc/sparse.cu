@@ -126,7 +126,7 @@ int aaf_kv_select(aaf_kv_pool *p, int32_t layer, const aaf_kv_select_desc *d, in
     k.q_stride = d->q_stride;
     k.max_blk = p->g.max_blk; k.BS = p->g.BS; k.H = p->g.H; k.G = d->n_q_heads / p->g.H; k.D = p->g.D;
     k.keep = d->keep; k.sink = d->sink; k.recent = d->recent;
-    const SelectShape z = select_shape(k, max_nq, m_tiles, p->sm_count, d->dtype == AAF_DTYPE_F16);
+    const SelectShape z = select_shape(k, n, max_nq, m_tiles, p->sm_count, d->dtype == AAF_DTYPE_F16);
     if (std::min(at_once, total) * p->g.H > (1ll << 31) - 1) return AAF_ERR_TOO_MANY;
     // what one launch takes: `units` CTAs a head, `tokens` lists a head
     struct Launch {

@@ -188,6 +188,23 @@ def test_select_equal_scores_of_a_long_context(n_q):
     check_select(pool, [c], [n_q], q, 5000, 7, 5)
 
 
+def test_select_scores_from_minus_to_plus_infinity():
+    # products far beyond the type's range, both signs, and small ones: whole binades apart, many equal
+    rows = R.rand((1, 2, 4 * 1500, 1, 16), 3)
+    size = torch.randint(-100, 120, (1500,), device="cuda").repeat_interleave(4)
+    rows[0, 0] = torch.where(torch.rand(6000, 1, 1, device="cuda") < 0.3, 0.0, rows[0, 0].float().sign() * torch.exp2(size.float())[:, None, None])
+    rows[0, 0, 4000:5000] = -1e30
+    pool = R.make_pool(1, 1, 16, 4, 1600)
+    c = R.add_ctx(pool, 6000, 0, rows)
+    q = R.rand((4, 2, 16), 5).sign()
+    q[1] *= 1e30
+    q[2] *= 1e-30
+    q[3] = 1e30
+    _, summary = check_select(pool, [c], [4], q, 40, 1, 1)
+    for keep in (200, 700, 1100, 1499):
+        check_select(pool, [c], [4], q, keep, 1, 1, summary)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_select_odd_values(dtype):
     big, tiny = torch.finfo(dtype).max, torch.finfo(dtype).smallest_normal
