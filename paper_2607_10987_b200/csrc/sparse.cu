@@ -146,7 +146,7 @@ int aaf_kv_select(aaf_kv_pool *p, int32_t layer, const aaf_kv_select_desc *d, in
             x.key0 = s.len - s.nq + j;
             x.tok0 = (int)l.tokens;
             x.unit0 = (int)l.units;
-            x.nsplit = ((x.key0 + x.nq - 1) / p->g.BS + 128 * z.reps) / (128 * z.reps);
+            x.nsplit = (int)(((x.key0 + x.nq - 1) / p->g.BS + (long long)z.blocks * z.reps) / ((long long)z.blocks * z.reps));
             l.units += (long long)((x.nq + z.tile - 1) / z.tile) * x.nsplit;
             l.tokens += x.nq;
             l.end += 1;

@@ -13,6 +13,9 @@ __device__ __forceinline__ int code_exponent(float top) {
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
+// s if v = 2^s, else -1
+__device__ __forceinline__ int log2_exact(int v) { return v & (v - 1) ? -1 : 31 - __clz(v); }
+
 // Floats as unsigned numbers of the same order (no NaN).
 __device__ __forceinline__ uint32_t ordered(float x) {
     const uint32_t b = __float_as_uint(x);

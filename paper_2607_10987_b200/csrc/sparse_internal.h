@@ -43,6 +43,8 @@ struct SelectShape {
     int slabs;     // 128-byte stretches of a head's codes
     int reps;      // m-tiles of a CTA
     int buffers;   // for their codes
+    int together;  // all kv heads of some blocks make an m-tile
+    int blocks;    // of an m-tile
     int f16;
 };
 
