@@ -264,7 +264,7 @@ def aaf_kv_strerror(status): return _fn("aaf_kv_strerror")(status).decode()
 
 def _ints(v):
     """A list as a C array of int32 (through the buffer protocol: a ctypes array takes its entries one by one)."""
-    return C.byref(C.c_int32.from_buffer(array("i", v or (0,))))
+    return C.byref(C.c_int32.from_buffer(array("i", v if len(v) else (0,))))
 
 
 def make_desc(n_layers, n_kv_heads, head_dim, block_size, elt_bytes, n_blocks, max_ctx, max_blocks_per_ctx,

@@ -153,7 +153,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 5 : 3)
     const int rows_token = z.heads_p, rows_all = tokens * rows_token;
     const int list_of_tile = s.tok0 + j0, mine = threadIdx.x & (SCORE_BLOCKS - 1);
     const long long list_pitch = p.H * p.pitch;
-    bool ok = true;
     int parity = 0;
     const uint32_t idesc = 2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(z.n / 8) << 17 | (SCORE_BLOCKS / 16) << 24;
     // a pass takes z.n rows: one, but for groups of more heads than that
@@ -210,7 +209,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 5 : 3)
                 mma_commit(s_bar);
             }
             __syncwarp();
-            ok = warp_wait(s_bar, parity, &abort_s, p.status) && ok;
+            warp_wait(s_bar, parity, &abort_s, p.status);  // if it gives up, the status says so and the scores are void
             parity ^= 1;
             tmem_after();
             const int block = first + m * SCORE_BLOCKS + mine;
@@ -339,7 +338,7 @@ __global__ void __launch_bounds__(128, 5)
             mma_commit(s_bar);
         }
         __syncwarp();
-        warp_wait(s_bar, parity, &abort_s, p.status);
+        warp_wait(s_bar, parity, &abort_s, p.status);  // if it gives up, the status says so and the scores are void
         parity ^= 1;
         tmem_after();
         if (m + 2 < m_tiles) {  // into the buffer whose codes have been multiplied
