@@ -342,6 +342,7 @@ class KVPool:
             d.free_order = self._fo.ctypes.data_as(_p32)
         self.desc = d
         self._attend_ws = None  # scratch of attend, allocated by its first call
+        self._like = None       # empty tensors of int32 and int64 on the pool's device
         self.h = C.c_void_p()
         st = aaf_kv_pool_create(d, self.h)
         if st != AAF_OK:
@@ -652,13 +653,15 @@ class KVPool:
                 cols = out["tables"].shape[-1]
             else:
                 cols = max([-(-(self.ctx_len(c) or 0) // self.BS) for c in ctxs], default=0)
-        i32, i64, dev = torch.int32, torch.int64, self.device
+        i32, i64 = torch.int32, torch.int64
         if out is None:
             if rows < 0 or tokens < 0 or cols < 0:
                 return AAF_ERR_DST_TOO_SMALL, None
-            out = {"tables": torch.empty((rows, cols), dtype=i32, device=dev), "lens": torch.empty(rows, dtype=i32, device=dev),
-                   "offsets": torch.empty(rows + 1, dtype=i32, device=dev), "token_row": torch.empty(tokens, dtype=i32, device=dev),
-                   "positions": torch.empty(tokens, dtype=i64, device=dev), "slots": torch.empty(tokens, dtype=i64, device=dev)}
+            if self._like is None:  # new_empty of a tensor of the same kind is the cheapest allocation
+                self._like = torch.empty(0, dtype=i32, device=self.device), torch.empty(0, dtype=i64, device=self.device)
+            e32, e64 = self._like[0].new_empty, self._like[1].new_empty
+            out = {"tables": e32((rows, cols)), "lens": e32((rows,)), "offsets": e32((rows + 1,)), "token_row": e32((tokens,)),
+                   "positions": e64((tokens,)), "slots": e64((tokens,))}
             ptrs = [x.data_ptr() for x in out.values()]
         else:
             shapes = {"tables": (rows, cols), "lens": (rows,), "offsets": (rows + 1,), "token_row": (tokens,), "positions": (tokens,),

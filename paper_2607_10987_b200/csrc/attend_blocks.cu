@@ -12,21 +12,24 @@
 
 namespace aafkv {
 
-template <int DP> struct ListShape {
+// CTAS of WARPS warps share an SM, as many as registers allow (a warp by itself waits for most of its time: twelve warps of two stages are
+// ahead of eight of three); a CTA that has an SM to itself has the warps of all of them.
+template <int DP, int NT> struct ListShape {
     static constexpr int PIECES = DP / 8;           // 16-byte pieces of a row
     static constexpr int ROW = DP * 2, HALF = 16 * ROW;  // bytes of a row, of a tile of 16 keys (or values)
     static constexpr int STAGE_BYTES = 2 * HALF;
-    static constexpr int WARPS = DP <= 128 ? 4 : 3;  // of a CTA that shares the SM with another; twice as many of one that does not
-    static constexpr int STAGES = DP == 64 ? 6 : (DP == 128 ? 3 : 2);
+    static constexpr int WARPS = DP <= 128 ? 4 : 3, CTAS = NT > 1 || DP > 128 ? 2 : (DP == 128 ? 3 : 4);
+    static constexpr int STAGES = DP > 128 ? 2 : (NT > 1 ? 384 : 768 / CTAS) / DP;
     static constexpr int WARP_BYTES = STAGES * STAGE_BYTES;
-    static_assert(2 * (WARPS * WARP_BYTES + 2048) <= 228 * 1024, "shared memory of a CTA");
+    static_assert(CTAS * (WARPS * WARP_BYTES + 2048) <= 228 * 1024, "shared memory of a CTA");
 };
 
-// SIMPLE: neither cap nor bias, a score is a multiple of the product
-template <typename T, int DP, int NT, bool SIMPLE, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32, WARPS == ListShape<DP>::WARPS ? 2 : 1)
+// SIMPLE: neither cap nor bias, a score is a multiple of the product.  WHOLE: a tile of 16 tokens lies within a block (of a multiple of 16), so
+// that one list entry, one table entry and one address do for all of it; two in five instructions of a tile are the look-up of single tokens
+template <typename T, int DP, int NT, bool SIMPLE, bool WHOLE, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, WARPS == ListShape<DP, NT>::WARPS ? ListShape<DP, NT>::CTAS : 1)
     attend_blocks_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ SmallSeqs small, int row_groups) {
-    using S = ListShape<DP>;
+    using S = ListShape<DP, NT>;
     extern __shared__ __align__(16) char smem[];
     __shared__ float2 ml_s[WARPS][NT * 8];  // of a warp's rows: base of the exponents, sum
     static_assert(NT * 8 * DP * 4 <= S::WARP_BYTES, "a warp's results fit where its copies were");
@@ -75,37 +78,52 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == ListShape<DP>::WARPS ? 2 
     const int *table = p.tables + (long long)sq.ctx * p.max_blk;
     const char *kb = p.kbase + (long long)head * p.D * 2;
 
-    // lane l looks after the tile's token l % 16: its block's table position, then its position in the context (-1: not seen)
-    // and its block
+    // Lane l looks after the tile's token l % 16 (WHOLE: every lane after the first): its block's table position, then its position in the
+    // context (-1: not seen; WHOLE: no token of the tile is) and where its key lies
+    const int own = WHOLE ? 0 : lane & 15;
     auto listed = [&](int tile) -> int {
-        const int u = first_of(tile) + (lane & 15);
+        const int u = first_of(tile) + own;
         return u < end ? __ldg(list + block_of(u, p.BS, p.bs_shift)) : -1;
     };
     struct Key {
-        int t, id;
+        int t, id, slot;
     };
     auto key_of = [&](int tile, int entry) -> Key {
-        Key k{-1, 0};
+        Key k{-1, 0, 0};
         if (entry >= 0 && entry < blocks) {
-            const int u = first_of(tile) + (lane & 15);
-            const int t = entry * p.BS + (u - block_of(u, p.BS, p.bs_shift) * p.BS);
-            if (t >= span.lo && t < span.hi) {
+            const int u = first_of(tile) + own;
+            k.slot = u - block_of(u, p.BS, p.bs_shift) * p.BS;
+            const int t = entry * p.BS + k.slot;
+            if (t + (WHOLE ? 15 : 0) >= span.lo && t < span.hi) {
                 k.t = t;
                 k.id = __ldg(table + entry);
             }
         }
         return k;
     };
+    constexpr int AT_ONCE = 32 / S::PIECES;  // rows of one copy instruction
+    const int c = lane % S::PIECES, r0 = lane / S::PIECES;
     auto issue = [&](int tile, const Key &k) {
-        if (tile < tiles) {
-            const int b = block_of(max(k.t, 0), p.BS, p.bs_shift);
-            const long long off = k.t < 0 ? -1 : (long long)k.id * 2 * p.run + (long long)(k.t - b * p.BS) * p.row;
+        if (WHOLE) {
+            if (k.t >= 0) {  // else nothing of the tile is looked at
+                const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
+                const char *src = kb + (long long)k.id * 2 * p.run + (long long)(k.slot + r0) * p.row + c * 16;
+                const bool all = k.t >= span.lo && k.t + 16 <= span.hi;
+#pragma unroll
+                for (int i = 0; i < 16 / AT_ONCE; ++i) {
+                    const int r = i * AT_ONCE + r0;
+                    const bool in = (all || (k.t + r >= span.lo && k.t + r < span.hi)) && c * 8 < p.D;
+                    copy16(st + k_at(r, c), in ? src : kb, in ? 16 : 0);
+                    copy16(st + v_at(r, c), in ? src + p.run : kb, in ? 16 : 0);
+                    src += AT_ONCE * p.row;
+                }
+            }
+        } else if (tile < tiles) {
+            const long long off = k.t < 0 ? -1 : (long long)k.id * 2 * p.run + (long long)k.slot * p.row;
             const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
-            constexpr int AT_ONCE = 32 / S::PIECES;  // rows of one copy instruction
-            const int c = lane % S::PIECES;
 #pragma unroll
             for (int i = 0; i < 16 / AT_ONCE; ++i) {
-                const int r = i * AT_ONCE + lane / S::PIECES;
+                const int r = i * AT_ONCE + r0;
                 const long long at = __shfl_sync(0xffffffffu, off, r);
                 const bool in = at >= 0 && c * 8 < p.D;
                 const char *src = kb + at + c * 16;
@@ -157,7 +175,9 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == ListShape<DP>::WARPS ? 2 
     for (int tile = 0; tile < tiles; ++tile) {
         copy_wait<S::STAGES - 1>();
         __syncwarp();  // every lane's pieces have landed
-        const unsigned seen = __ballot_sync(0xffffffffu, pos[0] >= 0);
+        // the tile's tokens that are seen, a bit each
+        const unsigned seen = !WHOLE ? __ballot_sync(0xffffffffu, pos[0] >= 0)
+                                     : (pos[0] < 0 ? 0u : (1u << max(0, min(16, span.hi - pos[0]))) - (1u << max(0, min(16, span.lo - pos[0]))));
         if (seen) {
             const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
             float s[NT][4];
@@ -172,7 +192,8 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == ListShape<DP>::WARPS ? 2 
                     Elt<T>::mma(s[nt], w.z, x.z, w.w, x.w, qf[nt][kk].z, qf[nt][kk].w);
                 }
             }
-            const int t_of[2] = {SIMPLE ? 0 : __shfl_sync(0xffffffffu, pos[0], g), SIMPLE ? 0 : __shfl_sync(0xffffffffu, pos[0], g + 8)};
+            const int t_of[2] = {SIMPLE ? 0 : (WHOLE ? pos[0] + g : __shfl_sync(0xffffffffu, pos[0], g)),
+                                 SIMPLE ? 0 : (WHOLE ? pos[0] + g + 8 : __shfl_sync(0xffffffffu, pos[0], g + 8))};
             uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -322,23 +343,30 @@ int attend_blocks_rows(int D, int G) {
     return 8 * (nt == 3 ? 4 : nt);
 }
 
-int attend_blocks_warps(int D) { return D <= 64 ? ListShape<64>::WARPS : (D <= 128 ? ListShape<128>::WARPS : ListShape<256>::WARPS); }
+int attend_blocks_warps(int D) { return D <= 128 ? ListShape<128, 1>::WARPS : ListShape<256, 1>::WARPS; }
+int attend_blocks_ctas(int D, int G) {
+    return list_tiles(D, G) > 1 || D > 128 ? ListShape<128, 2>::CTAS : (D <= 64 ? ListShape<64, 1>::CTAS : ListShape<128, 1>::CTAS);
+}
+static_assert(ListShape<64, 1>::WARPS == ListShape<128, 1>::WARPS && ListShape<256, 1>::CTAS == 2 && ListShape<64, 2>::CTAS == 2 &&
+              ListShape<64, 4>::CTAS == 2, "what the two functions say");
 
-template <typename T, int DP, int NT, bool SIMPLE, int WARPS>
+template <typename T, int DP, int NT, bool SIMPLE, bool WHOLE, int WARPS>
 static cudaError_t list_go(const AttnParams &p, const SmallSeqs &small, cudaStream_t st) {
     static SmemSeen seen{0};
-    constexpr int bytes = WARPS * ListShape<DP>::WARP_BYTES;
-    cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_blocks_kernel<T, DP, NT, SIMPLE, WARPS>), bytes, &seen);
+    constexpr int bytes = WARPS * ListShape<DP, NT>::WARP_BYTES;
+    cudaError_t e = allow_smem(reinterpret_cast<const void *>(attend_blocks_kernel<T, DP, NT, SIMPLE, WHOLE, WARPS>), bytes, &seen);
     if (e != cudaSuccess) return e;
     const int groups = (p.G + NT * 8 - 1) / (NT * 8);
-    attend_blocks_kernel<T, DP, NT, SIMPLE, WARPS><<<(unsigned)(p.total_units * p.H * groups), WARPS * 32, bytes, st>>>(p, small, groups);
+    attend_blocks_kernel<T, DP, NT, SIMPLE, WHOLE, WARPS><<<(unsigned)(p.total_units * p.H * groups), WARPS * 32, bytes, st>>>(p, small, groups);
     return cudaGetLastError();
 }
+template <typename T, int DP, int NT, bool SIMPLE> static cudaError_t list_whole(const AttnParams &p, const SmallSeqs &small, bool alone, cudaStream_t st) {
+    constexpr int W = ListShape<DP, NT>::WARPS, ALL = W * ListShape<DP, NT>::CTAS;
+    if (p.BS % 16 == 0) return alone ? list_go<T, DP, NT, SIMPLE, true, ALL>(p, small, st) : list_go<T, DP, NT, SIMPLE, true, W>(p, small, st);
+    return alone ? list_go<T, DP, NT, SIMPLE, false, ALL>(p, small, st) : list_go<T, DP, NT, SIMPLE, false, W>(p, small, st);
+}
 template <typename T, int DP, int NT> static cudaError_t list_kind(const AttnParams &p, const SmallSeqs &small, bool alone, cudaStream_t st) {
-    constexpr int W = ListShape<DP>::WARPS;
-    if (p.softcap == 0.0f && !p.slopes)
-        return alone ? list_go<T, DP, NT, true, 2 * W>(p, small, st) : list_go<T, DP, NT, true, W>(p, small, st);
-    return alone ? list_go<T, DP, NT, false, 2 * W>(p, small, st) : list_go<T, DP, NT, false, W>(p, small, st);
+    return p.softcap == 0.0f && !p.slopes ? list_whole<T, DP, NT, true>(p, small, alone, st) : list_whole<T, DP, NT, false>(p, small, alone, st);
 }
 template <typename T> static cudaError_t list_pick(const AttnParams &p, const SmallSeqs &small, bool alone, cudaStream_t st) {
     const int nt = list_tiles(p.D, p.G);

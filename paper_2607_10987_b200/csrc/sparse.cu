@@ -198,14 +198,14 @@ int aaf_kv_attend_blocks(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, in
     k.keep = keep;
     const int Hq = k.H * k.G, groups = (k.G + attend_blocks_rows(k.D, k.G) - 1) / attend_blocks_rows(k.D, k.G);
     // Lists are cut into parts so that the GPU is filled a whole number of times, by CTAs that share an SM or, where there is one for
-    // each of them, by CTAs that have it to themselves and twice the warps: a round costs its part's keys per warp and a start (about 24
+    // each of them, by CTAs that have it to themselves and more warps: a round costs its part's keys per warp and a start (about 24
     // keys' time), a join twice that.
     int longest = 0;
     for (AttnSeq &s : rec) {
         s.chunk = (int)(std::min<long long>(keep, nblk_of(p, s.len)) * BS);  // keys of a full list, for now
         longest = std::max(longest, s.chunk);
     }
-    const int warps = attend_blocks_warps(k.D);
+    const int warps = attend_blocks_warps(k.D), ctas = attend_blocks_ctas(k.D, k.G);
     int chunk = 16;
     long long best = 1ll << 62;
     bool alone = false;
@@ -214,13 +214,13 @@ int aaf_kv_attend_blocks(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, in
         long long t = 0;
         for (const AttnSeq &s : rec) t += (long long)((s.chunk + c - 1) / c) * s.nq;
         if (parts > 1 && t * Hq > PART_ROWS) break;  // partial results have to fit
-        for (int per_sm = 2; per_sm >= 1; --per_sm) {
-            const long long rounds = (t * k.H * groups + per_sm * p->sm_count - 1) / (per_sm * p->sm_count);
-            const long long cost = rounds * (c * per_sm / (2 * warps) + 24) + (parts > 1 ? 48 : 0);
-            if (cost < best && (per_sm == 2 || rounds == 1)) {
+        for (int one = 0; one < 2; ++one) {
+            const long long at_once = (one ? 1 : ctas) * p->sm_count, rounds = (t * k.H * groups + at_once - 1) / at_once;
+            const long long cost = rounds * (c / (one ? warps * ctas : warps) + 24) + (parts > 1 ? 48 : 0);
+            if (cost < best && (!one || rounds == 1)) {
                 best = cost;
                 chunk = c;
-                alone = per_sm == 1;
+                alone = one;
             }
         }
         if (t * k.H * groups > 16ll * p->sm_count) break;  // enough for even rounds

@@ -75,10 +75,11 @@ cudaError_t launch_summarize(const SummaryParams &p, const SmallSeqs &small, int
 SelectShape select_shape(const SelectParams &p, int n, int max_nq, long long m_tiles, int sm_count, int f16);
 cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, long long tokens, cudaStream_t st);
 // p.first is not read; a record's nsplit parts of `chunk` listed keys (lists of `keep` blocks); units are (query token, part).
-// alone: CTAs of twice as many warps that have an SM to themselves
+// alone: CTAs that have an SM to themselves
 cudaError_t launch_attend_blocks(const AttnParams &p, const SmallSeqs &small, int f16, bool alone, cudaStream_t st);
 int attend_blocks_rows(int D, int G);  // query rows of a CTA
 int attend_blocks_warps(int D);        // of a CTA that is not alone
+int attend_blocks_ctas(int D, int G);  // of those, that share an SM; one that is alone has the warps of all of them
 cudaError_t launch_batch_tables(const TablesParams &p, const TableRow *rows, cudaStream_t st);  // rows: the batch, on the host
 
 }  // namespace aafkv

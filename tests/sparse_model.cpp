@@ -21,5 +21,6 @@ cudaError_t launch_select_blocks(const SelectParams &, const SmallSeqs &, const 
 cudaError_t launch_attend_blocks(const AttnParams &, const SmallSeqs &, int, bool, cudaStream_t st) { return launch("attend_blocks", st); }
 int attend_blocks_rows(int, int) { return 8; }
 int attend_blocks_warps(int) { return 4; }
+int attend_blocks_ctas(int, int) { return 2; }
 cudaError_t launch_batch_tables(const TablesParams &, const TableRow *, cudaStream_t st) { return launch("tables", st); }
 }  // namespace aafkv
