@@ -12,6 +12,10 @@
 
 namespace aafkv {
 
+__device__ __forceinline__ void copy16_all(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
 // CTAS of WARPS warps share an SM, as many as registers allow (a warp by itself waits for most of its time: twelve warps of two stages are
 // ahead of eight of three); a CTA that has an SM to itself has the warps of all of them.
 template <int DP, int NT> struct ListShape {
@@ -108,14 +112,25 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == ListShape<DP, NT>::WARPS 
             if (k.t >= 0) {  // else nothing of the tile is looked at
                 const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
                 const char *src = kb + (long long)k.id * 2 * p.run + (long long)(k.slot + r0) * p.row + c * 16;
-                const bool all = k.t >= span.lo && k.t + 16 <= span.hi;
+                if (k.t >= span.lo && k.t + 16 <= span.hi && p.D == DP) {
+                    const char *val = src + p.run;
+                    const long long down = AT_ONCE * p.row;
 #pragma unroll
-                for (int i = 0; i < 16 / AT_ONCE; ++i) {
-                    const int r = i * AT_ONCE + r0;
-                    const bool in = (all || (k.t + r >= span.lo && k.t + r < span.hi)) && c * 8 < p.D;
-                    copy16(st + k_at(r, c), in ? src : kb, in ? 16 : 0);
-                    copy16(st + v_at(r, c), in ? src + p.run : kb, in ? 16 : 0);
-                    src += AT_ONCE * p.row;
+                    for (int i = 0; i < 16 / AT_ONCE; ++i) {
+                        copy16_all(st + k_at(i * AT_ONCE + r0, c), src);
+                        copy16_all(st + v_at(i * AT_ONCE + r0, c), val);
+                        src += down;
+                        val += down;
+                    }
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < 16 / AT_ONCE; ++i) {
+                        const int r = i * AT_ONCE + r0;
+                        const bool in = k.t + r >= span.lo && k.t + r < span.hi && c * 8 < p.D;
+                        copy16(st + k_at(r, c), in ? src : kb, in ? 16 : 0);
+                        copy16(st + v_at(r, c), in ? src + p.run : kb, in ? 16 : 0);
+                        src += AT_ONCE * p.row;
+                    }
                 }
             }
         } else if (tile < tiles) {
@@ -180,18 +195,24 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == ListShape<DP, NT>::WARPS 
                                      : (pos[0] < 0 ? 0u : (1u << max(0, min(16, span.hi - pos[0]))) - (1u << max(0, min(16, span.lo - pos[0]))));
         if (seen) {
             const uint32_t st = base + (tile % S::STAGES) * S::STAGE_BYTES;
-            float s[NT][4];
+            float s[NT][4], s2[NT][4];  // two sums, which take turns: a product waits for the one before it in the same sum
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[nt][i] = s2[nt][i] = 0.0f;
 #pragma unroll
             for (int kk = 0; kk < DP / 32; ++kk) {
                 const uint4 w = lds16(st + k_at(g, kk * 4 + t4)), x = lds16(st + k_at(g + 8, kk * 4 + t4));
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     Elt<T>::mma(s[nt], w.x, x.x, w.y, x.y, qf[nt][kk].x, qf[nt][kk].y);
-                    Elt<T>::mma(s[nt], w.z, x.z, w.w, x.w, qf[nt][kk].z, qf[nt][kk].w);
+                    Elt<T>::mma(s2[nt], w.z, x.z, w.w, x.w, qf[nt][kk].z, qf[nt][kk].w);
                 }
             }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[nt][i] += s2[nt][i];
             const int t_of[2] = {SIMPLE ? 0 : (WHOLE ? pos[0] + g : __shfl_sync(0xffffffffu, pos[0], g)),
                                  SIMPLE ? 0 : (WHOLE ? pos[0] + g + 8 : __shfl_sync(0xffffffffu, pos[0], g + 8))};
             uint32_t ph[NT][2], pl[NT][2];
