@@ -198,8 +198,9 @@ int aaf_kv_attend_blocks(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, in
     k.keep = keep;
     const int Hq = k.H * k.G, groups = (k.G + attend_blocks_rows(k.D, k.G) - 1) / attend_blocks_rows(k.D, k.G);
     // Lists are cut into parts so that the GPU is filled a whole number of times, by CTAs that share an SM or, where there is one for
-    // each of them, by CTAs that have it to themselves and more warps: a round costs its part's keys per warp and a start (about 24
-    // keys' time), a join twice that.
+    // each of them, by CTAs that have it to themselves and more warps: a round costs its part's keys per warp and a start (about 72
+    // keys' time), a join twice that.  Microseconds with 1, 2, 3, 4, 6 parts: 1024 lists of 2048 keys 105, 111, 118, 124, 139; 512 ragged
+    // ones of up to 4096 197, 179, 171, 169, 169; 128 of 1024 20.3, 19.8, 19.5, 19.6, 20.5, and 17.2 with an SM for each.
     int longest = 0;
     for (AttnSeq &s : rec) {
         s.chunk = (int)(std::min<long long>(keep, nblk_of(p, s.len)) * BS);  // keys of a full list, for now
@@ -216,7 +217,7 @@ int aaf_kv_attend_blocks(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, in
         if (parts > 1 && t * Hq > PART_ROWS) break;  // partial results have to fit
         for (int one = 0; one < 2; ++one) {
             const long long at_once = (one ? 1 : ctas) * p->sm_count, rounds = (t * k.H * groups + at_once - 1) / at_once;
-            const long long cost = rounds * (c / (one ? warps * ctas : warps) + 24) + (parts > 1 ? 48 : 0);
+            const long long cost = rounds * (c / (one ? warps * ctas : warps) + 72) + (parts > 1 ? 144 : 0);
             if (cost < best && (!one || rounds == 1)) {
                 best = cost;
                 chunk = c;
