@@ -20,7 +20,7 @@
 namespace aafkv {
 
 constexpr int SCORE_BLOCKS = 128;  // of an m-tile
-constexpr int PICK_WARPS = 8, PICK_KEYS = 12288;  // scores of a list that are kept in shared memory
+constexpr int PICK_KEYS = 12288;  // scores of a list that are kept in shared memory
 
 // 8-bit products, 32-bit sums
 __device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -588,9 +588,11 @@ __global__ void __launch_bounds__(WARPS * 32)
 static size_t score_smem(const SelectShape &z) { return (size_t)z.slabs * 128 * (z.buffers * SCORE_BLOCKS + z.n) + 1024; }
 constexpr int SCORE_SMEM = (4 * 128 * (2 * SCORE_BLOCKS + SELECT_ROWS)) + 1024;
 
-// How a batch is cut.  A token each, whose rows of all heads fit: whole records.  Else rows of a tile: 32 (the sums' columns that a thread
-// reads at once), or as many as the tokens fill, up to SELECT_ROWS.  A CTA takes so many m-tiles in turn that the CTAs are all there at once: its start (memory, record,
-// rows' codes) costs as much as several of them.
+// How a batch is cut.  Rows of a tile: 32 (the sums' columns that a thread reads at once), or as many as the tokens fill, up to SELECT_ROWS
+// (128 tokens behind 65531: 45 us with 128 rows and 256 threads, 49 with 128 threads, 49 with 64 rows, 60 with 32).  A CTA takes so many m-tiles
+// in turn that the CTAs are all there at once: its start (memory, record, rows' codes) costs as much as several of them.  A token each:
+// whole records, where the CTAs of single heads would not be there at once (32 ragged contexts, 55 thousand blocks: 46.8 us, head by head
+// 50.6; 16 contexts of 544 blocks: 18.5 and 16.5, since every CTA makes the codes of all heads' rows).
 SelectShape select_shape(const SelectParams &p, int n, int max_nq, long long m_tiles, int sm_count, int f16) {
     SelectShape z{};
     z.f16 = f16;
@@ -611,7 +613,10 @@ SelectShape select_shape(const SelectParams &p, int n, int max_nq, long long m_t
     while (z.heads_p < p.G) z.heads_p *= 2;
     z.slabs = (2 * p.D + 127) / 128;
     z.blocks = SCORE_BLOCKS;
-    if (max_nq == 1 && p.H * z.heads_p <= SELECT_ROWS && z.heads_p <= 32 && p.H <= 16) {  // a token each
+    z.n = 32;
+    z.buffers = 1;
+    const bool at_once = m_tiles * p.H <= std::min<long long>(5, 227 * 1024 / (long long)(score_smem(z) + 2048)) * sm_count;
+    if (max_nq == 1 && !at_once && p.H * z.heads_p <= SELECT_ROWS && z.heads_p <= 32 && p.H <= 16) {
         z.together = 1;
         z.tile = 1;
         for (z.n = 32; z.n < p.H * z.heads_p; z.n *= 2) {}
@@ -663,7 +668,8 @@ template <int HP> static cudaError_t records_go(const SelectParams &p, const Sma
     score_records_kernel<HP><<<(unsigned)units, 128, score_smem(z), st>>>(p, small, z);
     return cudaGetLastError();
 }
-cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, long long tokens, cudaStream_t st) {
+cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, const SelectShape &z, long long units, long long tokens, int sm_count,
+                                 cudaStream_t st) {
     cudaError_t e;
     switch (log2_up(std::min(z.heads_p, 32))) {
         case 0: e = z.together ? records_go<0>(p, small, z, units, st) : score_rows<0>(p, small, z, units, st); break;
@@ -674,7 +680,8 @@ cudaError_t launch_select_blocks(const SelectParams &p, const SmallSeqs &small, 
         default: e = z.together ? records_go<5>(p, small, z, units, st) : score_rows<5>(p, small, z, units, st); break;
     }
     if (e != cudaSuccess) return e;
-    return p.widest <= 1024 ? pick_go<4>(p, small, tokens, st) : pick_go<PICK_WARPS>(p, small, tokens, st);
+    // few lists: more warps for each (128 lists of 544 blocks 17.0 us with eight, 18.5 with four; 1024 lists of 4096 45.1 and 43.1)
+    return tokens * p.H > 2ll * sm_count ? pick_go<4>(p, small, tokens, st) : pick_go<8>(p, small, tokens, st);
 }
 
 }  // namespace aafkv

@@ -165,7 +165,7 @@ int aaf_kv_select(aaf_kv_pool *p, int32_t layer, const aaf_kv_select_desc *d, in
         const std::vector<AttnSeq> part(parts.begin() + (ptrdiff_t)l.first, parts.begin() + (ptrdiff_t)l.end);
         SmallSeqs small;
         k.n = (int)part.size();
-        ok = place_records(p, part, small, &k.seqs, 0, st) && launch_select_blocks(k, small, z, l.units, l.tokens, st) == cudaSuccess;
+        ok = place_records(p, part, small, &k.seqs, 0, st) && launch_select_blocks(k, small, z, l.units, l.tokens, p->sm_count, st) == cudaSuccess;
     }
     return ok && end_read(p, st) ? AAF_OK : broke(p);
 } catch (const std::bad_alloc &) {

@@ -15,7 +15,7 @@ SelectShape select_shape(const SelectParams &, int, int, long long, int, int f16
     z.f16 = f16;
     return z;
 }
-cudaError_t launch_select_blocks(const SelectParams &, const SmallSeqs &, const SelectShape &, long long, long long, cudaStream_t st) {
+cudaError_t launch_select_blocks(const SelectParams &, const SmallSeqs &, const SelectShape &, long long, long long, int, cudaStream_t st) {
     return launch("choose", st);
 }
 cudaError_t launch_attend_blocks(const AttnParams &, const SmallSeqs &, int, bool, cudaStream_t st) { return launch("attend_blocks", st); }

@@ -141,6 +141,31 @@ def test_select_ragged(heads, group, dim, block, dtype):
     check_select(pool, ctxs, [1] * len(lens), q, 6, 1, 2)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("heads,group,dim,tokens,times", [(8, 4, 128, 16 * 700 + 5, 20), (2, 16, 64, 16 * 3000 + 1, 20), (3, 5, 96, 16 * 1500, 30),
+                                                          (16, 1, 40, 16 * 399 + 9, 20), (1, 32, 256, 16 * 4900 + 2, 24), (5, 2, 8, 16 * 1111, 25),
+                                                          (8, 8, 128, 16 * 300 + 7, 64)])
+def test_select_from_whole_records(heads, group, dim, tokens, times, dtype):
+    # so many blocks that all heads of a block are taken together; three of the choices are looked at
+    pool = R.make_pool(1, heads, dim, 16, 4910, max_ctx=4, dtype=dtype)
+    longest = R.add_ctx(pool, tokens, 1)
+    summary = pool.new_summary()
+    assert pool.summarize(0, [longest.handle], None, summary, dtype)[0] == 0
+    q = R.rand((times, heads * group, dim), 5, dtype, 3.0)
+    scores = torch.empty(times, heads, 9, device="cuda")
+    st, blocks = pool.select(0, [longest.handle] * times, None, q, summary, 9, sink=1, recent=2, scores=scores)
+    assert st == 0
+    settle(pool)
+    codes, exps = S.read_summary(summary, 0, torch.from_numpy(pool.table(longest.handle)).cuda(), heads, dim)
+    last = (len(longest) - 1) // 16
+    for i in (0, times // 2, times - 1):
+        for h in range(heads):
+            s = S.scores_ref(codes[:, h], exps[:, h], q[i, h * group:(h + 1) * group])
+            want = S.select_ref(s, last, 9, 1, 2)
+            assert blocks[i, h].tolist() == want
+            assert scores[i, h].tolist() == [s[b] for b in want]
+
+
 @pytest.mark.parametrize("keep,sink,recent", [(1, 0, 1), (4, 0, 4), (4, 3, 1), (7, 2, 2), (33, 1, 4), (64, 0, 1), (100, 10, 20), (300, 1, 1)])
 def test_select_budgets(keep, sink, recent):
     pool, ctxs = pool_of(2, 64, 16, [1030, 500, 90])
