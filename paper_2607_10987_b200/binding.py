@@ -515,7 +515,7 @@ class KVPool:
         """Outputs of an attention call and its scratch, None for the latter if it is not there and must not be made."""
         torch = self.torch
         if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            out = torch.empty_like(q) if q.is_contiguous() else torch.empty_like(q, memory_format=torch.contiguous_format)
         elif self._rows(out, tokens, heads, "out", q.dtype) != heads * self.D:
             raise ValueError("out: dense tensor expected")
         if lse is None:
