@@ -173,16 +173,18 @@ def test_select_budgets(keep, sink, recent):
     check_select(pool, ctxs, [1, 1, 1], q, keep, sink, recent)
 
 
-@pytest.mark.parametrize("heads,group,dim", [(2, 4, 128), (1, 3, 64), (1, 1, 64), (1, 20, 64), (2, 2, 96)])
+@pytest.mark.parametrize("heads,group,dim", [(2, 4, 128), (1, 3, 64), (1, 1, 64), (1, 20, 64), (2, 2, 96), (1, 40, 64), (1, 2, 256), (2, 4, 40),
+                                             (1, 9, 8)])
 @pytest.mark.parametrize("n_q", [[2, 5], [33, 16], [70, 1]])
 def test_select_for_many_tokens(heads, group, dim, n_q):
     pool, ctxs = pool_of(heads, dim, 16, [300, 411])
     check_select(pool, ctxs, n_q, R.rand((sum(n_q), heads * group, dim), 5), 9, 1, 2)
 
 
-def test_select_from_the_first_token_on():
-    pool, ctxs = pool_of(1, 64, 4, [70])
-    check_select(pool, ctxs, [70], R.rand((70, 2, 64), 5), 5, 1, 2)
+@pytest.mark.parametrize("tokens,block", [(70, 4), (600, 2)])
+def test_select_from_the_first_token_on(tokens, block):
+    pool, ctxs = pool_of(1, 64, block, [tokens])
+    check_select(pool, ctxs, [tokens], R.rand((tokens, 2, 64), 5), 5, 1, 2)
 
 
 def test_select_equal_scores_go_to_the_lower_block():
@@ -322,7 +324,7 @@ def check_blocks(pool, ctxs, n_q, q, blocks, layer=0, **kw):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("heads,group,dim,block", [(2, 4, 64, 16), (8, 4, 128, 16), (1, 1, 128, 1), (3, 5, 96, 8), (2, 16, 128, 64), (4, 8, 64, 5),
                                                    (1, 8, 256, 16), (2, 1, 80, 24), (1, 32, 64, 32), (1, 3, 8, 16), (1, 17, 128, 16),
-                                                   (1, 50, 64, 16), (2, 9, 256, 16), (1, 24, 40, 7)])
+                                                   (1, 50, 64, 16), (2, 9, 256, 16), (1, 24, 40, 7), (3, 5, 96, 16), (2, 2, 80, 32), (1, 12, 200, 48)])
 def test_listed_ragged(heads, group, dim, block, dtype):
     lens = [1, 2, 15, 16, 17, 63, 130, 513]
     pool, ctxs = pool_of(heads, dim, block, lens, dtype)
