@@ -502,8 +502,8 @@ int aaf_kv_attend_blocks(aaf_kv_pool *pool, int32_t layer, const aaf_kv_attn *a,
  *   positions [tokens]      its index in its context, 0 behind the last
  *   slots     [tokens]      block id * block_size + place in the block, -1 behind the last: layer l's key row is at pool_base + l *
  *                           layer_stride_bytes + (slot / BS * 2 * BS + slot % BS) * row, the value row run bytes further
- * Errors: BAD_CTX, INVALID_ARG (n_new, pointers, nothing asked for), DST_TOO_SMALL (rows, tokens, or cols below a context's blocks), TOO_MANY,
- * TOO_LONG. */
+ * Errors: BAD_CTX, INVALID_ARG (n_new, pointers, nothing asked for), DST_TOO_SMALL (rows, tokens, or cols below a context's blocks), TOO_MANY
+ * (rows, tokens or cols above 2^30, too), TOO_LONG. */
 typedef struct aaf_kv_batch_desc {
     uint32_t struct_size; /* sizeof(aaf_kv_batch_desc) */
     int32_t rows, tokens, cols;

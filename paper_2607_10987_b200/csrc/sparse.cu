@@ -270,7 +270,7 @@ int aaf_kv_batch_tables(aaf_kv_pool *p, const aaf_kv_batch_desc *d, int32_t n, c
         return AAF_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(d->positions) | reinterpret_cast<uintptr_t>(d->slots)) & 7u) return AAF_ERR_INVALID_ARG;
     if (!d->tables && !d->lens && !d->offsets && !d->token_row && !d->positions && !d->slots) return AAF_ERR_INVALID_ARG;
-    if (d->rows > (1 << 30) || d->tokens > (1 << 30)) return AAF_ERR_TOO_MANY;
+    if (d->rows > (1 << 30) || d->tokens > (1 << 30) || (d->tables && d->cols > (1 << 30))) return AAF_ERR_TOO_MANY;  // ints in the kernel
     std::vector<AttnSeq> rec;
     long long total = 0;
     const int rc = batch_records(p, n, ctxs, n_new, false, rec, &total);

@@ -123,6 +123,15 @@ def test_refusals(lib, pool):
     assert lib.order_ops() == at + 1
 
 
+def test_tables_beyond_the_kernels_ints_are_refused(lib, pool):
+    st = lib.order_stream()
+    _, c = pool.imp(st, 160)
+    for kw in (dict(cols=(1 << 30) + 1), dict(cols=(1 << 31) - 1), dict(cols=(1 << 31) - 1, rows=1), dict(rows=(1 << 30) + 1), dict(tokens=(1 << 31) - 1)):
+        assert not pool.tables(st, [c], want=B.AAF_ERR_TOO_MANY, **kw), kw
+    assert pool.tables(st, [c], cols=1 << 30, rows=1)
+    assert pool.tables(st, [c], cols=(1 << 31) - 1, tables=None, lens=pool.base)  # not looked at
+
+
 @pytest.mark.parametrize("call", CALLS)
 def test_refused_in_a_capture_and_beside_one_not(lib, pool, call):
     a, b = lib.order_stream(), lib.order_stream()
