@@ -267,6 +267,15 @@ def _ints(v):
     return C.byref(C.c_int32.from_buffer(array("i", v if len(v) else (0,))))
 
 
+def _total(counts, n):
+    """Tokens of a batch of n contexts (counts None: one each).  The library reads n counts, however many there are."""
+    if counts is None:
+        return n
+    if len(counts) != n:
+        raise ValueError(f"{len(counts)} token counts for {n} contexts")
+    return sum(counts)
+
+
 def make_desc(n_layers, n_kv_heads, head_dim, block_size, elt_bytes, n_blocks, max_ctx, max_blocks_per_ctx,
               max_batch=0, device=0, model_id=0, config_hash=0) -> aaf_kv_pool_desc:
     d = aaf_kv_pool_desc()
@@ -595,6 +604,7 @@ class KVPool:
         """Sums up the blocks of the contexts' last n_new tokens (None: all blocks) in one layer (None: in all).  dtype: torch type of the
         pool's elements."""
         n = len(ctxs)
+        _total(n_new, n)
         code = self._codes.get(dtype)
         if code is None:
             raise ValueError(f"bfloat16 or float16 expected, got {dtype}")
@@ -607,7 +617,7 @@ class KVPool:
         """For every query token and kv head the `keep` blocks with the largest bound on a score, the first `sink` and the last `recent`
         among them: (status, blocks), int32 [tokens, kv heads, keep], -1 behind the last.  scores: float32 tensor of the same shape."""
         n = len(ctxs)
-        tokens = n if n_q is None else sum(n_q)
+        tokens = _total(n_q, n)
         heads = q.shape[1] if q.dim() == 3 else 0
         d = aaf_kv_select_desc(C.sizeof(aaf_kv_select_desc), self._code(q), heads, keep, sink, recent, self._rows(q, tokens, heads, "q", q.dtype))
         if blocks is None:
@@ -626,7 +636,7 @@ class KVPool:
     def attend_blocks(self, layer, ctxs, n_q, q, blocks, out=None, lse=None, scale=None, softcap=0.0, window=0, slopes=None, spans=None):
         """attend over the listed blocks alone: blocks is int32 [tokens, kv heads, keep]; returns (status, (out, lse))."""
         n = len(ctxs)
-        tokens = n if n_q is None else sum(n_q)
+        tokens = _total(n_q, n)
         a = self._attn(q, tokens, scale, softcap, window, slopes, spans)
         if blocks.dim() != 3 or blocks.shape[:2] != (tokens, self.H):
             raise ValueError(f"blocks: expected [{tokens}, {self.H}, keep], got {tuple(blocks.shape)}")
@@ -646,7 +656,7 @@ class KVPool:
         some or all of them to be filled instead."""
         torch = self.torch
         n = len(ctxs)
-        total = n if n_new is None else sum(n_new)
+        total = _total(n_new, n)
         rows, tokens = n if rows is None else rows, total if tokens is None else tokens
         if cols is None:
             if out is not None and "tables" in out:
