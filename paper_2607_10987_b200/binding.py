@@ -276,6 +276,11 @@ def _total(counts, n):
     return sum(counts)
 
 
+def _fits(*v):
+    """Whether numbers are what they are in 32 bits: ctypes drops the bits above."""
+    return all(-(1 << 31) <= x < 1 << 31 for x in v)
+
+
 def make_desc(n_layers, n_kv_heads, head_dim, block_size, elt_bytes, n_blocks, max_ctx, max_blocks_per_ctx,
               max_batch=0, device=0, model_id=0, config_hash=0) -> aaf_kv_pool_desc:
     d = aaf_kv_pool_desc()
@@ -608,6 +613,8 @@ class KVPool:
         code = self._codes.get(dtype)
         if code is None:
             raise ValueError(f"bfloat16 or float16 expected, got {dtype}")
+        if layer is not None and not _fits(layer):
+            return AAF_ERR_INVALID_ARG, None
         return load().aaf_kv_summarize(self.h, AAF_ALL_LAYERS if layer is None else layer, code, n, _ints(ctxs),
                                        None if n_new is None else _ints(n_new),
                                        self._flat(summary, self.torch.int8, self.summary_bytes(), "summary"), summary.numel(),
@@ -618,6 +625,8 @@ class KVPool:
         among them: (status, blocks), int32 [tokens, kv heads, keep], -1 behind the last.  scores: float32 tensor of the same shape."""
         n = len(ctxs)
         tokens = _total(n_q, n)
+        if not _fits(layer, keep, sink, recent):
+            return AAF_ERR_INVALID_ARG, None
         heads = q.shape[1] if q.dim() == 3 else 0
         d = aaf_kv_select_desc(C.sizeof(aaf_kv_select_desc), self._code(q), heads, keep, sink, recent, self._rows(q, tokens, heads, "q", q.dtype))
         if blocks is None:
@@ -637,6 +646,8 @@ class KVPool:
         """attend over the listed blocks alone: blocks is int32 [tokens, kv heads, keep]; returns (status, (out, lse))."""
         n = len(ctxs)
         tokens = _total(n_q, n)
+        if not _fits(layer, window):
+            return AAF_ERR_INVALID_ARG, None
         a = self._attn(q, tokens, scale, softcap, window, slopes, spans)
         if blocks.dim() != 3 or blocks.shape[:2] != (tokens, self.H):
             raise ValueError(f"blocks: expected [{tokens}, {self.H}, keep], got {tuple(blocks.shape)}")
@@ -663,6 +674,8 @@ class KVPool:
                 cols = out["tables"].shape[-1]
             else:
                 cols = max([-(-(self.ctx_len(c) or 0) // self.BS) for c in ctxs], default=0)
+        if not _fits(rows, tokens, cols):
+            return AAF_ERR_TOO_MANY, None
         i32, i64 = torch.int32, torch.int64
         if out is None:
             if rows < 0 or tokens < 0 or cols < 0:

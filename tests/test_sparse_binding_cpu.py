@@ -57,3 +57,20 @@ def test_as_many_counts_as_contexts(lib, kv, call):  # noqa: F811
             CALLS[call](kv, ctxs, counts)
     assert lib.order_ops() == at
     assert CALLS[call](kv, ctxs, [1, 2, 3, 4]) == 0 and lib.order_ops() == at + 1
+
+
+def test_numbers_that_do_not_fit_the_library_are_refused(lib, kv):  # noqa: F811
+    """They would arrive without their upper bits: a sink of 2^32 as none."""
+    kv, ctxs = kv
+    c, big, at = ctxs[:1], 1 << 32, lib.order_ops()
+    summary, q, blocks = kv.new_summary(), rows(1), torch.zeros(1, O.H, 4, dtype=torch.int32)
+    for kw in (dict(sink=big), dict(sink=1 - big), dict(recent=big + 1), dict(keep=big + 4)):
+        assert kv.select(0, c, None, q, summary, **{"keep": 4, **kw})[0] == B.AAF_ERR_INVALID_ARG, kw
+    for layer in (big, -big):
+        assert kv.summarize(layer, c, None, summary, torch.bfloat16)[0] == B.AAF_ERR_INVALID_ARG
+        assert kv.select(layer, c, None, q, summary, 4)[0] == B.AAF_ERR_INVALID_ARG
+        assert kv.attend_blocks(layer, c, None, q, blocks)[0] == B.AAF_ERR_INVALID_ARG
+    assert kv.attend_blocks(0, c, None, q, blocks, window=big + 16)[0] == B.AAF_ERR_INVALID_ARG
+    for kw in (dict(rows=big + 1), dict(tokens=big + 1), dict(cols=big + 10)):
+        assert kv.batch_tables(c, **kw)[0] == B.AAF_ERR_TOO_MANY, kw
+    assert lib.order_ops() == at
