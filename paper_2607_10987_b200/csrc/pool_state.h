@@ -275,21 +275,25 @@ inline AttnParams attn_params(const aaf_kv_pool *p, int layer, const aaf_kv_attn
 // Records of a batch: kernel parameters while they fit, else through the pinned ring into the pool's workspace on `st`
 // (the copies and their readers of all calls are ordered by begin_read).
 template <typename Rec, typename Small>
-bool place_records(aaf_kv_pool *p, const std::vector<Rec> &rec, Small &small, const Rec **dev, int which, cudaStream_t st) {
+bool place_records(aaf_kv_pool *p, const Rec *rec, size_t n, Small &small, const Rec **dev, int which, cudaStream_t st) {
     static_assert(sizeof(Rec) <= sizeof(AttnSeq), "records share the workspace of the attention records");
     *dev = nullptr;
-    if (rec.size() <= (size_t)SMALL_SEQS) {
-        std::copy(rec.begin(), rec.end(), small.e);
+    if (n <= (size_t)SMALL_SEQS) {
+        std::copy(rec, rec + n, small.e);
         return true;
     }
     char *pinned = acquire_args(p);
-    const size_t bytes = sizeof(Rec) * rec.size();
-    memcpy(pinned, rec.data(), bytes);
+    const size_t bytes = sizeof(Rec) * n;
+    memcpy(pinned, rec, bytes);
     char *dst = reinterpret_cast<char *>(p->desc.workspace) + p->lay.seq_records + sizeof(AttnSeq) * (size_t)p->lay.max_batch * which;
     const bool ok = cudaMemcpyAsync(dst, pinned, bytes, cudaMemcpyHostToDevice, st) == cudaSuccess;
     release_args(p, st);
     *dev = reinterpret_cast<const Rec *>(dst);
     return ok;
+}
+template <typename Rec, typename Small>
+bool place_records(aaf_kv_pool *p, const std::vector<Rec> &rec, Small &small, const Rec **dev, int which, cudaStream_t st) {
+    return place_records(p, rec.data(), rec.size(), small, dev, which, st);
 }
 
 }  // namespace aafkv

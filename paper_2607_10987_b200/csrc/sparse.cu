@@ -160,12 +160,12 @@ int aaf_kv_select(aaf_kv_pool *p, int32_t layer, const aaf_kv_select_desc *d, in
     p->last_stream = st;
     if (!begin_read(p, ctxs, n, st)) return broke(p);
     bool ok = true;
-    for (size_t i = 0; i < launches.size() && ok; ++i) {
+    for (size_t i = 0; i < launches.size() && ok; ++i) {  // nothing is allocated from here on
         const Launch &l = launches[i];
-        const std::vector<AttnSeq> part(parts.begin() + (ptrdiff_t)l.first, parts.begin() + (ptrdiff_t)l.end);
         SmallSeqs small;
-        k.n = (int)part.size();
-        ok = place_records(p, part, small, &k.seqs, 0, st) && launch_select_blocks(k, small, z, l.units, l.tokens, p->sm_count, st) == cudaSuccess;
+        k.n = (int)(l.end - l.first);
+        ok = place_records(p, parts.data() + l.first, l.end - l.first, small, &k.seqs, 0, st) &&
+             launch_select_blocks(k, small, z, l.units, l.tokens, p->sm_count, st) == cudaSuccess;
     }
     return ok && end_read(p, st) ? AAF_OK : broke(p);
 } catch (const std::bad_alloc &) {
