@@ -485,7 +485,13 @@ __global__ void __launch_bounds__(WARPS * 32)
                 }
                 if (digit == i) equal = (int)n[i];
             }
-            const int who = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+            const unsigned where = __ballot_sync(0xffffffffu, here);
+            if (!where) {  // fewer scores than are wanted: void ones, among them zeros, which no block has (a wait ran out).  All, then zeros
+                want -= __shfl_sync(0xffffffffu, (int)(above + mine), 0);
+                least = 0;
+                break;
+            }
+            const int who = __ffs(where) - 1;
             want = __shfl_sync(0xffffffffu, left, who);
             const uint32_t found = __shfl_sync(0xffffffffu, lane * 8 + digit, who);
             const int have = __shfl_sync(0xffffffffu, equal, who);
@@ -503,7 +509,10 @@ __global__ void __launch_bounds__(WARPS * 32)
             for (int i = i0 + lane * 4; i < i1; i += 128) {
                 const uint4 v = again(i);
                 auto gather = [&](uint32_t k) {
-                    if (k - a <= range && bin(k) == found) few_s[atomicAdd(&few_count, 1u)] = k;
+                    if (k - a <= range && bin(k) == found) {
+                        const uint32_t to = atomicAdd(&few_count, 1u);
+                        if (to < PICK_FEW) few_s[to] = k;  // always, unless the scores change meanwhile
+                    }
                 };
                 gather(v.x);
                 gather(v.y);
@@ -576,6 +585,7 @@ __global__ void __launch_bounds__(WARPS * 32)
                 const bool tie = v.y >> b & 1;
                 if (!tie || t_at < want) {
                     const int to = s_at + min(t_at, want);
+                    if ((unsigned)to >= (unsigned)p.keep) break;  // never, unless the scores change meanwhile
                     out[to] = i;
                     if (out_s) out_s[to] = from_ordered(stay && i >= m0 && i < m1 ? keys_s[i] : __ldcg(scores + i));
                 }
