@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 5 : 3)
         for (int m = 0; m < m_tiles; ++m) {
             const int e = __ldg(p.summary + (long long)(THREADS == 128 ? id : __ldg(table + min(first + m * SCORE_BLOCKS + mine, total - 1))) * p.record +
                                 (long long)p.H * 2 * p.D + head);
-            if (m + 1 < m_tiles && z.buffers > 1) {
+            if (m + 1 < m_tiles) {  // into the other buffer: there are two where there are several m-tiles
                 id = block_id(m + 1);
                 issue(m + 1, id);
                 copy_wait<1>();
@@ -236,10 +236,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 5 : 3)
             tmem_before();
             __syncthreads();  // sums and codes have been read
             tmem_after();
-            if (m + 1 < m_tiles && z.buffers == 1) {
-                id = block_id(m + 1);
-                issue(m + 1, id);
-            }
         }
     }
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_s), "r"(z.n));

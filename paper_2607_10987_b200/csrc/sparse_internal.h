@@ -42,7 +42,7 @@ struct SelectShape {
     int n;         // rows that are multiplied at a time
     int slabs;     // 128-byte stretches of a head's codes
     int reps;      // m-tiles of a CTA
-    int buffers;   // for their codes
+    int buffers;   // for their codes: two where reps > 1, else one
     int together;  // all kv heads of some blocks make an m-tile
     int blocks;    // of an m-tile
     int f16;
