@@ -138,14 +138,20 @@ def prepare(case, seed):
 
     row = 8 if kind == "tables" else hkv * d  # tables do not look at what the blocks hold
     pool = torch.empty(case["layers"], nb, 2, bs, row, dtype=dt, device=dev).view(case["layers"], nb, 2, bs, -1, 8 if kind == "tables" else d)
-    if own:  # the pool's handle and contexts, as a serving program holds them
+    if own:  # the pool's handle, sized for this batch, and its contexts: a token each, the others' slots reserved, no payload copied
+        import numpy
         from paper_2607_10987_b200 import KVPool
 
-        kv = KVPool(case["layers"], pool.shape[4], pool.shape[5], bs, 2, nb, len(lens) + 1, wide, free_order=order, pool_tensor=pool)
-        junk = torch.empty(kv.bpt * max(lens), dtype=torch.uint8, device=dev)
-        s["kv"], s["ctxs"] = kv, [_done(kv.imp(junk, t)) for t in lens]
-        torch.cuda.synchronize()
-        del junk
+        table = s["tables"].cpu().numpy()
+        later = numpy.arange(1, wide) < numpy.array(need)[:, None]
+        free = numpy.concatenate((table[:, 0], table[:, 1:][later], order[at:]))
+        kv = KVPool(case["layers"], pool.shape[4], pool.shape[5], bs, 2, nb, len(lens) + 1, max(wide, at // 2), free_order=free, max_batch=len(lens),
+                    pool_tensor=pool)
+        one = torch.empty(kv.bpt, dtype=torch.uint8, device=dev)
+        s["kv"], s["ctxs"] = kv, _done(kv.import_batch([one] * len(lens), [1] * len(lens)))
+        longer = [(c, t - 1) for c, t in zip(s["ctxs"], lens) if t > 1]
+        if longer:
+            _done(kv.reserve(*zip(*longer)))
     torch.randn(pool.shape, generator=g, device=dev, dtype=dt, out=pool)
     s["pool"] = pool
 
