@@ -462,16 +462,19 @@ int aaf_kv_summarize(aaf_kv_pool *pool, int32_t layer, int32_t dtype, int32_t n,
  *   f = the smallest exponent >= -60 with all |F(q_d)| <= 127 * 2^f;   c_d = F(q_d) / 2^f rounded to a whole number, half to even; 0 for a NaN
  *   dot_b = sum_d max(c_d * hi_bd, c_d * lo_bd)   over the codes of the block
  *   score_b = the largest of dot_b * 2^(e_b + f) over the query heads of the kv head's group, a 32-bit float
- * (up to the rounding of q the largest product that any key of the block could have with it; a positive attention scale is assumed) it
+ * (the largest product that any key of the block could have with the rounded q; a positive attention scale is assumed.  What is left out is
+ * limited by `keep`, not by its bounds: no block that is left out has a larger one than any that is taken by its score) it
  * takes blocks 0 .. sink - 1, blocks B - recent + 1 .. B, and of the others those with the largest scores (equal scores: the lower
- * block), at most keep in all.  All of it is exact: no rounding decides.  A block's summary covers tokens behind p too, where
+ * block), at most keep in all.  It knows nothing of a window, of spans or of slopes that aaf_kv_attend_blocks is given: with a mask, part of
+ * a list may be blocks that the row does not see; with a distance bias the order is that of the scores without it.
+ * All of it is exact: no rounding decides.  A block's summary covers tokens behind p too, where
  * the context has them: those of block B, which is always taken.
  * blocks_dev: [tokens][n_kv_heads][keep] block numbers within the context, ascending, -1 behind the last; scores_dev (may be NULL): the same
  * shape, their scores, -inf behind the last.  q: heads contiguous, q_stride elements from token to token (a multiple of 8).  n_q may be NULL
  * (one token each).  A context may be listed several times.  workspace_dev as for aaf_kv_attend, the same buffer: it holds scores.
  * Errors: BAD_CTX, INVALID_ARG (n_q, keep outside [1, AAF_LIST_MAX_BLOCKS], recent < 1, sink < 0, sink + recent > keep, pointers, strides),
- * INCOMPAT, DST_TOO_SMALL (summary, workspace), TOO_MANY, TOO_LONG (more blocks in the longest context, times n_kv_heads, than 65536 *
- * (head_dim + 2)). */
+ * INCOMPAT, DST_TOO_SMALL (summary, workspace), TOO_MANY, TOO_LONG (blocks of the longest context, rounded up to a multiple of 4, times
+ * n_kv_heads above 65536 * (head_dim + 2)). */
 typedef struct aaf_kv_select_desc {
     uint32_t struct_size; /* sizeof(aaf_kv_select_desc)      */
     int32_t dtype;        /* AAF_DTYPE_*                     */

@@ -9,8 +9,9 @@
 // come through the list and then the table, two loads that are asked for ahead of the copies; and all rows of a CTA belong to one
 // query token, so they see the same keys.  A key that is not seen is not read: its key and value are zeros, its score is -inf.
 //
-// 64 ragged contexts, up to 256 blocks for each kv head, 979 MB: 168 us with the join (5.8 TB/s); 16 contexts, 64 blocks, 67 MB: 17 us; 128
-// tokens, 128 blocks each, 1.07 GB of which 267 MB are distinct: 105 to 111 us, where instructions decide (450 a tile of 16 keys).
+// 64 ragged contexts, up to 256 blocks for each kv head, 979 MB: 168 to 177 us with the join (5.5 to 5.8 TB/s); 16 contexts, 64 blocks, 67 MB:
+// 18.5 us; 128 tokens, 128 blocks each, 1.07 GB of which 267 MB are distinct: 105 to 117 us, where instructions decide (450 a tile of 16
+// keys), 121 with a bias, 134 with a cap, 119 and 127 in blocks of 8 and 24 tokens.
 #include "sparse_device.cuh"
 
 namespace aafkv {

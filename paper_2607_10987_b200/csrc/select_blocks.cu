@@ -13,8 +13,8 @@
 // compared with one another; a list's scores come from L2 and stay in shared memory where they fit.
 //
 // Bound: the bytes of the summaries where there is a token each (and the start of the two kernels); instructions of the sums' and the
-// scores' passes where there are many tokens.  16 contexts of 544 blocks, 18 MB of summaries: 16.6 us; 32 ragged ones of 512 to 4096, 113 MB:
-// 46.8 us, of which the scores 32 (5.4 TB/s once they are under way); 128 tokens behind 4096 blocks: 43 us.
+// scores' passes where there are many tokens.  16 contexts of 544 blocks, 18 MB of summaries: 16.5 us; 32 ragged ones of 512 to 4096, 113 MB:
+// 47.5 us, of which the scores 32 (5.4 TB/s once they are under way); 128 tokens behind 4096 blocks: 44 us.
 #include "sparse_device.cuh"
 #include "tensor_device.cuh"
 

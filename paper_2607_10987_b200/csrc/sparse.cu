@@ -200,7 +200,10 @@ int aaf_kv_attend_blocks(aaf_kv_pool *p, int32_t layer, const aaf_kv_attn *a, in
     // Lists are cut into parts so that the GPU is filled a whole number of times, by CTAs that share an SM or, where there is one for
     // each of them, by CTAs that have it to themselves and more warps: a round costs its part's keys per warp and a start (about 72
     // keys' time), a join twice that.  Microseconds with 1, 2, 3, 4, 6 parts: 1024 lists of 2048 keys 105, 111, 118, 124, 139; 512 ragged
-    // ones of up to 4096 197, 179, 171, 169, 169; 128 of 1024 20.3, 19.8, 19.5, 19.6, 20.5, and 17.2 with an SM for each.
+    // ones of up to 4096 197, 179, 171, 169, 169; 128 of 1024 20.3, 19.8, 19.5, 19.6, 20.5, and 17.2 with an SM for each.  The figures are
+    // those of groups of 4, heads of 128 and blocks of 16; with blocks of 8, 24 and 40, heads of 64 and 256, groups of 16 and 32, with a
+    // bias and a cap (32 batches of 8 to 1024 lists) what the rule takes is within 4 % of the best of 1 to 12 parts, but for 64 lists of
+    // 1024 keys in heads of 256: 22.9 us in one part, 20.0 in two.
     int longest = 0;
     for (AttnSeq &s : rec) {
         s.chunk = (int)(std::min<long long>(keep, nblk_of(p, s.len)) * BS);  // keys of a full list, for now

@@ -8,7 +8,7 @@
 //
 // Bound: the bytes of the keys, read once.  D / 8 lanes take a head's channels, 16 bytes each, and walk the block's tokens with
 // the loads of SUMMARY_AHEAD tokens under way; maxima stay in the type itself, two channels an instruction.  8187 tokens in 32 layers, 537 MB
-// read: 92 us (5.8 TB/s); one block of 16 contexts: 6 us, three loads one behind the other.
+// read: 92 to 95 us (5.7 to 5.8 TB/s); one block of 16 contexts: 6 us, three loads one behind the other.
 #include "attend_device.cuh"
 #include "sparse_device.cuh"
 
