@@ -22,14 +22,17 @@ def pick(tmp_path_factory):
     text = re.sub(r"asm volatile\([^;]*griddepcontrol[^;]*;[^;]*;", "", text)
     assert "asm" not in text
     (at / "pick.inc").write_text(text)
-    subprocess.check_call(["g++", "-std=c++20", "-O1", "-g", "-fsanitize=address", "-pthread", "-I", os.path.join(O.CUDA, "include"),
+    subprocess.check_call(["g++", "-std=c++20", "-O1", "-g", "-fsanitize=address", "-static-libasan", "-pthread", "-I", os.path.join(O.CUDA, "include"),
                            f'-DPICK_SOURCE="{at / "pick.inc"}"', os.path.join(O.ROOT, "tests", "pick_model.cpp"), "-o", str(at / "pick")])
+
+    env = {k: v for k, v in os.environ.items() if k != "LD_PRELOAD"}  # the sanitizer wants to be loaded first
+    env["ASAN_OPTIONS"] = "detect_leaks=0"
 
     def run(keys, keep, sink, recent, warps=4, stay=True):
         keys = np.ascontiguousarray(keys, dtype=np.uint32)
         room = (len(keys) + 3) // 4 * 4 if stay else 0
         done = subprocess.run([str(at / "pick"), *map(str, (warps, len(keys), keep, sink, recent, room))], input=keys.tobytes(), capture_output=True,
-                              timeout=120)
+                              timeout=120, env=env)
         assert done.returncode == 0, done.stderr.decode()[-3000:]
         return np.frombuffer(done.stdout, dtype=np.int32).tolist()
 
